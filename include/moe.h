@@ -387,6 +387,71 @@ int moe_quant_fp8_tgroup(const void* src, moe_dtype src_dt, int rows, int cols,
                          const int32_t* offsets, int E, int32_t* pad_offsets,
                          uint8_t* codes_t, long ldt, uint8_t* e8m0, void* stream);
 
+/* ---- what follows the layer in a training step ------------------------------------------------
+ * (Section 2.1's training loop around the layer; the paper leaves these parts to the framework
+ * it runs in.)
+ *
+ * Vocabulary loss: softmax cross entropy of hidden rows x [T,d] against a vocabulary matrix
+ * w [V,d], both in `dt` (MOE_F32 or MOE_BF16):
+ *   z = x w^T, lse[t] = log sum_v exp z[t,v], loss[t] = lse[t] - z[t,target[t]].
+ * A token whose target is outside 0..V-1 (by custom -100) is left out: loss and lse are 0 there,
+ * its row is not read and its gradient is 0.  d is a multiple of 16, V is any.
+ * moe_vocab_score: loss and lse [T] alone.  In bf16 no logit reaches memory.
+ * moe_vocab_loss: with c[t] = token_w[t], or 1 / (number of tokens that count) where token_w is
+ * NULL, also total[0] = sum_t c[t] loss[t] and its gradients: dx [T,d] in `dt`, written, and
+ * d_w [V,d] in grad_dt (MOE_F32, or MOE_BF16 for bf16 data), written or with accumulate=1 added
+ * to.  No token that counts: total 0, gradients 0.  Results do not depend on what ran before.
+ * G = c (softmax(z) - onehot) is kept for piece_rows rows at a time (0: all), V elements of the
+ * data's type each (fp32 data: also the logits, in the same place, and in the score as well).
+ * More pieces cost launches and passes over d_w.  A power of two of at least 2048 rows, or all
+ * of them, fills the matrix cores.
+ * Workspace: moe_vocab_workspace_bytes with the same sizes (gradients = 0 for the score; grad_dt
+ * then does not matter); 0 on invalid sizes. */
+#define MOE_VOCAB_MAX (1 << 24)
+#define MOE_VOCAB_MAX_WIDTH (1 << 20)
+#define MOE_VOCAB_MAX_ROWS (1 << 24)
+size_t moe_vocab_workspace_bytes(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt,
+                                 int piece_rows, int gradients);
+int moe_vocab_score(const void* x, const void* w, const int32_t* target /*[T]*/, moe_dtype dt,
+                    int T, int d, int V, int piece_rows, float* loss /*[T]*/, float* lse /*[T]*/,
+                    void* workspace, size_t ws_bytes, void* stream);
+int moe_vocab_loss(const void* x, const void* w, const int32_t* target, const float* token_w,
+                   moe_dtype dt, int T, int d, int V, int piece_rows, float* total /*[1]*/,
+                   float* loss, float* lse, void* dx, void* d_w, moe_dtype grad_dt,
+                   int accumulate, void* workspace, size_t ws_bytes, void* stream);
+
+/* Gradient norm over n tensors and clipping: norm[0] = sqrt(sum of all squares), summed in 64
+ * bits in a fixed order, coef[0] = min(1, max_norm / (norm + 1e-6)); write=1: outs = coef * grads
+ * as well (an out may be its gradient; a NULL out is skipped).  A norm that is infinite or NaN
+ * gives a factor of 0 or NaN: the caller looks at it.
+ * The tensors are named by a table that is made once: moe_grad_clip_table fills
+ * moe_grad_clip_table_bytes(n) bytes of HOST memory from the tensors' device pointers (aligned
+ * to their elements, no more), element counts and types (MOE_F32 or MOE_BF16; an out has its
+ * gradient's), outs NULL for none; the caller copies them to the device and passes that copy.
+ * total = sum of numel. */
+size_t moe_grad_clip_table_bytes(int n);
+int moe_grad_clip_table(int n, const void* const* grads, void* const* outs, const int64_t* numel,
+                        const int32_t* dtypes, void* table);
+size_t moe_grad_clip_workspace_bytes(void);
+int moe_grad_clip(const void* table /*device*/, int n, int64_t total, double max_norm, int write,
+                  float* norm, float* coef, void* workspace, size_t ws_bytes, void* stream);
+
+/* AdamW over n tensors, in place: with g = coef[0] * grad (coef NULL: 1) and t = step[0] + 1
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32, the new p rounded to bf16 into weights (NULL, or a NULL entry: none), step[0] = t.
+ * lr, step and coef are read on the device, so a captured step follows a schedule.  params, m, v
+ * fp32; grads all in grad_dt (MOE_F32 or MOE_BF16).  The table as above.  Workspace:
+ * MOE_ADAMW_WS_BYTES that the caller has cleared once; every call leaves them cleared. */
+#define MOE_ADAMW_WS_BYTES ((size_t)16)
+size_t moe_adamw_table_bytes(int n);
+int moe_adamw_table(int n, void* const* params, const void* const* grads, void* const* m,
+                    void* const* v, void* const* weights, const int64_t* numel,
+                    moe_dtype grad_dt, void* table);
+int moe_adamw(const void* table /*device*/, int n, int64_t total, moe_dtype grad_dt,
+              const float* lr, int32_t* step, const float* coef, double beta1, double beta2,
+              double eps, double weight_decay, void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,6 +30,9 @@ EXPORTS = (
     "moe_route_capacity_workspace_bytes", "moe_route_capacity", "moe_balance_loss", "moe_balance_loss_bwd",
     "moe_row_map", "moe_expert_ffn_fused_workspace_bytes", "moe_expert_ffn_fused_fwd", "moe_expert_ffn_fused_bwd",
     "moe_route_noalloc", "moe_init", "moe_transpose",
+    "moe_vocab_workspace_bytes", "moe_vocab_score", "moe_vocab_loss",
+    "moe_grad_clip_table_bytes", "moe_grad_clip_table", "moe_grad_clip_workspace_bytes", "moe_grad_clip",
+    "moe_adamw_table_bytes", "moe_adamw_table", "moe_adamw",
 )
 
 
@@ -80,6 +83,12 @@ def _load() -> ctypes.CDLL:
         "moe_expert_ffn_bwd_fp8": (I, [ctypes.POINTER(FfnBwdFp8Args), P]),
         "moe_tgroup_tokens": (Z, [I, I]),
         "moe_expert_ffn_fused_workspace_bytes": (Z, [I, I, I, I]),
+        "moe_vocab_workspace_bytes": (Z, [I, I, I, I, I, I, I]),
+        "moe_grad_clip_table_bytes": (Z, [I]),
+        "moe_grad_clip_table": (I, [I, P, P, P, P, P]),
+        "moe_grad_clip_workspace_bytes": (Z, []),
+        "moe_adamw_table_bytes": (Z, [I]),
+        "moe_adamw_table": (I, [I, P, P, P, P, P, P, I, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -316,3 +325,95 @@ def moe_expert_ffn_fused_bwd(x, dy, h_save, inv_perm, topk_w, row_w, offsets, w1
     _check("moe_expert_ffn_fused_bwd", _native.moe_expert_ffn_fused_bwd(
         x, dy, h_save, inv_perm, topk_w, row_w, offsets, w1, w2, T, k, d, E, two_f // 2, d_xp, d_w1, d_w2,
         dtype_code(d_w1.dtype), int(accumulate), d_topk_w, workspace, workspace.numel() * workspace.element_size()))
+
+
+# ---- what follows the layer in a training step ---------------------------------------------------------------------
+ADAMW_WS_BYTES = 16
+
+
+def moe_vocab_workspace_bytes(T, d, V, dt, grad_dt, piece_rows, gradients) -> int:
+    return _lib.moe_vocab_workspace_bytes(T, d, V, dt, grad_dt, piece_rows, int(gradients))
+
+
+def _vocab_shapes(x, w, target, loss, lse, token_w=None, dx=None, d_w=None):
+    T, d = x.shape
+    V = w.shape[0]
+    assert tuple(w.shape) == (V, d) and w.dtype == x.dtype, "x [T, d] and w [V, d] of one type"
+    assert tuple(target.shape) == (T,) and target.dtype == torch.int32, "target [T] int32"
+    for t in (loss, lse) + ((token_w,) if token_w is not None else ()):
+        assert tuple(t.shape) == (T,) and t.dtype == torch.float32, "loss, lse and token_w [T] fp32"
+    if dx is not None:
+        assert dx.shape == x.shape and dx.dtype == x.dtype, "dx like x"
+        assert d_w.shape == w.shape, "d_w like w"
+    return T, d, V
+
+
+def moe_vocab_score(x, w, target, piece_rows, loss, lse, workspace):
+    T, d, V = _vocab_shapes(x, w, target, loss, lse)
+    _check("moe_vocab_score", _native.moe_vocab_score(
+        x, w, target, dtype_code(x.dtype), T, d, V, piece_rows, loss, lse, workspace, workspace.numel() *
+        workspace.element_size()))
+
+
+def moe_vocab_loss(x, w, target, token_w, piece_rows, total, loss, lse, dx, d_w, accumulate, workspace):
+    T, d, V = _vocab_shapes(x, w, target, loss, lse, token_w, dx, d_w)
+    _check("moe_vocab_loss", _native.moe_vocab_loss(
+        x, w, target, token_w, dtype_code(x.dtype), T, d, V, piece_rows, total, loss, lse, dx, d_w,
+        dtype_code(d_w.dtype), int(accumulate), workspace, workspace.numel() * workspace.element_size()))
+
+
+def _pointers(tensors):
+    """Host array of device pointers (None -> NULL; an empty tensor's is not looked at)."""
+    return (c_void_p * max(1, len(tensors)))(*[None if t is None or t.numel() == 0 else _p(t) for t in tensors])
+
+
+def _table(fn, tensors, size, fill):
+    """Fills a table in host memory and copies it to the device of the tensors."""
+    host = torch.zeros((size,), dtype=torch.uint8)
+    _check(fn, fill(host.data_ptr()))
+    return host.to(tensors[0].device if tensors else "cuda")
+
+
+def _numel(tensors):
+    return (ctypes.c_int64 * max(1, len(tensors)))(*[t.numel() for t in tensors])
+
+
+def moe_grad_clip_table(grads, outs=None):
+    """The device table of moe_grad_clip for these gradients; outs: None, or a tensor (or None) for each."""
+    for g, o in zip(grads, outs or grads):
+        assert o is None or (o.shape == g.shape and o.dtype == g.dtype), "an out has its gradient's shape and type"
+    assert outs is None or len(outs) == len(grads), "an out for each gradient"
+    n = len(grads)
+    types = (ctypes.c_int32 * max(1, n))(*[dtype_code(g.dtype) for g in grads])
+    return _table("moe_grad_clip_table", grads, _lib.moe_grad_clip_table_bytes(n), lambda host: _lib.moe_grad_clip_table(
+        n, _pointers(grads), _pointers(outs) if outs is not None else None, _numel(grads), types, host))
+
+
+def moe_grad_clip_workspace_bytes() -> int:
+    return _lib.moe_grad_clip_workspace_bytes()
+
+
+def moe_grad_clip(table, n, total, max_norm, write, norm, coef, workspace):
+    _check("moe_grad_clip", _native.moe_grad_clip(table, n, total, max_norm, int(write), norm, coef, workspace,
+                                                  workspace.numel() * workspace.element_size()))
+
+
+def moe_adamw_table(params, grads, m, v, weights=None):
+    """The device table of moe_adamw; weights: None, or a bf16 tensor (or None) for each parameter."""
+    n = len(params)
+    assert len(grads) == len(m) == len(v) == n and (weights is None or len(weights) == n), "one of each for each parameter"
+    grad_dt = grads[0].dtype if n else torch.float32
+    for i, p in enumerate(params):
+        for t in (p, m[i], v[i]):
+            assert t.dtype == torch.float32 and t.shape == p.shape, "parameters and moments are fp32, of one shape"
+        assert grads[i].shape == p.shape and grads[i].dtype == grad_dt, "gradients have one type and their parameters' shapes"
+        w = weights[i] if weights is not None else None
+        assert w is None or (w.shape == p.shape and w.dtype == torch.bfloat16), "weights are bf16, of their parameters' shapes"
+    return _table("moe_adamw_table", params, _lib.moe_adamw_table_bytes(n), lambda host: _lib.moe_adamw_table(
+        n, _pointers(params), _pointers(grads), _pointers(m), _pointers(v),
+        _pointers(weights) if weights is not None else None, _numel(params), dtype_code(grad_dt), host))
+
+
+def moe_adamw(table, n, total, grad_dt, lr, step, coef, beta1, beta2, eps, weight_decay, workspace):
+    _check("moe_adamw", _native.moe_adamw(table, n, total, grad_dt, lr, step, coef, beta1, beta2, eps, weight_decay,
+                                          workspace, workspace.numel() * workspace.element_size()))

@@ -1,0 +1,133 @@
+// extern "C" entry points of what follows the layer in a training step: the vocabulary loss, clipping and the AdamW update.  Arguments are
+// checked before any HIP call; declarations and contracts are in include/moe.h.
+#include "optim.h"
+#include "vocab_loss.h"
+
+namespace moe {
+namespace {
+
+// V * d may pass 2^32 elements: operands are addressed from a tile's first row
+bool vocab_sizes_ok(int T, int d, int V) { return T >= 0 && d > 0 && V > 0; }
+bool vocab_types_ok(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt) {
+  if (dt != MOE_F32 && dt != MOE_BF16) return false;
+  if (dt == MOE_F32 ? grad_dt != MOE_F32 : grad_dt != MOE_F32 && grad_dt != MOE_BF16) return false;
+  return d % 16 == 0 && d <= MOE_VOCAB_MAX_WIDTH && V <= MOE_VOCAB_MAX && T <= MOE_VOCAB_MAX_ROWS;
+}
+
+int vocab_call(const VocabProblem& q, int piece_rows, void* workspace, size_t ws_bytes, void* stream) {
+  const VocabPlan p = vocab_plan(q.T, q.d, q.V, q.dt, q.grad_dt, piece_rows, q.grad);
+  if (!workspace || !aligned16(workspace) || ws_bytes < p.bytes) return MOE_ERR_WORKSPACE;
+  return launch_vocab_loss(q, p, static_cast<char*>(workspace), as_stream(stream));
+}
+
+// sums of numel into entries[i].first and entries[n].first
+template <typename Entry> bool number_entries(const int64_t* numel, int n, Entry* table) {
+  int64_t at = 0;
+  for (int i = 0; i <= n; ++i) {
+    if (i == n) table[i] = Entry{};
+    table[i].first = at;
+    if (i < n) {
+      if (numel[i] < 0 || numel[i] > INT64_MAX / 16 - at) return false;
+      at += numel[i];
+    }
+  }
+  return true;
+}
+
+bool at_elements(const void* p, size_t es) { return (reinterpret_cast<uintptr_t>(p) & (es - 1)) == 0; }
+
+}  // namespace
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" {
+
+size_t moe_vocab_workspace_bytes(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int piece_rows, int gradients) {
+  if (!vocab_sizes_ok(T, d, V) || piece_rows < 0 || !vocab_types_ok(T, d, V, dt, gradients ? grad_dt : dt)) return 0;
+  return T == 0 ? 256 : vocab_plan(T, d, V, dt, gradients ? grad_dt : dt, piece_rows, gradients != 0).bytes;
+}
+
+int moe_vocab_score(const void* x, const void* w, const int32_t* target, moe_dtype dt, int T, int d, int V, int piece_rows, float* loss, float* lse,
+                    void* workspace, size_t ws_bytes, void* stream) {
+  if (!vocab_sizes_ok(T, d, V) || piece_rows < 0) return MOE_ERR_INVALID;
+  if (!vocab_types_ok(T, d, V, dt, dt)) return MOE_ERR_UNSUPPORTED;
+  if (T == 0) return MOE_OK;
+  if (!x || !w || !target || !loss || !lse) return MOE_ERR_INVALID;
+  if (!aligned16(x) || !aligned16(w) || !at_elements(target, 4) || !at_elements(loss, 4) || !at_elements(lse, 4)) return MOE_ERR_UNSUPPORTED;
+  VocabProblem q{};
+  q.x = x; q.w = w; q.target = target; q.T = T; q.d = d; q.V = V; q.dt = dt; q.grad_dt = dt; q.loss = loss; q.lse = lse;
+  return vocab_call(q, piece_rows, workspace, ws_bytes, stream);
+}
+
+int moe_vocab_loss(const void* x, const void* w, const int32_t* target, const float* token_w, moe_dtype dt, int T, int d, int V, int piece_rows,
+                   float* total, float* loss, float* lse, void* dx, void* d_w, moe_dtype grad_dt, int accumulate, void* workspace, size_t ws_bytes,
+                   void* stream) {
+  if (!vocab_sizes_ok(T, d, V) || piece_rows < 0) return MOE_ERR_INVALID;
+  if (!vocab_types_ok(T, d, V, dt, grad_dt)) return MOE_ERR_UNSUPPORTED;
+  if (T == 0) return MOE_OK;
+  if (!x || !w || !target || !total || !loss || !lse || !dx || !d_w) return MOE_ERR_INVALID;
+  if (!aligned16(x) || !aligned16(w) || !aligned16(dx) || !aligned16(d_w) || !at_elements(target, 4) || !at_elements(token_w, 4) ||
+      !at_elements(total, 4) || !at_elements(loss, 4) || !at_elements(lse, 4))
+    return MOE_ERR_UNSUPPORTED;
+  VocabProblem q{};
+  q.x = x; q.w = w; q.target = target; q.token_w = token_w; q.T = T; q.d = d; q.V = V; q.dt = dt;
+  q.loss = loss; q.lse = lse; q.grad = true; q.total = total; q.dx = dx; q.d_w = d_w; q.grad_dt = grad_dt; q.accumulate = accumulate != 0;
+  return vocab_call(q, piece_rows, workspace, ws_bytes, stream);
+}
+
+size_t moe_grad_clip_table_bytes(int n) { return n < 0 ? 0 : ((size_t)n + 1) * sizeof(ClipEntry); }
+
+int moe_grad_clip_table(int n, const void* const* grads, void* const* outs, const int64_t* numel, const int32_t* dtypes, void* table) {
+  if (n < 0 || !table || (n > 0 && (!grads || !numel || !dtypes))) return MOE_ERR_INVALID;
+  ClipEntry* e = static_cast<ClipEntry*>(table);
+  for (int i = 0; i < n; ++i) {
+    if (dtypes[i] != MOE_F32 && dtypes[i] != MOE_BF16) return MOE_ERR_UNSUPPORTED;
+    const size_t es = dtype_size((moe_dtype)dtypes[i]);
+    if (numel[i] > 0 && !grads[i]) return MOE_ERR_INVALID;
+    if (!at_elements(grads[i], es) || (outs && !at_elements(outs[i], es))) return MOE_ERR_UNSUPPORTED;
+    e[i] = ClipEntry{grads[i], outs ? outs[i] : nullptr, 0, dtypes[i], 0};
+  }
+  return number_entries(numel, n, e) ? MOE_OK : MOE_ERR_INVALID;
+}
+
+size_t moe_grad_clip_workspace_bytes(void) { return kNormParts * sizeof(double); }
+
+int moe_grad_clip(const void* table, int n, int64_t total, double max_norm, int write, float* norm, float* coef, void* workspace, size_t ws_bytes,
+                  void* stream) {
+  if (n < 0 || total < 0 || !(max_norm >= 0)) return MOE_ERR_INVALID;
+  if (!table || !norm || !coef) return MOE_ERR_INVALID;
+  if (!at_elements(table, 8) || !at_elements(norm, 4) || !at_elements(coef, 4)) return MOE_ERR_UNSUPPORTED;
+  if (!workspace || !aligned16(workspace) || ws_bytes < moe_grad_clip_workspace_bytes()) return MOE_ERR_WORKSPACE;
+  return launch_grad_clip(static_cast<const ClipEntry*>(table), n, total, max_norm, write, norm, coef, static_cast<double*>(workspace), as_stream(stream));
+}
+
+size_t moe_adamw_table_bytes(int n) { return n < 0 ? 0 : ((size_t)n + 1) * sizeof(AdamwEntry); }
+
+int moe_adamw_table(int n, void* const* params, const void* const* grads, void* const* m, void* const* v, void* const* weights, const int64_t* numel,
+                    moe_dtype grad_dt, void* table) {
+  if (n < 0 || !table || (n > 0 && (!params || !grads || !m || !v || !numel))) return MOE_ERR_INVALID;
+  if (grad_dt != MOE_F32 && grad_dt != MOE_BF16) return MOE_ERR_UNSUPPORTED;
+  AdamwEntry* e = static_cast<AdamwEntry*>(table);
+  for (int i = 0; i < n; ++i) {
+    if (numel[i] > 0 && (!params[i] || !grads[i] || !m[i] || !v[i])) return MOE_ERR_INVALID;
+    void* w = weights ? weights[i] : nullptr;
+    if (!at_elements(params[i], 4) || !at_elements(m[i], 4) || !at_elements(v[i], 4) || !at_elements(grads[i], dtype_size(grad_dt)) || !at_elements(w, 2))
+      return MOE_ERR_UNSUPPORTED;
+    e[i] = AdamwEntry{params[i], grads[i], m[i], v[i], w, 0};
+  }
+  return number_entries(numel, n, e) ? MOE_OK : MOE_ERR_INVALID;
+}
+
+int moe_adamw(const void* table, int n, int64_t total, moe_dtype grad_dt, const float* lr, int32_t* step, const float* coef, double beta1, double beta2,
+              double eps, double weight_decay, void* workspace, size_t ws_bytes, void* stream) {
+  if (n < 0 || total < 0 || !table || !lr || !step) return MOE_ERR_INVALID;
+  if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0) || !(weight_decay >= 0)) return MOE_ERR_INVALID;
+  if (grad_dt != MOE_F32 && grad_dt != MOE_BF16) return MOE_ERR_UNSUPPORTED;
+  if (!at_elements(table, 8) || !at_elements(lr, 4) || !at_elements(step, 4) || !at_elements(coef, 4)) return MOE_ERR_UNSUPPORTED;
+  if (!workspace || !at_elements(workspace, 4) || ws_bytes < MOE_ADAMW_WS_BYTES) return MOE_ERR_WORKSPACE;
+  return launch_adamw(static_cast<const AdamwEntry*>(table), n, total, grad_dt, lr, step, coef, AdamwHyper{beta1, beta2, eps, weight_decay},
+                      static_cast<unsigned*>(workspace), as_stream(stream));
+}
+
+}  // extern "C"

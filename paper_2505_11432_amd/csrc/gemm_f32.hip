@@ -99,6 +99,7 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmProblem& p, int tiles_n,
   const float* __restrict__ A = static_cast<const float*>(p.A);
   const float* __restrict__ B = static_cast<const float*>(p.B) + (long)e * p.b_es;
   const long lda = AK ? p.a_rs : p.a_cs, ldb = BKF ? p.b_cs : p.b_rs;
+  const int b_n = (p.b_rows ? p.b_rows : p.N) - n0, m_store = p.c_rows ? min(m_end, p.c_rows) : m_end;
 
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -113,7 +114,7 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmProblem& p, int tiles_n,
   auto load = [&](int set, int k) __attribute__((always_inline)) {
     fetch<AK, BM, BK>(A, lda, m0, m_end - m0, k, k_end, ra[set]);
     if constexpr (FUSE == FROM_H) fetch<AK, BM, BK>(A + p.K, lda, m0, m_end - m0, k, k_end, up_in[set]);
-    fetch<BKF, BN, BK>(B, ldb, n0, p.N - n0, k, k_end, rb[set]);
+    fetch<BKF, BN, BK>(B, ldb, n0, b_n, k, k_end, rb[set]);
   };
   auto put = [&](int set, int buf) __attribute__((always_inline)) {
     if constexpr (FUSE == FROM_H)
@@ -209,7 +210,7 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmProblem& p, int tiles_n,
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int m = m0 + wm * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-    if (m >= m_end) continue;
+    if (m >= m_store) continue;
     float* dst = C + (long)m * p.ldc + n;
     float v = acc[r] + bias;
     if (p.accumulate) v += *dst;

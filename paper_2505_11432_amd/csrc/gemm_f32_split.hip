@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) gemm_f32_split_kernel(GemmPro
   Share<AK, BM> a;
   Share<BKF, BN> b;
   a.open(static_cast<const float*>(p.A), AK ? p.a_rs : p.a_cs, m0, m_end - m0, t.k0);
-  b.open(static_cast<const float*>(p.B) + (long)t.e * p.b_es, BKF ? p.b_cs : p.b_rs, n0, p.N - n0, t.k0);
+  b.open(static_cast<const float*>(p.B) + (long)t.e * p.b_es, BKF ? p.b_cs : p.b_rs, n0, (p.b_rows ? p.b_rows : p.N) - n0, t.k0);
   float va[2][8], vb[2][8];
   auto load = [&](int set, int s) __attribute__((always_inline)) {
     a.load(va[set], s, klen - s * kStep);
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) gemm_f32_split_kernel(GemmPro
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     const int m = m0 + wm * WTM + i * 16 + i16;
-    if (m >= m_end) continue;
+    if (m >= m_end || (p.c_rows && m >= p.c_rows)) continue;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int n = n0 + wn * WTN + j * 16 + g * 4;
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(256, 2) gemm_f32_split128_kernel(GemmProblem p
   ShareA a;
   ShareB b;
   a.open(static_cast<const float*>(p.A), AK ? p.a_rs : p.a_cs, m0, m_end - m0, t.k0);
-  b.open(static_cast<const float*>(p.B) + (long)t.e * p.b_es, BKF ? p.b_cs : p.b_rs, n0, p.N - n0, t.k0);
+  b.open(static_cast<const float*>(p.B) + (long)t.e * p.b_es, BKF ? p.b_cs : p.b_rs, n0, (p.b_rows ? p.b_rows : p.N) - n0, t.k0);
   float va[CA][8], vb[CB][8];
   auto load_a = [&](int c, int s) __attribute__((always_inline)) { a.load(va[c], c, s, klen - s * kStep); };
   auto load_b = [&](int c, int s) __attribute__((always_inline)) { b.load(vb[c], c, s, klen - s * kStep); };
@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(256, 2) gemm_f32_split128_kernel(GemmProblem p
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     const int m = m0 + wm * WTM + i * 16 + i16;
-    if (m >= m_end) continue;
+    if (m >= m_end || (p.c_rows && m >= p.c_rows)) continue;
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int n = n0 + wn * WTN + j * 16 + g * 4;

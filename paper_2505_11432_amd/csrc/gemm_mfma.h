@@ -18,10 +18,13 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 enum Layout { KMAJOR = 0, MNMAJOR = 1 };
-enum Mode { ROWSEG = 0, KSEG = 1, PLAIN = 2 };   // PLAIN: one dense GEMM, no expert segments
+// PLAIN: one dense GEMM, no expert segments.  DENSE: the same with the number of rows read on the device and the contraction cut into
+// E parts, each with a result of its own (the vocabulary products)
+enum Mode { ROWSEG = 0, KSEG = 1, PLAIN = 2, DENSE = 3 };
 // EPI_SWIGLU_W / EPI_SWIGLU_BWD_W: the Section 4.1 operator order (gate weight multiplied right after SwiGLU; the
 // forward one also selects its A rows through an index map, Section 4.2)
-enum Epi { EPI_STORE = 0, EPI_SWIGLU = 1, EPI_SWIGLU_BWD = 2, EPI_BIAS_F32 = 3, EPI_SWIGLU_W = 4, EPI_SWIGLU_BWD_W = 5 };
+// EPI_LSE / EPI_CE: a row's softmax statistics over a wave's columns instead of the logits, and with them exp(logit - maximum)
+enum Epi { EPI_STORE = 0, EPI_SWIGLU = 1, EPI_SWIGLU_BWD = 2, EPI_BIAS_F32 = 3, EPI_SWIGLU_W = 4, EPI_SWIGLU_BWD_W = 5, EPI_LSE = 6, EPI_CE = 7 };
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 
@@ -56,6 +59,13 @@ struct Args {
   int a_phys_rows;                   //   rows of that buffer (for the 32-bit offset check)
   const float* row_w;                // [M] gate weight of each row: A_out = w * SwiGLU(G, U) in both epilogues
   float* dw_part;                    // EPI_SWIGLU_BWD_W: [n-tiles * waves along n][M] partial sums of <dA'[r,:], A[r,:]>
+  // vocabulary products
+  const int32_t* rows;               // DENSE: number of rows (at most M, the rows that A and C have room for), or NULL for M
+  int kpart;                         // DENSE: contraction of one of the E parts (whole k-steps); part e writes C + e * c_es
+  int c_rows;                        // KSEG: rows of C where A is padded to M columns (0: M)
+  float* stats; int parts;           // EPI_LSE, EPI_CE: [M][parts] pairs of maximum and sum of exp(logit - maximum), one per n-tile and wave along n
+  const int32_t* target;             // EPI_LSE, EPI_CE: [M] column whose logit goes to z_target [M] (columns outside the width: none)
+  float* z_target;
 };
 
 // (LDS addresses in bytes)

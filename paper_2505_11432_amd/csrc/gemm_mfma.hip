@@ -40,7 +40,8 @@ std::vector<configure_fn>& configure_registry() {
 
 template <int BM, int BN, int BKT, int NS, int WM, int WN, Layout LA, Layout LB, Mode MODE, Epi EPI, typename TC, typename TIN>
 struct KernelSetup {
-  static constexpr int smem = dma_smem_bytes<BM, BN, BKT, NS, WM * WN, LA, LB, (int)sizeof(TIN)>();
+  static constexpr int smem = dma_smem_bytes<BM, BN, BKT, NS, WM * WN, LA, LB, (int)sizeof(TIN)>(EPI == EPI_LSE || EPI == EPI_CE);
+  static_assert(smem <= 160 * 1024, "LDS of a CU");
   static auto kernel() { return grouped_gemm_dma_kernel<BM, BN, BKT, NS, WM, WN, LA, LB, MODE, EPI, TC, TIN>; }
   // Idempotent and safe to race: the attribute value is the same on every call, the per-device bit only saves work.
   static int configure(int dev) {
@@ -70,7 +71,7 @@ int launch(const Args& a, long tiles_upper_bound, hipStream_t s) {
     const unsigned long long a_span = (EPI == EPI_SWIGLU_W) ? (unsigned long long)a.a_phys_rows * a.lda * esz   // absolute row offsets
                                       : (LA == KMAJOR)      ? (unsigned long long)BM * a.lda * esz
                                                             : ((unsigned long long)BKT * a.lda + a.M) * esz;
-    const unsigned long long b_rows = (EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_W) ? 2ull * a.f : (unsigned long long)a.N;
+    const unsigned long long b_rows = MODE == DENSE && LB == KMAJOR ? (unsigned long long)BN : (EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_W) ? 2ull * a.f : (unsigned long long)a.N;
     const unsigned long long b_span = (LB == KMAJOR) ? b_rows * a.ldb * esz : ((unsigned long long)BKT * a.ldb + a.N) * esz;
     if (a_span >= lim || b_span >= lim) return MOE_ERR_UNSUPPORTED;
   }
@@ -315,6 +316,82 @@ int mfma_router_fwd(const void* x, const void* w_r, const float* bias, int T, in
   if (E <= 32) return launch<64, 32, 64, 8, 2, 1, KMAJOR, KMAJOR, PLAIN, EPI_BIAS_F32, float>(a, cdiv(T, 64), s);
   if (E <= 64) return launch<64, 64, 64, 8, 2, 1, KMAJOR, KMAJOR, PLAIN, EPI_BIAS_F32, float>(a, cdiv(T, 64), s);
   return launch<256, 128, 64, 2, 4, 2, KMAJOR, KMAJOR, PLAIN, EPI_BIAS_F32, float>(a, mt * cdiv(E, 128), s);
+}
+
+// ---- vocabulary products (vocab_loss.hip).  `rows` (device, at most R) is the number of rows present.
+namespace {
+// Tile of z = x w^T with its softmax epilogue, as for a plain store.  WTN columns of a wave share one pair of statistics.
+RowTile vocab_tile(int R, int V, int d) { return plan_rows({false, true, false}, R, 1, V, d, 2).tile; }
+}  // namespace
+VocabTiles mfma_vocab_tiles(int R, int V, int d) {
+  return vocab_tile(R, V, d) == RowTile::FULL ? VocabTiles{cdiv(V, 256) * 2, 7} : VocabTiles{cdiv(V, 128) * 2, 6};
+}
+int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const int32_t* target, int R, int V, int d, void* P, long ldp,
+                       float* stats, float* z_target, hipStream_t s) {
+  Args a{};
+  a.A = x; a.lda = d;
+  a.B = w; a.ldb = d;
+  a.C = P; a.ldc = ldp;
+  a.E = 1; a.M = R; a.N = V; a.K = d; a.kpart = d;
+  a.rows = rows; a.target = target; a.stats = stats; a.z_target = z_target; a.parts = mfma_vocab_tiles(R, V, d).parts;
+  const RowTile tile = vocab_tile(R, V, d);
+  if (P) {
+    if (tile == RowTile::FEW) return launch<64, 128, 128, 3, 2, 2, KMAJOR, KMAJOR, DENSE, EPI_CE, bf16>(a, 1, s);
+    if (tile == RowTile::MID) return launch<128, 128, 64, 3, 4, 2, KMAJOR, KMAJOR, DENSE, EPI_CE, bf16>(a, 1, s);
+    return launch<256, 256, 64, 2, 4, 2, KMAJOR, KMAJOR, DENSE, EPI_CE, bf16>(a, 1, s);
+  }
+  if (tile == RowTile::FEW) return launch<64, 128, 128, 3, 2, 2, KMAJOR, KMAJOR, DENSE, EPI_LSE, bf16>(a, 1, s);
+  if (tile == RowTile::MID) return launch<128, 128, 64, 3, 4, 2, KMAJOR, KMAJOR, DENSE, EPI_LSE, bf16>(a, 1, s);
+  return launch<256, 256, 64, 2, 4, 2, KMAJOR, KMAJOR, DENSE, EPI_LSE, bf16>(a, 1, s);
+}
+
+// dx = G w, [R, V] by [V, d], contracted over the vocabulary: few tiles of a very long contraction, so that it is cut into parts (fp32, part e at
+// out + e * R * d) that the pass which rounds and places the rows adds up.
+VocabDxPlan mfma_vocab_dx_plan(int R, int V, int d) {
+  // rounds of the tiles (times as in row_plan.h) and the parts' way through memory and back at 5 TB/s
+  VocabDxPlan best{};
+  double best_us = 0;
+  for (const bool full : {true, false}) {
+    const int b = full ? 256 : 128, steps = cdiv(V, 64);
+    const long tiles = (long)cdiv(R, b) * cdiv(d, b);
+    for (int parts = 1; parts <= 32 && (parts == 1 || steps / parts >= 8); ++parts) {
+      const int each = cdiv(steps, parts), real = cdiv(steps, each);
+      const double rounds = (double)((tiles * real + 255) / 256);
+      const double us = rounds * (full ? 13 + 1.5 * each : 6 + 0.66 * each) + real * (double)R * d * 8 / 5e6;
+      if (best.parts == 0 || us < best_us) {
+        best = {full, real, each * 64};
+        best_us = us;
+      }
+    }
+  }
+  return best;
+}
+int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, int R, int V, int d, float* out, hipStream_t s) {
+  const VocabDxPlan plan = mfma_vocab_dx_plan(R, V, d);
+  Args a{};
+  a.A = G; a.lda = ldg;
+  a.B = w; a.ldb = d;
+  a.C = out; a.ldc = d; a.c_es = (long)R * d;
+  a.E = plan.parts; a.M = R; a.N = d; a.K = V; a.kpart = plan.kpart;
+  a.rows = rows;
+  if (plan.full) return launch<256, 256, 64, 2, 2, 4, KMAJOR, MNMAJOR, DENSE, EPI_STORE, float>(a, 1, s);
+  return launch<128, 128, 64, 3, 4, 2, KMAJOR, MNMAJOR, DENSE, EPI_STORE, float>(a, 1, s);
+}
+
+// d_w (+)= G^T x over the rows of range[0] .. range[1] - 1 (device); R bounds their number.  G [rows, ldg] with ldg a multiple of 8, V <= ldg.
+int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* range, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate,
+                  hipStream_t s) {
+  Args a{};
+  a.A = G; a.lda = ldg;
+  a.B = x; a.ldb = d;
+  a.C = d_w; a.ldc = d; a.offsets = range; a.E = 1; a.M = (int)ldg; a.N = d; a.c_rows = V;
+  a.accumulate = accumulate;
+  if (wgrad_in_pairs(R, 1, V, d)) {
+    if (dt == MOE_F32) return launch<128, 128, 64, 2, 2, 2, MNMAJOR, MNMAJOR, KSEG, EPI_STORE, float>(a, 1, s);
+    return launch<128, 128, 64, 2, 2, 2, MNMAJOR, MNMAJOR, KSEG, EPI_STORE, bf16>(a, 1, s);
+  }
+  if (dt == MOE_F32) return launch<256, 256, 64, 2, 2, 4, MNMAJOR, MNMAJOR, KSEG, EPI_STORE, float>(a, 1, s);
+  return launch<256, 256, 64, 2, 2, 4, MNMAJOR, MNMAJOR, KSEG, EPI_STORE, bf16>(a, 1, s);
 }
 
 // Sets up every grouped-GEMM kernel of this library for the current device (see moe_init).

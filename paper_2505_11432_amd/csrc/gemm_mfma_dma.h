@@ -354,10 +354,11 @@ __global__ void __launch_bounds__(256) splitk_fixup_kernel(const float* __restri
 }
 
 template <int BM, int BN, int BKT, int NSTAGE, int NW, Layout LA, Layout LB, int ESZ = 2>
-constexpr int dma_smem_bytes() {
+constexpr int dma_smem_bytes(bool targets = false) {
   // the ring, the per-expert tile table and one epilogue patch per wave
   return NSTAGE * (DmaTileBytes<LA, BM, BKT, ESZ>::value + DmaTileBytes<LB, BN, BKT, ESZ>::value) + (MOE_MAX_EXPERTS + 8) * 4 +
-         NW * STG_BYTES + 256 + 1024;       // + the dump area of the L2 touches + the block-scale ring
+         NW * STG_BYTES + 256 + 1024 +       // + the dump area of the L2 touches + the block-scale ring
+         (targets ? NW * 256 : 0);          // + the targets of each wave's rows (vocabulary products)
 }
 
 // Two workgroups of such a kernel share a CU's LDS; the launch makes twice the workgroups.
@@ -392,6 +393,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   constexpr bool SWI = EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_W;              // FC1 + SwiGLU epilogue
   constexpr bool FOLD = EPI == EPI_SWIGLU_W || EPI == EPI_SWIGLU_BWD_W;       // gate weight folded in (Section 4.1)
   constexpr bool GATHER_A = EPI == EPI_SWIGLU_W;                              // A rows selected by index map (Section 4.2)
+  constexpr bool VOCAB = EPI == EPI_LSE || EPI == EPI_CE;
+  static_assert(!VOCAB || (MODE == DENSE && !FP8), "the softmax epilogues exist for dense bf16 products");
   static_assert(!FOLD || (!FP8 && MODE == ROWSEG && LA == KMAJOR), "the folded order exists for the bf16 row-segmented kernels");
   constexpr int BN_OUT = SWI ? BN / 2 : BN;
   // Store instructions a wave issues in the epilogue of a full tile (branch-free buffer stores, bf16 kernels): two
@@ -400,6 +403,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
                                  : SWI ? TM * TN * 3
                                  : EPI == EPI_SWIGLU_BWD ? TM * TN * 6
                                  : EPI == EPI_SWIGLU_BWD_W ? TM * TN * 6 + TM
+                                 : EPI == EPI_CE ? TM * (TN * 2 + 3)
+                                 : EPI == EPI_LSE ? TM * 3
                                  : 0;
   constexpr int EPI_STORES = (NSTAGE - 2) * LOADS + EPI_STORES_RAW <= 63 ? EPI_STORES_RAW : 0;   // vmcnt is a 6-bit field
   // what this wave's epilogue of the previous tile put into the memory queue (wave-uniform): exactly EPI_STORES stores,
@@ -440,13 +445,17 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   // XCDs work on eight neighbouring windows, mostly the next m-tiles of the same n-tiles, i.e. the same B
   // panels (shared through the Infinity Cache) and disjoint A panels.
   const int tiles_n = (p.N + BN_OUT - 1) / BN_OUT;
-  const int tiles_m_fixed = (p.M + BM - 1) / BM;              // KSEG / PLAIN
+  int m_rows = p.M;                                           // KSEG / PLAIN / DENSE
+  if constexpr (MODE == DENSE) {
+    if (p.rows) m_rows = __builtin_amdgcn_readfirstlane(max(min(*p.rows, p.M), 0));
+  }
+  const int tiles_m_fixed = (m_rows + BM - 1) / BM;
   int total_tiles;
   if constexpr (MODE == ROWSEG) {
     tile_table<BM>(p.offsets, p.E, cum_tiles);
     __syncthreads();
     total_tiles = __builtin_amdgcn_readfirstlane(cum_tiles[p.E]) * tiles_n;
-  } else if constexpr (MODE == KSEG) {
+  } else if constexpr (MODE == KSEG || MODE == DENSE) {
     total_tiles = p.E * tiles_m_fixed * tiles_n;
   } else {
     total_tiles = tiles_m_fixed * tiles_n;
@@ -495,13 +504,17 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   // slower); at the end of the step they gain 1.2 to 3 %; one or two steps further ahead: no change; touching the B
   // panel as well, or half of A, or from two waves: slower again (each touch instruction costs the address unit as
   // much as a 1 KB tile load).  Not for e4m3 operands: half the time per k-step for the same loads, touches cost 2 %.
-  constexpr bool TOUCH = MODE == ROWSEG && NSTAGE == 2 && SPLIT && !FP8;
+  constexpr bool TOUCH = (MODE == ROWSEG || MODE == DENSE) && NSTAGE == 2 && SPLIT && !FP8;
   // the same for the bf16 weight-gradient kernel (four stages of 32 k-rows): two k-steps per touch, every other step
   constexpr bool TOUCH_K = MODE == KSEG && !FP8 && SPLIT && LA == MNMAJOR && LB == MNMAJOR && NSTAGE == 4;
   constexpr bool TOUCH_K2 = MODE == KSEG && !FP8 && SPLIT && LA == MNMAJOR && LB == MNMAJOR && NSTAGE == 2 && BKT == 64;
   const bool is_toucher = (TOUCH || TOUCH_K || TOUCH_K2) && wave == NL;
   const unsigned lds_dump = smem_lds + RING_BYTES + TABLE_BYTES + NW * STG_BYTES;
   const unsigned scale_lds = lds_dump + 256;                                   // block-scale ring: 2 stages x (256 + 256) bytes
+  constexpr int TARGETS_AT = RING_BYTES + TABLE_BYTES + NW * STG_BYTES + 256 + 1024;       // behind the block-scale ring
+  static_assert(!VOCAB || WTM <= 64, "a lane per row");
+  const unsigned target_lds = smem_lds + TARGETS_AT + (unsigned)wave * 256u;
+  const char* target_smem = smem + TARGETS_AT + wave * 256;
   const char* scale_smem = smem + RING_BYTES + TABLE_BYTES + NW * STG_BYTES + 256;
   unsigned ta_off = 0;
   // rotation of this workgroup's load order within the A / B tile (see open_tile); only where it pays: the e4m3
@@ -556,7 +569,10 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
       mt_e = tiles_m_fixed;
       e = l / (mt_e * tiles_n);          // always 0 in PLAIN mode
       l -= e * mt_e * tiles_n;
-      m_lo = 0; m_hi = p.M;
+      m_lo = 0; m_hi = m_rows;
+      if constexpr (MODE == KSEG) {
+        if (p.c_rows) m_hi = p.c_rows;
+      }
     }
     const int ng = l / (mt_e * GN);
     const int r = l - ng * mt_e * GN;
@@ -573,6 +589,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
     }
     int k_begin, k_end;
     if constexpr (MODE == KSEG) { k_begin = p.offsets[e]; k_end = p.offsets[e + 1]; }
+    else if constexpr (MODE == DENSE) { k_begin = e * p.kpart; k_end = min(p.K, k_begin + p.kpart); }
     else { k_begin = 0; k_end = p.K; }
     klen = k_end - k_begin;
     nk = (klen + BKT - 1) / BKT;
@@ -591,7 +608,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
     if constexpr (GATHER_A) a_base = uniform_ptr(Ag + (long)k_begin * ESZ);          // row offsets are absolute
     else if constexpr (LA == KMAJOR) a_base = uniform_ptr(Ag + ((long)m0 * p.lda + k_begin) * ESZ);
     else a_base = uniform_ptr(Ag + (long)k_begin * p.lda * ESZ);
-    if constexpr (LB == KMAJOR) b_base = uniform_ptr(Bg + (long)k_begin * ESZ);
+    if constexpr (MODE == DENSE && LB == KMAJOR) b_base = uniform_ptr(Bg + ((long)n0 * p.ldb + k_begin) * ESZ);
+    else if constexpr (LB == KMAJOR) b_base = uniform_ptr(Bg + (long)k_begin * ESZ);
     else b_base = uniform_ptr(Bg + (long)k_begin * p.ldb * ESZ);
 #pragma unroll
     for (int j = 0; j < A_DMA; ++j) {
@@ -625,6 +643,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
           const int qq = row >> 5;
           const int n = min(n0 + (qq >> 1) * 32 + (row & 31), p.f - 1);
           gr = (qq & 1) ? p.f + n : n;
+        } else if constexpr (MODE == DENSE) {
+          gr = min(row, p.N - 1 - n0);            // (from the tile's first row: a vocabulary matrix may pass 4 GiB)
         } else {
           gr = min(n0 + row, p.N - 1);
         }
@@ -674,7 +694,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   // sixteenth after that.  Measured on the 64-row tile (us; one start, one per XCD, this): 8 experts, 4 rows, FC1 of 4096 x
   // 14336 334, 303, 304, FC2 180, 168, 155; 64 experts, 32 rows, FC1 of 2048 x 1408 164, 143, 143; 8 experts, 8 rows, FC1 of
   // 2048 x 8192 116, 96, 97.  A start of its own for every workgroup of an XCD: 362, 159, 141, 106.
-  constexpr bool KROT = (MODE == ROWSEG && BM <= 128) || STAGGER;
+  constexpr bool KROT = ((MODE == ROWSEG || MODE == DENSE) && BM <= 128) || STAGGER;
   // Issue the loads of k-step `ks` of the open tile into ring slot ks % NSTAGE.  Only the last step can be ragged.
   auto issue = [&](int ks) __attribute__((always_inline)) {
     if (!is_loader) return;
@@ -730,6 +750,9 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
     }
   };
   auto issue_prologue = [&]() __attribute__((always_inline)) {
+    // The targets of this wave's rows go to LDS ahead of the tile, without a register that the compiler would guard (a wait in front of the
+    // fragment reads): the waits of the k loop, which ends with nothing outstanding, cover them.
+    if constexpr (VOCAB) touch4s(reinterpret_cast<const char*>(p.target), (unsigned)min(m0 + wm * WTM + lane, p.M - 1) * 4u, target_lds);
 #pragma unroll
     for (int s = 0; s < NSTAGE - 1; ++s)
       if (s < nk) issue(s);
@@ -984,6 +1007,14 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
       fg_first = stage_fetch_bf16(hrow, 2L * p.N, m_end - mb, p.N - nb, lane);
       fu_first = stage_fetch_bf16(hrow + p.N, 2L * p.N, m_end - mb, p.N - nb, lane);
     }
+    int row_target[VOCAB ? FM : 1];
+    if constexpr (VOCAB) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) row_target[i] = *reinterpret_cast<const int*>(target_smem + (i * 16 + (lane & 15)) * 4);
+      wait_lgkmcnt0();                    // read before the next tile's arrive
+#pragma unroll
+      for (int i = 0; i < FM; ++i) asm volatile("" : "+v"(row_target[i]));
+    }
     slot += 1;
     __syncthreads();                      // every wave has read its last fragments: the ring is free
     const bool has_next = open_tile(slot);
@@ -1080,6 +1111,87 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
               const int n = n0 + wn * WTN + j * 16 + ((lane >> 4) << 2) + r;
               if (n < p.N) Cg[(long)m * p.ldc + n] = acc[i][j][r] + (p.bias ? p.bias[n] : 0.f);
             }
+        }
+      } else if constexpr (VOCAB) {
+        // Softmax over this wave's WTN columns of every row but the target's: maximum and sum of exp(z - maximum), which a later pass joins with
+        // the other waves'.  (The target's logit goes out by itself: in a row that is nearly certain of it, 1 - p is the sum of the others, which
+        // a sum that holds it would round away.)  EPI_CE also stores exp(z - maximum) in fp16: it lies in [0, 1], where fp16 keeps 11 bits (bf16 8) and its smallest step,
+        // 2^-24, is nothing beside the row's sum, which is at least 1 here; the pass that scales it rounds to bf16 once.
+        const int nb0 = n0 + wn * WTN, part = n0 / BN * WN + wn;
+        constexpr float LOG2E = 1.44269504088896341f, LOWEST = -3.402823466e38f;
+        if (nb0 + WTN > p.N) {                      // (uniform) columns past the width take no part
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (nb0 + j * 16 + ((lane >> 4) << 2) + r >= p.N)
+#pragma unroll
+                for (int i = 0; i < FM; ++i) acc[i][j][r] = -__builtin_inff();
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          const int mb = m0 + wm * WTM + i * 32;
+          const int rows_valid = m_end - mb;
+          if (rows_valid <= 0) continue;
+          float top[2], sum[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            f32x4 (&z)[FN] = acc[2 * i + h];
+            const int r_lane = h * 16 + (lane & 15);
+            // the target's logit, if it is one of this lane's, leaves the row
+            const int c = row_target[2 * i + h] - nb0;
+            float zt = 0.f;
+            const bool mine = r_lane < rows_valid && c >= 0 && c < WTN && nb0 + c < p.N && ((c >> 2) & 3) == lane >> 4;
+            if (__any(mine)) {
+#pragma unroll
+              for (int j = 0; j < FN; ++j) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  if (mine && (c >> 4 << 2 | (c & 3)) == j * 4 + r) {
+                    zt = z[j][r];
+                    z[j][r] = -__builtin_inff();
+                  }
+              }
+            }
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, zt), block_rsrc(p.z_target + mb), mine ? (unsigned)r_lane * 4u : BUF_OOB, 0, 0);
+            float m = LOWEST;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) m = fmaxf(m, z[j][r]);
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                z[j][r] = __builtin_amdgcn_exp2f((z[j][r] - m) * LOG2E);
+                s += z[j][r];
+              }
+            s += __shfl_xor(s, 16);
+            s += __shfl_xor(s, 32);
+            top[h] = m;
+            sum[h] = s;
+          }
+          typedef unsigned int u32x2v __attribute__((ext_vector_type(2)));
+          const u32x2v pair = {__builtin_bit_cast(unsigned, lane < 16 ? top[0] : top[1]), __builtin_bit_cast(unsigned, lane < 16 ? sum[0] : sum[1])};
+          __builtin_amdgcn_raw_buffer_store_b64(pair, block_rsrc(p.stats + ((long)mb * p.parts + part) * 2),
+                                                lane < 32 && lane < rows_valid ? (unsigned)lane * (unsigned)(p.parts * 8) : BUF_OOB, 0, 0);
+          if constexpr (EPI == EPI_CE) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+              const int nb = nb0 + j * 32, cols_valid = p.N - nb;
+              if (cols_valid <= 0) continue;
+              typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+              const Block b = block(i, j);
+              bf16x4 v[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                v[q] = __builtin_bit_cast(bf16x4, f16x4{(_Float16)b.q[q][0], (_Float16)b.q[q][1], (_Float16)b.q[q][2], (_Float16)b.q[q][3]});
+              stage_store_bf16(stg, v, static_cast<bf16*>(p.C) + (long)mb * p.ldc + nb, p.ldc, rows_valid, cols_valid, lane);
+            }
+          }
         }
       } else if constexpr (SWI) {
         // block 2j holds G and block 2j+1 holds U for the same 32 output columns

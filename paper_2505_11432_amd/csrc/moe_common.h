@@ -77,6 +77,9 @@ struct GemmProblem {
   // fp32 products of mode 0 may be cut along K, the parts going here: scratch_floats floats, or NULL (no cutting)
   float* scratch; size_t scratch_floats;
   long part_stride;                          // (kernel argument: floats from one part to the next)
+  // operands padded in memory: rows of B that exist where K runs along them (0: N; N may be up to the next multiple of 16), rows of C that
+  // exist in mode 1 (0: M)
+  int b_rows, c_rows;
 };
 bool gemm_f32_covers(const GemmProblem& p);      // the operands can be read in 16-byte pieces; launch_gemm_f32 needs that
 int launch_gemm_f32(const GemmProblem& p, hipStream_t s);
@@ -157,6 +160,16 @@ int mfma_router_fwd(const void* x, const void* w_r, const float* bias, int T, in
 int mfma_router_dwr(const void* g, const void* x, const int32_t* chunk_offsets, int chunks, int E, int d, float* partial,
                     int accumulate, hipStream_t s);
 int mfma_router_dx(const void* g, const void* w_r, int T, int d, int E, void* dx, hipStream_t s);
+// vocabulary products in bf16 (gemm_mfma.hip); `rows` is read on the device
+struct VocabTiles { int parts, shift; };           // pairs of softmax statistics per row, each of 2^shift columns
+VocabTiles mfma_vocab_tiles(int R, int V, int d);
+int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const int32_t* target, int R, int V, int d, void* P, long ldp,
+                       float* stats, float* z_target, hipStream_t s);
+struct VocabDxPlan { bool full; int parts, kpart; };
+VocabDxPlan mfma_vocab_dx_plan(int R, int V, int d);
+int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, int R, int V, int d, float* out, hipStream_t s);
+int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* range, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate,
+                  hipStream_t s);
 size_t router_bwd_ws_bytes(int T, int d, int E);
 int mfma_configure_all();          // per-device set-up of every grouped-GEMM kernel (moe_init)
 int route_noalloc_prepare();       // looks up this device's static routing scratch (moe_init)

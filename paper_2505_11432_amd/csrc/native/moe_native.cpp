@@ -103,7 +103,7 @@ PyMethodDef methods[] = {
     MOE_BOUND(moe_route_bwd), MOE_BOUND(moe_dispatch), MOE_BOUND(moe_combine), MOE_BOUND(moe_gate_grad),
     MOE_BOUND(moe_expert_ffn_fwd), MOE_BOUND(moe_expert_ffn_bwd), MOE_BOUND(moe_row_map), MOE_BOUND(moe_expert_ffn_fused_fwd),
     MOE_BOUND(moe_expert_ffn_fused_bwd), MOE_BOUND(moe_quant_fp8), MOE_BOUND(moe_dequant_fp8), MOE_BOUND(moe_quant_fp8_tgroup),
-    MOE_BOUND(moe_transpose), {nullptr, nullptr, 0, nullptr}};
+    MOE_BOUND(moe_transpose), MOE_BOUND(moe_vocab_score), MOE_BOUND(moe_vocab_loss), MOE_BOUND(moe_grad_clip), MOE_BOUND(moe_adamw), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_moe_native", "Calls of the MoE library on torch tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,30 @@
+// What the entry points (api_train.hip) and the kernels (vocab_loss.hip) of the vocabulary loss share.
+#pragma once
+#include "moe_common.h"
+
+namespace moe {
+
+struct VocabCounts { int n; };          // rows that count
+
+// Layout of a workspace (offsets in bytes) and the choices that follow from sizes alone
+struct VocabPlan {
+  int R, pieces;                 // rows of a piece
+  long ld;                       // elements of a row of G (whole 128-byte lines)
+  bool gather;                   // the rows that count are gathered first
+  bool twice;                    // d_w's contraction holds what the rounding of G left as further rows
+  bool dw_sum_used;              // several pieces add up d_w in fp32 before it is rounded to bf16
+  VocabTiles tiles;              // bf16: statistics per row
+  size_t counts, ranges, token, target_of, xc, G, stats, z_target, weighted, rest, dxc, dx_parts, dx_floats, dw_sum, bytes;
+};
+VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int piece_rows, bool grad);
+
+struct VocabProblem {
+  const void* x; const void* w; const int32_t* target; const float* token_w;
+  int T, d, V; moe_dtype dt;
+  float* loss; float* lse;
+  bool grad;
+  float* total; void* dx; void* d_w; moe_dtype grad_dt; int accumulate;
+};
+int launch_vocab_loss(const VocabProblem& q, const VocabPlan& p, char* ws, hipStream_t s);
+
+}  // namespace moe
