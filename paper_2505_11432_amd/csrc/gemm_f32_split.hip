@@ -564,13 +564,16 @@ int launch(const GemmProblem& p, F32Plan plan, hipStream_t s) {
 
 }  // namespace
 
-// Operands that the kernel can take, where it is the faster way.
-bool gemm_f32_splits(const GemmProblem& p) {
+// Operands that the kernel can take
+static bool takes(const GemmProblem& p) {
   if (p.mode == 2 || p.bias || !aligned16(p.C) || p.N % 4 || p.ldc % 4 || p.c_es % 4) return false;
   const long lda = p.a_cs == 1 ? p.a_rs : p.a_cs, ldb = p.b_rs == 1 ? p.b_cs : p.b_rs;
   if (lda >= 1 << 20 || ldb >= 1 << 20) return false;                   // 128 rows of a tile span less than kSpan
-  if (f32_blocks(p, 64, 64) * 256 >= 1L << 31) return false;            // a launch holds less than 2^32 threads
-  return f32_split_pays({p.mode == 0, p.M, p.N, p.K, p.E});
+  return f32_blocks(p, 64, 64) * 256 < 1L << 31;                        // a launch holds less than 2^32 threads
+}
+// where it is the faster way as well
+bool gemm_f32_splits(const GemmProblem& p) {
+  return takes(p) && f32_split_pays({p.mode == 0, p.M, p.N, p.K, p.E});
 }
 
 int launch_gemm_f32_split(const GemmProblem& p, hipStream_t s) {
@@ -590,6 +593,14 @@ int launch_gemm_f32_split(const GemmProblem& p, hipStream_t s) {
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }
+
+// The parts of `plan` to C, C + M * ldc, ... (nobody adds them here); only for operands that gemm_f32_cuts takes.
+int launch_gemm_f32_cut(const GemmProblem& p, F32Plan plan, hipStream_t s) {
+  GemmProblem q = p;
+  q.part_stride = (long)p.M * p.ldc;
+  return launch(q, plan, s);
+}
+bool gemm_f32_cuts(const GemmProblem& p) { return takes(p); }
 
 // The tiles of eight waves need their dynamic-LDS limit raised once per device; moe_init does it ahead of a graph capture.  The
 // values are the same on every call, the bit only saves work.

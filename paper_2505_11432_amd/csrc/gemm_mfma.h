@@ -18,8 +18,8 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 enum Layout { KMAJOR = 0, MNMAJOR = 1 };
-// PLAIN: one dense GEMM, no expert segments.  DENSE: the same with the number of rows read on the device and the contraction cut into
-// E parts, each with a result of its own (the vocabulary products)
+// PLAIN: one dense GEMM, no expert segments.  DENSE: the same with the number of rows, or the length of the contraction, read on the device, and
+// the tiles of the last round cut along the contraction (the vocabulary products)
 enum Mode { ROWSEG = 0, KSEG = 1, PLAIN = 2, DENSE = 3 };
 // EPI_SWIGLU_W / EPI_SWIGLU_BWD_W: the Section 4.1 operator order (gate weight multiplied right after SwiGLU; the
 // forward one also selects its A rows through an index map, Section 4.2)
@@ -61,8 +61,9 @@ struct Args {
   float* dw_part;                    // EPI_SWIGLU_BWD_W: [n-tiles * waves along n][M] partial sums of <dA'[r,:], A[r,:]>
   // vocabulary products
   const int32_t* rows;               // DENSE: number of rows (at most M, the rows that A and C have room for), or NULL for M
-  int kpart;                         // DENSE: contraction of one of the E parts (whole k-steps); part e writes C + e * c_es
-  int c_rows;                        // KSEG: rows of C where A is padded to M columns (0: M)
+  const int32_t* k_rows;             // DENSE: length of the contraction (at most K), or NULL for K
+  int c_rows;                        // DENSE: rows of C where an M-major A is padded to M columns (0: M)
+  CutCost cut;                       // DENSE: costs by which the last round's tiles are cut; the parts go to splitk_ws (NULL: no cutting)
   float* stats; int parts;           // EPI_LSE, EPI_CE: [M][parts] pairs of maximum and sum of exp(logit - maximum), one per n-tile and wave along n
   const int32_t* target;             // EPI_LSE, EPI_CE: [M] column whose logit goes to z_target [M] (columns outside the width: none)
   float* z_target;

@@ -88,7 +88,9 @@ int launch(const Args& a, long tiles_upper_bound, hipStream_t s) {
   if constexpr (dma_in_pairs<BM, BN, BKT, NS, WM * WN, LA, LB, (int)sizeof(TIN)>()) blocks *= 2;
   Args args = a;
   constexpr bool kSplitK = MODE == ROWSEG && EPI == EPI_STORE && sizeof(TC) == 2;
-  if (!kSplitK || args.accumulate || blocks > MOE_SPLITK_MAX_PARTS) args.splitk_ws = nullptr;
+  if constexpr (MODE != DENSE) {
+    if (!kSplitK || args.accumulate || blocks > MOE_SPLITK_MAX_PARTS) args.splitk_ws = nullptr;
+  }
   kern<<<dim3((unsigned)blocks), dim3(WM * WN * 64), smem, s>>>(args);
   MOE_LAUNCH_CHECK();
   if constexpr (kSplitK) {
@@ -332,7 +334,7 @@ int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const 
   a.A = x; a.lda = d;
   a.B = w; a.ldb = d;
   a.C = P; a.ldc = ldp;
-  a.E = 1; a.M = R; a.N = V; a.K = d; a.kpart = d;
+  a.E = 1; a.M = R; a.N = V; a.K = d;
   a.rows = rows; a.target = target; a.stats = stats; a.z_target = z_target; a.parts = mfma_vocab_tiles(R, V, d).parts;
   const RowTile tile = vocab_tile(R, V, d);
   if (P) {
@@ -345,53 +347,87 @@ int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const 
   return launch<256, 256, 64, 2, 4, 2, KMAJOR, KMAJOR, DENSE, EPI_LSE, bf16>(a, 1, s);
 }
 
-// dx = G w, [R, V] by [V, d], contracted over the vocabulary: few tiles of a very long contraction, so that it is cut into parts (fp32, part e at
-// out + e * R * d) that the pass which rounds and places the rows adds up.
+// Costs of their tiles (row_plan.h): dx on 256 x 256 and on 128 x 128, whose parts the pass that rounds and places the rows reads anyway; d_w on
+// 256 x 256 and on 128 x 128 in pairs of workgroups, whose parts take a launch.
+namespace {
+constexpr CutCost kDxFull = {13000, 1500, 105, 0}, kDxMid = {6000, 660, 26, 0}, kDwFull = {13000, 1500, 105, 4000}, kDwPair = {11000, 750, 26, 4000};
+constexpr int kPlanGroups = 256;            // workgroups that sizes are worked out for: one per CU
+}  // namespace
+
 VocabDxPlan mfma_vocab_dx_plan(int R, int V, int d) {
-  // rounds of the tiles (times as in row_plan.h) and the parts' way through memory and back at 5 TB/s
-  VocabDxPlan best{};
-  double best_us = 0;
-  for (const bool full : {true, false}) {
-    const int b = full ? 256 : 128, steps = cdiv(V, 64);
-    const long tiles = (long)cdiv(R, b) * cdiv(d, b);
-    for (int parts = 1; parts <= 32 && (parts == 1 || steps / parts >= 8); ++parts) {
-      const int each = cdiv(steps, parts), real = cdiv(steps, each);
-      const double rounds = (double)((tiles * real + 255) / 256);
-      const double us = rounds * (full ? 13 + 1.5 * each : 6 + 0.66 * each) + real * (double)R * d * 8 / 5e6;
-      if (best.parts == 0 || us < best_us) {
-        best = {full, real, each * 64};
-        best_us = us;
-      }
-    }
-  }
-  return best;
+  const int steps = cdiv(V, 64);
+  const long full = (long)cdiv(R, 256) * cdiv(d, 256), mid = (long)cdiv(R, 128) * cdiv(d, 128);
+  VocabDxPlan p{};
+  p.tile = dense_ns(mid, kPlanGroups, steps, kDxMid) < dense_ns(full, kPlanGroups, steps, kDxFull) ? 128 : 256;
+  p.cost = p.tile == 256 ? kDxFull : kDxMid;
+  p.part_floats = (size_t)cut_items(p.tile == 256 ? full : mid, kPlanGroups, steps) * p.tile * p.tile;
+  return p;
 }
-int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, int R, int V, int d, float* out, hipStream_t s) {
-  const VocabDxPlan plan = mfma_vocab_dx_plan(R, V, d);
+// out [R][d] fp32 gets the whole tiles, `parts` the others' parts; *groups is what dense_plan needs to know which they are
+int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, int R, int V, int d, const VocabDxPlan& plan, float* out, float* parts,
+                  int* groups, hipStream_t s) {
+  int dev = 0;
+  MOE_HIP_TRY(hipGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return MOE_ERR_UNSUPPORTED;
+  int rc = persistent_grid(dev, groups);
+  if (rc != MOE_OK) return rc;
+  if (*groups > kPlanGroups) return MOE_ERR_UNSUPPORTED;
   Args a{};
   a.A = G; a.lda = ldg;
   a.B = w; a.ldb = d;
-  a.C = out; a.ldc = d; a.c_es = (long)R * d;
-  a.E = plan.parts; a.M = R; a.N = d; a.K = V; a.kpart = plan.kpart;
-  a.rows = rows;
-  if (plan.full) return launch<256, 256, 64, 2, 2, 4, KMAJOR, MNMAJOR, DENSE, EPI_STORE, float>(a, 1, s);
+  a.C = out; a.ldc = d;
+  a.E = 1; a.M = R; a.N = d; a.K = V;
+  a.rows = rows; a.cut = plan.cost; a.splitk_ws = parts;
+  if (plan.tile == 256) return launch<256, 256, 64, 2, 2, 4, KMAJOR, MNMAJOR, DENSE, EPI_STORE, float>(a, 1, s);
   return launch<128, 128, 64, 3, 4, 2, KMAJOR, MNMAJOR, DENSE, EPI_STORE, float>(a, 1, s);
 }
 
-// d_w (+)= G^T x over the rows of range[0] .. range[1] - 1 (device); R bounds their number.  G [rows, ldg] with ldg a multiple of 8, V <= ldg.
-int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* range, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate,
+// d_w (+)= G^T x over *rows rows (device; at most R).  G [R, ldg] with ldg a multiple of 8, V <= ldg.
+namespace {
+bool vocab_dw_pairs(int R, int V, int d) {
+  const int steps = cdiv(R, 64);
+  const long full = (long)cdiv(V, 256) * cdiv(d, 256), small = (long)cdiv(V, 128) * cdiv(d, 128);
+  // (in long lists the estimate is too near to go by: 102400 words, 2048 wide, 8200 rows in pairs 4270 us, else 2760)
+  return full <= 2 * kPlanGroups && dense_ns(small, 2 * kPlanGroups, steps, kDwPair) < dense_ns(full, kPlanGroups, steps, kDwFull);
+}
+template <int BM, typename TC> int launch_dense_dw(const Args& a, int groups, int most_tiles, hipStream_t s) {
+  int rc;
+  if constexpr (BM == 256) rc = launch<256, 256, 64, 2, 2, 4, MNMAJOR, MNMAJOR, DENSE, EPI_STORE, TC>(a, 1, s);
+  else rc = launch<128, 128, 64, 2, 2, 2, MNMAJOR, MNMAJOR, DENSE, EPI_STORE, TC>(a, 1, s);
+  if (rc != MOE_OK || !a.splitk_ws) return rc;
+  dense_fixup_kernel<BM, BM, TC><<<dim3((unsigned)most_tiles * 16), dim3(256), 0, s>>>(a.splitk_ws, a.k_rows, a.c_rows, a.N, a.K, 64, groups, a.cut, a.accumulate,
+                                                                                   static_cast<TC*>(a.C), a.ldc);
+  MOE_LAUNCH_CHECK();
+  return MOE_OK;
+}
+}  // namespace
+size_t mfma_vocab_dw_part_floats(int R, int V, int d) {
+  const bool pairs = vocab_dw_pairs(R, V, d);
+  const int b = pairs ? 128 : 256, groups = pairs ? 2 * kPlanGroups : kPlanGroups;
+  return (size_t)cut_items((long)cdiv(V, b) * cdiv(d, b), groups, cdiv(R, 64)) * b * b;
+}
+int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
                   hipStream_t s) {
+  int dev = 0, groups = 0;
+  MOE_HIP_TRY(hipGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return MOE_ERR_UNSUPPORTED;
+  int rc = persistent_grid(dev, &groups);
+  if (rc != MOE_OK) return rc;
+  if (groups > kPlanGroups) return MOE_ERR_UNSUPPORTED;
+  const bool pairs = vocab_dw_pairs(R, V, d);
+  if (pairs) groups *= 2;
   Args a{};
   a.A = G; a.lda = ldg;
   a.B = x; a.ldb = d;
-  a.C = d_w; a.ldc = d; a.offsets = range; a.E = 1; a.M = (int)ldg; a.N = d; a.c_rows = V;
+  a.C = d_w; a.ldc = d; a.k_rows = rows; a.E = 1; a.M = (int)ldg; a.c_rows = V; a.N = d; a.K = R;
   a.accumulate = accumulate;
-  if (wgrad_in_pairs(R, 1, V, d)) {
-    if (dt == MOE_F32) return launch<128, 128, 64, 2, 2, 2, MNMAJOR, MNMAJOR, KSEG, EPI_STORE, float>(a, 1, s);
-    return launch<128, 128, 64, 2, 2, 2, MNMAJOR, MNMAJOR, KSEG, EPI_STORE, bf16>(a, 1, s);
-  }
-  if (dt == MOE_F32) return launch<256, 256, 64, 2, 2, 4, MNMAJOR, MNMAJOR, KSEG, EPI_STORE, float>(a, 1, s);
-  return launch<256, 256, 64, 2, 2, 4, MNMAJOR, MNMAJOR, KSEG, EPI_STORE, bf16>(a, 1, s);
+  a.cut = pairs ? kDwPair : kDwFull;
+  const long tiles = (long)cdiv(V, pairs ? 128 : 256) * cdiv(d, pairs ? 128 : 256);
+  const int rem = (int)(tiles % groups);
+  // with fewer rows than R the device may cut less or into other parts; where R itself is not worth cutting, no launch is made for it
+  if (rem != 0 && cut_parts(rem, groups, cdiv(R, 64), a.cut) > 1) a.splitk_ws = parts;
+  if (pairs) return dt == MOE_F32 ? launch_dense_dw<128, float>(a, groups, rem, s) : launch_dense_dw<128, bf16>(a, groups, rem, s);
+  return dt == MOE_F32 ? launch_dense_dw<256, float>(a, groups, rem, s) : launch_dense_dw<256, bf16>(a, groups, rem, s);
 }
 
 // Sets up every grouped-GEMM kernel of this library for the current device (see moe_init).

@@ -28,6 +28,7 @@
 #pragma once
 #include <type_traits>
 
+#include "dense_plan.h"
 #include "gemm_mfma.h"
 #include "row_plan.h"
 
@@ -353,6 +354,44 @@ __global__ void __launch_bounds__(256) splitk_fixup_kernel(const float* __restri
   }
 }
 
+// Adds the parts of a dense product's cut tiles: 16 workgroups per tile, BM / 16 rows each, as many tiles as the launch could have cut.
+template <int BM, int BN, typename TC>
+__global__ void __launch_bounds__(256) dense_fixup_kernel(const float* __restrict__ parts, const int32_t* __restrict__ k_rows, int M, int N, int K, int bkt,
+                                                          int groups, CutCost cost, int accumulate, TC* __restrict__ C, long ldc) {
+  const int k_all = k_rows ? max(min(*k_rows, K), 0) : K;
+  const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
+  const DensePlan cut = dense_plan(tiles_m * tiles_n, groups, (k_all + bkt - 1) / bkt, cost, true);
+  const int r_tile = blockIdx.x / 16, slice = blockIdx.x % 16;
+  int l = cut.full_tiles + r_tile;
+  if (cut.split == 1 || l >= tiles_m * tiles_n) return;
+  const int ng = l / (tiles_m * kDenseGroupN), r = l - ng * tiles_m * kDenseGroupN, gw = min(kDenseGroupN, tiles_n - ng * kDenseGroupN);
+  const int mt = r / gw, nt = ng * kDenseGroupN + (r - mt * gw), m0 = mt * BM, n0 = nt * BN;
+  const float* base = parts + (long)r_tile * cut.split * (BM * BN);
+  constexpr int ROWS = BM / 16;
+  for (int i = threadIdx.x; i < ROWS * BN / 8; i += 256) {
+    const int row = slice * ROWS + i / (BN / 8), col = i % (BN / 8) * 8;
+    if (m0 + row >= M || n0 + col >= N) continue;          // N is a multiple of 8
+    f32x4 v[2] = {};
+    const float* src = base + row * BN + col;
+    for (int s = 0; s < cut.split; ++s, src += BM * BN) {
+      v[0] += *reinterpret_cast<const f32x4*>(src);
+      v[1] += *reinterpret_cast<const f32x4*>(src + 4);
+    }
+    TC* dst = C + (long)(m0 + row) * ldc + n0 + col;
+    if constexpr (sizeof(TC) == 4) {
+      f32x4* d4 = reinterpret_cast<f32x4*>(dst);
+      d4[0] = accumulate ? v[0] + d4[0] : v[0];
+      d4[1] = accumulate ? v[1] + d4[1] : v[1];
+    } else {
+      bf16x8 o, old = {};
+      if (accumulate) old = *reinterpret_cast<const bf16x8*>(dst);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) o[q] = static_cast<bf16>(accumulate ? v[q >> 2][q & 3] + static_cast<float>(old[q]) : v[q >> 2][q & 3]);
+      *reinterpret_cast<bf16x8*>(dst) = o;
+    }
+  }
+}
+
 template <int BM, int BN, int BKT, int NSTAGE, int NW, Layout LA, Layout LB, int ESZ = 2>
 constexpr int dma_smem_bytes(bool targets = false) {
   // the ring, the per-expert tile table and one epilogue patch per wave
@@ -411,7 +450,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   // nothing, or an unknown number
   enum { EPI_UNKNOWN = 0, EPI_ALL = 1, EPI_NONE = 2 };
   int epi_state = EPI_NONE;
-  constexpr int GN = 8, XCDS = 8;   // GN n-tiles per group: a window of 32 tiles is 4 m-tiles x 8 n-tiles (measured against 8 x 4, 16 x 2, 2 x 16)
+  constexpr int GN = kDenseGroupN, XCDS = 8;   // GN n-tiles per group: a window of 32 tiles is 4 m-tiles x 8 n-tiles (measured against 8 x 4, 16 x 2, 2 x 16)
   static_assert(A_BYTES % (1024 * NL) == 0 && B_BYTES % (1024 * NL) == 0, "tile does not split over the loader waves");
   static_assert(NSTAGE >= 2 && (NSTAGE - 2) * LOADS < 64, "pipeline depth exceeds the vmcnt range");
   static_assert(!SWI || TN % 2 == 0, "SwiGLU pairs gate/up MFMA tiles inside a wave");
@@ -445,9 +484,11 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   // XCDs work on eight neighbouring windows, mostly the next m-tiles of the same n-tiles, i.e. the same B
   // panels (shared through the Infinity Cache) and disjoint A panels.
   const int tiles_n = (p.N + BN_OUT - 1) / BN_OUT;
-  int m_rows = p.M;                                           // KSEG / PLAIN / DENSE
+  int m_rows = p.M, k_all = p.K;                              // KSEG / PLAIN / DENSE
   if constexpr (MODE == DENSE) {
     if (p.rows) m_rows = __builtin_amdgcn_readfirstlane(max(min(*p.rows, p.M), 0));
+    if (p.k_rows) k_all = __builtin_amdgcn_readfirstlane(max(min(*p.k_rows, p.K), 0));
+    if (p.c_rows) m_rows = p.c_rows;
   }
   const int tiles_m_fixed = (m_rows + BM - 1) / BM;
   int total_tiles;
@@ -455,15 +496,18 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
     tile_table<BM>(p.offsets, p.E, cum_tiles);
     __syncthreads();
     total_tiles = __builtin_amdgcn_readfirstlane(cum_tiles[p.E]) * tiles_n;
-  } else if constexpr (MODE == KSEG || MODE == DENSE) {
+  } else if constexpr (MODE == KSEG) {
     total_tiles = p.E * tiles_m_fixed * tiles_n;
   } else {
     total_tiles = tiles_m_fixed * tiles_n;
   }
   // split-K plan for the partly filled last round (see Args::splitk_ws); identical arithmetic in splitk_fixup_kernel
-  constexpr bool SPLITK = MODE == ROWSEG && EPI == EPI_STORE && sizeof(TC) == 2;
+  constexpr bool SPLITK = (MODE == ROWSEG && EPI == EPI_STORE && sizeof(TC) == 2) || (MODE == DENSE && EPI == EPI_STORE);
   int full_tiles = total_tiles, split = 1, total_items = total_tiles;
-  if constexpr (SPLITK) {
+  if constexpr (SPLITK && MODE == DENSE) {
+    const DensePlan cut = dense_plan(total_tiles, (int)gridDim.x, (k_all + BKT - 1) / BKT, p.cut, p.splitk_ws != nullptr);
+    full_tiles = cut.full_tiles; split = cut.split; total_items = cut.items;
+  } else if constexpr (SPLITK) {
     if (p.splitk_ws != nullptr) splitk_plan(total_tiles, (int)gridDim.x, (p.K + BKT - 1) / BKT, full_tiles, split, total_items);
   }
   const int xcd = blockIdx.x % XCDS;
@@ -504,10 +548,10 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   // slower); at the end of the step they gain 1.2 to 3 %; one or two steps further ahead: no change; touching the B
   // panel as well, or half of A, or from two waves: slower again (each touch instruction costs the address unit as
   // much as a 1 KB tile load).  Not for e4m3 operands: half the time per k-step for the same loads, touches cost 2 %.
-  constexpr bool TOUCH = (MODE == ROWSEG || MODE == DENSE) && NSTAGE == 2 && SPLIT && !FP8;
+  constexpr bool TOUCH = (MODE == ROWSEG || (MODE == DENSE && LA == KMAJOR)) && NSTAGE == 2 && SPLIT && !FP8;
   // the same for the bf16 weight-gradient kernel (four stages of 32 k-rows): two k-steps per touch, every other step
   constexpr bool TOUCH_K = MODE == KSEG && !FP8 && SPLIT && LA == MNMAJOR && LB == MNMAJOR && NSTAGE == 4;
-  constexpr bool TOUCH_K2 = MODE == KSEG && !FP8 && SPLIT && LA == MNMAJOR && LB == MNMAJOR && NSTAGE == 2 && BKT == 64;
+  constexpr bool TOUCH_K2 = (MODE == KSEG || MODE == DENSE) && !FP8 && SPLIT && LA == MNMAJOR && LB == MNMAJOR && NSTAGE == 2 && BKT == 64;
   const bool is_toucher = (TOUCH || TOUCH_K || TOUCH_K2) && wave == NL;
   const unsigned lds_dump = smem_lds + RING_BYTES + TABLE_BYTES + NW * STG_BYTES;
   const unsigned scale_lds = lds_dump + 256;                                   // block-scale ring: 2 stages x (256 + 256) bytes
@@ -570,9 +614,6 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
       e = l / (mt_e * tiles_n);          // always 0 in PLAIN mode
       l -= e * mt_e * tiles_n;
       m_lo = 0; m_hi = m_rows;
-      if constexpr (MODE == KSEG) {
-        if (p.c_rows) m_hi = p.c_rows;
-      }
     }
     const int ng = l / (mt_e * GN);
     const int r = l - ng * mt_e * GN;
@@ -589,8 +630,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
     }
     int k_begin, k_end;
     if constexpr (MODE == KSEG) { k_begin = p.offsets[e]; k_end = p.offsets[e + 1]; }
-    else if constexpr (MODE == DENSE) { k_begin = e * p.kpart; k_end = min(p.K, k_begin + p.kpart); }
-    else { k_begin = 0; k_end = p.K; }
+    else { k_begin = 0; k_end = k_all; }
     klen = k_end - k_begin;
     nk = (klen + BKT - 1) / BKT;
     if (part_slot >= 0) {            // this item covers k-steps [s0, s1) of the tile
@@ -694,7 +734,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   // sixteenth after that.  Measured on the 64-row tile (us; one start, one per XCD, this): 8 experts, 4 rows, FC1 of 4096 x
   // 14336 334, 303, 304, FC2 180, 168, 155; 64 experts, 32 rows, FC1 of 2048 x 1408 164, 143, 143; 8 experts, 8 rows, FC1 of
   // 2048 x 8192 116, 96, 97.  A start of its own for every workgroup of an XCD: 362, 159, 141, 106.
-  constexpr bool KROT = ((MODE == ROWSEG || MODE == DENSE) && BM <= 128) || STAGGER;
+  constexpr bool KROT = ((MODE == ROWSEG || (MODE == DENSE && LA == KMAJOR)) && BM <= 128) || STAGGER;
   // Issue the loads of k-step `ks` of the open tile into ring slot ks % NSTAGE.  Only the last step can be ragged.
   auto issue = [&](int ks) __attribute__((always_inline)) {
     if (!is_loader) return;

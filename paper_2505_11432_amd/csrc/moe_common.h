@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "../../include/moe.h"
+#include "row_plan.h"
 
 namespace moe {
 
@@ -83,6 +84,8 @@ struct GemmProblem {
 };
 bool gemm_f32_covers(const GemmProblem& p);      // the operands can be read in 16-byte pieces; launch_gemm_f32 needs that
 int launch_gemm_f32(const GemmProblem& p, hipStream_t s);
+bool gemm_f32_cuts(const GemmProblem& p);        // launch_gemm_f32_cut can take the operands
+int launch_gemm_f32_cut(const GemmProblem& p, F32Plan plan, hipStream_t s);
 int launch_gemm_f32_fc2(const GemmProblem& fc2, const void* H, void* A, hipStream_t s);
 int launch_gemm_f32_dgrad2(const GemmProblem& dgrad2, const void* H, void* dH, void* A, hipStream_t s);
 int launch_gemm_f32_trio(const GemmProblem& dw2, const GemmProblem& dxp, const GemmProblem& dw1, hipStream_t s);
@@ -165,10 +168,12 @@ struct VocabTiles { int parts, shift; };           // pairs of softmax statistic
 VocabTiles mfma_vocab_tiles(int R, int V, int d);
 int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const int32_t* target, int R, int V, int d, void* P, long ldp,
                        float* stats, float* z_target, hipStream_t s);
-struct VocabDxPlan { bool full; int parts, kpart; };
+struct VocabDxPlan { int tile; CutCost cost; size_t part_floats; };
 VocabDxPlan mfma_vocab_dx_plan(int R, int V, int d);
-int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, int R, int V, int d, float* out, hipStream_t s);
-int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* range, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate,
+int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, int R, int V, int d, const VocabDxPlan& plan, float* out, float* parts,
+                  int* groups, hipStream_t s);
+size_t mfma_vocab_dw_part_floats(int R, int V, int d);
+int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
                   hipStream_t s);
 size_t router_bwd_ws_bytes(int T, int d, int E);
 int mfma_configure_all();          // per-device set-up of every grouped-GEMM kernel (moe_init)

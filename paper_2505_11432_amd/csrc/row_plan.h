@@ -150,6 +150,37 @@ inline bool wgrad_in_pairs(int rows, int E, int M, int N) {
   return pairs_us(small, {11, 0.75, 6, 0.8}, steps) < rounds * (9.5 + 1.5 * steps) + 6.5 * large / 256;
 }
 
+// ---- dense products (the vocabulary's): one long contraction and any number of tiles, so that the last round may leave most CUs idle.  Its `rem`
+// tiles are cut along their `steps` k-steps into parts that run on different workgroups and write fp32 tiles, which another kernel adds up: 1 to
+// 64 parts, of four steps at least, by the time of the rounds.  The number of rows is known on the device only, so the choice is made there, by
+// every kernel that needs it.
+struct CutCost { int fixed, step, part, extra; };      // ns: of a tile, of a k-step, of a part's way through memory and back (whole chip), of cutting at all
+constexpr int kCutMost = 64, kCutItems = 4;            // parts of a tile; items of the last round, in rounds
+constexpr long long kCutNever = 1LL << 60;
+constexpr long long cut_ns(int parts, int rem, int groups, int steps, CutCost c) {
+  if (parts <= 1) return c.fixed + (long long)c.step * steps;
+  if (parts > kCutMost || parts * 4 > steps || rem * parts > kCutItems * groups) return kCutNever;
+  const int rounds = (rem * parts + groups - 1) / groups, each = (steps + parts - 1) / parts;
+  return (long long)rounds * (c.fixed + (long long)c.step * each) + (long long)rem * parts * c.part + c.extra;
+}
+inline int cut_parts(int rem, int groups, int steps, CutCost c) {
+  int best = 1;
+  for (int s = 2; s <= kCutMost; ++s)
+    if (cut_ns(s, rem, groups, steps, c) < cut_ns(best, rem, groups, steps, c)) best = s;
+  return best;
+}
+// estimated time of a whole launch, ns
+inline double dense_ns(long tiles, int groups, int steps, CutCost c) {
+  const int rem = (int)(tiles % groups);
+  const double whole = (double)(tiles / groups) * (c.fixed + (double)c.step * steps);
+  return rem == 0 ? whole : whole + (double)cut_ns(cut_parts(rem, groups, steps, c), rem, groups, steps, c);
+}
+// most parts that a launch of up to `tiles` tiles of up to `steps` k-steps writes
+inline long cut_items(long tiles, int groups, int steps) {
+  const long rem = tiles < groups ? tiles : groups - 1, parts = steps / 4 < kCutMost ? steps / 4 : kCutMost;
+  return rem * parts < (long)kCutItems * groups ? rem * parts : (long)kCutItems * groups;
+}
+
 // ---- fp32 expert products (gemm_f32_split.hip): the split into bf16 parts or the fp32 instruction, 64 x 64 or 128 x 128 tiles.
 constexpr int kF32SplitStep = 32;        // contraction per step
 struct F32Product { bool rows; int M, N, K, E; };      // rows: the segments lie along M (forward, dgrad), else along K (weight gradients)
@@ -242,6 +273,25 @@ inline F32Plan f32_plan(const F32Product& p, long room) {
     if (us < best_us) {
       best_us = us;
       best = {us128 < us64 ? F32_128 : F32_64, n};
+    }
+  }
+  return best;
+}
+
+// Products whose parts the caller adds up in a pass that it makes anyway (the fp32 vocabulary products): up to `room` parts of at least four steps,
+// by the time of the rounds and the parts' way through memory and back.
+inline F32Plan f32_cut_plan(const F32Product& p, long room) {
+  const int steps = f32_steps(p);
+  const double t64 = f32_tiles64(p), t128 = f32_tiles128(p);
+  F32Plan best = {F32_64, 1};
+  double best_us = 1e30;
+  for (int n = 1; n <= 32 && (n == 1 || (n <= room && steps / n >= 4)); ++n) {
+    const int each = (steps + n - 1) / n;
+    const double way = n * (double)p.M * p.N * 8 / 5e6, us64 = f32_us64(t64 * n, each) + way, us128 = f32_us128(t128 * n, each) + way;
+    const double us = us128 < us64 && t128 * n > 1.5 * 256 ? us128 : us64;
+    if (us < best_us) {
+      best_us = us;
+      best = {us == us64 ? F32_64 : F32_128, n};
     }
   }
   return best;

@@ -14,7 +14,8 @@ struct VocabPlan {
   bool twice;                    // d_w's contraction holds what the rounding of G left as further rows
   bool dw_sum_used;              // several pieces add up d_w in fp32 before it is rounded to bf16
   VocabTiles tiles;              // bf16: statistics per row
-  size_t counts, ranges, token, target_of, xc, G, stats, z_target, weighted, rest, dxc, dx_parts, dx_floats, dw_sum, bytes;
+  F32Plan z, dx, dw;             // fp32: parts of the products
+  size_t counts, ranges, token, target_of, xc, G, stats, z_target, weighted, rest, dxc, parts, dw_sum, bytes;
 };
 VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int piece_rows, bool grad);
 

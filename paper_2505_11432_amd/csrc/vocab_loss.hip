@@ -13,6 +13,7 @@
 // Rounding.  G is rounded to bf16 once, 2^-8 of an element at most.  In the column of the target it is nearly the whole row, and the rows of
 // few tokens would carry its rounding error undivided, so what the rounding took off (`rest`) is kept in fp32: dx gets rest * w[target] when its
 // parts are added, d_w one more row per token with rest in the target's column where the tokens are few (kFewRows), where that is free.
+#include "dense_plan.h"
 #include "moe_common.h"
 #include "vocab_loss.h"
 
@@ -74,11 +75,21 @@ __global__ void __launch_bounds__(1024) vocab_compact_kernel(const int32_t* __re
   for (int t0 = 0; t0 < T; t0 += 8192) {
     const int t = t0 + threadIdx.x * 8;
     int tg[8], mine = 0;
+    if (t + 8 <= T) {
+      typedef __attribute__((ext_vector_type(4))) int i32x4;
+      typedef i32x4 i32x4_u __attribute__((aligned(4)));
+      const i32x4 a = *reinterpret_cast<const i32x4_u*>(target + t), b = *reinterpret_cast<const i32x4_u*>(target + t + 4);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      tg[i] = t + i < T ? target[t + i] : -1;
-      mine += tg[i] >= 0 && tg[i] < V;
+      for (int i = 0; i < 4; ++i) {
+        tg[i] = a[i];
+        tg[4 + i] = b[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) tg[i] = t + i < T ? target[t + i] : -1;
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mine += tg[i] >= 0 && tg[i] < V;
     int incl = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -114,56 +125,112 @@ __global__ void __launch_bounds__(1024) vocab_compact_kernel(const int32_t* __re
   }
 }
 
-// The rows of a piece to the front of xc (a second time behind them for `twice`), a wave per row; with the first piece also the zeros of the
-// tokens left out.
 template <typename T_> struct Row16 { static constexpr int N = 16 / (int)sizeof(T_); };
+
+// The zeros of a token that is left out, by a wave
+template <typename TX> __device__ __forceinline__ void clear_token(int t, int d, float* loss, float* lse, TX* dx) {
+  const int lane = threadIdx.x & 63;
+  if (lane == 0) loss[t] = lse[t] = 0.f;
+  if (!dx) return;
+  u32x4* dst = reinterpret_cast<u32x4*>(dx + (long)t * d);
+  for (int i = lane; i < d / Row16<TX>::N; i += 64) dst[i] = u32x4{0u, 0u, 0u, 0u};
+}
+
+// Few tokens, one piece: compacting and gathering in one launch.  Every workgroup counts all targets and moves the rows of four tokens, a wave
+// each.  (131 tokens, 1040 wide, fp32: 9.4 us in two launches.)
 template <typename TX>
-__global__ void __launch_bounds__(256) vocab_gather_kernel(const TX* __restrict__ x, const int32_t* __restrict__ target, const int32_t* __restrict__ token,
-                                                           const int32_t* __restrict__ range, int T, int V, int d, int row0, int twice,
-                                                           TX* __restrict__ xc, float* __restrict__ loss, float* __restrict__ lse, TX* __restrict__ dx) {
-  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int vecs = d / Row16<TX>::N, n = range[1];
-  if (r < n) {
-    const u32x4* src = reinterpret_cast<const u32x4*>(x + (long)token[row0 + r] * d);
-    u32x4* dst = reinterpret_cast<u32x4*>(xc + (long)r * d);
-    u32x4* again = reinterpret_cast<u32x4*>(xc + (long)(n + r) * d);
-    for (int i = lane; i < vecs; i += 64) {
-      const u32x4 v = src[i];
-      dst[i] = v;
-      if (twice) again[i] = v;
-    }
+__global__ void __launch_bounds__(256) vocab_prepare_kernel(const TX* __restrict__ x, const int32_t* __restrict__ target, int T, int V, int d, int twice,
+                                                            int32_t* __restrict__ token, int32_t* __restrict__ target_of, VocabCounts* __restrict__ counts,
+                                                            int32_t* __restrict__ ranges, TX* __restrict__ xc, float* __restrict__ loss,
+                                                            float* __restrict__ lse, TX* __restrict__ dx) {
+  __shared__ int before[4], all[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * 4;
+  int lower = 0, kept = 0;                  // tokens that count: before this workgroup's, and all
+  for (int t = threadIdx.x; t < T; t += 256) {
+    const int tg = target[t], keeps = tg >= 0 && tg < V;
+    kept += keeps;
+    lower += keeps && t < first;
   }
-  if (row0 == 0 && r < T) {
-    const int tg = target[r];
-    if (tg < 0 || tg >= V) {
-      if (lane == 0) loss[r] = lse[r] = 0.f;
-      if (dx) {
-        u32x4* dst = reinterpret_cast<u32x4*>(dx + (long)r * d);
-        for (int i = lane; i < vecs; i += 64) dst[i] = u32x4{0u, 0u, 0u, 0u};
-      }
-    }
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    lower += __shfl_xor(lower, off);
+    kept += __shfl_xor(kept, off);
+  }
+  if (lane == 0) {
+    before[wave] = lower;
+    all[wave] = kept;
+  }
+  __syncthreads();
+  const int n = all[0] + all[1] + all[2] + all[3];
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    counts->n = n;
+    ranges[0] = ranges[2] = 0;
+    ranges[1] = n;
+    ranges[3] = 2 * n;
+  }
+  const int t = first + wave;
+  if (t >= T) return;
+  const int tg = target[t];
+  if (tg < 0 || tg >= V) {
+    clear_token(t, d, loss, lse, dx);
+    return;
+  }
+  int r = before[0] + before[1] + before[2] + before[3];
+  for (int i = first; i < t; ++i) r += target[i] >= 0 && target[i] < V;
+  if (lane == 0) {
+    token[r] = t;
+    target_of[r] = tg;
+  }
+  const u32x4* src = reinterpret_cast<const u32x4*>(x + (long)t * d);
+  u32x4* dst = reinterpret_cast<u32x4*>(xc + (long)r * d);
+  u32x4* again = reinterpret_cast<u32x4*>(xc + (long)(n + r) * d);
+  for (int i = lane; i < d / Row16<TX>::N; i += 64) {
+    const u32x4 v = src[i];
+    dst[i] = v;
+    if (twice) again[i] = v;
   }
 }
 
-// loss and lse of a row from its parts, a wave per row (forward only).  token: the row's token (NULL: rows are tokens).
+// The rows of a piece to the front of xc, a wave per row; with the first piece also the zeros of the tokens left out.
+template <typename TX>
+__global__ void __launch_bounds__(256) vocab_gather_kernel(const TX* __restrict__ x, const int32_t* __restrict__ target, const int32_t* __restrict__ token,
+                                                           const int32_t* __restrict__ range, int T, int V, int d, int row0, TX* __restrict__ xc,
+                                                           float* __restrict__ loss, float* __restrict__ lse, TX* __restrict__ dx) {
+  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6), n = range[1];
+  if (r < n) {
+    const u32x4* src = reinterpret_cast<const u32x4*>(x + (long)token[row0 + r] * d);
+    u32x4* dst = reinterpret_cast<u32x4*>(xc + (long)r * d);
+    for (int i = lane; i < d / Row16<TX>::N; i += 64) dst[i] = src[i];
+  }
+  if (row0 == 0 && r < T) {
+    const int tg = target[r];
+    if (tg < 0 || tg >= V) clear_token(r, d, loss, lse, dx);
+  }
+}
+
+// loss and lse of a row from its parts, WAVES waves per row (forward only).  token: the row's token (NULL: rows are tokens).
+template <int WAVES>
 __global__ void __launch_bounds__(256) vocab_score_kernel(const f32x2* __restrict__ stats, int parts, const float* __restrict__ z_target,
                                                           const int32_t* __restrict__ target, const int32_t* __restrict__ token,
                                                           const int32_t* __restrict__ range, int R, int V, float* __restrict__ loss, float* __restrict__ lse) {
-  const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  __shared__ f32x2 lds[4];
+  const int r = WAVES == 4 ? (int)blockIdx.x : (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), in_row = threadIdx.x & (64 * WAVES - 1);
   if (r >= (range ? min(range[1], R) : R)) return;
   const int t = token ? token[r] : r;
   if (!token && (target[r] < 0 || target[r] >= V)) {
-    if (lane == 0) loss[t] = lse[t] = 0.f;
+    if (in_row == 0) loss[t] = lse[t] = 0.f;
     return;
   }
+  const float zt = z_target[r];
   float m = kLowest, s = 0.f;
-  for (int i = lane; i < parts; i += 64) {
+  for (int i = in_row; i < parts; i += 64 * WAVES) {
     const f32x2 p = stats[(long)r * parts + i];
     join(m, s, p[0], p[1]);
   }
-  join_wave(m, s);
-  if (lane == 0) {
-    const RowLoss l = row_loss(z_target[r], m, s);
+  if constexpr (WAVES == 4) join_block(m, s, lds);
+  else join_wave(m, s);
+  if (in_row == 0) {
+    const RowLoss l = row_loss(zt, m, s);
     loss[t] = l.loss;
     lse[t] = l.lse;
   }
@@ -225,18 +292,24 @@ __global__ void __launch_bounds__(256) vocab_grad_rows_kernel(const f32x2* __res
   }
 }
 
-// fp32: the logits of a piece are in Z; loss and lse, and with GRAD G in their place.
+// fp32: the logits of a piece are in Z, in n_parts parts; loss and lse, and with GRAD G in the place of the first part.
 template <bool GRAD>
-__global__ void __launch_bounds__(256) vocab_rows_f32_kernel(float* __restrict__ Z, int V, long ld, RowOut o) {
+__global__ void __launch_bounds__(256) vocab_rows_f32_kernel(float* __restrict__ Z, int n_parts, long part_stride, int V, long ld, RowOut o) {
   __shared__ f32x2 lds[4];
   const int r = blockIdx.x;
   if (r >= o.range[1]) return;
   float* row = Z + (long)r * ld;
   const int t = o.token[r], tg = o.target_of[r];
-  const float zt = row[tg];
+  float zt = row[tg];
+  for (int p = 1; p < n_parts; ++p) zt += row[p * part_stride + tg];
+  if (n_parts > 1) __syncthreads();        // (the sums go over the first part)
   float m = kLowest, s = 0.f;
   for (int v = threadIdx.x * 4; v < V; v += 1024) {
     f32x4 z = *reinterpret_cast<const f32x4*>(row + v);
+    if (n_parts > 1) {
+      for (int p = 1; p < n_parts; ++p) z += *reinterpret_cast<const f32x4*>(row + p * part_stride + v);
+      if (GRAD) *reinterpret_cast<f32x4*>(row + v) = z;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (v + i >= V || v + i == tg) z[i] = -__builtin_inff();
@@ -262,19 +335,50 @@ __global__ void __launch_bounds__(256) vocab_rows_f32_kernel(float* __restrict__
   }
 }
 
-// dx of the piece's rows: the sum of the product's parts, with what the rounding of G took off in the target's column, rounded once.
-__global__ void __launch_bounds__(256) vocab_dx_kernel(const float* __restrict__ parts, int n_parts, long part_stride, const bf16* __restrict__ w, int d,
-                                                       const RowOut o, bf16* __restrict__ dx) {
-  const int vecs = d / 8;
-  const long total = (long)o.range[1] * vecs;
-  for (long i = blockIdx.x * 256L + threadIdx.x; i < total; i += gridDim.x * 256L) {
+// total = sum of the weighted losses, in a fixed order, in 64 bits, by one workgroup of 256
+__device__ __forceinline__ void sum_total(const float* __restrict__ weighted, int n, float* __restrict__ total) {
+  __shared__ double lds[4];
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  for (int i = threadIdx.x; i < n; i += 1024)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (i + q * 256 < n) s[q] += (double)weighted[i + q * 256];
+  double all = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) all += __shfl_xor(all, off);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = all;
+  __syncthreads();
+  if (threadIdx.x == 0) *total = (float)((lds[0] + lds[1]) + (lds[2] + lds[3]));
+}
+
+// dx of the piece's rows: the product's whole tiles, or the sum of a cut tile's parts, with what the rounding of G took off in the target's
+// column, rounded once.  With the last piece a further workgroup makes the total.
+template <int TILE>
+__global__ void __launch_bounds__(256) vocab_dx_kernel(const float* __restrict__ whole, const float* __restrict__ parts, int groups, CutCost cost,
+                                                       const bf16* __restrict__ w, int d, int V, const RowOut o, bf16* __restrict__ dx,
+                                                       const float* __restrict__ weighted, float* __restrict__ total) {
+  if (total && blockIdx.x == gridDim.x - 1) {
+    sum_total(weighted, o.counts->n, total);
+    return;
+  }
+  const int n = o.range[1], vecs = d / 8, tiles_m = (n + TILE - 1) / TILE, tiles_n = (d + TILE - 1) / TILE;
+  const DensePlan cut = dense_plan(tiles_m * tiles_n, groups, (V + 63) / 64, cost, true);
+  const long items = (long)n * vecs, blocks = gridDim.x - (total ? 1 : 0);
+  for (long i = blockIdx.x * 256L + threadIdx.x; i < items; i += blocks * 256L) {
     const int r = (int)(i / vecs), c = (int)(i - (long)r * vecs) * 8;
-    const float* src = parts + (long)r * d + c;
-    f32x4 a = *reinterpret_cast<const f32x4*>(src), b = *reinterpret_cast<const f32x4*>(src + 4);
-    for (int p = 1; p < n_parts; ++p) {
-      src += part_stride;
-      a += *reinterpret_cast<const f32x4*>(src);
-      b += *reinterpret_cast<const f32x4*>(src + 4);
+    const int l = dense_tile_index(r / TILE, c / TILE, tiles_m, tiles_n);
+    f32x4 a, b;
+    if (l < cut.full_tiles) {
+      const float* src = whole + (long)r * d + c;
+      a = *reinterpret_cast<const f32x4*>(src);
+      b = *reinterpret_cast<const f32x4*>(src + 4);
+    } else {
+      const float* src = parts + (long)(l - cut.full_tiles) * cut.split * (TILE * TILE) + (r % TILE) * TILE + c % TILE;
+      a = b = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int p = 0; p < cut.split; ++p, src += TILE * TILE) {
+        a += *reinterpret_cast<const f32x4*>(src);
+        b += *reinterpret_cast<const f32x4*>(src + 4);
+      }
     }
     const bf16x8 wt = *reinterpret_cast<const bf16x8*>(w + (long)o.target_of[r] * d + c);
     const float rest = o.rest[r];
@@ -287,27 +391,30 @@ __global__ void __launch_bounds__(256) vocab_dx_kernel(const float* __restrict__
     *reinterpret_cast<bf16x8*>(dx + (long)o.token[r] * d + c) = out;
   }
 }
-__global__ void __launch_bounds__(256) vocab_dx_f32_kernel(const float* __restrict__ src, int d, const RowOut o, float* __restrict__ dx) {
+__global__ void __launch_bounds__(256) vocab_dx_f32_kernel(const float* __restrict__ parts, int n_parts, long part_stride, int d, const RowOut o,
+                                                           float* __restrict__ dx, const float* __restrict__ weighted, float* __restrict__ total) {
+  if (total && blockIdx.x == gridDim.x - 1) {
+    sum_total(weighted, o.counts->n, total);
+    return;
+  }
   const int vecs = d / 4;
-  const long total = (long)o.range[1] * vecs;
-  for (long i = blockIdx.x * 256L + threadIdx.x; i < total; i += gridDim.x * 256L) {
+  const long items = (long)o.range[1] * vecs, blocks = gridDim.x - (total ? 1 : 0);
+  for (long i = blockIdx.x * 256L + threadIdx.x; i < items; i += blocks * 256L) {
     const int r = (int)(i / vecs), c = (int)(i - (long)r * vecs) * 4;
-    *reinterpret_cast<f32x4*>(dx + (long)o.token[r] * d + c) = *reinterpret_cast<const f32x4*>(src + (long)r * d + c);
+    const float* src = parts + (long)r * d + c;
+    f32x4 a = *reinterpret_cast<const f32x4*>(src);
+    for (int p = 1; p < n_parts; ++p) a += *reinterpret_cast<const f32x4*>(src + p * part_stride);
+    *reinterpret_cast<f32x4*>(dx + (long)o.token[r] * d + c) = a;
   }
 }
-
-// total = sum of the weighted losses, in a fixed order, in 64 bits
-__global__ void __launch_bounds__(1024) vocab_total_kernel(const float* __restrict__ weighted, const VocabCounts* __restrict__ counts, float* __restrict__ total) {
-  __shared__ double lds[16];
-  double s = 0.0;
-  for (int i = threadIdx.x; i < counts->n; i += 1024) s += (double)weighted[i];
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) s += __shfl_xor(s, off);
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 16; ++w) s += lds[w];
-    *total = (float)s;
+// d_w (+)= the sum of its parts
+__global__ void __launch_bounds__(256) vocab_dw_f32_kernel(const float* __restrict__ parts, int n_parts, long part_stride, long vecs, int accumulate,
+                                                           float* __restrict__ d_w) {
+  for (long i = blockIdx.x * 256L + threadIdx.x; i < vecs; i += gridDim.x * 256L) {
+    f32x4 a = *reinterpret_cast<const f32x4*>(parts + 4 * i);
+    for (int p = 1; p < n_parts; ++p) a += *reinterpret_cast<const f32x4*>(parts + p * part_stride + 4 * i);
+    f32x4* dst = reinterpret_cast<f32x4*>(d_w + 4 * i);
+    *dst = accumulate ? a + *dst : a;
   }
 }
 
@@ -334,13 +441,52 @@ size_t take(size_t& at, size_t bytes) {
   return here;
 }
 
-}  // namespace
-
 // Up to so many rows d_w takes a second row per token with what the rounding of G left (its product then waits for the gradient to be written,
 // V * d elements, not for the matrix cores).
 constexpr int kFewRows = 128;
 // Forward only: up to so many rows nothing is gathered.  They are one row of tiles whether they count or not, and rows do not mix.
 constexpr int kScoreAsIs = 256;
+// Up to so many tokens every workgroup of the gathering counts them itself.
+constexpr int kPrepareTokens = 2048;
+// fp32 products in parts: floats that all parts may take
+constexpr size_t kPartFloats = (size_t)64 << 20;
+
+GemmProblem f32_logits(const VocabPlan& p, const void* x, const void* w, const int32_t* range, int d, int V, float* Z) {
+  GemmProblem g{};
+  g.offsets = range; g.E = 1; g.mode = 0; g.M = p.R;
+  g.A = x; g.a_rs = d; g.a_cs = 1;
+  g.B = w; g.b_rs = 1; g.b_cs = d;
+  g.C = Z; g.ldc = p.ld; g.N = (int)align_up((size_t)V, 16); g.K = d; g.b_rows = V;
+  return g;
+}
+GemmProblem f32_dx(const VocabPlan& p, const float* G, const void* w, const int32_t* range, int d, int V, float* out) {
+  GemmProblem g{};
+  g.offsets = range; g.E = 1; g.mode = 0; g.M = p.R;
+  g.A = G; g.a_rs = p.ld; g.a_cs = 1;
+  g.B = w; g.b_rs = d; g.b_cs = 1;
+  g.C = out; g.ldc = d; g.N = d; g.K = V;
+  return g;
+}
+GemmProblem f32_dw(const VocabPlan& p, const float* G, const void* x, const int32_t* range, int d, int V, float* out) {
+  GemmProblem g{};
+  g.offsets = range; g.E = 1; g.mode = 1; g.M = (int)p.ld; g.c_rows = V;
+  g.A = G; g.a_rs = 1; g.a_cs = p.ld;
+  g.B = x; g.b_rs = d; g.b_cs = 1;
+  g.C = out; g.ldc = d; g.N = d; g.K = p.R;
+  return g;
+}
+// as one product, whichever way is the faster one, or in the plan's parts
+int launch_f32(const GemmProblem& g, F32Plan plan, hipStream_t s) {
+  return plan.parts > 1 ? launch_gemm_f32_cut(g, plan, s) : launch_gemm_f32(g, s);
+}
+F32Plan plan_f32(const GemmProblem& g) {
+  // a product that fills the chip as it is stays whole
+  const F32Product q{g.mode == 0, g.M, g.N, g.K, 1};
+  if (f32_tiles64(q) >= 1536 || !gemm_f32_cuts(g)) return F32Plan{F32_64, 1};
+  return f32_cut_plan(q, (long)(kPartFloats / ((size_t)g.M * g.ldc)));
+}
+
+}  // namespace
 
 VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int piece_rows, bool grad) {
   VocabPlan p{};
@@ -362,7 +508,8 @@ VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int p
     p.xc = take(at, copies * R * d * es);
   }
   if (f32) {
-    p.G = take(at, R * p.ld * 4);
+    p.z = plan_f32(f32_logits(p, nullptr, nullptr, nullptr, d, V, nullptr));
+    p.G = take(at, (size_t)p.z.parts * R * p.ld * 4);
   } else {
     p.tiles = mfma_vocab_tiles(p.R, V, d);
     p.stats = take(at, R * p.tiles.parts * 8);
@@ -372,125 +519,145 @@ VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int p
   if (grad) {
     p.weighted = take(at, rows * 4);
     p.rest = take(at, R * 4);
+    size_t part_floats;
     if (f32) {
-      const size_t one = R * d, most = (size_t)64 << 20;
-      p.dx_floats = one * 6 < most ? one * 6 : one < most ? most / one * one : 0;
-      p.dxc = take(at, one * 4);
-      p.dx_parts = take(at, p.dx_floats * 4);
+      p.dx = plan_f32(f32_dx(p, nullptr, nullptr, nullptr, d, V, nullptr));
+      p.dw = plan_f32(f32_dw(p, nullptr, nullptr, nullptr, d, V, nullptr));
+      p.dxc = take(at, (size_t)p.dx.parts * R * d * 4);
+      part_floats = p.dw.parts > 1 ? (size_t)p.dw.parts * p.ld * d : 0;
     } else {
-      p.dx_floats = (size_t)mfma_vocab_dx_plan(p.R, V, d).parts * R * d;
-      p.dx_parts = take(at, p.dx_floats * 4);
+      const size_t dx_floats = mfma_vocab_dx_plan(p.R, V, d).part_floats, dw_floats = mfma_vocab_dw_part_floats(p.twice ? 2 * p.R : p.R, V, d);
+      p.dxc = take(at, R * d * 4);
+      part_floats = dx_floats > dw_floats ? dx_floats : dw_floats;
       p.dw_sum_used = p.pieces > 1 && grad_dt == MOE_BF16;
       if (p.dw_sum_used) p.dw_sum = take(at, (size_t)V * d * 4);
     }
+    p.parts = take(at, part_floats * 4);
   }
   p.bytes = at;
   return p;
 }
 
-int launch_vocab_loss(const VocabProblem& q, const VocabPlan& p, char* ws, hipStream_t s) {
-  const bool f32 = q.dt == MOE_F32, grad = q.grad;
-  const int T = q.T, d = q.d, V = q.V;
-  VocabCounts* counts = reinterpret_cast<VocabCounts*>(ws + p.counts);
-  int32_t* ranges = reinterpret_cast<int32_t*>(ws + p.ranges);
-  int32_t* token = p.gather ? reinterpret_cast<int32_t*>(ws + p.token) : nullptr;
+namespace {
+
+template <typename TX> int gather_rows(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, hipStream_t s) {
+  int32_t* token = reinterpret_cast<int32_t*>(ws + p.token);
   int32_t* target_of = reinterpret_cast<int32_t*>(ws + p.target_of);
-  float* z_target = reinterpret_cast<float*>(ws + p.z_target);
-  float* stats = reinterpret_cast<float*>(ws + p.stats);
-  if (!p.gather) {
-    int rc = mfma_vocab_softmax(q.x, q.w, nullptr, q.target, T, V, d, nullptr, 0, stats, z_target, s);
-    if (rc != MOE_OK) return rc;
-    vocab_score_kernel<<<dim3(cdiv(T, 4)), dim3(256), 0, s>>>(reinterpret_cast<const f32x2*>(stats), p.tiles.parts, z_target, q.target, nullptr, nullptr, T, V,
-                                                             q.loss, q.lse);
+  int32_t* ranges = reinterpret_cast<int32_t*>(ws + p.ranges);
+  VocabCounts* counts = reinterpret_cast<VocabCounts*>(ws + p.counts);
+  TX* xc = reinterpret_cast<TX*>(ws + p.xc);
+  const TX* x = static_cast<const TX*>(q.x);
+  TX* dx = static_cast<TX*>(q.grad ? q.dx : nullptr);
+  if (p.pieces == 1 && q.T <= kPrepareTokens) {
+    vocab_prepare_kernel<TX><<<dim3(cdiv(q.T, 4)), dim3(256), 0, s>>>(x, q.target, q.T, q.V, q.d, p.twice, token, target_of, counts, ranges, xc, q.loss, q.lse, dx);
     MOE_LAUNCH_CHECK();
     return MOE_OK;
   }
-  vocab_compact_kernel<<<dim3(1), dim3(1024), 0, s>>>(q.target, T, V, p.R, p.pieces, token, target_of, counts, ranges);
+  if (piece == 0) {
+    vocab_compact_kernel<<<dim3(1), dim3(1024), 0, s>>>(q.target, q.T, q.V, p.R, p.pieces, token, target_of, counts, ranges);
+    MOE_LAUNCH_CHECK();
+  }
+  vocab_gather_kernel<TX><<<dim3(cdiv(piece == 0 ? q.T : p.R, 4)), dim3(256), 0, s>>>(x, q.target, token, ranges + 2 * piece, q.T, q.V, q.d, piece * p.R, xc,
+                                                                                    q.loss, q.lse, dx);
   MOE_LAUNCH_CHECK();
+  return MOE_OK;
+}
+
+// loss and lse of rows from their statistics: a workgroup per row where rows are few
+int score_rows(const VocabProblem& q, const VocabPlan& p, const float* stats, const float* z_target, const int32_t* target, const int32_t* token,
+               const int32_t* range, hipStream_t s) {
+  const f32x2* st = reinterpret_cast<const f32x2*>(stats);
+  if (p.R <= 1024) vocab_score_kernel<4><<<dim3(p.R), dim3(256), 0, s>>>(st, p.tiles.parts, z_target, target, token, range, p.R, q.V, q.loss, q.lse);
+  else vocab_score_kernel<1><<<dim3(cdiv(p.R, 4)), dim3(256), 0, s>>>(st, p.tiles.parts, z_target, target, token, range, p.R, q.V, q.loss, q.lse);
+  MOE_LAUNCH_CHECK();
+  return MOE_OK;
+}
+
+int f32_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, const RowOut& o, hipStream_t s) {
+  const int R = p.R, d = q.d, V = q.V;
+  float* Z = reinterpret_cast<float*>(ws + p.G);
+  const void* xc = ws + p.xc;
+  int rc = launch_f32(f32_logits(p, xc, q.w, o.range, d, V, Z), p.z, s);
+  if (rc != MOE_OK) return rc;
+  if (!q.grad) {
+    vocab_rows_f32_kernel<false><<<dim3(R), dim3(256), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
+    MOE_LAUNCH_CHECK();
+    return MOE_OK;
+  }
+  vocab_rows_f32_kernel<true><<<dim3(R), dim3(256), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
+  MOE_LAUNCH_CHECK();
+  float* dxc = reinterpret_cast<float*>(ws + p.dxc);
+  rc = launch_f32(f32_dx(p, Z, q.w, o.range, d, V, dxc), p.dx, s);
+  if (rc != MOE_OK) return rc;
+  const bool last = piece + 1 == p.pieces;
+  vocab_dx_f32_kernel<<<dim3(blocks_for((long)R * d / 4) + last), dim3(256), 0, s>>>(dxc, p.dx.parts, (long)R * d, d, o, static_cast<float*>(q.dx),
+                                                                                    reinterpret_cast<float*>(ws + p.weighted), last ? q.total : nullptr);
+  MOE_LAUNCH_CHECK();
+  const int accumulate = q.accumulate || piece > 0;
+  float* dw_parts = reinterpret_cast<float*>(ws + p.parts);
+  GemmProblem g = f32_dw(p, Z, xc, o.range, d, V, p.dw.parts > 1 ? dw_parts : static_cast<float*>(q.d_w));
+  g.accumulate = p.dw.parts > 1 ? 0 : accumulate;
+  rc = launch_f32(g, p.dw, s);
+  if (rc != MOE_OK || p.dw.parts == 1) return rc;
+  const long vecs = (long)V * d / 4;
+  vocab_dw_f32_kernel<<<dim3(blocks_for(vecs)), dim3(256), 0, s>>>(dw_parts, p.dw.parts, p.ld * d, vecs, accumulate, static_cast<float*>(q.d_w));
+  MOE_LAUNCH_CHECK();
+  return MOE_OK;
+}
+
+int bf16_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, const RowOut& o, hipStream_t s) {
+  const int R = p.R, d = q.d, V = q.V;
+  float* z_target = reinterpret_cast<float*>(ws + p.z_target);
+  float* stats = reinterpret_cast<float*>(ws + p.stats);
+  const void* xc = ws + p.xc;
+  int rc = mfma_vocab_softmax(xc, q.w, o.range + 1, o.target_of, R, V, d, q.grad ? ws + p.G : nullptr, p.ld, stats, z_target, s);
+  if (rc != MOE_OK) return rc;
+  if (!q.grad) return score_rows(q, p, stats, z_target, o.target_of, o.token, o.range, s);
+  vocab_grad_rows_kernel<<<dim3(R), dim3(256), 0, s>>>(reinterpret_cast<const f32x2*>(stats), p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
+  MOE_LAUNCH_CHECK();
+  float* dxc = reinterpret_cast<float*>(ws + p.dxc);
+  float* parts = reinterpret_cast<float*>(ws + p.parts);
+  const VocabDxPlan plan = mfma_vocab_dx_plan(R, V, d);
+  int groups = 0;
+  rc = mfma_vocab_dx(ws + p.G, p.ld, q.w, o.range + 1, R, V, d, plan, dxc, parts, &groups, s);
+  if (rc != MOE_OK) return rc;
+  const bool last = piece + 1 == p.pieces;
+  const dim3 grid(blocks_for((long)R * d / 8) + last);
+  float* total = last ? q.total : nullptr;
+  const float* weighted = reinterpret_cast<float*>(ws + p.weighted);
+  const bf16* w = static_cast<const bf16*>(q.w);
+  if (plan.tile == 256) vocab_dx_kernel<256><<<grid, dim3(256), 0, s>>>(dxc, parts, groups, plan.cost, w, d, V, o, static_cast<bf16*>(q.dx), weighted, total);
+  else vocab_dx_kernel<128><<<grid, dim3(256), 0, s>>>(dxc, parts, groups, plan.cost, w, d, V, o, static_cast<bf16*>(q.dx), weighted, total);
+  MOE_LAUNCH_CHECK();
+  const int32_t* n_dw = p.twice ? o.range + 3 : o.range + 1;
+  if (p.dw_sum_used) return mfma_vocab_dw(ws + p.G, p.ld, xc, n_dw, R, V, d, ws + p.dw_sum, MOE_F32, piece > 0, parts, s);
+  return mfma_vocab_dw(ws + p.G, p.ld, xc, n_dw, p.twice ? 2 * R : R, V, d, q.d_w, q.grad_dt, q.accumulate || piece > 0, parts, s);
+}
+
+}  // namespace
+
+int launch_vocab_loss(const VocabProblem& q, const VocabPlan& p, char* ws, hipStream_t s) {
+  if (!p.gather) {
+    float* z_target = reinterpret_cast<float*>(ws + p.z_target);
+    float* stats = reinterpret_cast<float*>(ws + p.stats);
+    const int rc = mfma_vocab_softmax(q.x, q.w, nullptr, q.target, q.T, q.V, q.d, nullptr, 0, stats, z_target, s);
+    return rc != MOE_OK ? rc : score_rows(q, p, stats, z_target, q.target, nullptr, nullptr, s);
+  }
   for (int piece = 0; piece < p.pieces; ++piece) {
-    const int row0 = piece * p.R, R = p.R;          // (rows past the last one: none, as the device knows)
-    const int32_t* range = ranges + 2 * piece;
-    const dim3 gather_grid(cdiv(piece == 0 ? T : R, 4));
-    if (f32)
-      vocab_gather_kernel<float><<<gather_grid, dim3(256), 0, s>>>((const float*)q.x, q.target, token, range, T, V, d, row0, 0, (float*)(ws + p.xc), q.loss,
-                                                                   q.lse, (float*)(grad ? q.dx : nullptr));
-    else
-      vocab_gather_kernel<bf16><<<gather_grid, dim3(256), 0, s>>>((const bf16*)q.x, q.target, token, range, T, V, d, row0, p.twice, (bf16*)(ws + p.xc),
-                                                                  q.loss, q.lse, (bf16*)(grad ? q.dx : nullptr));
-    MOE_LAUNCH_CHECK();
-    RowOut o{token + row0, target_of + row0, range, counts, q.token_w, q.loss, q.lse, reinterpret_cast<float*>(ws + p.weighted) + row0,
-             reinterpret_cast<float*>(ws + p.rest)};
-    const void* xc = ws + p.xc;
-    const int first = piece == 0;
-    int rc;
-    if (f32) {
-      GemmProblem g{};
-      float* Z = reinterpret_cast<float*>(ws + p.G);
-      g.offsets = range; g.E = 1; g.mode = 0; g.M = R;
-      g.A = xc; g.a_rs = d; g.a_cs = 1;
-      g.B = q.w; g.b_rs = 1; g.b_cs = d;
-      g.C = Z; g.ldc = p.ld; g.N = (int)align_up((size_t)V, 16); g.K = d; g.b_rows = V;
-      rc = launch_gemm_f32(g, s);
-      if (rc != MOE_OK) return rc;
-      if (!grad) {
-        vocab_rows_f32_kernel<false><<<dim3(R), dim3(256), 0, s>>>(Z, V, p.ld, o);
-        MOE_LAUNCH_CHECK();
-        continue;
-      }
-      vocab_rows_f32_kernel<true><<<dim3(R), dim3(256), 0, s>>>(Z, V, p.ld, o);
-      MOE_LAUNCH_CHECK();
-      GemmProblem h{};
-      float* dxc = reinterpret_cast<float*>(ws + p.dxc);
-      h.offsets = range; h.E = 1; h.mode = 0; h.M = R;
-      h.A = Z; h.a_rs = p.ld; h.a_cs = 1;
-      h.B = q.w; h.b_rs = d; h.b_cs = 1;
-      h.C = dxc; h.ldc = d; h.N = d; h.K = V;
-      h.scratch = reinterpret_cast<float*>(ws + p.dx_parts); h.scratch_floats = p.dx_floats;
-      rc = launch_gemm_f32(h, s);
-      if (rc != MOE_OK) return rc;
-      vocab_dx_f32_kernel<<<dim3(blocks_for((long)R * d / 4)), dim3(256), 0, s>>>(dxc, d, o, static_cast<float*>(q.dx));
-      MOE_LAUNCH_CHECK();
-      GemmProblem k{};
-      k.offsets = range; k.E = 1; k.mode = 1; k.M = (int)p.ld; k.c_rows = V;
-      k.A = Z; k.a_rs = 1; k.a_cs = p.ld;
-      k.B = xc; k.b_rs = d; k.b_cs = 1;
-      k.C = q.d_w; k.ldc = d; k.N = d; k.K = R;
-      k.accumulate = q.accumulate || !first;
-      rc = launch_gemm_f32(k, s);
-      if (rc != MOE_OK) return rc;
-      continue;
-    }
-    rc = mfma_vocab_softmax(xc, q.w, range + 1, target_of + row0, R, V, d, grad ? ws + p.G : nullptr, p.ld, stats, z_target, s);
+    int rc = q.dt == MOE_F32 ? gather_rows<float>(q, p, ws, piece, s) : gather_rows<bf16>(q, p, ws, piece, s);
     if (rc != MOE_OK) return rc;
-    if (!grad) {
-      vocab_score_kernel<<<dim3(cdiv(R, 4)), dim3(256), 0, s>>>(reinterpret_cast<const f32x2*>(stats), p.tiles.parts, z_target, target_of + row0, token + row0, range, R,
-                                                               V, q.loss, q.lse);
-      MOE_LAUNCH_CHECK();
-      continue;
-    }
-    vocab_grad_rows_kernel<<<dim3(R), dim3(256), 0, s>>>(reinterpret_cast<const f32x2*>(stats), p.tiles.parts, p.tiles.shift, z_target, V, p.ld,
-                                                         p.twice, ws + p.G, o);
-    MOE_LAUNCH_CHECK();
-    float* dx_parts = reinterpret_cast<float*>(ws + p.dx_parts);
-    rc = mfma_vocab_dx(ws + p.G, p.ld, q.w, range + 1, R, V, d, dx_parts, s);
-    if (rc != MOE_OK) return rc;
-    vocab_dx_kernel<<<dim3(blocks_for((long)R * d / 8)), dim3(256), 0, s>>>(dx_parts, mfma_vocab_dx_plan(R, V, d).parts, (long)R * d, (const bf16*)q.w, d, o,
-                                                                           (bf16*)q.dx);
-    MOE_LAUNCH_CHECK();
-    if (p.dw_sum_used)
-      rc = mfma_vocab_dw(ws + p.G, p.ld, xc, range, R, V, d, ws + p.dw_sum, MOE_F32, !first, s);
-    else
-      rc = mfma_vocab_dw(ws + p.G, p.ld, xc, p.twice ? ranges + 2 : range, p.twice ? 2 * R : R, V, d, q.d_w, q.grad_dt, q.accumulate || !first, s);
+    const long row0 = (long)piece * p.R;
+    const RowOut o{reinterpret_cast<int32_t*>(ws + p.token) + row0, reinterpret_cast<int32_t*>(ws + p.target_of) + row0,
+                   reinterpret_cast<int32_t*>(ws + p.ranges) + 2 * piece, reinterpret_cast<VocabCounts*>(ws + p.counts), q.token_w, q.loss, q.lse,
+                   reinterpret_cast<float*>(ws + p.weighted) + row0, reinterpret_cast<float*>(ws + p.rest)};
+    rc = q.dt == MOE_F32 ? f32_piece(q, p, ws, piece, o, s) : bf16_piece(q, p, ws, piece, o, s);
     if (rc != MOE_OK) return rc;
   }
-  if (!grad) return MOE_OK;
   if (p.dw_sum_used) {
-    const long vecs = (long)V * d / 8;
+    const long vecs = (long)q.V * q.d / 8;
     vocab_dw_round_kernel<<<dim3(blocks_for(vecs)), dim3(256), 0, s>>>(reinterpret_cast<const float*>(ws + p.dw_sum), vecs, q.accumulate, (bf16*)q.d_w);
     MOE_LAUNCH_CHECK();
   }
-  vocab_total_kernel<<<dim3(1), dim3(1024), 0, s>>>(reinterpret_cast<const float*>(ws + p.weighted), counts, q.total);
-  MOE_LAUNCH_CHECK();
   return MOE_OK;
 }
 
