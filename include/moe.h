@@ -443,7 +443,7 @@ int moe_grad_clip(const void* table /*device*/, int n, int64_t total, double max
  * lr, step and coef are read on the device, so a captured step follows a schedule.  params, m, v
  * fp32; grads all in grad_dt (MOE_F32 or MOE_BF16).  The table as above.  Workspace:
  * MOE_ADAMW_WS_BYTES that the caller has cleared once; every call leaves them cleared. */
-#define MOE_ADAMW_WS_BYTES ((size_t)16)
+#define MOE_ADAMW_WS_BYTES ((size_t)4096)
 size_t moe_adamw_table_bytes(int n);
 int moe_adamw_table(int n, void* const* params, const void* const* grads, void* const* m,
                     void* const* v, void* const* weights, const int64_t* numel,

@@ -328,7 +328,7 @@ def moe_expert_ffn_fused_bwd(x, dy, h_save, inv_perm, topk_w, row_w, offsets, w1
 
 
 # ---- what follows the layer in a training step ---------------------------------------------------------------------
-ADAMW_WS_BYTES = 16
+ADAMW_WS_BYTES = 4096
 
 
 def moe_vocab_workspace_bytes(T, d, V, dt, grad_dt, piece_rows, gradients) -> int:

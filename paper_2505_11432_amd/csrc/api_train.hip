@@ -1,5 +1,7 @@
 // extern "C" entry points of what follows the layer in a training step: the vocabulary loss, clipping and the AdamW update.  Arguments are
 // checked before any HIP call; declarations and contracts are in include/moe.h.
+#include <type_traits>
+
 #include "optim.h"
 #include "vocab_loss.h"
 
@@ -20,16 +22,18 @@ int vocab_call(const VocabProblem& q, int piece_rows, void* workspace, size_t ws
   return launch_vocab_loss(q, p, static_cast<char*>(workspace), as_stream(stream));
 }
 
-// sums of numel into entries[i].first and entries[n].first
+// sums of elements and chunks into the entries, whose types are set
 template <typename Entry> bool number_entries(const int64_t* numel, int n, Entry* table) {
-  int64_t at = 0;
+  int64_t at = 0, chunk = 0;
   for (int i = 0; i <= n; ++i) {
     if (i == n) table[i] = Entry{};
     table[i].first = at;
-    if (i < n) {
-      if (numel[i] < 0 || numel[i] > INT64_MAX / 16 - at) return false;
-      at += numel[i];
-    }
+    if constexpr (std::is_same_v<Entry, ClipEntry>) table[i].chunk = (int32_t)chunk;
+    if (i == n) break;
+    if (numel[i] < 0 || numel[i] > INT64_MAX / 16 - at) return false;
+    at += numel[i];
+    chunk += (numel[i] + chunk_elements(table[i]) - 1) / chunk_elements(table[i]) + 1;
+    if (chunk > INT32_MAX / 2) return false;
   }
   return true;
 }

@@ -2,15 +2,22 @@
 //   norm = sqrt(sum g^2),  coef = min(1, max_norm / (norm + 1e-6)),  out = coef g
 //   g' = coef g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,
 //   p = p (1 - lr wd) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
-// All of it is bound by memory (3 and 15 operations per element).  The tensors are one sequence of elements, cut into equal ranges for the
-// workgroups: one search in the table per workgroup, and tensors of any size fill the chip alike.
+// All of it is bound by memory (3 and 15 operations per element).
 //
-// Alignment: a tensor may begin at any element.  A range is walked four elements at a time from the first one that is a multiple of four from
-// the tensor's 16-byte aligned element on; loads and stores of the other lists may then be unaligned, which the hardware takes.
+// The tensors are one sequence of chunks, 2 KB each (AdamW: 512 elements), which the workgroups take in turn, a few at a time, so that all of
+// them stay near one another in memory.  A tensor takes one chunk more than it fills, for what its entry and its ends cost.  Probe of the
+// access patterns on 1.7 GB per list (TB/s; a contiguous range per workgroup, in turn; 2048 workgroups, 32768): read 6.0, 6.3; read and write 5.05,
+// 5.57; AdamW's streams 5.02, 5.22.
+// What is not read again is read and written past the caches (nontemporal): read 7.0, read and write 6.0, AdamW's streams 5.4.
+//
+// Alignment: a tensor may begin at any element.  Its elements in front of the first whole 128-byte line go one by one; chunks begin at lines.  The
+// other lists of an update may then be unaligned, which the hardware takes.
 //
 // The norm is summed in 64 bits (squares of single-precision numbers neither overflow nor vanish there; the conversion and the sum hide behind
 // the loads) and in a fixed order: a sum per workgroup, and every workgroup of the second launch adds those up in the same order.  The second
-// launch walks each range backwards: what the first one read last is still in the Infinity Cache (256 MB).
+// launch takes the chunks from the last one on: what the first one read last is still in the Infinity Cache (256 MB).
+#include <type_traits>
+
 #include "moe_common.h"
 #include "optim.h"
 
@@ -18,70 +25,128 @@ namespace moe {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef f32x4 f32x4_u __attribute__((aligned(4)));
 typedef bf16x4 bf16x4_u __attribute__((aligned(2)));
+typedef bf16x8 bf16x8_u __attribute__((aligned(2)));
 
-template <typename T> struct Quad;
-template <> struct Quad<float> {
-  __device__ static __forceinline__ f32x4 load(const float* p) { return *reinterpret_cast<const f32x4_u*>(p); }
-  __device__ static __forceinline__ void store(float* p, f32x4 v) { *reinterpret_cast<f32x4_u*>(p) = v; }
+// N elements as floats
+template <typename T, int N> struct Piece;
+template <> struct Piece<float, 4> {
+  typedef f32x4 values;
+  __device__ static __forceinline__ f32x4 load(const float* p) { return __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(p)); }
+  __device__ static __forceinline__ f32x4 load_kept(const float* p) { return *reinterpret_cast<const f32x4_u*>(p); }
+  __device__ static __forceinline__ void store(float* p, f32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<f32x4_u*>(p)); }
 };
-template <> struct Quad<bf16> {
-  __device__ static __forceinline__ f32x4 load(const bf16* p) { return __builtin_convertvector(*reinterpret_cast<const bf16x4_u*>(p), f32x4); }
-  __device__ static __forceinline__ void store(bf16* p, f32x4 v) { *reinterpret_cast<bf16x4_u*>(p) = __builtin_convertvector(v, bf16x4); }
+template <> struct Piece<bf16, 4> {
+  typedef f32x4 values;
+  __device__ static __forceinline__ f32x4 load(const bf16* p) {
+    return __builtin_convertvector(__builtin_nontemporal_load(reinterpret_cast<const bf16x4_u*>(p)), f32x4);
+  }
+  __device__ static __forceinline__ void store(bf16* p, f32x4 v) {
+    __builtin_nontemporal_store(__builtin_convertvector(v, bf16x4), reinterpret_cast<bf16x4_u*>(p));
+  }
 };
+template <> struct Piece<bf16, 8> {
+  typedef f32x8 values;
+  __device__ static __forceinline__ f32x8 load(const bf16* p) {
+    return __builtin_convertvector(__builtin_nontemporal_load(reinterpret_cast<const bf16x8_u*>(p)), f32x8);
+  }
+  __device__ static __forceinline__ f32x8 load_kept(const bf16* p) { return __builtin_convertvector(*reinterpret_cast<const bf16x8_u*>(p), f32x8); }
+  __device__ static __forceinline__ void store(bf16* p, f32x8 v) {
+    __builtin_nontemporal_store(__builtin_convertvector(v, bf16x8), reinterpret_cast<bf16x8_u*>(p));
+  }
+};
+template <typename T> using Wide = Piece<T, 16 / (int)sizeof(T)>;
 
-// elements in front of the first whole group of four
+// elements in front of the first whole line
 template <typename T> __device__ __forceinline__ long misfit(const T* p) {
-  return (long)((4 - (reinterpret_cast<uintptr_t>(p) / sizeof(T) & 3)) & 3);
+  constexpr int LINE = 128 / sizeof(T);
+  return (long)((LINE - (reinterpret_cast<uintptr_t>(p) / sizeof(T) & (LINE - 1))) & (LINE - 1));
+}
+__device__ __forceinline__ long misfit(const ClipEntry& e) {
+  return e.dt == MOE_F32 ? misfit(static_cast<const float*>(e.g)) : misfit(static_cast<const bf16*>(e.g));
+}
+__device__ __forceinline__ long misfit(const AdamwEntry& e) { return misfit(static_cast<const float*>(e.p)); }
+
+// The tensor that holds chunk `at`: 64 entries at a time, a lane each.
+template <typename Entry> __device__ __forceinline__ int find(const Entry* __restrict__ table, int n, int at) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, len = n;
+  while (len > 1) {
+    const int step = (len + 63) / 64;
+    const unsigned long long before = __ballot(lane * step < len && first_chunk(table, lo + lane * step) <= at);
+    const int k = __popcll(before) - 1;
+    lo += k * step;
+    len = min(step, len - k * step);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// last entry whose first element is at or before `at`
-template <typename Entry> __device__ __forceinline__ int find(const Entry* __restrict__ table, int n, long at) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (table[mid].first <= at) lo = mid; else hi = mid;
+// Takes groups of `per` chunks in turn with the other workgroups, from the first or from the last on, and calls body(entry, first element, number
+// of elements) for the part of every tensor that lies in them.  Only the first part of a tensor begins in front of a line, and only the last one
+// ends anywhere.
+template <bool BACKWARDS, typename Entry, typename Body> __device__ __forceinline__ void for_parts(const Entry* __restrict__ table, int n, int per, Body body) {
+  const int chunks = first_chunk(table, n), groups = (chunks + per - 1) / per;
+  int e = 0, chunk = 0, next = 0;          // the open tensor and its chunks
+  Entry t{};
+  long numel = 0, head = 0;
+  for (int g = blockIdx.x; g < groups; g += gridDim.x) {
+    int at = (BACKWARDS ? groups - 1 - g : g) * per;
+    const int end = min(at + per, chunks);
+    while (at < end) {
+      if (at < chunk || at >= next) {
+        e = at == next && next != 0 ? e + 1 : find(table, n, at);
+        chunk = first_chunk(table, e);
+        next = first_chunk(table, e + 1);
+        t = table[e];
+        numel = table[e + 1].first - t.first;
+        head = misfit(t);
+      }
+      const long size = chunk_elements(t);
+      const int stop = min(end, next);
+      const long lo = at == chunk ? 0 : min((at - chunk) * size + head, numel), hi = min((stop - chunk) * size + head, numel);
+      if (lo < hi) body(t, lo, hi - lo);
+      at = stop;
+    }
   }
-  return lo;
 }
 
 constexpr int kThreads = 256;
 
-template <typename T> __device__ __forceinline__ double square_sum(const T* __restrict__ g, long n) {
-  double s0 = 0, s1 = 0;
-  const long head = min(misfit(g), n), quads = (n - head) >> 2;
-  if (threadIdx.x < head) {
-    const double v = (double)to_f32(g[threadIdx.x]);
-    s0 += v * v;
-  }
-  const T* q = g + head;
-  constexpr int U = 4;
-  long i = threadIdx.x;
-  for (; i + (U - 1) * kThreads < quads; i += U * kThreads) {
-    f32x4 v[U];
+// f(first element) for pieces of N elements from the first line on, U of them in flight per thread, and single(element) for the others
+template <int N, int U, typename T, typename Single, typename Pieces>
+__device__ __forceinline__ void walk(const T* p, long n, Single single, Pieces pieces) {
+  const long head = min(misfit(p), n), count = (n - head) / N, tail = head + N * count + threadIdx.x;
+  if (threadIdx.x < head) single((long)threadIdx.x);
+  for (long i = threadIdx.x; i < count; i += U * kThreads) pieces(head + N * i, (int)min((count - i + kThreads - 1) / kThreads, (long)U));
+  if (tail < n) single(tail);
+}
+
+template <bool KEEP, typename T> __device__ __forceinline__ double square_sum(const T* __restrict__ g, long n) {
+  typedef Wide<T> P;
+  constexpr int N = 16 / (int)sizeof(T), U = 4;
+  double sum[2] = {0, 0};
+  walk<N, U>(g, n,
+             [&](long i) __attribute__((always_inline)) {
+               const double v = (double)to_f32(g[i]);
+               sum[0] = fma(v, v, sum[0]);
+             },
+             [&](long at, int count) __attribute__((always_inline)) {
+               typename P::values v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = Quad<T>::load(q + 4 * (i + u * kThreads));
+               for (int u = 0; u < U; ++u) {
+                 v[u] = typename P::values{};
+                 if (u < count) v[u] = KEEP ? P::load_kept(g + at + N * u * kThreads) : P::load(g + at + N * u * kThreads);
+               }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      s0 = fma((double)v[u][0], (double)v[u][0], s0);
-      s1 = fma((double)v[u][1], (double)v[u][1], s1);
-      s0 = fma((double)v[u][2], (double)v[u][2], s0);
-      s1 = fma((double)v[u][3], (double)v[u][3], s1);
-    }
-  }
-  for (; i < quads; i += kThreads) {
-    const f32x4 v = Quad<T>::load(q + 4 * i);
+               for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) s1 = fma((double)v[c], (double)v[c], s1);
-  }
-  const long tail = head + 4 * quads + threadIdx.x;
-  if (tail < n) {
-    const double v = (double)to_f32(g[tail]);
-    s0 += v * v;
-  }
-  return s0 + s1;
+                 for (int c = 0; c < N; ++c) sum[c & 1] = fma((double)v[u][c], (double)v[u][c], sum[c & 1]);
+             });
+  return sum[0] + sum[1];
 }
 
 __device__ __forceinline__ double block_sum(double s, double (&lds)[4]) {
@@ -92,19 +157,15 @@ __device__ __forceinline__ double block_sum(double s, double (&lds)[4]) {
   return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-__global__ void __launch_bounds__(kThreads) norm_parts_kernel(const ClipEntry* __restrict__ table, int n, long total, long per, double* __restrict__ parts) {
+// (eight workgroups of every CU at a time, as many as are launched).  KEEP: the second launch finds them in the Infinity Cache.
+template <bool KEEP>
+__global__ void __launch_bounds__(kThreads, 8) norm_parts_kernel(const ClipEntry* __restrict__ table, int n, int per, double* __restrict__ parts) {
   __shared__ double lds[4];
-  long at = blockIdx.x * per;
-  const long end = min(at + per, total);
   double s = 0;
-  for (int e = at < end ? find(table, n, at) : n; at < end; ++e) {
-    const ClipEntry t = table[e];
-    const long stop = min(end, table[e + 1].first), k = stop - at;
-    if (k <= 0) continue;
-    if (t.dt == MOE_F32) s += square_sum(static_cast<const float*>(t.g) + (at - t.first), k);
-    else s += square_sum(static_cast<const bf16*>(t.g) + (at - t.first), k);
-    at = stop;
-  }
+  for_parts<false>(table, n, per, [&](const ClipEntry& t, long first, long k) __attribute__((always_inline)) {
+    if (t.dt == MOE_F32) s += square_sum<KEEP>(static_cast<const float*>(t.g) + first, k);
+    else s += square_sum<KEEP>(static_cast<const bf16*>(t.g) + first, k);
+  });
   s = block_sum(s, lds);
   if (threadIdx.x == 0) parts[blockIdx.x] = s;
 }
@@ -120,27 +181,23 @@ __device__ __forceinline__ float clip_coef(double norm, double max_norm) {
   return c < 1.0 ? (float)c : c == c ? 1.0f : (float)c;          // (a norm that is no number gives a factor that is none)
 }
 
-// four elements at a time, the last ones first
 template <typename T> __device__ __forceinline__ void scale_range(const T* g, T* out, long n, float c) {
-  const long head = min(misfit(g), n), quads = (n - head) >> 2, tail = head + 4 * quads + threadIdx.x;
-  if (tail < n) out[tail] = from_f32<T>(c * to_f32(g[tail]));
-  const T* q = g + head;
-  T* o = out + head;
-  constexpr int U = 4;
-  long i = quads - 1 - threadIdx.x;
-  for (; i - (U - 1) * kThreads >= 0; i -= U * kThreads) {
-    f32x4 v[U];
+  typedef Wide<T> P;
+  constexpr int N = 16 / (int)sizeof(T), U = 4;
+  walk<N, U>(g, n, [&](long i) __attribute__((always_inline)) { out[i] = from_f32<T>(c * to_f32(g[i])); },
+             [&](long at, int count) __attribute__((always_inline)) {
+               typename P::values v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = Quad<T>::load(q + 4 * (i - u * kThreads));
+               for (int u = 0; u < U; ++u)
+                 if (u < count) v[u] = P::load(g + at + N * u * kThreads);
 #pragma unroll
-    for (int u = 0; u < U; ++u) Quad<T>::store(o + 4 * (i - u * kThreads), v[u] * c);
-  }
-  for (; i >= 0; i -= kThreads) Quad<T>::store(o + 4 * i, Quad<T>::load(q + 4 * i) * c);
-  if (threadIdx.x < head) out[threadIdx.x] = from_f32<T>(c * to_f32(g[threadIdx.x]));
+               for (int u = 0; u < U; ++u)
+                 if (u < count) P::store(out + at + N * u * kThreads, v[u] * c);
+             });
 }
 
-__global__ void __launch_bounds__(kThreads) clip_kernel(const ClipEntry* __restrict__ table, int n, long total, long per, const double* __restrict__ parts,
-                                                        int n_parts, double max_norm, int write, float* __restrict__ norm, float* __restrict__ coef) {
+__global__ void __launch_bounds__(kThreads, 8) clip_kernel(const ClipEntry* __restrict__ table, int n, int per, const double* __restrict__ parts, int n_parts,
+                                                           double max_norm, int write, float* __restrict__ norm, float* __restrict__ coef) {
   __shared__ double lds[4];
   const double full = norm_of(parts, n_parts, lds);
   const float c = clip_coef(full, max_norm);
@@ -149,20 +206,12 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const ClipEntry* __restr
     *coef = c;
   }
   if (!write) return;
-  const long begin = blockIdx.x * per;
-  long end = min(begin + per, total);
-  for (int e = begin < end ? find(table, n, end - 1) : 0; begin < end; --e) {
-    const ClipEntry t = table[e];
-    const long start = max(begin, (long)t.first), k = end - start;
-    if (k <= 0) continue;
-    const long off = start - t.first;
+  for_parts<true>(table, n, per, [&](const ClipEntry& t, long first, long k) __attribute__((always_inline)) {
     // gradients in place that are within the limit stay as they are
-    if (t.out && !(t.out == t.g && c == 1.0f)) {
-      if (t.dt == MOE_F32) scale_range(static_cast<const float*>(t.g) + off, static_cast<float*>(t.out) + off, k, c);
-      else scale_range(static_cast<const bf16*>(t.g) + off, static_cast<bf16*>(t.out) + off, k, c);
-    }
-    end = start;
-  }
+    if (!t.out || (t.out == t.g && c == 1.0f)) return;
+    if (t.dt == MOE_F32) scale_range(static_cast<const float*>(t.g) + first, static_cast<float*>(t.out) + first, k, c);
+    else scale_range(static_cast<const bf16*>(t.g) + first, static_cast<bf16*>(t.out) + first, k, c);
+  });
 }
 
 struct AdamwScalars { float coef, b1, g1, b2, g2, keep, lr, r1, r2, eps; };
@@ -177,50 +226,46 @@ __device__ __forceinline__ void adamw_one(float& p, float g, float& m, float& v,
 template <typename TG>
 __device__ __forceinline__ void adamw_range(float* __restrict__ p, const TG* __restrict__ g, float* __restrict__ m, float* __restrict__ v, bf16* __restrict__ w,
                                             long n, const AdamwScalars& a) {
-  const long head = min(misfit(p), n), quads = (n - head) >> 2;
-  auto single = [&](long i) __attribute__((always_inline)) {
-    float pi = p[i], mi = m[i], vi = v[i];
-    adamw_one(pi, to_f32(g[i]), mi, vi, a);
-    p[i] = pi;
-    m[i] = mi;
-    v[i] = vi;
-    if (w) w[i] = from_f32<bf16>(pi);
-  };
-  if (threadIdx.x < head) single(threadIdx.x);
+  typedef Piece<float, 4> P;
   constexpr int U = 2;
-  long i = threadIdx.x;
-  auto group = [&](auto count) __attribute__((always_inline)) {
-    constexpr int N = decltype(count)::value;
-    f32x4 pv[N], gv[N], mv[N], vv[N];
+  walk<4, U>(p, n,
+             [&](long i) __attribute__((always_inline)) {
+               float pi = p[i], mi = m[i], vi = v[i];
+               adamw_one(pi, to_f32(g[i]), mi, vi, a);
+               p[i] = pi;
+               m[i] = mi;
+               v[i] = vi;
+               if (w) w[i] = from_f32<bf16>(pi);
+             },
+             [&](long at, int count) __attribute__((always_inline)) {
+               f32x4 pv[U], gv[U], mv[U], vv[U];
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const long at = head + 4 * (i + u * kThreads);
-      gv[u] = Quad<TG>::load(g + at);
-      mv[u] = Quad<float>::load(m + at);
-      vv[u] = Quad<float>::load(v + at);
-      pv[u] = Quad<float>::load(p + at);
-    }
+               for (int u = 0; u < U; ++u)
+                 if (u < count) {
+                   const long i = at + 4 * u * kThreads;
+                   gv[u] = Piece<TG, 4>::load(g + i);
+                   mv[u] = P::load(m + i);
+                   vv[u] = P::load(v + i);
+                   pv[u] = P::load(p + i);
+                 }
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const long at = head + 4 * (i + u * kThreads);
+               for (int u = 0; u < U; ++u)
+                 if (u < count) {
+                   const long i = at + 4 * u * kThreads;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        float pi = pv[u][c], mi = mv[u][c], vi = vv[u][c];
-        adamw_one(pi, gv[u][c], mi, vi, a);
-        pv[u][c] = pi;
-        mv[u][c] = mi;
-        vv[u][c] = vi;
-      }
-      Quad<float>::store(p + at, pv[u]);
-      Quad<float>::store(m + at, mv[u]);
-      Quad<float>::store(v + at, vv[u]);
-      if (w) Quad<bf16>::store(w + at, pv[u]);
-    }
-  };
-  for (; i + (U - 1) * kThreads < quads; i += U * kThreads) group(std::integral_constant<int, U>());
-  for (; i < quads; i += kThreads) group(std::integral_constant<int, 1>());
-  const long tail = head + 4 * quads + threadIdx.x;
-  if (tail < n) single(tail);
+                   for (int c = 0; c < 4; ++c) {
+                     float pi = pv[u][c], mi = mv[u][c], vi = vv[u][c];
+                     adamw_one(pi, gv[u][c], mi, vi, a);
+                     pv[u][c] = pi;
+                     mv[u][c] = mi;
+                     vv[u][c] = vi;
+                   }
+                   P::store(p + i, pv[u]);
+                   P::store(m + i, mv[u]);
+                   P::store(v + i, vv[u]);
+                   if (w) Piece<bf16, 4>::store(w + i, pv[u]);
+                 }
+             });
 }
 
 // base^t in 64 bits by squaring
@@ -231,10 +276,13 @@ __device__ __forceinline__ double power(double base, unsigned t) {
   return r;
 }
 
+constexpr int kShards = 16, kShardWords = 32;              // a line each
+static_assert((kShards + 1) * kShardWords * 4 <= MOE_ADAMW_WS_BYTES, "the workspace holds the counters");
+
 // Every workgroup reads the step count before any has changed it: the last one to finish writes the new one.
 template <typename TG>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwEntry* __restrict__ table, int n, long total, long per, const float* __restrict__ lr,
-                                                         int32_t* step, const float* __restrict__ coef, AdamwHyper h, unsigned* done) {
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwEntry* __restrict__ table, int n, int per, const float* __restrict__ lr, int32_t* step,
+                                                         const float* __restrict__ coef, AdamwHyper h, unsigned* done) {
   const int t = *step + 1;
   AdamwScalars a;
   a.coef = coef ? *coef : 1.0f;
@@ -247,51 +295,54 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwEntry* __res
   a.r1 = (float)(1.0 / (1.0 - power(h.beta1, (unsigned)t)));
   a.r2 = (float)(1.0 / (1.0 - power(h.beta2, (unsigned)t)));
   a.eps = (float)h.eps;
-  long at = blockIdx.x * per;
-  const long end = min(at + per, total);
-  for (int e = at < end ? find(table, n, at) : n; at < end; ++e) {
-    const AdamwEntry q = table[e];
-    const long stop = min(end, table[e + 1].first), k = stop - at, off = at - q.first;
-    if (k <= 0) continue;
-    adamw_range(static_cast<float*>(q.p) + off, static_cast<const TG*>(q.g) + off, static_cast<float*>(q.m) + off, static_cast<float*>(q.v) + off,
-                q.w ? static_cast<bf16*>(q.w) + off : nullptr, k, a);
-    at = stop;
-  }
+  for_parts<false>(table, n, per, [&](const AdamwEntry& q, long first, long k) __attribute__((always_inline)) {
+    adamw_range(static_cast<float*>(q.p) + first, static_cast<const TG*>(q.g) + first, static_cast<float*>(q.m) + first, static_cast<float*>(q.v) + first,
+                q.w ? static_cast<bf16*>(q.w) + first : nullptr, k, a);
+  });
   __syncthreads();
   if (threadIdx.x == 0) {
-    __threadfence();
-    if (atomicAdd(done, 1u) == gridDim.x - 1) {
-      *step = t;
-      *done = 0;
+    // (no fence: what counts is that this workgroup has read the step, which the values above have needed; a fence would write back its L2)
+    // Counters on one address take a workgroup's turn each, 10 ns: every 16th workgroup shares one, and who fills it counts in the last.
+    const unsigned shard = blockIdx.x % kShards, members = (gridDim.x + kShards - 1 - shard) / kShards, shards = min(gridDim.x, (unsigned)kShards);
+    if (atomicAdd(done + shard * kShardWords, 1u) == members - 1) {
+      done[shard * kShardWords] = 0;
+      if (atomicAdd(done + kShards * kShardWords, 1u) == shards - 1) {
+        done[kShards * kShardWords] = 0;
+        *step = t;
+      }
     }
   }
 }
 
-// Workgroups and elements of a range: ranges of whole groups, up to 2048 of them (eight per CU).
-struct Cut { int blocks; long per; };
-Cut cut(long total, long least) {
-  long per = (total + 2047) / 2048;
-  per = per < least ? least : (per + 1023) / 1024 * 1024;
-  const long blocks = (total + per - 1) / per;
-  return {blocks < 1 ? 1 : (int)blocks, per};
+// How many chunks a workgroup takes at a time, and how many workgroups: about so many chunks are there, at most `most` workgroups run.
+struct Cut { unsigned blocks; int per; };
+Cut cut(long chunks, int per, long most) {
+  // small lists: four each (460 thousand elements of AdamW in 1, 2, 4, 8: 7.3, 6.35, 6.4, 7.5 us)
+  if (chunks < 1024) per = 4;
+  else if (chunks < 2048L * per) per = (int)((chunks + 2047) / 2048);
+  const long blocks = (chunks + per - 1) / per;
+  return {(unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most), per};
 }
 
 }  // namespace
 
 int launch_grad_clip(const ClipEntry* table, int n, long total, double max_norm, int write, float* norm, float* coef, double* parts, hipStream_t s) {
-  const Cut c = cut(total, 2048);
-  norm_parts_kernel<<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, total, c.per, parts);
+  // (the host does not know the types: chunks as if all were single precision)
+  const Cut c = cut(total / (kChunkBytes / 4) + n, 8, kNormParts);
+  // up to 128 MB, which the second launch then finds in the caches, reads are kept
+  if (write && total <= (32L << 20)) norm_parts_kernel<true><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, parts);
+  else norm_parts_kernel<false><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, parts);
   MOE_LAUNCH_CHECK();
-  clip_kernel<<<dim3(write ? c.blocks : 1), dim3(kThreads), 0, s>>>(table, n, total, c.per, parts, c.blocks, max_norm, write, norm, coef);
+  clip_kernel<<<dim3(write ? c.blocks : 1), dim3(kThreads), 0, s>>>(table, n, c.per, parts, (int)c.blocks, max_norm, write, norm, coef);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }
 
 int launch_adamw(const AdamwEntry* table, int n, long total, moe_dtype grad_dt, const float* lr, int32_t* step, const float* coef, const AdamwHyper& h,
                  unsigned* done, hipStream_t s) {
-  const Cut c = cut(total, 2048);
-  if (grad_dt == MOE_F32) adamw_kernel<float><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, total, c.per, lr, step, coef, h, done);
-  else adamw_kernel<bf16><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, total, c.per, lr, step, coef, h, done);
+  const Cut c = cut(total / kAdamwChunk + 2L * n, 8, 1L << 20);
+  if (grad_dt == MOE_F32) adamw_kernel<float><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, lr, step, coef, h, done);
+  else adamw_kernel<bf16><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, lr, step, coef, h, done);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }
