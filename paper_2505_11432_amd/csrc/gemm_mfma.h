@@ -63,6 +63,7 @@ struct Args {
   const int32_t* rows;               // DENSE: number of rows (at most M, the rows that A and C have room for), or NULL for M
   const int32_t* k_rows;             // DENSE: length of the contraction (at most K), or NULL for K
   int c_rows;                        // DENSE: rows of C where an M-major A is padded to M columns (0: M)
+  const float* scale;                // DENSE, EPI_STORE: factor of the whole product (device), or NULL
   CutCost cut;                       // DENSE: costs by which the last round's tiles are cut; the parts go to splitk_ws (NULL: no cutting)
   float* stats; int parts;           // EPI_LSE, EPI_CE: [M][parts] pairs of maximum and sum of exp(logit - maximum), one per n-tile and wave along n
   const int32_t* target;             // EPI_LSE, EPI_CE: [M] column whose logit goes to z_target [M] (columns outside the width: none)

@@ -364,7 +364,7 @@ VocabDxPlan mfma_vocab_dx_plan(int R, int V, int d) {
   return p;
 }
 // out [R][d] fp32 gets the whole tiles, `parts` the others' parts; *groups is what dense_plan needs to know which they are
-int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, int R, int V, int d, const VocabDxPlan& plan, float* out, float* parts,
+int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, const float* scale, int R, int V, int d, const VocabDxPlan& plan, float* out, float* parts,
                   int* groups, hipStream_t s) {
   int dev = 0;
   MOE_HIP_TRY(hipGetDevice(&dev));
@@ -377,7 +377,7 @@ int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, i
   a.B = w; a.ldb = d;
   a.C = out; a.ldc = d;
   a.E = 1; a.M = R; a.N = d; a.K = V;
-  a.rows = rows; a.cut = plan.cost; a.splitk_ws = parts;
+  a.rows = rows; a.scale = scale; a.cut = plan.cost; a.splitk_ws = parts;
   if (plan.tile == 256) return launch<256, 256, 64, 2, 2, 4, KMAJOR, MNMAJOR, DENSE, EPI_STORE, float>(a, 1, s);
   return launch<128, 128, 64, 3, 4, 2, KMAJOR, MNMAJOR, DENSE, EPI_STORE, float>(a, 1, s);
 }
@@ -406,7 +406,7 @@ size_t mfma_vocab_dw_part_floats(int R, int V, int d) {
   const int b = pairs ? 128 : 256, groups = pairs ? 2 * kPlanGroups : kPlanGroups;
   return (size_t)cut_items((long)cdiv(V, b) * cdiv(d, b), groups, cdiv(R, 64)) * b * b;
 }
-int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
+int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, const float* scale, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
                   hipStream_t s) {
   int dev = 0, groups = 0;
   MOE_HIP_TRY(hipGetDevice(&dev));
@@ -419,7 +419,7 @@ int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, i
   Args a{};
   a.A = G; a.lda = ldg;
   a.B = x; a.ldb = d;
-  a.C = d_w; a.ldc = d; a.k_rows = rows; a.E = 1; a.M = (int)ldg; a.c_rows = V; a.N = d; a.K = R;
+  a.C = d_w; a.ldc = d; a.k_rows = rows; a.E = 1; a.M = (int)ldg; a.c_rows = V; a.N = d; a.K = R; a.scale = scale;
   a.accumulate = accumulate;
   a.cut = pairs ? kDwPair : kDwFull;
   const long tiles = (long)cdiv(V, pairs ? 128 : 256) * cdiv(d, pairs ? 128 : 256);

@@ -490,6 +490,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
     if (p.k_rows) k_all = __builtin_amdgcn_readfirstlane(max(min(*p.k_rows, p.K), 0));
     if (p.c_rows) m_rows = p.c_rows;
   }
+  const float scale = MODE == DENSE && EPI == EPI_STORE && p.scale ? *p.scale : 1.0f;
   const int tiles_m_fixed = (m_rows + BM - 1) / BM;
   int total_tiles;
   if constexpr (MODE == ROWSEG) {
@@ -1069,6 +1070,10 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
       // channel scales are live at a time
       auto block = [&](int i, int j) __attribute__((always_inline)) -> Block {
         Block b = {{acc[2 * i][2 * j], acc[2 * i][2 * j + 1], acc[2 * i + 1][2 * j], acc[2 * i + 1][2 * j + 1]}};
+        if constexpr (MODE == DENSE && EPI == EPI_STORE) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) b.q[q] *= scale;
+        }
         if constexpr (FP8 && !BSCALE) {
           float rs[2] = {1.f, 1.f};
           f32x4 cs[2];

@@ -170,10 +170,10 @@ int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const 
                        float* stats, float* z_target, hipStream_t s);
 struct VocabDxPlan { int tile; CutCost cost; size_t part_floats; };
 VocabDxPlan mfma_vocab_dx_plan(int R, int V, int d);
-int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, int R, int V, int d, const VocabDxPlan& plan, float* out, float* parts,
+int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, const float* scale, int R, int V, int d, const VocabDxPlan& plan, float* out, float* parts,
                   int* groups, hipStream_t s);
 size_t mfma_vocab_dw_part_floats(int R, int V, int d);
-int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
+int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, const float* scale, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
                   hipStream_t s);
 size_t router_bwd_ws_bytes(int T, int d, int E);
 int mfma_configure_all();          // per-device set-up of every grouped-GEMM kernel (moe_init)

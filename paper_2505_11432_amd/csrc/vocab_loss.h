@@ -4,7 +4,7 @@
 
 namespace moe {
 
-struct VocabCounts { int n; };          // rows that count
+struct VocabCounts { int n; float mean; };          // rows that count, 1 / n (0 without any)
 
 // Layout of a workspace (offsets in bytes) and the choices that follow from sizes alone
 struct VocabPlan {

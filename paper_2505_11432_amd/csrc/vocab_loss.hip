@@ -10,7 +10,8 @@
 // Rows whose target is left out are not computed: the rows that count are gathered to the front first, so that they cost nothing and whatever
 // they hold, NaN included, reaches no result.
 //
-// Rounding.  G is rounded to bf16 once, 2^-8 of an element at most.  In the column of the target it is nearly the whole row, and the rows of
+// Rounding.  G is rounded to bf16 once, 2^-8 of an element at most.  Where every token has the same weight G is kept without it and the products
+// take it as a factor: most rows then hold -1, which needs no rounding, in the column of the target.  In the column of the target it is nearly the whole row, and the rows of
 // few tokens would carry its rounding error undivided, so what the rounding took off (`rest`) is kept in fp32: dx gets rest * w[target] when its
 // parts are added, d_w one more row per token with rest in the target's column where the tokens are few (kFewRows), where that is free.
 #include "dense_plan.h"
@@ -112,7 +113,7 @@ __global__ void __launch_bounds__(1024) vocab_compact_kernel(const int32_t* __re
       }
     __syncthreads();
   }
-  if (threadIdx.x == 0) counts->n = base;
+  if (threadIdx.x == 0) *counts = VocabCounts{base, base ? 1.0f / (float)base : 0.f};
   for (int p = threadIdx.x; p < pieces; p += 1024) {
     const long left = (long)base - (long)p * R;
     const int n = left < 0 ? 0 : left < R ? (int)left : R;
@@ -163,7 +164,7 @@ __global__ void __launch_bounds__(256) vocab_prepare_kernel(const TX* __restrict
   __syncthreads();
   const int n = all[0] + all[1] + all[2] + all[3];
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    counts->n = n;
+    *counts = VocabCounts{n, n ? 1.0f / (float)n : 0.f};
     ranges[0] = ranges[2] = 0;
     ranges[1] = n;
     ranges[3] = 2 * n;
@@ -247,7 +248,7 @@ struct RowOut {
   float* rest;                   // what rounding took off G in the target's column
 };
 
-__device__ __forceinline__ float row_weight(const RowOut& o, int t) { return o.token_w ? o.token_w[t] : 1.0f / (float)o.counts->n; }
+__device__ __forceinline__ float row_weight(const RowOut& o, int t) { return o.token_w ? o.token_w[t] : o.counts->mean; }
 
 // exp(z - maximum of its part) in fp16 -> G in bf16, in place, a workgroup per row.  Bound by memory: 4 bytes per element.
 __global__ void __launch_bounds__(256) vocab_grad_rows_kernel(const f32x2* __restrict__ stats, int parts, int part_shift, const float* __restrict__ z_target,
@@ -261,14 +262,14 @@ __global__ void __launch_bounds__(256) vocab_grad_rows_kernel(const f32x2* __res
   join_block(m, s, lds);
   const int t = o.token[r], tg = o.target_of[r];
   const RowLoss l = row_loss(z_target[r], m, s);
-  const float c = row_weight(o, t), g_target = -c * l.miss;
+  const float weight = row_weight(o, t), c = o.token_w ? weight : 1.0f, g_target = -c * l.miss;
   const bf16 g_rounded = static_cast<bf16>(g_target);
   const float rest = g_target - static_cast<float>(g_rounded);
   if (threadIdx.x == 0) {
     o.loss[t] = l.loss;
     o.lse[t] = l.lse;
-    o.weighted[r] = c * l.loss;
-    o.rest[r] = rest;
+    o.weighted[r] = weight * l.loss;
+    o.rest[r] = o.token_w ? rest : weight * rest;
   }
   char* row = G + (long)r * ld * 2;
   for (int v = threadIdx.x * 8; v < ld; v += 256 * 8) {
@@ -618,8 +619,9 @@ int bf16_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, c
   float* dxc = reinterpret_cast<float*>(ws + p.dxc);
   float* parts = reinterpret_cast<float*>(ws + p.parts);
   const VocabDxPlan plan = mfma_vocab_dx_plan(R, V, d);
+  const float* scale = q.token_w ? nullptr : &o.counts->mean;
   int groups = 0;
-  rc = mfma_vocab_dx(ws + p.G, p.ld, q.w, o.range + 1, R, V, d, plan, dxc, parts, &groups, s);
+  rc = mfma_vocab_dx(ws + p.G, p.ld, q.w, o.range + 1, scale, R, V, d, plan, dxc, parts, &groups, s);
   if (rc != MOE_OK) return rc;
   const bool last = piece + 1 == p.pieces;
   const dim3 grid(blocks_for((long)R * d / 8) + last);
@@ -630,8 +632,8 @@ int bf16_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, c
   else vocab_dx_kernel<128><<<grid, dim3(256), 0, s>>>(dxc, parts, groups, plan.cost, w, d, V, o, static_cast<bf16*>(q.dx), weighted, total);
   MOE_LAUNCH_CHECK();
   const int32_t* n_dw = p.twice ? o.range + 3 : o.range + 1;
-  if (p.dw_sum_used) return mfma_vocab_dw(ws + p.G, p.ld, xc, n_dw, R, V, d, ws + p.dw_sum, MOE_F32, piece > 0, parts, s);
-  return mfma_vocab_dw(ws + p.G, p.ld, xc, n_dw, p.twice ? 2 * R : R, V, d, q.d_w, q.grad_dt, q.accumulate || piece > 0, parts, s);
+  if (p.dw_sum_used) return mfma_vocab_dw(ws + p.G, p.ld, xc, n_dw, scale, R, V, d, ws + p.dw_sum, MOE_F32, piece > 0, parts, s);
+  return mfma_vocab_dw(ws + p.G, p.ld, xc, n_dw, scale, p.twice ? 2 * R : R, V, d, q.d_w, q.grad_dt, q.accumulate || piece > 0, parts, s);
 }
 
 }  // namespace
