@@ -40,7 +40,7 @@ std::vector<configure_fn>& configure_registry() {
 
 template <int BM, int BN, int BKT, int NS, int WM, int WN, Layout LA, Layout LB, Mode MODE, Epi EPI, typename TC, typename TIN>
 struct KernelSetup {
-  static constexpr int smem = dma_smem_bytes<BM, BN, BKT, NS, WM * WN, LA, LB, (int)sizeof(TIN)>(EPI == EPI_LSE || EPI == EPI_CE);
+  static constexpr int smem = dma_smem_bytes<BM, BN, BKT, NS, WM * WN, LA, LB, (int)sizeof(TIN)>(EPI != EPI_LSE, EPI == EPI_LSE || EPI == EPI_CE ? target_bytes<BM / WM>() : 0);
   static_assert(smem <= 160 * 1024, "LDS of a CU");
   static auto kernel() { return grouped_gemm_dma_kernel<BM, BN, BKT, NS, WM, WN, LA, LB, MODE, EPI, TC, TIN>; }
   // Idempotent and safe to race: the attribute value is the same on every call, the per-device bit only saves work.
@@ -322,11 +322,22 @@ int mfma_router_fwd(const void* x, const void* w_r, const float* bias, int T, in
 
 // ---- vocabulary products (vocab_loss.hip).  `rows` (device, at most R) is the number of rows present.
 namespace {
-// Tile of z = x w^T with its softmax epilogue, as for a plain store.  WTN columns of a wave share one pair of statistics.
-RowTile vocab_tile(int R, int V, int d) { return plan_rows({false, true, false}, R, 1, V, d, 2).tile; }
+template <Epi EPI> int launch_softmax(const Args& a, VocabTile tile, hipStream_t s) {
+  switch (tile) {
+    case VocabTile::ROWS64: return launch<64, 128, 128, 3, 2, 2, KMAJOR, KMAJOR, DENSE, EPI, bf16>(a, 1, s);
+    case VocabTile::ROWS128: return launch<128, 128, 64, 3, 4, 2, KMAJOR, KMAJOR, DENSE, EPI, bf16>(a, 1, s);
+    case VocabTile::ROWS192: return launch<192, 256, 64, 2, 2, 4, KMAJOR, KMAJOR, DENSE, EPI, bf16>(a, 1, s);
+    case VocabTile::ROWS320:
+      if constexpr (EPI == EPI_LSE) return launch<320, 256, 64, 2, 2, 4, KMAJOR, KMAJOR, DENSE, EPI, bf16>(a, 1, s);
+      else return MOE_ERR_UNSUPPORTED;
+    default: return launch<256, 256, 64, 2, 4, 2, KMAJOR, KMAJOR, DENSE, EPI, bf16>(a, 1, s);
+  }
+}
 }  // namespace
-VocabTiles mfma_vocab_tiles(int R, int V, int d) {
-  return vocab_tile(R, V, d) == RowTile::FULL ? VocabTiles{cdiv(V, 256) * 2, 7} : VocabTiles{cdiv(V, 128) * 2, 6};
+VocabTiles mfma_vocab_tiles(int R, int V, int d, bool grad) {
+  const VocabTile t = vocab_tile(R, V, d, grad);
+  const bool narrow = t == VocabTile::ROWS64 || t == VocabTile::ROWS128, by64 = narrow || t != VocabTile::ROWS256;
+  return {narrow ? cdiv(V, 128) * 2 : cdiv(V, 256) * (by64 ? 4 : 2), by64 ? 6 : 7};
 }
 int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const int32_t* target, int R, int V, int d, void* P, long ldp,
                        float* stats, float* z_target, hipStream_t s) {
@@ -335,16 +346,9 @@ int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const 
   a.B = w; a.ldb = d;
   a.C = P; a.ldc = ldp;
   a.E = 1; a.M = R; a.N = V; a.K = d;
-  a.rows = rows; a.target = target; a.stats = stats; a.z_target = z_target; a.parts = mfma_vocab_tiles(R, V, d).parts;
-  const RowTile tile = vocab_tile(R, V, d);
-  if (P) {
-    if (tile == RowTile::FEW) return launch<64, 128, 128, 3, 2, 2, KMAJOR, KMAJOR, DENSE, EPI_CE, bf16>(a, 1, s);
-    if (tile == RowTile::MID) return launch<128, 128, 64, 3, 4, 2, KMAJOR, KMAJOR, DENSE, EPI_CE, bf16>(a, 1, s);
-    return launch<256, 256, 64, 2, 4, 2, KMAJOR, KMAJOR, DENSE, EPI_CE, bf16>(a, 1, s);
-  }
-  if (tile == RowTile::FEW) return launch<64, 128, 128, 3, 2, 2, KMAJOR, KMAJOR, DENSE, EPI_LSE, bf16>(a, 1, s);
-  if (tile == RowTile::MID) return launch<128, 128, 64, 3, 4, 2, KMAJOR, KMAJOR, DENSE, EPI_LSE, bf16>(a, 1, s);
-  return launch<256, 256, 64, 2, 4, 2, KMAJOR, KMAJOR, DENSE, EPI_LSE, bf16>(a, 1, s);
+  a.rows = rows; a.target = target; a.stats = stats; a.z_target = z_target; a.parts = mfma_vocab_tiles(R, V, d, P != nullptr).parts;
+  const VocabTile tile = vocab_tile(R, V, d, P != nullptr);
+  return P ? launch_softmax<EPI_CE>(a, tile, s) : launch_softmax<EPI_LSE>(a, tile, s);
 }
 
 // Costs of their tiles (row_plan.h): dx on 256 x 256 and on 128 x 128, whose parts the pass that rounds and places the rows reads anyway; d_w on

@@ -392,12 +392,15 @@ __global__ void __launch_bounds__(256) dense_fixup_kernel(const float* __restric
   }
 }
 
+// LDS of the targets of a wave's rows (vocabulary products): a 4-byte load per lane, 64 rows at a time
+template <int WTM> constexpr int target_bytes() { return (WTM + 63) / 64 * 256; }
+
 template <int BM, int BN, int BKT, int NSTAGE, int NW, Layout LA, Layout LB, int ESZ = 2>
-constexpr int dma_smem_bytes(bool targets = false) {
+constexpr int dma_smem_bytes(bool patches = true, int targets = 0) {
   // the ring, the per-expert tile table and one epilogue patch per wave
   return NSTAGE * (DmaTileBytes<LA, BM, BKT, ESZ>::value + DmaTileBytes<LB, BN, BKT, ESZ>::value) + (MOE_MAX_EXPERTS + 8) * 4 +
-         NW * STG_BYTES + 256 + 1024 +       // + the dump area of the L2 touches + the block-scale ring
-         (targets ? NW * 256 : 0);          // + the targets of each wave's rows (vocabulary products)
+         (patches ? NW * STG_BYTES : 0) + 256 + 1024 +       // + the dump area of the L2 touches + the block-scale ring
+         NW * targets;                      // + the targets of each wave's rows
 }
 
 // Two workgroups of such a kernel share a CU's LDS; the launch makes twice the workgroups.
@@ -464,6 +467,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   int* cum_tiles = reinterpret_cast<int*>(smem + RING_BYTES);          // [E+1] running count of m-tiles (ROWSEG)
   constexpr int TABLE_BYTES = (MOE_MAX_EXPERTS + 8) * 4;
 
+  constexpr int PATCHES = EPI == EPI_LSE ? 0 : NW * STG_BYTES;          // (statistics alone need no patch)
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // Waves w and w + 4 of eight share a SIMD.  In FC1 they lie in opposite halves of the tile along both sides, elsewhere along one.  Of 8
@@ -554,13 +558,12 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   constexpr bool TOUCH_K = MODE == KSEG && !FP8 && SPLIT && LA == MNMAJOR && LB == MNMAJOR && NSTAGE == 4;
   constexpr bool TOUCH_K2 = (MODE == KSEG || MODE == DENSE) && !FP8 && SPLIT && LA == MNMAJOR && LB == MNMAJOR && NSTAGE == 2 && BKT == 64;
   const bool is_toucher = (TOUCH || TOUCH_K || TOUCH_K2) && wave == NL;
-  const unsigned lds_dump = smem_lds + RING_BYTES + TABLE_BYTES + NW * STG_BYTES;
+  const unsigned lds_dump = smem_lds + RING_BYTES + TABLE_BYTES + PATCHES;
   const unsigned scale_lds = lds_dump + 256;                                   // block-scale ring: 2 stages x (256 + 256) bytes
-  constexpr int TARGETS_AT = RING_BYTES + TABLE_BYTES + NW * STG_BYTES + 256 + 1024;       // behind the block-scale ring
-  static_assert(!VOCAB || WTM <= 64, "a lane per row");
-  const unsigned target_lds = smem_lds + TARGETS_AT + (unsigned)wave * 256u;
-  const char* target_smem = smem + TARGETS_AT + wave * 256;
-  const char* scale_smem = smem + RING_BYTES + TABLE_BYTES + NW * STG_BYTES + 256;
+  constexpr int TARGETS_AT = RING_BYTES + TABLE_BYTES + PATCHES + 256 + 1024;       // behind the block-scale ring
+  const unsigned target_lds = smem_lds + TARGETS_AT + (unsigned)(wave * target_bytes<WTM>());
+  const char* target_smem = smem + TARGETS_AT + wave * target_bytes<WTM>();
+  const char* scale_smem = smem + RING_BYTES + TABLE_BYTES + PATCHES + 256;
   unsigned ta_off = 0;
   // rotation of this workgroup's load order within the A / B tile (see open_tile); only where it pays: the e4m3
   // row-segmented kernels (in the others the extra scalar state pushes tile offsets out of registers)
@@ -793,7 +796,11 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   auto issue_prologue = [&]() __attribute__((always_inline)) {
     // The targets of this wave's rows go to LDS ahead of the tile, without a register that the compiler would guard (a wait in front of the
     // fragment reads): the waits of the k loop, which ends with nothing outstanding, cover them.
-    if constexpr (VOCAB) touch4s(reinterpret_cast<const char*>(p.target), (unsigned)min(m0 + wm * WTM + lane, p.M - 1) * 4u, target_lds);
+    if constexpr (VOCAB) {
+#pragma unroll
+      for (int r = 0; r < WTM; r += 64)
+        touch4s(reinterpret_cast<const char*>(p.target), (unsigned)min(m0 + wm * WTM + r + lane, p.M - 1) * 4u, target_lds + r * 4);
+    }
 #pragma unroll
     for (int s = 0; s < NSTAGE - 1; ++s)
       if (s < nk) issue(s);

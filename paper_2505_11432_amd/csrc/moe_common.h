@@ -165,7 +165,7 @@ int mfma_router_dwr(const void* g, const void* x, const int32_t* chunk_offsets, 
 int mfma_router_dx(const void* g, const void* w_r, int T, int d, int E, void* dx, hipStream_t s);
 // vocabulary products in bf16 (gemm_mfma.hip); `rows` is read on the device
 struct VocabTiles { int parts, shift; };           // pairs of softmax statistics per row, each of 2^shift columns
-VocabTiles mfma_vocab_tiles(int R, int V, int d);
+VocabTiles mfma_vocab_tiles(int R, int V, int d, bool grad);
 int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const int32_t* target, int R, int V, int d, void* P, long ldp,
                        float* stats, float* z_target, hipStream_t s);
 struct VocabDxPlan { int tile; CutCost cost; size_t part_floats; };

@@ -150,6 +150,33 @@ inline bool wgrad_in_pairs(int rows, int E, int M, int N) {
   return pairs_us(small, {11, 0.75, 6, 0.8}, steps) < rounds * (9.5 + 1.5 * steps) + 6.5 * large / 256;
 }
 
+// Tile of the vocabulary product x w^T with its softmax epilogue: 64 or 128 rows by 128 words, 192, 256 or 320 rows (forward only: with what a
+// gradient keeps it does not fit LDS) by 256.  Rows that a tile has too many cost as much as rows that count, and its tiles cannot be cut along the
+// contraction: the softmax needs whole sums.  So by the time of the rounds (us per tile, and per 64 of the contraction).
+// Measured (us, forward; 64, 128, 192, 256, 320 rows):
+//   50257 words, 2048 wide: 64 rows 40, 43, 43, 44, 53; 150 76, 78, 42, 46, 54; 257 122, 101, 77, 89, 65; 500 191, 141, 119, 98, 121; 640 232, 164, 147, 137, 122
+//   32000 words, 4096 wide: 100 rows 62, 46, 69, 74, 93; 257 145, 120, 85, 91, 105; 700 302, 230, 171, 178, 213; 2500 1060, 780, 556, 495, 487
+//   8000 words, 1024 wide: 128 rows 13.5, 16.1, 23.5, 26.3, 30.7; 500 27.5, 22.0, 29.5, 33.4, 39.3; 1500 60, 45, 34, 37, 43
+enum class VocabTile { ROWS64, ROWS128, ROWS192, ROWS256, ROWS320 };
+inline VocabTile vocab_tile(int R, int V, int d, bool grad) {
+  auto up = [](long a, long b) { return (a + b - 1) / b; };
+  const struct { VocabTile tile; int rows, words; double fixed, step; } all[] = {
+      {VocabTile::ROWS256, 256, 256, 7, 1.4}, {VocabTile::ROWS64, 64, 128, 5, 0.33}, {VocabTile::ROWS128, 128, 128, 3, 0.55},
+      {VocabTile::ROWS192, 192, 256, 8, 1.1}, {VocabTile::ROWS320, 320, 256, 10, 1.75}};
+  const double steps = (double)up(d, 64);
+  VocabTile best = VocabTile::ROWS256;
+  double best_us = 1e30;
+  for (const auto& t : all) {
+    if (grad && t.tile == VocabTile::ROWS320) continue;
+    const double us = (double)up(up(R, t.rows) * up(V, t.words), 256) * (t.fixed + t.step * steps);
+    if (us < best_us) {
+      best_us = us;
+      best = t.tile;
+    }
+  }
+  return best;
+}
+
 // ---- dense products (the vocabulary's): one long contraction and any number of tiles, so that the last round may leave most CUs idle.  Its `rem`
 // tiles are cut along their `steps` k-steps into parts that run on different workgroups and write fp32 tiles, which another kernel adds up: 1 to
 // 64 parts, of four steps at least, by the time of the rounds.  The number of rows is known on the device only, so the choice is made there, by

@@ -41,15 +41,15 @@ __device__ __forceinline__ void join_wave(float& m, float& s) {
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) join(m, s, __shfl_xor(m, off), __shfl_xor(s, off));
 }
-// over the 256 threads of a workgroup; every thread gets the result
-__device__ __forceinline__ void join_block(float& m, float& s, f32x2 (&lds)[4]) {
+// over the WAVES waves of a workgroup; every thread gets the result
+template <int WAVES> __device__ __forceinline__ void join_block(float& m, float& s, f32x2 (&lds)[WAVES]) {
   join_wave(m, s);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = f32x2{m, s};
   __syncthreads();
   m = lds[0][0];
   s = lds[0][1];
 #pragma unroll
-  for (int i = 1; i < 4; ++i) join(m, s, lds[i][0], lds[i][1]);
+  for (int i = 1; i < WAVES; ++i) join(m, s, lds[i][0], lds[i][1]);
 }
 
 // A row's loss from its target's logit and the other words' maximum m and sum s of exp(z - m): 1 - p keeps its precision where p is near 1.
@@ -250,15 +250,17 @@ struct RowOut {
 
 __device__ __forceinline__ float row_weight(const RowOut& o, int t) { return o.token_w ? o.token_w[t] : o.counts->mean; }
 
-// exp(z - maximum of its part) in fp16 -> G in bf16, in place, a workgroup per row.  Bound by memory: 4 bytes per element.
-__global__ void __launch_bounds__(256) vocab_grad_rows_kernel(const f32x2* __restrict__ stats, int parts, int part_shift, const float* __restrict__ z_target,
+// exp(z - maximum of its part) in fp16 -> G in bf16, in place, a workgroup per row, of 256 threads or, where rows are few, of 1024.  Bound by
+// memory: 4 bytes per element (8192 rows of 32000 words 197 us, 5.3 TB/s).
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) vocab_grad_rows_kernel(const f32x2* __restrict__ stats, int parts, int part_shift, const float* __restrict__ z_target,
                                                               int V, long ld, int twice, char* __restrict__ G, RowOut o) {
-  __shared__ f32x2 lds[4];
+  __shared__ f32x2 lds[THREADS / 64];
   const int r = blockIdx.x, n = o.range[1];
   if (r >= n) return;
   const f32x2* row_stats = stats + (long)r * parts;
   float m = kLowest, s = 0.f;
-  for (int i = threadIdx.x; i < parts; i += 256) join(m, s, row_stats[i][0], row_stats[i][1]);
+  for (int i = threadIdx.x; i < parts; i += THREADS) join(m, s, row_stats[i][0], row_stats[i][1]);
   join_block(m, s, lds);
   const int t = o.token[r], tg = o.target_of[r];
   const RowLoss l = row_loss(z_target[r], m, s);
@@ -272,7 +274,7 @@ __global__ void __launch_bounds__(256) vocab_grad_rows_kernel(const f32x2* __res
     o.rest[r] = o.token_w ? rest : weight * rest;
   }
   char* row = G + (long)r * ld * 2;
-  for (int v = threadIdx.x * 8; v < ld; v += 256 * 8) {
+  for (int v = threadIdx.x * 8; v < ld; v += THREADS * 8) {
     const f16x8 p = *reinterpret_cast<const f16x8*>(row + (long)v * 2);
     bf16x8 g;
     // eight columns lie in one part; past the width nothing was written
@@ -294,9 +296,9 @@ __global__ void __launch_bounds__(256) vocab_grad_rows_kernel(const f32x2* __res
 }
 
 // fp32: the logits of a piece are in Z, in n_parts parts; loss and lse, and with GRAD G in the place of the first part.
-template <bool GRAD>
-__global__ void __launch_bounds__(256) vocab_rows_f32_kernel(float* __restrict__ Z, int n_parts, long part_stride, int V, long ld, RowOut o) {
-  __shared__ f32x2 lds[4];
+template <bool GRAD, int THREADS>
+__global__ void __launch_bounds__(THREADS) vocab_rows_f32_kernel(float* __restrict__ Z, int n_parts, long part_stride, int V, long ld, RowOut o) {
+  __shared__ f32x2 lds[THREADS / 64];
   const int r = blockIdx.x;
   if (r >= o.range[1]) return;
   float* row = Z + (long)r * ld;
@@ -305,7 +307,7 @@ __global__ void __launch_bounds__(256) vocab_rows_f32_kernel(float* __restrict__
   for (int p = 1; p < n_parts; ++p) zt += row[p * part_stride + tg];
   if (n_parts > 1) __syncthreads();        // (the sums go over the first part)
   float m = kLowest, s = 0.f;
-  for (int v = threadIdx.x * 4; v < V; v += 1024) {
+  for (int v = threadIdx.x * 4; v < V; v += THREADS * 4) {
     f32x4 z = *reinterpret_cast<const f32x4*>(row + v);
     if (n_parts > 1) {
       for (int p = 1; p < n_parts; ++p) z += *reinterpret_cast<const f32x4*>(row + p * part_stride + v);
@@ -327,7 +329,7 @@ __global__ void __launch_bounds__(256) vocab_rows_f32_kernel(float* __restrict__
   if constexpr (GRAD) {                    // (every thread has read the target's logit and its share of the row: join_block waits for all)
     const float c = row_weight(o, t), g_target = -c * l.miss;
     if (threadIdx.x == 0) o.weighted[r] = c * l.loss;
-    for (int v = threadIdx.x * 4; v < ld; v += 1024) {
+    for (int v = threadIdx.x * 4; v < ld; v += THREADS * 4) {
       f32x4 z = *reinterpret_cast<const f32x4*>(row + v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) z[i] = v + i >= V ? 0.f : v + i == tg ? g_target : c * exp_f32((z[i] - l.top) - l.log_sum);
@@ -376,6 +378,7 @@ __global__ void __launch_bounds__(256) vocab_dx_kernel(const float* __restrict__
     } else {
       const float* src = parts + (long)(l - cut.full_tiles) * cut.split * (TILE * TILE) + (r % TILE) * TILE + c % TILE;
       a = b = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
       for (int p = 0; p < cut.split; ++p, src += TILE * TILE) {
         a += *reinterpret_cast<const f32x4*>(src);
         b += *reinterpret_cast<const f32x4*>(src + 4);
@@ -449,6 +452,8 @@ constexpr int kFewRows = 128;
 constexpr int kScoreAsIs = 256;
 // Up to so many tokens every workgroup of the gathering counts them itself.
 constexpr int kPrepareTokens = 2048;
+// Up to so many rows a row's pass has 1024 threads instead of 256: the CUs hold no more workgroups anyway.
+constexpr int kFewGroups = 512;
 // fp32 products in parts: floats that all parts may take
 constexpr size_t kPartFloats = (size_t)64 << 20;
 
@@ -512,7 +517,7 @@ VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int p
     p.z = plan_f32(f32_logits(p, nullptr, nullptr, nullptr, d, V, nullptr));
     p.G = take(at, (size_t)p.z.parts * R * p.ld * 4);
   } else {
-    p.tiles = mfma_vocab_tiles(p.R, V, d);
+    p.tiles = mfma_vocab_tiles(p.R, V, d, grad);
     p.stats = take(at, R * p.tiles.parts * 8);
     p.z_target = take(at, R * 4);
     if (grad) p.G = take(at, copies * R * p.ld * 2);
@@ -581,11 +586,13 @@ int f32_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, co
   int rc = launch_f32(f32_logits(p, xc, q.w, o.range, d, V, Z), p.z, s);
   if (rc != MOE_OK) return rc;
   if (!q.grad) {
-    vocab_rows_f32_kernel<false><<<dim3(R), dim3(256), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
+    if (R <= kFewGroups) vocab_rows_f32_kernel<false, 1024><<<dim3(R), dim3(1024), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
+    else vocab_rows_f32_kernel<false, 256><<<dim3(R), dim3(256), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
     MOE_LAUNCH_CHECK();
     return MOE_OK;
   }
-  vocab_rows_f32_kernel<true><<<dim3(R), dim3(256), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
+  if (R <= kFewGroups) vocab_rows_f32_kernel<true, 1024><<<dim3(R), dim3(1024), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
+  else vocab_rows_f32_kernel<true, 256><<<dim3(R), dim3(256), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
   MOE_LAUNCH_CHECK();
   float* dxc = reinterpret_cast<float*>(ws + p.dxc);
   rc = launch_f32(f32_dx(p, Z, q.w, o.range, d, V, dxc), p.dx, s);
@@ -614,7 +621,9 @@ int bf16_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, c
   int rc = mfma_vocab_softmax(xc, q.w, o.range + 1, o.target_of, R, V, d, q.grad ? ws + p.G : nullptr, p.ld, stats, z_target, s);
   if (rc != MOE_OK) return rc;
   if (!q.grad) return score_rows(q, p, stats, z_target, o.target_of, o.token, o.range, s);
-  vocab_grad_rows_kernel<<<dim3(R), dim3(256), 0, s>>>(reinterpret_cast<const f32x2*>(stats), p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
+  const f32x2* st = reinterpret_cast<const f32x2*>(stats);
+  if (R <= kFewGroups) vocab_grad_rows_kernel<1024><<<dim3(R), dim3(1024), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
+  else vocab_grad_rows_kernel<256><<<dim3(R), dim3(256), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
   MOE_LAUNCH_CHECK();
   float* dxc = reinterpret_cast<float*>(ws + p.dxc);
   float* parts = reinterpret_cast<float*>(ws + p.parts);
