@@ -193,8 +193,8 @@ __device__ __forceinline__ unsigned block_offset(int r, int c, long ld, int esz,
   return (r < rows_valid && c < cols_valid) ? (unsigned)(((long)r * ld + c) * esz) : BUF_OOB;
 }
 
-// 32 rows x 32 bf16 columns from registers to global memory (row-major, leading dimension ld elements).
-__device__ __forceinline__ void stage_store_bf16(char* stg, const bf16x4 (&v)[4], bf16* g, long ld, int rows_valid,
+// 32 rows x 32 bf16 columns from registers to global memory (row-major, leading dimension ld elements).  AUX 2: past the caches.
+template <int AUX = 0> __device__ __forceinline__ void stage_store_bf16(char* stg, const bf16x4 (&v)[4], bf16* g, long ld, int rows_valid,
                                                  int cols_valid, int lane) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) *reinterpret_cast<bf16x4*>(stg + patch_row(q, lane) * STG_STRIDE + patch_col(q, lane) * 2) = v[q];
@@ -203,7 +203,7 @@ __device__ __forceinline__ void stage_store_bf16(char* stg, const bf16x4 (&v)[4]
   for (int pass = 0; pass < 2; ++pass) {
     const int r = pass * 16 + (lane >> 2), c = (lane & 3) * 8;
     const u32x4v val = *reinterpret_cast<const u32x4v*>(stg + r * STG_STRIDE + c * 2);
-    __builtin_amdgcn_raw_buffer_store_b128(val, rs, block_offset(r, c, ld, 2, rows_valid, cols_valid), 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(val, rs, block_offset(r, c, ld, 2, rows_valid, cols_valid), 0, AUX);
   }
 }
 
@@ -246,7 +246,7 @@ __device__ __forceinline__ void stage_unpack_bf16(char* stg, const StageFetch& f
 }
 
 // 32 rows x 32 fp32 columns, as two halves of 16 columns; optional read-modify-write accumulation.
-__device__ __forceinline__ void stage_store_f32(char* stg, const Block& acc, float* g, long ld, int rows_valid,
+template <int AUX = 0> __device__ __forceinline__ void stage_store_f32(char* stg, const Block& acc, float* g, long ld, int rows_valid,
                                                 int cols_valid, bool accumulate, int lane) {
   const __amdgpu_buffer_rsrc_t rs = block_rsrc(g);
 #pragma unroll
@@ -260,7 +260,7 @@ __device__ __forceinline__ void stage_store_f32(char* stg, const Block& acc, flo
       f32x4 val = *reinterpret_cast<const f32x4*>(stg + r * STG_STRIDE + (lane & 3) * 16);
       const unsigned off = block_offset(r, c, ld, 4, rows_valid, cols_valid);
       if (accumulate) val += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));   // (uniform)
-      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4v, val), rs, off, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4v, val), rs, off, 0, AUX);
     }
   }
 }
@@ -435,6 +435,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
   constexpr bool SWI = EPI == EPI_SWIGLU || EPI == EPI_SWIGLU_W;              // FC1 + SwiGLU epilogue
   constexpr bool FOLD = EPI == EPI_SWIGLU_W || EPI == EPI_SWIGLU_BWD_W;       // gate weight folded in (Section 4.1)
   constexpr bool GATHER_A = EPI == EPI_SWIGLU_W;                              // A rows selected by index map (Section 4.2)
+  // the vocabulary gradient is not read again before much else has been
+  constexpr int STORE_AUX = MODE == DENSE && LA == MNMAJOR ? 2 : 0;
   constexpr bool VOCAB = EPI == EPI_LSE || EPI == EPI_CE;
   static_assert(!VOCAB || (MODE == DENSE && !FP8), "the softmax epilogues exist for dense bf16 products");
   static_assert(!FOLD || (!FP8 && MODE == ROWSEG && LA == KMAJOR), "the folded order exists for the bf16 row-segmented kernels");
@@ -1128,7 +1130,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
             const Block b = block(i, j);
             if constexpr (sizeof(TC) == 4) {
               float* g = static_cast<float*>(p.C) + (long)e * p.c_es + (long)mb * p.ldc + nb;
-              stage_store_f32(stg, b, g, p.ldc, rows_valid, cols_valid, p.accumulate != 0, lane);
+              stage_store_f32<STORE_AUX>(stg, b, g, p.ldc, rows_valid, cols_valid, p.accumulate != 0, lane);
             } else {
               bf16* g = static_cast<bf16*>(p.C) + (long)e * p.c_es + (long)mb * p.ldc + nb;
               bf16x4 v[4];
@@ -1146,7 +1148,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
 #pragma unroll
                   for (int t = 0; t < 4; ++t) v[q][t] = static_cast<bf16>(b.q[q][t]);
               }
-              stage_store_bf16(stg, v, g, p.ldc, rows_valid, cols_valid, lane);
+              stage_store_bf16<STORE_AUX>(stg, v, g, p.ldc, rows_valid, cols_valid, lane);
             }
           }
         }

@@ -66,7 +66,7 @@ __device__ __forceinline__ RowLoss row_loss(float zt, float m, float s) {
 }
 
 // Rows that count, in their order: token[i] = t, target_of[i] = its target; n; the pieces' numbers of rows.
-// One workgroup: 8192 targets at a time, eight per thread.
+// One workgroup: 8192 targets at a time, eight per thread.  (For lists that are too long for vocab_compact_few_kernel.)
 __global__ void __launch_bounds__(1024) vocab_compact_kernel(const int32_t* __restrict__ target, int T, int V, int R, int pieces,
                                                              int32_t* __restrict__ token, int32_t* __restrict__ target_of,
                                                              VocabCounts* __restrict__ counts, int32_t* __restrict__ ranges) {
@@ -123,6 +123,67 @@ __global__ void __launch_bounds__(1024) vocab_compact_kernel(const int32_t* __re
   if (threadIdx.x == 0) {                   // behind the pieces: the rows of d_w's contraction where every row comes twice
     ranges[2 * pieces] = 0;
     ranges[2 * pieces + 1] = 2 * base;
+  }
+}
+
+// The same by a workgroup per 1024 tokens, each of which counts all targets in front of its own (16384 tokens: one workgroup 17 us).
+__global__ void __launch_bounds__(256) vocab_compact_few_kernel(const int32_t* __restrict__ target, int T, int V, int R, int pieces, int32_t* __restrict__ token,
+                                                                int32_t* __restrict__ target_of, VocabCounts* __restrict__ counts, int32_t* __restrict__ ranges) {
+  __shared__ int sums[2][4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * 1024;
+  auto keeps = [&](int tg) __attribute__((always_inline)) { return tg >= 0 && tg < V ? 1 : 0; };
+  typedef __attribute__((ext_vector_type(4))) int i32x4;
+  typedef i32x4 i32x4_u __attribute__((aligned(4)));
+  int lower = 0;
+#pragma unroll 4
+  for (int t = threadIdx.x * 4; t < first; t += 1024) {             // (whole quads: `first` is a multiple of 1024)
+    const i32x4 tg = *reinterpret_cast<const i32x4_u*>(target + t);
+    lower += keeps(tg[0]) + keeps(tg[1]) + keeps(tg[2]) + keeps(tg[3]);
+  }
+  const int t0 = first + threadIdx.x * 4;
+  int tg[4], mine = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    tg[i] = t0 + i < T ? target[t0 + i] : -1;
+    mine += keeps(tg[i]);
+  }
+  int incl = mine;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int o = __shfl_up(incl, off);
+    if (lane >= off) incl += o;
+    lower += __shfl_xor(lower, off);
+  }
+  if (lane == 63) {
+    sums[0][wave] = lower;
+    sums[1][wave] = incl;
+  }
+  __syncthreads();
+  int at = incl - mine, base = 0;
+  for (int w = 0; w < 4; ++w) {
+    base += sums[0][w];
+    if (w < wave) at += sums[1][w];
+  }
+  at += base;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (keeps(tg[i])) {
+      token[at] = t0 + i;
+      target_of[at] = tg[i];
+      ++at;
+    }
+  if (blockIdx.x + 1 == gridDim.x) {                      // the last one has them all
+    const int n = base + sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+    if (threadIdx.x == 0) {
+      *counts = VocabCounts{n, n ? 1.0f / (float)n : 0.f};
+      ranges[2 * pieces] = 0;
+      ranges[2 * pieces + 1] = 2 * n;
+    }
+    for (int p = threadIdx.x; p < pieces; p += 256) {
+      const long left = (long)n - (long)p * R;
+      ranges[2 * p] = 0;
+      ranges[2 * p + 1] = left < 0 ? 0 : left < R ? (int)left : R;
+    }
   }
 }
 
@@ -250,7 +311,7 @@ struct RowOut {
 
 __device__ __forceinline__ float row_weight(const RowOut& o, int t) { return o.token_w ? o.token_w[t] : o.counts->mean; }
 
-// exp(z - maximum of its part) in fp16 -> G in bf16, in place, a workgroup per row, of 256 threads or, where rows are few, of 1024.  Bound by
+// exp(z - maximum of its part) in fp16 -> G in bf16, in place, a workgroup per row, of 256 threads, where rows are few of 1024, where they are short of one wave.  Bound by
 // memory: 4 bytes per element (8192 rows of 32000 words 197 us, 5.3 TB/s).
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) vocab_grad_rows_kernel(const f32x2* __restrict__ stats, int parts, int part_shift, const float* __restrict__ z_target,
@@ -355,9 +416,9 @@ __device__ __forceinline__ void sum_total(const float* __restrict__ weighted, in
 }
 
 // dx of the piece's rows: the product's whole tiles, or the sum of a cut tile's parts, with what the rounding of G took off in the target's
-// column, rounded once.  With the last piece a further workgroup makes the total.
+// column, rounded once; `each` pieces of 16 bytes per thread.  With the last piece a further workgroup makes the total.
 template <int TILE>
-__global__ void __launch_bounds__(256) vocab_dx_kernel(const float* __restrict__ whole, const float* __restrict__ parts, int groups, CutCost cost,
+__global__ void __launch_bounds__(256) vocab_dx_kernel(int each, const float* __restrict__ whole, const float* __restrict__ parts, int groups, CutCost cost,
                                                        const bf16* __restrict__ w, int d, int V, const RowOut o, bf16* __restrict__ dx,
                                                        const float* __restrict__ weighted, float* __restrict__ total) {
   if (total && blockIdx.x == gridDim.x - 1) {
@@ -365,10 +426,12 @@ __global__ void __launch_bounds__(256) vocab_dx_kernel(const float* __restrict__
     return;
   }
   const int n = o.range[1], vecs = d / 8, tiles_m = (n + TILE - 1) / TILE, tiles_n = (d + TILE - 1) / TILE;
+  const long first = (long)blockIdx.x * each * 256, left = (long)n * vecs - first;
+  if (left <= 0) return;
+  const int row0 = (int)(first / vecs), in_row0 = (int)(first - (long)row0 * vecs), items = (int)min(left, each * 256L);
   const DensePlan cut = dense_plan(tiles_m * tiles_n, groups, (V + 63) / 64, cost, true);
-  const long items = (long)n * vecs, blocks = gridDim.x - (total ? 1 : 0);
-  for (long i = blockIdx.x * 256L + threadIdx.x; i < items; i += blocks * 256L) {
-    const int r = (int)(i / vecs), c = (int)(i - (long)r * vecs) * 8;
+  for (int i = threadIdx.x; i < items; i += 256) {
+    const int q = (in_row0 + i) / vecs, r = row0 + q, c = (in_row0 + i - q * vecs) * 8;
     const int l = dense_tile_index(r / TILE, c / TILE, tiles_m, tiles_n);
     f32x4 a, b;
     if (l < cut.full_tiles) {
@@ -452,6 +515,8 @@ constexpr int kFewRows = 128;
 constexpr int kScoreAsIs = 256;
 // Up to so many tokens every workgroup of the gathering counts them itself.
 constexpr int kPrepareTokens = 2048;
+// Up to so many tokens every workgroup that compacts a part of them counts the ones before it.
+constexpr int kCompactFew = 65536;
 // Up to so many rows a row's pass has 1024 threads instead of 256: the CUs hold no more workgroups anyway.
 constexpr int kFewGroups = 512;
 // fp32 products in parts: floats that all parts may take
@@ -560,7 +625,10 @@ template <typename TX> int gather_rows(const VocabProblem& q, const VocabPlan& p
     return MOE_OK;
   }
   if (piece == 0) {
-    vocab_compact_kernel<<<dim3(1), dim3(1024), 0, s>>>(q.target, q.T, q.V, p.R, p.pieces, token, target_of, counts, ranges);
+    if (q.T <= kCompactFew)
+      vocab_compact_few_kernel<<<dim3(cdiv(q.T, 1024)), dim3(256), 0, s>>>(q.target, q.T, q.V, p.R, p.pieces, token, target_of, counts, ranges);
+    else
+      vocab_compact_kernel<<<dim3(1), dim3(1024), 0, s>>>(q.target, q.T, q.V, p.R, p.pieces, token, target_of, counts, ranges);
     MOE_LAUNCH_CHECK();
   }
   vocab_gather_kernel<TX><<<dim3(cdiv(piece == 0 ? q.T : p.R, 4)), dim3(256), 0, s>>>(x, q.target, token, ranges + 2 * piece, q.T, q.V, q.d, piece * p.R, xc,
@@ -622,7 +690,8 @@ int bf16_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, c
   if (rc != MOE_OK) return rc;
   if (!q.grad) return score_rows(q, p, stats, z_target, o.target_of, o.token, o.range, s);
   const f32x2* st = reinterpret_cast<const f32x2*>(stats);
-  if (R <= kFewGroups) vocab_grad_rows_kernel<1024><<<dim3(R), dim3(1024), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
+  if (V <= 1024) vocab_grad_rows_kernel<64><<<dim3(R), dim3(64), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
+  else if (R <= kFewGroups) vocab_grad_rows_kernel<1024><<<dim3(R), dim3(1024), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
   else vocab_grad_rows_kernel<256><<<dim3(R), dim3(256), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
   MOE_LAUNCH_CHECK();
   float* dxc = reinterpret_cast<float*>(ws + p.dxc);
@@ -633,12 +702,14 @@ int bf16_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, c
   rc = mfma_vocab_dx(ws + p.G, p.ld, q.w, o.range + 1, scale, R, V, d, plan, dxc, parts, &groups, s);
   if (rc != MOE_OK) return rc;
   const bool last = piece + 1 == p.pieces;
-  const dim3 grid(blocks_for((long)R * d / 8) + last);
+  const long pieces = (long)R * d / 8;
+  const int each = pieces < 256 * 2048 ? 1 : 4;           // (a workgroup works out the plan of the cut tiles first)
+  const dim3 grid((unsigned)((pieces + each * 256 - 1) / (each * 256)) + last);
   float* total = last ? q.total : nullptr;
   const float* weighted = reinterpret_cast<float*>(ws + p.weighted);
   const bf16* w = static_cast<const bf16*>(q.w);
-  if (plan.tile == 256) vocab_dx_kernel<256><<<grid, dim3(256), 0, s>>>(dxc, parts, groups, plan.cost, w, d, V, o, static_cast<bf16*>(q.dx), weighted, total);
-  else vocab_dx_kernel<128><<<grid, dim3(256), 0, s>>>(dxc, parts, groups, plan.cost, w, d, V, o, static_cast<bf16*>(q.dx), weighted, total);
+  if (plan.tile == 256) vocab_dx_kernel<256><<<grid, dim3(256), 0, s>>>(each, dxc, parts, groups, plan.cost, w, d, V, o, static_cast<bf16*>(q.dx), weighted, total);
+  else vocab_dx_kernel<128><<<grid, dim3(256), 0, s>>>(each, dxc, parts, groups, plan.cost, w, d, V, o, static_cast<bf16*>(q.dx), weighted, total);
   MOE_LAUNCH_CHECK();
   const int32_t* n_dw = p.twice ? o.range + 3 : o.range + 1;
   if (p.dw_sum_used) return mfma_vocab_dw(ws + p.G, p.ld, xc, n_dw, scale, R, V, d, ws + p.dw_sum, MOE_F32, piece > 0, parts, s);

@@ -303,3 +303,34 @@ def test_refused_tensors():
             bad()
     with pytest.raises(AssertionError):
         make(T, d, V, torch.bfloat16, gradients=False).step(x, w, target)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,tol", [(torch.bfloat16, 2 * U16), (torch.float32, F32_TOL)])
+@pytest.mark.parametrize("T,d,V", [(2048, 32, 300), (2049, 32, 300), (9001, 48, 130), (65536, 16, 70), (66001, 16, 70)])
+def test_many_tokens(dtype, tol, T, d, V):
+    """Sizes around those at which the rows that count are found in another way."""
+    x, w, target, token_w = inputs(T, d, V, dtype, seed=T, ignored=0.3)
+    op = make(T, d, V, dtype)
+    op.step(x, w, target, token_w=token_w)
+    check(op, x, w, target, token_w, tol, tol)
+    op.loss.fill_(-1.0)
+    loss, _ = op.score(x, w, target)
+    _, want, _, _, _ = reference(x, w, target)
+    assert float((loss.double().cpu() - want).abs().max()) <= F32_TOL * 64
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [60, 128, 150, 192, 260, 320, 400, 640])
+@pytest.mark.parametrize("V", [2000, 30000])
+def test_row_tiles(T, V):
+    """Numbers of rows around the tiles', words that fill no tile, most rows counting."""
+    d = 208
+    x, w, target, _ = inputs(T, d, V + 13, torch.bfloat16, seed=T + V, ignored=0.05)
+    op = make(T, d, V + 13, torch.bfloat16)
+    op.step(x, w, target)
+    check(op, x, w, target, None, 2 * U16, U16)
+    want = op.loss.clone(), op.lse.clone()
+    op.score(x, w, target)
+    for a, b in zip(want, (op.loss, op.lse)):
+        assert float((a - b).abs().max()) <= 2 * F32_TOL * max(1.0, float(op.lse.abs().max()))
