@@ -8,7 +8,6 @@
 namespace moe {
 namespace {
 
-// V * d may pass 2^32 elements: operands are addressed from a tile's first row
 bool vocab_sizes_ok(int T, int d, int V) { return T >= 0 && d > 0 && V > 0; }
 bool vocab_types_ok(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt) {
   if (dt != MOE_F32 && dt != MOE_BF16) return false;
@@ -19,6 +18,12 @@ bool vocab_types_ok(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt) {
 int vocab_call(const VocabProblem& q, int piece_rows, void* workspace, size_t ws_bytes, void* stream) {
   const VocabPlan p = vocab_plan(q.T, q.d, q.V, q.dt, q.grad_dt, piece_rows, q.grad);
   if (!workspace || !aligned16(workspace) || ws_bytes < p.bytes) return MOE_ERR_WORKSPACE;
+  if (q.grad) {
+    // d_w's product reads x after dx is written
+    const size_t es = dtype_size(q.dt), x = (size_t)q.T * q.d * es, w = (size_t)q.V * q.d * es, d_w = (size_t)q.V * q.d * dtype_size(q.grad_dt);
+    if (!apart(q.dx, x, q.x, x) || !apart(q.dx, x, q.w, w) || !apart(q.d_w, d_w, q.x, x) || !apart(q.d_w, d_w, q.w, w) || !apart(q.dx, x, q.d_w, d_w))
+      return MOE_ERR_INVALID;
+  }
   return launch_vocab_loss(q, p, static_cast<char*>(workspace), as_stream(stream));
 }
 

@@ -62,6 +62,8 @@ struct Args {
   // vocabulary products
   const int32_t* rows;               // DENSE: number of rows (at most M, the rows that A and C have room for), or NULL for M
   const int32_t* k_rows;             // DENSE: length of the contraction (at most K), or NULL for K
+  const void* a_all; const void* b_all;   // DENSE: taken instead of A (B) if *all_if == all_total (NULL: never)
+  const int32_t* all_if; int all_total;
   int c_rows;                        // DENSE: rows of C where an M-major A is padded to M columns (0: M)
   const float* scale;                // DENSE, EPI_STORE: factor of the whole product (device), or NULL
   CutCost cut;                       // DENSE: costs by which the last round's tiles are cut; the parts go to splitk_ws (NULL: no cutting)

@@ -339,10 +339,10 @@ VocabTiles mfma_vocab_tiles(int R, int V, int d, bool grad) {
   const bool narrow = t == VocabTile::ROWS64 || t == VocabTile::ROWS128, by64 = narrow || t != VocabTile::ROWS256;
   return {narrow ? cdiv(V, 128) * 2 : cdiv(V, 256) * (by64 ? 4 : 2), by64 ? 6 : 7};
 }
-int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const int32_t* target, int R, int V, int d, void* P, long ldp,
+int mfma_vocab_softmax(const VocabRows& x, const void* w, const int32_t* rows, const int32_t* target, int R, int V, int d, void* P, long ldp,
                        float* stats, float* z_target, hipStream_t s) {
   Args a{};
-  a.A = x; a.lda = d;
+  a.A = x.gathered; a.lda = d; a.a_all = x.all; a.all_if = x.n; a.all_total = x.total;
   a.B = w; a.ldb = d;
   a.C = P; a.ldc = ldp;
   a.E = 1; a.M = R; a.N = V; a.K = d;
@@ -410,7 +410,7 @@ size_t mfma_vocab_dw_part_floats(int R, int V, int d) {
   const int b = pairs ? 128 : 256, groups = pairs ? 2 * kPlanGroups : kPlanGroups;
   return (size_t)cut_items((long)cdiv(V, b) * cdiv(d, b), groups, cdiv(R, 64)) * b * b;
 }
-int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, const float* scale, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
+int mfma_vocab_dw(const void* G, long ldg, const VocabRows& x, const int32_t* rows, const float* scale, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
                   hipStream_t s) {
   int dev = 0, groups = 0;
   MOE_HIP_TRY(hipGetDevice(&dev));
@@ -422,7 +422,7 @@ int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, c
   if (pairs) groups *= 2;
   Args a{};
   a.A = G; a.lda = ldg;
-  a.B = x; a.ldb = d;
+  a.B = x.gathered; a.ldb = d; a.b_all = x.all; a.all_if = x.n; a.all_total = x.total;
   a.C = d_w; a.ldc = d; a.k_rows = rows; a.E = 1; a.M = (int)ldg; a.c_rows = V; a.N = d; a.K = R; a.scale = scale;
   a.accumulate = accumulate;
   a.cut = pairs ? kDwPair : kDwFull;

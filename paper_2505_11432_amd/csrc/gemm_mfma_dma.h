@@ -496,6 +496,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
     if (p.k_rows) k_all = __builtin_amdgcn_readfirstlane(max(min(*p.k_rows, p.K), 0));
     if (p.c_rows) m_rows = p.c_rows;
   }
+  const bool all = MODE == DENSE && p.all_if && __builtin_amdgcn_readfirstlane(*p.all_if) == p.all_total;
   const float scale = MODE == DENSE && EPI == EPI_STORE && p.scale ? *p.scale : 1.0f;
   const int tiles_m_fixed = (m_rows + BM - 1) / BM;
   int total_tiles;
@@ -647,8 +648,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
     }
     if constexpr (STAGGER) k_start = nk > 0 ? lag % nk : 0;
     else k_start = (xcd * 2 + in_window * 2 / window) * nk / (2 * XCDS);
-    const char* Ag = static_cast<const char*>(p.A);
-    const char* Bg = static_cast<const char*>(p.B) + (long)e * p.b_es * ESZ;
+    const char* Ag = static_cast<const char*>(MODE == DENSE && all && p.a_all ? p.a_all : p.A);
+    const char* Bg = static_cast<const char*>(MODE == DENSE && all && p.b_all ? p.b_all : p.B) + (long)e * p.b_es * ESZ;
     // Base of each operand at the tile's first k (wave-uniform) and this lane's fixed byte offset from it.
     // Load j of loader wave lw fills DMA slot q = lw + j*NL of the tile (1 KiB of LDS each).
     if constexpr (GATHER_A) a_base = uniform_ptr(Ag + (long)k_begin * ESZ);          // row offsets are absolute

@@ -166,14 +166,16 @@ int mfma_router_dx(const void* g, const void* w_r, int T, int d, int E, void* dx
 // vocabulary products in bf16 (gemm_mfma.hip); `rows` is read on the device
 struct VocabTiles { int parts, shift; };           // pairs of softmax statistics per row, each of 2^shift columns
 VocabTiles mfma_vocab_tiles(int R, int V, int d, bool grad);
-int mfma_vocab_softmax(const void* x, const void* w, const int32_t* rows, const int32_t* target, int R, int V, int d, void* P, long ldp,
+// the rows that count, gathered, or all of them where every one counts: `gathered`, or `all` (NULL: never) if *n, read on the device, is `total`
+struct VocabRows { const void* gathered; const void* all; const int32_t* n; int total; };
+int mfma_vocab_softmax(const VocabRows& x, const void* w, const int32_t* rows, const int32_t* target, int R, int V, int d, void* P, long ldp,
                        float* stats, float* z_target, hipStream_t s);
 struct VocabDxPlan { int tile; CutCost cost; size_t part_floats; };
 VocabDxPlan mfma_vocab_dx_plan(int R, int V, int d);
 int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, const float* scale, int R, int V, int d, const VocabDxPlan& plan, float* out, float* parts,
                   int* groups, hipStream_t s);
 size_t mfma_vocab_dw_part_floats(int R, int V, int d);
-int mfma_vocab_dw(const void* G, long ldg, const void* x, const int32_t* rows, const float* scale, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
+int mfma_vocab_dw(const void* G, long ldg, const VocabRows& x, const int32_t* rows, const float* scale, int R, int V, int d, void* d_w, moe_dtype dt, int accumulate, float* parts,
                   hipStream_t s);
 size_t router_bwd_ws_bytes(int T, int d, int E);
 int mfma_configure_all();          // per-device set-up of every grouped-GEMM kernel (moe_init)

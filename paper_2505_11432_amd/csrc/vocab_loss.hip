@@ -14,6 +14,8 @@
 // take it as a factor: most rows then hold -1, which needs no rounding, in the column of the target.  In the column of the target it is nearly the whole row, and the rows of
 // few tokens would carry its rounding error undivided, so what the rounding took off (`rest`) is kept in fp32: dx gets rest * w[target] when its
 // parts are added, d_w one more row per token with rest in the target's column where the tokens are few (kFewRows), where that is free.
+#include <type_traits>
+
 #include "dense_plan.h"
 #include "moe_common.h"
 #include "vocab_loss.h"
@@ -253,12 +255,14 @@ __global__ void __launch_bounds__(256) vocab_prepare_kernel(const TX* __restrict
   }
 }
 
-// The rows of a piece to the front of xc, a wave per row; with the first piece also the zeros of the tokens left out.
+// The rows of a piece to the front of xc, a wave per row; with the first piece also the zeros of the tokens left out.  Nothing where every token
+// counts and there is one piece (`all`): the products then read x itself.
 template <typename TX>
 __global__ void __launch_bounds__(256) vocab_gather_kernel(const TX* __restrict__ x, const int32_t* __restrict__ target, const int32_t* __restrict__ token,
-                                                           const int32_t* __restrict__ range, int T, int V, int d, int row0, TX* __restrict__ xc,
+                                                           const int32_t* __restrict__ range, int all, int T, int V, int d, int row0, TX* __restrict__ xc,
                                                            float* __restrict__ loss, float* __restrict__ lse, TX* __restrict__ dx) {
   const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6), n = range[1];
+  if (all && n == T) return;
   if (r < n) {
     const u32x4* src = reinterpret_cast<const u32x4*>(x + (long)token[row0 + r] * d);
     u32x4* dst = reinterpret_cast<u32x4*>(xc + (long)r * d);
@@ -311,8 +315,10 @@ struct RowOut {
 
 __device__ __forceinline__ float row_weight(const RowOut& o, int t) { return o.token_w ? o.token_w[t] : o.counts->mean; }
 
-// exp(z - maximum of its part) in fp16 -> G in bf16, in place, a workgroup per row, of 256 threads, where rows are few of 1024, where they are short of one wave.  Bound by
-// memory: 4 bytes per element (8192 rows of 32000 words 197 us, 5.3 TB/s).
+// exp(z - maximum of its part) in fp16 -> G in bf16, in place, a workgroup per row.  Bound by memory: 4 bytes per element (8192 rows
+// of 32000 words 197 us, 5.3 TB/s).  Threads by the row's length, so that each has some pieces of it, and 1024 where rows are few.  Whole steps of
+// 16384 tokens, 256 wide (us; 64, 128, 256, 1024 threads): 1200 words 126, 131, 143, -; 2500 182, 185, 197, 334; 5000 282, 279, 286, -; 10000 529, 520,
+// 514, 616; 2000 tokens, 512 wide, 102400 words -, -, 867, 845.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) vocab_grad_rows_kernel(const f32x2* __restrict__ stats, int parts, int part_shift, const float* __restrict__ z_target,
                                                               int V, long ld, int twice, char* __restrict__ G, RowOut o) {
@@ -631,7 +637,7 @@ template <typename TX> int gather_rows(const VocabProblem& q, const VocabPlan& p
       vocab_compact_kernel<<<dim3(1), dim3(1024), 0, s>>>(q.target, q.T, q.V, p.R, p.pieces, token, target_of, counts, ranges);
     MOE_LAUNCH_CHECK();
   }
-  vocab_gather_kernel<TX><<<dim3(cdiv(piece == 0 ? q.T : p.R, 4)), dim3(256), 0, s>>>(x, q.target, token, ranges + 2 * piece, q.T, q.V, q.d, piece * p.R, xc,
+  vocab_gather_kernel<TX><<<dim3(cdiv(piece == 0 ? q.T : p.R, 4)), dim3(256), 0, s>>>(x, q.target, token, ranges + 2 * piece, p.pieces == 1 && q.dt == MOE_BF16, q.T, q.V, q.d, piece * p.R, xc,
                                                                                     q.loss, q.lse, dx);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
@@ -686,13 +692,20 @@ int bf16_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, c
   float* z_target = reinterpret_cast<float*>(ws + p.z_target);
   float* stats = reinterpret_cast<float*>(ws + p.stats);
   const void* xc = ws + p.xc;
-  int rc = mfma_vocab_softmax(xc, q.w, o.range + 1, o.target_of, R, V, d, q.grad ? ws + p.G : nullptr, p.ld, stats, z_target, s);
+  const VocabRows x{xc, p.pieces == 1 && q.T > kPrepareTokens ? q.x : nullptr, o.range + 1, q.T};
+  int rc = mfma_vocab_softmax(x, q.w, o.range + 1, o.target_of, R, V, d, q.grad ? ws + p.G : nullptr, p.ld, stats, z_target, s);
   if (rc != MOE_OK) return rc;
   if (!q.grad) return score_rows(q, p, stats, z_target, o.target_of, o.token, o.range, s);
   const f32x2* st = reinterpret_cast<const f32x2*>(stats);
-  if (V <= 1024) vocab_grad_rows_kernel<64><<<dim3(R), dim3(64), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
-  else if (R <= kFewGroups) vocab_grad_rows_kernel<1024><<<dim3(R), dim3(1024), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
-  else vocab_grad_rows_kernel<256><<<dim3(R), dim3(256), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
+  auto rows = [&](auto threads) {
+    constexpr int N = decltype(threads)::value;
+    vocab_grad_rows_kernel<N><<<dim3(R), dim3(N), 0, s>>>(st, p.tiles.parts, p.tiles.shift, z_target, V, p.ld, p.twice, ws + p.G, o);
+  };
+  const bool few = R <= kFewGroups && V > 1024;
+  if (!few && V <= 4096) rows(std::integral_constant<int, 64>());
+  else if (!few && V <= 8192) rows(std::integral_constant<int, 128>());
+  else if (!few && V <= 65536) rows(std::integral_constant<int, 256>());
+  else rows(std::integral_constant<int, 1024>());
   MOE_LAUNCH_CHECK();
   float* dxc = reinterpret_cast<float*>(ws + p.dxc);
   float* parts = reinterpret_cast<float*>(ws + p.parts);
@@ -712,8 +725,8 @@ int bf16_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, c
   else vocab_dx_kernel<128><<<grid, dim3(256), 0, s>>>(each, dxc, parts, groups, plan.cost, w, d, V, o, static_cast<bf16*>(q.dx), weighted, total);
   MOE_LAUNCH_CHECK();
   const int32_t* n_dw = p.twice ? o.range + 3 : o.range + 1;
-  if (p.dw_sum_used) return mfma_vocab_dw(ws + p.G, p.ld, xc, n_dw, scale, R, V, d, ws + p.dw_sum, MOE_F32, piece > 0, parts, s);
-  return mfma_vocab_dw(ws + p.G, p.ld, xc, n_dw, scale, p.twice ? 2 * R : R, V, d, q.d_w, q.grad_dt, q.accumulate || piece > 0, parts, s);
+  if (p.dw_sum_used) return mfma_vocab_dw(ws + p.G, p.ld, x, n_dw, scale, R, V, d, ws + p.dw_sum, MOE_F32, piece > 0, parts, s);
+  return mfma_vocab_dw(ws + p.G, p.ld, x, n_dw, scale, p.twice ? 2 * R : R, V, d, q.d_w, q.grad_dt, q.accumulate || piece > 0, parts, s);
 }
 
 }  // namespace
@@ -722,7 +735,7 @@ int launch_vocab_loss(const VocabProblem& q, const VocabPlan& p, char* ws, hipSt
   if (!p.gather) {
     float* z_target = reinterpret_cast<float*>(ws + p.z_target);
     float* stats = reinterpret_cast<float*>(ws + p.stats);
-    const int rc = mfma_vocab_softmax(q.x, q.w, nullptr, q.target, q.T, q.V, q.d, nullptr, 0, stats, z_target, s);
+    const int rc = mfma_vocab_softmax(VocabRows{q.x, nullptr, nullptr, 0}, q.w, nullptr, q.target, q.T, q.V, q.d, nullptr, 0, stats, z_target, s);
     return rc != MOE_OK ? rc : score_rows(q, p, stats, z_target, q.target, nullptr, nullptr, s);
   }
   for (int piece = 0; piece < p.pieces; ++piece) {

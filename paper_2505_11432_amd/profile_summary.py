@@ -20,14 +20,14 @@ LEGEND = """labels: grouped_gemm<BMxBNxBK sS wMxN LAYOUT MODE EPILOGUE out=T in=
   moe::mfma::grouped_gemm_dma_kernel<BM, BN, BKT, NSTAGE, WM, WN, LA, LB, MODE, EPI, TC, TIN> in that order:
   LAYOUT from (LA, LB): (0,0) NT = both operands K-major (forward), (0,1) NN = B N-major (dgrad), (1,1) TN = both
   M/N-major (wgrad); MODE 0 rowseg (rows segmented by expert), 1 kseg (contraction segmented: weight gradient),
-  2 plain; EPI 0 store, 1 swiglu (FC1), 2 swiglu_bwd (dgrad2), 3 bias_f32 (router), 4 swiglu_w, 5 swiglu_bwd_w
-  (gate weight folded in); TC f = fp32 output, else bf16; TIN h = e4m3 operands, else bf16 (where the profiler
+  2 plain, 3 dense (rows or contraction read on the device); EPI 0 store, 1 swiglu (FC1), 2 swiglu_bwd (dgrad2), 3 bias_f32 (router), 4 swiglu_w,
+  5 swiglu_bwd_w (gate weight folded in), 6 lse (softmax statistics), 7 ce (those and exp(z - maximum)); TC f = fp32 output, else bf16; TIN h = e4m3 operands, else bf16 (where the profiler
   prints the type pair as "bool _Accum", 128-deep steps mean e4m3 operands with bf16 output).
   Other kernels: the function name without namespaces and template arguments."""
 
 _LAYOUT = {(0, 0): "NT", (0, 1): "NN", (1, 1): "TN", (1, 0): "TT"}
-_MODE = {0: "rowseg", 1: "kseg", 2: "plain"}
-_EPI = {0: "store", 1: "swiglu", 2: "swiglu_bwd", 3: "bias_f32", 4: "swiglu_w", 5: "swiglu_bwd_w"}
+_MODE = {0: "rowseg", 1: "kseg", 2: "plain", 3: "dense"}
+_EPI = {0: "store", 1: "swiglu", 2: "swiglu_bwd", 3: "bias_f32", 4: "swiglu_w", 5: "swiglu_bwd_w", 6: "lse", 7: "ce"}
 
 
 def label(name: str) -> str:

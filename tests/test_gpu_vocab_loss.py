@@ -334,3 +334,26 @@ def test_row_tiles(T, V):
     op.score(x, w, target)
     for a, b in zip(want, (op.loss, op.lse)):
         assert float((a - b).abs().max()) <= 2 * F32_TOL * max(1.0, float(op.lse.abs().max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,tol", [(torch.bfloat16, 2 * U16), (torch.float32, F32_TOL)])
+@pytest.mark.parametrize("T,d,V", [(2049, 48, 300), (4500, 32, 1500), (6000, 16, 5000)])
+def test_every_token_counts(dtype, tol, T, d, V):
+    """Nothing is left out, then one token is, with the same buffers: rows are read in place or gathered."""
+    x, w, target, token_w = inputs(T, d, V, dtype, seed=T, ignored=0.0)
+    op = make(T, d, V, dtype)
+    for _ in range(2):
+        op.step(x, w, target)
+        check(op, x, w, target, None, tol, tol)
+        loss, _ = op.score(x, w, target)
+        _, want, _, _, _ = reference(x, w, target)
+        assert float((loss.double().cpu() - want).abs().max()) <= F32_TOL * 64
+        target[T // 2] = -1
+        x[T // 2] = float("nan")
+        w = w.clone()
+        clean = x.clone()
+        clean[T // 2] = 0
+        op.step(x, w, target)
+        check(op, clean, w, target, None, tol, tol)
+        x, target = clean, torch.where(target < 0, torch.zeros_like(target), target)

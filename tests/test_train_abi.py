@@ -104,3 +104,17 @@ def test_adamw_table_and_arguments(lib):
     assert step(b1=1.0) == step(b2=-0.1) == step(b1=float("nan")) == step(eps=-1.0) == step(wd=float("nan")) == -1
     assert step(dt=E4M3) == step(lr=P(4098)) == step(coef=P(4098)) == step(table=P(4100)) == -2
     assert step(ws=NULL) == step(b=8) == -3
+
+
+def test_vocab_outputs_lie_apart(lib):
+    """x, w, dx and d_w of 8 x 64, 100 x 64 bf16 (d_w fp32): refused where an output touches an operand or the other output."""
+    need = lib.moe_vocab_workspace_bytes(8, 64, 100, BF16, F32, 0, 1)
+    at = {"x": 1 << 20, "w": 2 << 20, "dx": 3 << 20, "d_w": 4 << 20}
+
+    def step(**k):
+        a = {**at, **k}
+        return lib.moe_vocab_loss(P(a["x"]), P(a["w"]), FAKE, NULL, BF16, 8, 64, 100, 0, FAKE, FAKE, FAKE, P(a["dx"]), P(a["d_w"]), F32, 0, FAKE, need, None)
+
+    x_bytes, w_bytes, d_w_bytes = 8 * 64 * 2, 100 * 64 * 2, 100 * 64 * 4
+    assert step(dx=at["x"]) == step(dx=at["x"] + x_bytes - 16) == step(dx=at["w"] + w_bytes - 16) == -1
+    assert step(d_w=at["w"]) == step(d_w=at["w"] - d_w_bytes + 16) == step(d_w=at["x"]) == step(d_w=at["dx"] - 16) == -1
