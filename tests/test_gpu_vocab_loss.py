@@ -357,3 +357,39 @@ def test_every_token_counts(dtype, tol, T, d, V):
         op.step(x, w, target)
         check(op, clean, w, target, None, tol, tol)
         x, target = clean, torch.where(target < 0, torch.zeros_like(target), target)
+
+
+@pytest.mark.gpu
+def test_past_32_bits():
+    """A vocabulary matrix of more than 2^31 elements (4.4 GB), targets at both ends of it.  The reference is fp32 on the GPU, in chunks of words:
+    its own error is far below the tolerances."""
+    T, d, V, step = 24, 4096, 530_000, 53_000
+    g = torch.Generator(device=DEV).manual_seed(5)
+    w = torch.empty((V, d), dtype=torch.bfloat16, device=DEV)
+    for part in w.split(step):
+        part.copy_(torch.randn(part.shape, device=DEV, generator=g) * (1.28 / math.sqrt(d)))
+    target = torch.randint(0, V, (T,), device=DEV, generator=g)
+    target[:3], target[3:6] = torch.tensor([V - 1, V - 2, V - 300]), torch.tensor([0, 1, 255])
+    target[6] = -100
+    kept = (target >= 0).nonzero().squeeze(1)
+    x = torch.randn((T, d), device=DEV, generator=g) + 5.0 * w[target.clamp(min=0)].float()
+    x = x.to(torch.bfloat16)
+    op = make(T, d, V, torch.bfloat16, grad_dtype=torch.bfloat16)
+    op.step(x, w, target.to(torch.int32))
+    xf = x.float()[kept]
+    z = torch.cat([xf @ part.float().t() for part in w.split(step)], 1)
+    lse = torch.logsumexp(z.double(), 1)
+    at, tg = torch.arange(len(kept), device=DEV), target[kept]
+    loss = lse - z[at, tg].double()
+    assert float((op.loss.double()[kept] - loss).abs().max()) <= F32_TOL * float(lse.abs().max())
+    p = torch.exp(z - lse.float()[:, None])
+    p[at, tg] -= 1.0
+    p /= len(kept)
+    dx = torch.zeros((len(kept), d), device=DEV)
+    for i, part in enumerate(w.split(step)):
+        dx += p[:, i * step:i * step + len(part)] @ part.float()
+        d_w = p[:, i * step:i * step + len(part)].t() @ xf
+        got = op.d_w[i * step:i * step + len(part)].float()
+        assert float((got - d_w).norm()) <= 2 * U16 * float(d_w.norm()), i
+    assert float((op.dx.float()[kept] - dx).norm()) <= 2 * U16 * float(dx.norm())
+    assert not bool(op.dx[6].any())
