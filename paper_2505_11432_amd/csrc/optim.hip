@@ -14,8 +14,8 @@
 // other lists of an update may then be unaligned, which the hardware takes.
 //
 // The norm is summed in 64 bits (squares of single-precision numbers neither overflow nor vanish there; the conversion and the sum hide behind
-// the loads) and in a fixed order: a sum per workgroup, and every workgroup of the second launch adds those up in the same order.  The second
-// launch takes the chunks from the last one on: what the first one read last is still in the Infinity Cache (256 MB).
+// the loads) and in a fixed order: a sum per workgroup, and every workgroup of the second launch adds those up in the same order.  (The second launch
+// from the last chunk on, which the Infinity Cache might still hold, is slower: 20 M elements 37.6 us, from the first on 32.4; 300 M 357, 345.)
 #include <type_traits>
 
 #include "moe_common.h"
@@ -85,16 +85,16 @@ template <typename Entry> __device__ __forceinline__ int find(const Entry* __res
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Takes groups of `per` chunks in turn with the other workgroups, from the first or from the last on, and calls body(entry, first element, number
+// Takes groups of `per` chunks in turn with the other workgroups and calls body(entry, first element, number
 // of elements) for the part of every tensor that lies in them.  Only the first part of a tensor begins in front of a line, and only the last one
 // ends anywhere.
-template <bool BACKWARDS, typename Entry, typename Body> __device__ __forceinline__ void for_parts(const Entry* __restrict__ table, int n, int per, Body body) {
+template <typename Entry, typename Body> __device__ __forceinline__ void for_parts(const Entry* __restrict__ table, int n, int per, Body body) {
   const int chunks = first_chunk(table, n), groups = (chunks + per - 1) / per;
   int e = 0, chunk = 0, next = 0;          // the open tensor and its chunks
   Entry t{};
   long numel = 0, head = 0;
   for (int g = blockIdx.x; g < groups; g += gridDim.x) {
-    int at = (BACKWARDS ? groups - 1 - g : g) * per;
+    int at = g * per;
     const int end = min(at + per, chunks);
     while (at < end) {
       if (at < chunk || at >= next) {
@@ -162,7 +162,7 @@ template <bool KEEP>
 __global__ void __launch_bounds__(kThreads, 8) norm_parts_kernel(const ClipEntry* __restrict__ table, int n, int per, double* __restrict__ parts) {
   __shared__ double lds[4];
   double s = 0;
-  for_parts<false>(table, n, per, [&](const ClipEntry& t, long first, long k) __attribute__((always_inline)) {
+  for_parts(table, n, per, [&](const ClipEntry& t, long first, long k) __attribute__((always_inline)) {
     if (t.dt == MOE_F32) s += square_sum<KEEP>(static_cast<const float*>(t.g) + first, k);
     else s += square_sum<KEEP>(static_cast<const bf16*>(t.g) + first, k);
   });
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 8) clip_kernel(const ClipEntry* __re
     *coef = c;
   }
   if (!write) return;
-  for_parts<true>(table, n, per, [&](const ClipEntry& t, long first, long k) __attribute__((always_inline)) {
+  for_parts(table, n, per, [&](const ClipEntry& t, long first, long k) __attribute__((always_inline)) {
     // gradients in place that are within the limit stay as they are
     if (!t.out || (t.out == t.g && c == 1.0f)) return;
     if (t.dt == MOE_F32) scale_range(static_cast<const float*>(t.g) + first, static_cast<float*>(t.out) + first, k, c);
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwEntry* __res
   a.r1 = (float)(1.0 / (1.0 - power(h.beta1, (unsigned)t)));
   a.r2 = (float)(1.0 / (1.0 - power(h.beta2, (unsigned)t)));
   a.eps = (float)h.eps;
-  for_parts<false>(table, n, per, [&](const AdamwEntry& q, long first, long k) __attribute__((always_inline)) {
+  for_parts(table, n, per, [&](const AdamwEntry& q, long first, long k) __attribute__((always_inline)) {
     adamw_range(static_cast<float*>(q.p) + first, static_cast<const TG*>(q.g) + first, static_cast<float*>(q.m) + first, static_cast<float*>(q.v) + first,
                 q.w ? static_cast<bf16*>(q.w) + first : nullptr, k, a);
   });
@@ -327,10 +327,13 @@ Cut cut(long chunks, int per, long most) {
 }  // namespace
 
 int launch_grad_clip(const ClipEntry* table, int n, long total, double max_norm, int write, float* norm, float* coef, double* parts, hipStream_t s) {
-  // (the host does not know the types: chunks as if all were single precision)
-  const Cut c = cut(total / (kChunkBytes / 4) + n, 8, kNormParts);
-  // up to 128 MB, which the second launch then finds in the caches, reads are kept
-  if (write && total <= (32L << 20)) norm_parts_kernel<true><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, parts);
+  // The host does not know the types: chunks as if all were single precision.  Eight at a time, 64 in the longest lists: 300 M elements by 4, 8, 16 chunks
+  // 374, 329, 334 us, 20 M 34.8, 32.3, 32.4; 1.4 G by 32, 64, 128 2985, 2925, 2915.
+  const long chunks = total / (kChunkBytes / 4) + n;
+  const Cut c = cut(chunks, chunks < (2 << 20) ? 8 : 64, kNormParts);
+  // Where the second launch may find some of them in the Infinity Cache, reads are not made past the caches: 60 M elements 124 -> 115 us, 300 M (660 MB)
+  // 354 -> 340; but 1.4 G (5.6 GB) 2926 -> 3000.
+  if (write && total <= (512L << 20)) norm_parts_kernel<true><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, parts);
   else norm_parts_kernel<false><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, parts);
   MOE_LAUNCH_CHECK();
   clip_kernel<<<dim3(write ? c.blocks : 1), dim3(kThreads), 0, s>>>(table, n, c.per, parts, (int)c.blocks, max_norm, write, norm, coef);
@@ -340,7 +343,8 @@ int launch_grad_clip(const ClipEntry* table, int n, long total, double max_norm,
 
 int launch_adamw(const AdamwEntry* table, int n, long total, moe_dtype grad_dt, const float* lr, int32_t* step, const float* coef, const AdamwHyper& h,
                  unsigned* done, hipStream_t s) {
-  const Cut c = cut(total / kAdamwChunk + 2L * n, 8, 1L << 20);
+  // four chunks, 2048 elements, at a time, two pieces per thread: 400 M elements by 2, 4, 8, 16 chunks 1965, 1925, 2045, 2130 us, 20 M 102, 102, 112, 120
+  const Cut c = cut(total / kAdamwChunk + 2L * n, 4, 1L << 20);
   if (grad_dt == MOE_F32) adamw_kernel<float><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, lr, step, coef, h, done);
   else adamw_kernel<bf16><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, lr, step, coef, h, done);
   MOE_LAUNCH_CHECK();
