@@ -12,7 +12,9 @@ bool vocab_sizes_ok(int T, int d, int V) { return T >= 0 && d > 0 && V > 0; }
 bool vocab_types_ok(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt) {
   if (dt != MOE_F32 && dt != MOE_BF16) return false;
   if (dt == MOE_F32 ? grad_dt != MOE_F32 : grad_dt != MOE_F32 && grad_dt != MOE_BF16) return false;
-  return d % 16 == 0 && d <= MOE_VOCAB_MAX_WIDTH && V <= MOE_VOCAB_MAX && T <= MOE_VOCAB_MAX_ROWS;
+  // (tiles are counted in 32 bits)
+  const long tiles = ((long)T / 64 + 1) * ((long)V / 128 + 1);
+  return d % 16 == 0 && d <= MOE_VOCAB_MAX_WIDTH && V <= MOE_VOCAB_MAX && T <= MOE_VOCAB_MAX_ROWS && tiles <= 0x3fffffffL;
 }
 
 int vocab_call(const VocabProblem& q, int piece_rows, void* workspace, size_t ws_bytes, void* stream) {

@@ -11,9 +11,10 @@
 // they hold, NaN included, reaches no result.
 //
 // Rounding.  G is rounded to bf16 once, 2^-8 of an element at most.  Where every token has the same weight G is kept without it and the products
-// take it as a factor: most rows then hold -1, which needs no rounding, in the column of the target.  In the column of the target it is nearly the whole row, and the rows of
-// few tokens would carry its rounding error undivided, so what the rounding took off (`rest`) is kept in fp32: dx gets rest * w[target] when its
-// parts are added, d_w one more row per token with rest in the target's column where the tokens are few (kFewRows), where that is free.
+// take it as a factor: most rows then hold nearly -1 in the column of the target, where numbers lie closest for their size.  That element is nearly
+// the whole row, and the results of few tokens would carry its rounding error undivided, so what the rounding took off (`rest`) is kept in fp32:
+// dx gets rest * w[target] when its parts are added, d_w one more row per token with rest in the target's column where the tokens are few
+// (kFewRows) and that is free.
 #include <type_traits>
 
 #include "dense_plan.h"
@@ -519,6 +520,8 @@ size_t take(size_t& at, size_t bytes) {
 constexpr int kFewRows = 128;
 // Forward only: up to so many rows nothing is gathered.  They are one row of tiles whether they count or not, and rows do not mix.
 constexpr int kScoreAsIs = 256;
+// and so many rows at a time, which bounds the statistics (128 k words: 0.5 GB)
+constexpr int kScorePiece = 65536;
 // Up to so many tokens every workgroup of the gathering counts them itself.
 constexpr int kPrepareTokens = 2048;
 // Up to so many tokens every workgroup that compacts a part of them counts the ones before it.
@@ -570,7 +573,7 @@ VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int p
   const bool f32 = dt == MOE_F32;
   const size_t es = dtype_size(dt);
   p.R = piece_rows > 0 && piece_rows < T ? piece_rows : T;
-  if (!grad && !f32) p.R = T;                              // nothing is kept per element
+  if (!grad && !f32) p.R = T < kScorePiece ? T : kScorePiece;          // nothing is kept per element
   p.pieces = (T + p.R - 1) / p.R;
   p.ld = (long)align_up((size_t)V, 64);
   p.gather = grad || f32 || T > kScoreAsIs;

@@ -118,3 +118,12 @@ def test_vocab_outputs_lie_apart(lib):
     x_bytes, w_bytes, d_w_bytes = 8 * 64 * 2, 100 * 64 * 2, 100 * 64 * 4
     assert step(dx=at["x"]) == step(dx=at["x"] + x_bytes - 16) == step(dx=at["w"] + w_bytes - 16) == -1
     assert step(d_w=at["w"]) == step(d_w=at["w"] - d_w_bytes + 16) == step(d_w=at["x"]) == step(d_w=at["dx"] - 16) == -1
+
+
+def test_vocab_size_limits(lib):
+    size = lib.moe_vocab_workspace_bytes
+    assert size(1 << 24, 16, 1 << 18, BF16, BF16, 0, 0) > 0
+    assert size(1 << 24, 16, 1 << 20, BF16, BF16, 0, 0) == 0            # more tiles than are counted
+    # the statistics of a score are those of a piece of rows
+    assert size(1 << 22, 64, 131072, BF16, BF16, 0, 0) < 1 << 30
+    assert lib.moe_vocab_score(FAKE, FAKE, FAKE, BF16, 1 << 24, 16, 1 << 20, 0, FAKE, FAKE, FAKE, 1 << 40, None) == -2
