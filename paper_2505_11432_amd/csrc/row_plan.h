@@ -305,23 +305,43 @@ inline F32Plan f32_plan(const F32Product& p, long room) {
   return best;
 }
 
-// Products whose parts the caller adds up in a pass that it makes anyway (the fp32 vocabulary products): up to `room` parts of at least four steps,
-// by the time of the rounds and the parts' way through memory and back.
-inline F32Plan f32_cut_plan(const F32Product& p, long room) {
+// Products whose parts the caller adds up in a pass that it makes anyway (dx and d_w of the fp32 vocabulary loss).  Few tiles: as many 64 x 64 ones as the
+// CUs hold, parts of twelve steps or more (up to five parts of four), or as many 128 x 128, where parts of those are long.  Up to two rounds of 64 x 64: by
+// the estimated time of the rounds and of the parts' way through memory and back (10000 tokens, 8000 words, 512 wide 1490, whole 1660).  Measured, whole steps
+// (us; dx in 1, 4, 8, 16, 32 parts): 131 tokens, 5003 words, 1040 wide (51 tiles) 103, 87, 82, 84, 89; 40, 16000, 2048 (32) 270, 223, 196, 182, 184;
+// 3, 8000, 1024 (16) 114, 92, 71, 67, 70; 1000, 5000, 512 (128) 172, 161, 155, 161, 170; 600, 30000, 128 (20) 377, 283, 207, 187, 176; d_w of 16384, 600,
+// 128 (20) 264, 201, 163, 154, 152; of 4000, 1500, 304 (120) 156, 136, 140, 144, 154; 1000, 32000, 1024 1203 in three of 64 x 64, 1072 in eight of 128 x 128.
+inline F32Plan f32_parts(const F32Product& p, long room) {
   const int steps = f32_steps(p);
   const double t64 = f32_tiles64(p), t128 = f32_tiles128(p);
   F32Plan best = {F32_64, 1};
-  double best_us = 1e30;
-  for (int n = 1; n <= 32 && (n == 1 || (n <= room && steps / n >= 4)); ++n) {
-    const int each = (steps + n - 1) / n;
-    const double way = n * (double)p.M * p.N * 8 / 5e6, us64 = f32_us64(t64 * n, each) + way, us128 = f32_us128(t128 * n, each) + way;
-    const double us = us128 < us64 && t128 * n > 1.5 * 256 ? us128 : us64;
-    if (us < best_us) {
-      best_us = us;
-      best = {us == us64 ? F32_64 : F32_128, n};
+  if (t64 >= 1536) return best;
+  if (t64 > 384) {
+    double best_us = 1e30;
+    for (int n = 1; n <= 32 && (n == 1 || (n <= room && steps / n >= 4)); ++n) {
+      const int each = (steps + n - 1) / n;
+      const double way = n * (double)p.M * p.N * 8 / 5e6, us64 = f32_us64(t64 * n, each) + way, us128 = f32_us128(t128 * n, each) + way;
+      const bool large = us128 < us64 && t128 * n > 1.5 * 256;
+      if ((large ? us128 : us64) < best_us) {
+        best_us = large ? us128 : us64;
+        best = {large ? F32_128 : F32_64, n};
+      }
     }
+    return best;
   }
-  return best;
+  const double large = 512 / t128, fit = 768 / t64;
+  if (large >= 4 && large <= 16 && large <= room && steps / large >= 24) return {F32_128, (int)large};
+  const int longest = steps / 12, few = steps / 4 < 5 ? steps / 4 : 5, most = longest > few ? longest : few;
+  long n = fit < 32 ? (long)fit : 32;
+  if (n > most) n = most;
+  if (n > room) n = room;
+  return {F32_64, n > 1 ? (int)n : 1};
+}
+// The logits, whose contraction is short, only from half to one round of tiles, in two (131 tokens as above 94, 88; 40 tokens 152, 145; 3 tokens 67, 73; 300,
+// 16000, 1024 264, 273).
+inline F32Plan f32_logit_parts(const F32Product& p, long room) {
+  const double tiles = f32_tiles64(p);
+  return {F32_64, tiles >= 192 && tiles < 384 && f32_steps(p) >= 24 && room >= 2 ? 2 : 1};
 }
 
 }  // namespace moe

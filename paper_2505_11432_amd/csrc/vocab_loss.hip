@@ -560,10 +560,10 @@ int launch_f32(const GemmProblem& g, F32Plan plan, hipStream_t s) {
   return plan.parts > 1 ? launch_gemm_f32_cut(g, plan, s) : launch_gemm_f32(g, s);
 }
 F32Plan plan_f32(const GemmProblem& g) {
-  // a product that fills the chip as it is stays whole
   const F32Product q{g.mode == 0, g.M, g.N, g.K, 1};
-  if (f32_tiles64(q) >= 1536 || !gemm_f32_cuts(g)) return F32Plan{F32_64, 1};
-  return f32_cut_plan(q, (long)(kPartFloats / ((size_t)g.M * g.ldc)));
+  const long room = (long)(kPartFloats / ((size_t)g.M * g.ldc));
+  if (!gemm_f32_cuts(g)) return F32Plan{F32_64, 1};
+  return g.mode == 0 && g.b_rs == 1 ? f32_logit_parts(q, room) : f32_parts(q, room);
 }
 
 }  // namespace
