@@ -362,9 +362,19 @@ def moe_vocab_loss(x, w, target, token_w, piece_rows, total, loss, lse, dx, d_w,
         dtype_code(d_w.dtype), int(accumulate), workspace, workspace.numel() * workspace.element_size()))
 
 
-def _pointers(tensors):
-    """Host array of device pointers (None -> NULL; an empty tensor's is not looked at)."""
-    return (c_void_p * max(1, len(tensors)))(*[None if t is None or t.numel() == 0 else _p(t) for t in tensors])
+class _List:
+    """Pointers, element counts and types of a list of tensors (host arrays); None: no tensor."""
+
+    def __init__(self, tensors):
+        self.pointers, self.numel, self.types = _native.tensor_list(tensors)
+
+    def like(self, other, dtype=None) -> bool:
+        """Where there is a tensor: as many elements as the other list's, of its type (or of the one given)."""
+        mine, theirs = memoryview(self.numel).cast("q"), memoryview(other.numel).cast("q")
+        if len(mine) != len(theirs):
+            return False
+        types, want = memoryview(self.types).cast("i"), memoryview(other.types).cast("i")
+        return all(a < 0 or (a == b and t == (w if dtype is None else dtype)) for a, b, t, w in zip(mine, theirs, types, want))
 
 
 def _table(fn, tensors, size, fill):
@@ -374,19 +384,14 @@ def _table(fn, tensors, size, fill):
     return host.to(tensors[0].device if tensors else "cuda")
 
 
-def _numel(tensors):
-    return (ctypes.c_int64 * max(1, len(tensors)))(*[t.numel() for t in tensors])
-
-
 def moe_grad_clip_table(grads, outs=None):
     """The device table of moe_grad_clip for these gradients; outs: None, or a tensor (or None) for each."""
-    for g, o in zip(grads, outs or grads):
-        assert o is None or (o.shape == g.shape and o.dtype == g.dtype), "an out has its gradient's shape and type"
-    assert outs is None or len(outs) == len(grads), "an out for each gradient"
+    g = _List(grads)
+    o = _List(outs) if outs is not None else None
+    assert o is None or o.like(g), "an out for each gradient, of its size and type"
     n = len(grads)
-    types = (ctypes.c_int32 * max(1, n))(*[dtype_code(g.dtype) for g in grads])
     return _table("moe_grad_clip_table", grads, _lib.moe_grad_clip_table_bytes(n), lambda host: _lib.moe_grad_clip_table(
-        n, _pointers(grads), _pointers(outs) if outs is not None else None, _numel(grads), types, host))
+        n, g.pointers, o.pointers if o else None, g.numel, g.types, host))
 
 
 def moe_grad_clip_workspace_bytes() -> int:
@@ -401,17 +406,14 @@ def moe_grad_clip(table, n, total, max_norm, write, norm, coef, workspace):
 def moe_adamw_table(params, grads, m, v, weights=None):
     """The device table of moe_adamw; weights: None, or a bf16 tensor (or None) for each parameter."""
     n = len(params)
-    assert len(grads) == len(m) == len(v) == n and (weights is None or len(weights) == n), "one of each for each parameter"
-    grad_dt = grads[0].dtype if n else torch.float32
-    for i, p in enumerate(params):
-        for t in (p, m[i], v[i]):
-            assert t.dtype == torch.float32 and t.shape == p.shape, "parameters and moments are fp32, of one shape"
-        assert grads[i].shape == p.shape and grads[i].dtype == grad_dt, "gradients have one type and their parameters' shapes"
-        w = weights[i] if weights is not None else None
-        assert w is None or (w.shape == p.shape and w.dtype == torch.bfloat16), "weights are bf16, of their parameters' shapes"
+    grad_dt = dtype_code(grads[0].dtype) if grads else F32
+    p, g, m1, v1 = _List(params), _List(grads), _List(m), _List(v)
+    w = _List(weights) if weights is not None else None
+    assert p.like(p, F32) and m1.like(p, F32) and v1.like(p, F32), "parameters and moments are fp32, of one size"
+    assert g.like(p, grad_dt), "gradients have one type and their parameters' sizes"
+    assert w is None or w.like(p, BF16), "weights are bf16, of their parameters' sizes"
     return _table("moe_adamw_table", params, _lib.moe_adamw_table_bytes(n), lambda host: _lib.moe_adamw_table(
-        n, _pointers(params), _pointers(grads), _pointers(m), _pointers(v),
-        _pointers(weights) if weights is not None else None, _numel(params), dtype_code(grad_dt), host))
+        n, p.pointers, g.pointers, m1.pointers, v1.pointers, w.pointers if w else None, p.numel, grad_dt, host))
 
 
 def moe_adamw(table, n, total, grad_dt, lr, step, coef, beta1, beta2, eps, weight_decay, workspace):

@@ -95,6 +95,60 @@ template <typename... A, int (*FN)(A...)> struct Bound<FN> {
   }
 };
 
+// tensor_list(tensors) -> (pointers, element counts, types) of a list of tensors as three bytes objects of int64, int64 and int32: what the tables of
+// tensors are made from.  None gives (0, -1, -1), an empty tensor the pointer 0.  The checks are those of a call's arguments; the types are MOE_F32
+// and MOE_BF16.  (Asked through Python, 300 tensors in five lists take 0.5 ms.)
+PyObject* tensor_list(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  if (n_args != 1) {
+    PyErr_SetString(PyExc_TypeError, "takes a list of tensors");
+    return nullptr;
+  }
+  PyObject* seq = PySequence_Fast(args[0], "takes a list of tensors");
+  if (!seq) return nullptr;
+  PyObject* result = nullptr;
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+  PyObject* bytes[3] = {PyBytes_FromStringAndSize(nullptr, n * 8), PyBytes_FromStringAndSize(nullptr, n * 8), PyBytes_FromStringAndSize(nullptr, n * 4)};
+  bool ok = bytes[0] && bytes[1] && bytes[2];
+  try {
+    for (Py_ssize_t i = 0; ok && i < n; ++i) {
+      PyObject* o = PySequence_Fast_GET_ITEM(seq, i);
+      int64_t pointer = 0, numel = -1;
+      int32_t type = -1;
+      if (o != Py_None) {
+        if (!THPVariable_Check(o)) {
+          PyErr_SetString(PyExc_TypeError, "takes a list of tensors");
+          ok = false;
+          break;
+        }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        const auto dt = t.scalar_type();
+        if (!t.is_cuda() || !t.is_contiguous()) {
+          ok = refuse_tensor();
+          break;
+        }
+        if (dt != at::kFloat && dt != at::kBFloat16) {
+          PyErr_SetString(PyExc_TypeError, "unsupported dtype: tensors are float32 or bfloat16");
+          ok = false;
+          break;
+        }
+        numel = t.numel();
+        pointer = numel ? reinterpret_cast<int64_t>(t.data_ptr()) : 0;
+        type = dt == at::kFloat ? MOE_F32 : MOE_BF16;
+      }
+      reinterpret_cast<int64_t*>(PyBytes_AS_STRING(bytes[0]))[i] = pointer;
+      reinterpret_cast<int64_t*>(PyBytes_AS_STRING(bytes[1]))[i] = numel;
+      reinterpret_cast<int32_t*>(PyBytes_AS_STRING(bytes[2]))[i] = type;
+    }
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    ok = false;
+  }
+  if (ok) result = PyTuple_Pack(3, bytes[0], bytes[1], bytes[2]);
+  for (PyObject* b : bytes) Py_XDECREF(b);
+  Py_DECREF(seq);
+  return result;
+}
+
 #define MOE_BOUND(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&Bound<&name>::call)), METH_FASTCALL, nullptr}
 
 PyMethodDef methods[] = {
@@ -103,7 +157,8 @@ PyMethodDef methods[] = {
     MOE_BOUND(moe_route_bwd), MOE_BOUND(moe_dispatch), MOE_BOUND(moe_combine), MOE_BOUND(moe_gate_grad),
     MOE_BOUND(moe_expert_ffn_fwd), MOE_BOUND(moe_expert_ffn_bwd), MOE_BOUND(moe_row_map), MOE_BOUND(moe_expert_ffn_fused_fwd),
     MOE_BOUND(moe_expert_ffn_fused_bwd), MOE_BOUND(moe_quant_fp8), MOE_BOUND(moe_dequant_fp8), MOE_BOUND(moe_quant_fp8_tgroup),
-    MOE_BOUND(moe_transpose), MOE_BOUND(moe_vocab_score), MOE_BOUND(moe_vocab_loss), MOE_BOUND(moe_grad_clip), MOE_BOUND(moe_adamw), {nullptr, nullptr, 0, nullptr}};
+    MOE_BOUND(moe_transpose), MOE_BOUND(moe_vocab_score), MOE_BOUND(moe_vocab_loss), MOE_BOUND(moe_grad_clip), MOE_BOUND(moe_adamw),
+    {"tensor_list", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&tensor_list)), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_moe_native", "Calls of the MoE library on torch tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
