@@ -31,6 +31,7 @@
 #include "dense_plan.h"
 #include "gemm_mfma.h"
 #include "row_plan.h"
+#include "unit16.h"
 
 namespace moe {
 namespace mfma {
@@ -1170,8 +1171,8 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
       } else if constexpr (VOCAB) {
         // Softmax over this wave's WTN columns of every row but the target's: maximum and sum of exp(z - maximum), which a later pass joins with
         // the other waves'.  (The target's logit goes out by itself: in a row that is nearly certain of it, 1 - p is the sum of the others, which
-        // a sum that holds it would round away.)  EPI_CE also stores exp(z - maximum) in fp16: it lies in [0, 1], where fp16 keeps 11 bits (bf16 8) and its smallest step,
-        // 2^-24, is nothing beside the row's sum, which is at least 1 here; the pass that scales it rounds to bf16 once.
+        // a sum that holds it would round away.)  EPI_CE also stores exp(z - maximum), as unit16.h has it: ten bits, and no word beside a dominating one
+        // vanishes before it would in single precision; the pass that scales it rounds to bf16 once.
         const int nb0 = n0 + wn * WTN, part = n0 / BN * WN + wn;
         constexpr float LOG2E = 1.44269504088896341f, LOWEST = -3.402823466e38f;
         if (nb0 + WTN > p.N) {                      // (uniform) columns past the width take no part
@@ -1238,12 +1239,11 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) grouped_gemm_dma_kernel(Args 
             for (int j = 0; j < TN; ++j) {
               const int nb = nb0 + j * 32, cols_valid = p.N - nb;
               if (cols_valid <= 0) continue;
-              typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
               const Block b = block(i, j);
               bf16x4 v[4];
 #pragma unroll
               for (int q = 0; q < 4; ++q)
-                v[q] = __builtin_bit_cast(bf16x4, f16x4{(_Float16)b.q[q][0], (_Float16)b.q[q][1], (_Float16)b.q[q][2], (_Float16)b.q[q][3]});
+                v[q] = __builtin_bit_cast(bf16x4, u32x2v{unit16_pack(b.q[q][0], b.q[q][1]), unit16_pack(b.q[q][2], b.q[q][3])});
               stage_store_bf16(stg, v, static_cast<bf16*>(p.C) + (long)mb * p.ldc + nb, p.ldc, rows_valid, cols_valid, lane);
             }
           }

@@ -4,7 +4,7 @@
 // The products are those of gemm_mfma_dma.h (bf16) and gemm_f32*.hip (fp32); here are the passes between them.
 //
 // bf16: the logits never reach memory.  The first product leaves, per row and per 64 or 128 columns, the maximum and the sum of
-// exp(z - maximum), and for a gradient exp(z - maximum) itself in fp16.  One pass per row joins the statistics and scales what was kept to G in
+// exp(z - maximum), and for a gradient exp(z - maximum) itself in 16 bits (unit16.h).  One pass per row joins the statistics and scales what was kept to G in
 // bf16, in place.  G exists for one piece of rows at a time.  (To keep nothing and multiply x w^T again for the gradient would be 8 T V d
 // operations instead of 6 T V d: a third more of a step that the matrix cores bound.)
 // Rows whose target is left out are not computed: the rows that count are gathered to the front first, so that they cost nothing and whatever
@@ -19,13 +19,13 @@
 
 #include "dense_plan.h"
 #include "moe_common.h"
+#include "unit16.h"
 #include "vocab_loss.h"
 
 namespace moe {
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
@@ -316,7 +316,7 @@ struct RowOut {
 
 __device__ __forceinline__ float row_weight(const RowOut& o, int t) { return o.token_w ? o.token_w[t] : o.counts->mean; }
 
-// exp(z - maximum of its part) in fp16 -> G in bf16, in place, a workgroup per row.  Bound by memory: 4 bytes per element (8192 rows
+// exp(z - maximum of its part) in 16 bits (unit16.h) -> G in bf16, in place, a workgroup per row.  Bound by memory: 4 bytes per element (8192 rows
 // of 32000 words 197 us, 5.3 TB/s).  Threads by the row's length, so that each has some pieces of it, and 1024 where rows are few.  Whole steps of
 // 16384 tokens, 256 wide (us; 64, 128, 256, 1024 threads): 1200 words 126, 131, 143, -; 2500 182, 185, 197, 334; 5000 282, 279, 286, -; 10000 529, 520,
 // 514, 616; 2000 tokens, 512 wide, 102400 words -, -, 867, 845.
@@ -343,12 +343,12 @@ __global__ void __launch_bounds__(THREADS) vocab_grad_rows_kernel(const f32x2* _
   }
   char* row = G + (long)r * ld * 2;
   for (int v = threadIdx.x * 8; v < ld; v += THREADS * 8) {
-    const f16x8 p = *reinterpret_cast<const f16x8*>(row + (long)v * 2);
+    const u32x4 p = *reinterpret_cast<const u32x4*>(row + (long)v * 2);
     bf16x8 g;
     // eight columns lie in one part; past the width nothing was written
     const float f = v < V ? c * exp_f32((row_stats[v >> part_shift][0] - l.top) - l.log_sum) : 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = v + i < V ? static_cast<bf16>((float)p[i] * f) : static_cast<bf16>(0.f);
+    for (int i = 0; i < 8; ++i) g[i] = v + i < V ? static_cast<bf16>((i & 1 ? unit16_high(p[i / 2]) : unit16_low(p[i / 2])) * f) : static_cast<bf16>(0.f);
     const unsigned at = (unsigned)(tg - v);
 #pragma unroll
     for (int i = 0; i < 8; ++i)

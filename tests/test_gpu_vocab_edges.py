@@ -1,0 +1,62 @@
+"""The vocabulary loss word by word and at the ends of the number range.
+
+Tolerances (u16 = 2^-8, u32 = 2^-24, as half steps): an element of G is exp of a logit that is up to 2^-16 of the largest |lse| off, and with bf16 data
+is kept once with 10 bits (2^-10) and once in bf16 (u16).  So with r the sum of these every element of d_w = G^T x is at most r |G|^T |x| off, and
+half a step of its own where it is rounded to bf16.
+"""
+import math
+
+import pytest
+import torch
+
+DEV = "cuda:0"
+U16 = 2.0 ** -8
+
+
+def make(T, d, V, dtype, **kw):
+    from paper_2505_11432_amd.head import VocabLoss
+    return VocabLoss(T, d, V, dtype=dtype, **kw)
+
+
+def softmax_gradient(x, w, target, token_w):
+    """In 64 bits on the CPU: G, lse."""
+    x, w, target = x.double().cpu(), w.double().cpu(), target.long().cpu()
+    z = x @ w.t()
+    lse = torch.logsumexp(z, 1)
+    g = torch.exp(z - lse[:, None])
+    at = torch.arange(len(target))
+    others = z.clone()
+    others[at, target] = -math.inf
+    g[at, target] = -torch.exp(torch.logsumexp(others, 1) - lse)      # p - 1 without the cancellation
+    c = token_w.double().cpu() if token_w is not None else torch.full((len(target),), 1.0 / len(target), dtype=torch.float64)
+    return g * c[:, None], lse
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,grad", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("T", [70, 300])
+@pytest.mark.parametrize("weights", [0, 1])
+@pytest.mark.parametrize("nats", [8.0, 14.0, 30.0, 60.0])
+def test_every_word(nats, weights, T, dtype, grad):
+    """A word that is no target dominates every row by `nats`: its neighbours' rows of d_w are tiny, not zero."""
+    d, V = 64, 700
+    g = torch.Generator().manual_seed(int(nats) + T)
+    w = torch.randn((V, d), generator=g) * (1.0 / math.sqrt(d))
+    x = torch.randn((T, d), generator=g)
+    w[0] = 0.0
+    w[:, 0] = 0.0
+    w[0, 0], x[:, 0] = nats / 4.0, 4.0
+    target = torch.randint(300, V, (T,), generator=g).to(torch.int32)      # none in the first words' neighbourhood
+    token_w = torch.rand((T,), generator=g).add_(0.25) / T if weights else None
+    x, w, target = x.to(dtype).to(DEV), w.to(dtype).to(DEV), target.to(DEV)
+    token_w = token_w.to(DEV) if weights else None
+    op = make(T, d, V, dtype, grad_dtype=grad)
+    op.step(x, w, target, token_w=token_w)
+    G, lse = softmax_gradient(x, w, target, token_w)
+    want, size = G.t() @ x.double().cpu(), G.abs().t() @ x.double().abs().cpu()
+    r = 2.0 ** -16 * max(1.0, float(lse.abs().max()))
+    if dtype == torch.bfloat16:
+        r += 2.0 ** -10 + U16
+    far = (op.d_w.double().cpu() - want).abs()
+    assert bool((far <= r * size + (U16 if grad == torch.bfloat16 else 2.0 ** -22) * want.abs()).all())
+    assert bool((op.d_w[:V].abs().sum(1) > 0).all())
