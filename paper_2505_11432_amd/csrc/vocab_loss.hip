@@ -56,6 +56,7 @@ template <int WAVES> __device__ __forceinline__ void join_block(float& m, float&
 }
 
 // A row's loss from its target's logit and the other words' maximum m and sum s of exp(z - m): 1 - p keeps its precision where p is near 1.
+// A target's logit of +inf leaves no number, as the row's lse and gradient have none: log1p of the others alone would be 0.
 struct RowLoss { float loss, lse, top, log_sum, miss; };          // lse = top + log_sum, miss = 1 - p
 __device__ __forceinline__ RowLoss row_loss(float zt, float m, float s) {
   RowLoss r;
@@ -63,7 +64,7 @@ __device__ __forceinline__ RowLoss row_loss(float zt, float m, float s) {
   const float others = s * exp_f32(m - r.top), all = others + exp_f32(zt - r.top);
   r.log_sum = logf(all);
   r.lse = r.top + r.log_sum;
-  r.loss = zt >= m ? log1pf(others) : (m - zt) + r.log_sum;
+  r.loss = zt >= m && zt < __builtin_inff() ? log1pf(others) : (m - zt) + r.log_sum;
   r.miss = others / all;
   return r;
 }

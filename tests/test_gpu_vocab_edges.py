@@ -60,3 +60,34 @@ def test_every_word(nats, weights, T, dtype, grad):
     far = (op.d_w.double().cpu() - want).abs()
     assert bool((far <= r * size + (U16 if grad == torch.bfloat16 else 2.0 ** -22) * want.abs()).all())
     assert bool((op.d_w[:V].abs().sum(1) > 0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [40, 300])
+@pytest.mark.parametrize("which", ["target", "other", "target below"])
+def test_infinite_logits(which, T, dtype):
+    """A logit that overflows: log sum exp z - z[target] is no number where the target's is +inf, not finite where another's is, and +inf where the
+    target's is -inf.  The other rows stay as they are."""
+    d, V = 32, 333
+    g = torch.Generator().manual_seed(T)
+    w, x = torch.randn((V, d), generator=g) * 0.2, torch.randn((T, d), generator=g)
+    target = torch.randint(0, V, (T,), generator=g).to(torch.int32)
+    row, hit = 7, int(target[7]) if which != "other" else (int(target[7]) + 100) % V
+    w[:, 0], x[:, 0] = 0.0, 0.0
+    w[hit, 0], x[row, 0] = (-16.0 if which == "target below" else 16.0), 3e38
+    x, w, target = x.to(dtype).to(DEV), w.to(dtype).to(DEV), target.to(DEV)
+    op = make(T, d, V, dtype)
+    clean = x.clone()
+    clean[row, 0] = 0.0
+    others = [t for t in range(T) if t != row]
+    op.step(clean, w, target)
+    want = op.loss[others].clone()
+    for call in (lambda: float(op.step(x, w, target)), lambda: float(op.score(x, w, target)[0].sum())):
+        total, loss = call(), float(op.loss[row])
+        if which == "target below":
+            assert loss == math.inf and total == math.inf and math.isfinite(float(op.lse[row]))
+        else:
+            assert not math.isfinite(loss) and not math.isfinite(total)
+            assert which != "target" or math.isnan(loss)
+        assert float((op.loss[others] - want).abs().max()) <= 2.0 ** -16 * float(op.lse[others].abs().max())
