@@ -407,8 +407,8 @@ int moe_quant_fp8_tgroup(const void* src, moe_dtype src_dt, int rows, int cols,
  * More pieces cost launches and passes over d_w.  A power of two of at least 2048 rows, or all
  * of them, fills the matrix cores.
  * Workspace: moe_vocab_workspace_bytes with the same sizes (gradients = 0 for the score; grad_dt
- * then does not matter); 0 on invalid sizes.  T and V are bounded each, and their product by
- * (T / 64 + 1) (V / 128 + 1) < 2^30. */
+ * then does not matter); 0 on invalid sizes.  T and V are bounded each, with bf16 gradients V by
+ * MOE_VOCAB_MAX - 64, and their product by (T / 64 + 1) (V / 128 + 1) < 2^30. */
 #define MOE_VOCAB_MAX (1 << 24)
 #define MOE_VOCAB_MAX_WIDTH (1 << 20)
 #define MOE_VOCAB_MAX_ROWS (1 << 24)

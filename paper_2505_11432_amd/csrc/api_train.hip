@@ -9,11 +9,12 @@ namespace moe {
 namespace {
 
 bool vocab_sizes_ok(int T, int d, int V) { return T >= 0 && d > 0 && V > 0; }
-bool vocab_types_ok(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt) {
+bool vocab_types_ok(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, bool grad) {
   if (dt != MOE_F32 && dt != MOE_BF16) return false;
   if (dt == MOE_F32 ? grad_dt != MOE_F32 : grad_dt != MOE_F32 && grad_dt != MOE_BF16) return false;
   // (tiles are counted in 32 bits)
   const long tiles = ((long)T / 64 + 1) * ((long)V / 128 + 1);
+  if (grad && dt == MOE_BF16 && !vocab_dx_takes(128, (long)align_up((size_t)V, 64))) return false;
   return d % 16 == 0 && d <= MOE_VOCAB_MAX_WIDTH && V <= MOE_VOCAB_MAX && T <= MOE_VOCAB_MAX_ROWS && tiles <= 0x3fffffffL;
 }
 
@@ -55,14 +56,14 @@ using namespace moe;
 extern "C" {
 
 size_t moe_vocab_workspace_bytes(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int piece_rows, int gradients) {
-  if (!vocab_sizes_ok(T, d, V) || piece_rows < 0 || !vocab_types_ok(T, d, V, dt, gradients ? grad_dt : dt)) return 0;
+  if (!vocab_sizes_ok(T, d, V) || piece_rows < 0 || !vocab_types_ok(T, d, V, dt, gradients ? grad_dt : dt, gradients != 0)) return 0;
   return T == 0 ? 256 : vocab_plan(T, d, V, dt, gradients ? grad_dt : dt, piece_rows, gradients != 0).bytes;
 }
 
 int moe_vocab_score(const void* x, const void* w, const int32_t* target, moe_dtype dt, int T, int d, int V, int piece_rows, float* loss, float* lse,
                     void* workspace, size_t ws_bytes, void* stream) {
   if (!vocab_sizes_ok(T, d, V) || piece_rows < 0) return MOE_ERR_INVALID;
-  if (!vocab_types_ok(T, d, V, dt, dt)) return MOE_ERR_UNSUPPORTED;
+  if (!vocab_types_ok(T, d, V, dt, dt, false)) return MOE_ERR_UNSUPPORTED;
   if (T == 0) return MOE_OK;
   if (!x || !w || !target || !loss || !lse) return MOE_ERR_INVALID;
   if (!aligned16(x) || !aligned16(w) || !at_elements(target, 4) || !at_elements(loss, 4) || !at_elements(lse, 4)) return MOE_ERR_UNSUPPORTED;
@@ -75,7 +76,7 @@ int moe_vocab_loss(const void* x, const void* w, const int32_t* target, const fl
                    float* total, float* loss, float* lse, void* dx, void* d_w, moe_dtype grad_dt, int accumulate, void* workspace, size_t ws_bytes,
                    void* stream) {
   if (!vocab_sizes_ok(T, d, V) || piece_rows < 0) return MOE_ERR_INVALID;
-  if (!vocab_types_ok(T, d, V, dt, grad_dt)) return MOE_ERR_UNSUPPORTED;
+  if (!vocab_types_ok(T, d, V, dt, grad_dt, true)) return MOE_ERR_UNSUPPORTED;
   if (T == 0) return MOE_OK;
   if (!x || !w || !target || !total || !loss || !lse || !dx || !d_w) return MOE_ERR_INVALID;
   if (!aligned16(x) || !aligned16(w) || !aligned16(dx) || !aligned16(d_w) || !at_elements(target, 4) || !at_elements(token_w, 4) ||

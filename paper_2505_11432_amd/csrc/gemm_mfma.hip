@@ -351,20 +351,16 @@ int mfma_vocab_softmax(const VocabRows& x, const void* w, const int32_t* rows, c
   return P ? launch_softmax<EPI_CE>(a, tile, s) : launch_softmax<EPI_LSE>(a, tile, s);
 }
 
-// Costs of their tiles (row_plan.h): dx on 256 x 256 and on 128 x 128, whose parts the pass that rounds and places the rows reads anyway; d_w on
-// 256 x 256 and on 128 x 128 in pairs of workgroups, whose parts take a launch.
+// Costs of d_w's tiles (row_plan.h): on 256 x 256 and on 128 x 128 in pairs of workgroups, whose parts take a launch.
 namespace {
-constexpr CutCost kDxFull = {13000, 1500, 105, 0}, kDxMid = {6000, 660, 26, 0}, kDwFull = {13000, 1500, 105, 4000}, kDwPair = {11000, 750, 26, 4000};
-constexpr int kPlanGroups = 256;            // workgroups that sizes are worked out for: one per CU
+constexpr CutCost kDwFull = {13000, 1500, 105, 4000}, kDwPair = {11000, 750, 26, 4000};
 }  // namespace
 
 VocabDxPlan mfma_vocab_dx_plan(int R, int V, int d) {
-  const int steps = cdiv(V, 64);
-  const long full = (long)cdiv(R, 256) * cdiv(d, 256), mid = (long)cdiv(R, 128) * cdiv(d, 128);
   VocabDxPlan p{};
-  p.tile = dense_ns(mid, kPlanGroups, steps, kDxMid) < dense_ns(full, kPlanGroups, steps, kDxFull) ? 128 : 256;
+  p.tile = vocab_dx_tile(R, V, d);
   p.cost = p.tile == 256 ? kDxFull : kDxMid;
-  p.part_floats = (size_t)cut_items(p.tile == 256 ? full : mid, kPlanGroups, steps) * p.tile * p.tile;
+  p.part_floats = (size_t)cut_items((long)cdiv(R, p.tile) * cdiv(d, p.tile), kPlanGroups, cdiv(V, 64)) * p.tile * p.tile;
   return p;
 }
 // out [R][d] fp32 gets the whole tiles, `parts` the others' parts; *groups is what dense_plan needs to know which they are

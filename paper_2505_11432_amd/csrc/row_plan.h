@@ -208,6 +208,19 @@ inline long cut_items(long tiles, int groups, int steps) {
   return rem * parts < (long)kCutItems * groups ? rem * parts : (long)kCutItems * groups;
 }
 
+// dx of the vocabulary loss, G w, on 256 x 256 or on 128 x 128 tiles; the pass that rounds and places its rows reads the parts anyway.  G's rows of ld bf16
+// are addressed in 32 bits from a tile's first one, so 256 of them have to span less than 4 GiB, and 128 of them for the product to exist.
+constexpr CutCost kDxFull = {13000, 1500, 105, 0}, kDxMid = {6000, 660, 26, 0};
+constexpr int kPlanGroups = 256;            // workgroups that sizes are worked out for: one per CU
+inline bool vocab_dx_takes(int tile, long ld) { return tile * ld * 2 < 1L << 32; }
+inline int vocab_dx_tile(int R, int V, int d) {
+  auto up = [](long a, long b) { return (a + b - 1) / b; };
+  const int steps = (int)up(V, 64);
+  const long full = up(R, 256) * up(d, 256), mid = up(R, 128) * up(d, 128);
+  if (!vocab_dx_takes(256, steps * 64L)) return 128;
+  return dense_ns(mid, kPlanGroups, steps, kDxMid) < dense_ns(full, kPlanGroups, steps, kDxFull) ? 128 : 256;
+}
+
 // ---- fp32 expert products (gemm_f32_split.hip): the split into bf16 parts or the fp32 instruction, 64 x 64 or 128 x 128 tiles.
 constexpr int kF32SplitStep = 32;        // contraction per step
 struct F32Product { bool rows; int M, N, K, E; };      // rows: the segments lie along M (forward, dgrad), else along K (weight gradients)

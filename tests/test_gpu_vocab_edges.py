@@ -91,3 +91,36 @@ def test_infinite_logits(which, T, dtype):
             assert not math.isfinite(loss) and not math.isfinite(total)
             assert which != "target" or math.isnan(loss)
         assert float((op.loss[others] - want).abs().max()) <= 2.0 ** -16 * float(op.lse[others].abs().max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,V", [(300, 64, 2 ** 23 + 77), (640, 256, 2 ** 23), (5, 16, 2 ** 24 - 64)])
+def test_millions_of_words(T, d, V):
+    """bf16, from the number of words on at which 256 rows of G span 4 GiB; the reference in fp32 on the GPU, in chunks of words (its error is far below
+    the tolerances, which are two roundings of dx and one of d_w)."""
+    step = 2 ** 20
+    g = torch.Generator(device=DEV).manual_seed(T)
+    w = torch.empty((V, d), dtype=torch.bfloat16, device=DEV)
+    for part in w.split(step):
+        part.copy_(torch.randn(part.shape, device=DEV, generator=g) * (1.28 / math.sqrt(d)))
+    target = torch.randint(0, V, (T,), device=DEV, generator=g)
+    target[0], target[1] = V - 1, 0
+    x = (torch.randn((T, d), device=DEV, generator=g) + 5.0 * w[target].float()).to(torch.bfloat16)
+    op = make(T, d, V, torch.bfloat16, piece_bytes=16 << 30)
+    assert op.piece_rows == 0
+    op.step(x, w, target.to(torch.int32))
+    xf, at = x.float(), torch.arange(T, device=DEV)
+    lse = torch.logsumexp(torch.stack([torch.logsumexp((xf @ part.float().t()).double(), 1) for part in w.split(step)], 1), 1)
+    assert float((op.lse.double() - lse).abs().max()) <= 2.0 ** -16 * float(lse.abs().max())
+    loss = lse - (xf * w[target].float()).sum(1).double()
+    assert float((op.loss.double() - loss).abs().max()) <= 2.0 ** -16 * float(lse.abs().max())
+    dx = torch.zeros((T, d), device=DEV)
+    for i, part in enumerate(w.split(step)):
+        p = torch.exp((xf @ part.float().t()).double() - lse[:, None]).float()
+        here = (target >= i * step) & (target < i * step + len(part))
+        p[at[here], target[here] - i * step] -= 1.0
+        p /= T
+        dx += p @ part.float()
+        want, got = p.t() @ xf, op.d_w[i * step:i * step + len(part)]
+        assert float((got - want).norm()) <= U16 * float(want.norm()), i
+    assert float((op.dx.float() - dx).norm()) <= 2 * U16 * float(dx.norm())
