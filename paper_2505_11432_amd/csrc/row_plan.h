@@ -350,6 +350,14 @@ inline F32Plan f32_parts(const F32Product& p, long room) {
   if (n > room) n = room;
   return {F32_64, n > 1 ? (int)n : 1};
 }
+// Rows of a piece of the fp32 vocabulary loss, at most R: a launch holds less than 2^32 threads, 256 per row in the pass over the logits (2^24 rows of 16 words
+// are 4 GB of them) and per tile of x w^T and G w, one row of tiles more than R fills; the tiles stay below 2^31, as f32_blocks is asked for.
+inline int vocab_f32_rows(int R, int V, int d) {
+  auto up = [](long a, long b) { return (a + b - 1) / b; };
+  const long columns = up(V > d ? V : d, 64), by_tiles = (((1L << 23) - 1) / columns - 1) * 64, by_rows = 1L << 23;
+  const long most = by_tiles < by_rows ? by_tiles : by_rows;
+  return R < most ? R : (int)most;
+}
 // The logits, whose contraction is short, only from half to one round of tiles, in two (131 tokens as above 94, 88; 40 tokens 152, 145; 3 tokens 67, 73; 300,
 // 16000, 1024 264, 273).
 inline F32Plan f32_logit_parts(const F32Product& p, long room) {

@@ -575,6 +575,7 @@ VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int p
   const size_t es = dtype_size(dt);
   p.R = piece_rows > 0 && piece_rows < T ? piece_rows : T;
   if (!grad && !f32) p.R = T < kScorePiece ? T : kScorePiece;          // nothing is kept per element
+  if (f32) p.R = vocab_f32_rows(p.R, V, d);
   p.pieces = (T + p.R - 1) / p.R;
   p.ld = (long)align_up((size_t)V, 64);
   p.gather = grad || f32 || T > kScoreAsIs;

@@ -124,3 +124,39 @@ def test_millions_of_words(T, d, V):
         want, got = p.t() @ xf, op.d_w[i * step:i * step + len(part)]
         assert float((got - want).norm()) <= U16 * float(want.norm()), i
     assert float((op.dx.float() - dx).norm()) <= 2 * U16 * float(dx.norm())
+
+
+@pytest.mark.gpu
+def test_most_rows():
+    """2^24 rows in fp32, the most that are taken, of few words: more than a launch over all of them holds.  d_w is a sum of 2^24 terms in fp32, 2^-24 of
+    it off per step of a random walk: 2^-12; the rest as in the tests of fewer rows."""
+    T, d, V, step = 1 << 24, 16, 16, 1 << 21
+    g = torch.Generator(device=DEV).manual_seed(2)
+    w = torch.randn((V, d), device=DEV, generator=g) * 0.5
+    target = torch.randint(0, V, (T,), device=DEV, generator=g)
+    x = torch.randn((T, d), device=DEV, generator=g) + w[target]
+    target[::5] = -100
+    op = make(T, d, V, torch.float32)
+    op.step(x, w, target.to(torch.int32))
+    n, total = int((target >= 0).sum()), 0.0
+    d_w = torch.zeros((V, d), dtype=torch.float64, device=DEV)
+    for a in range(0, T, step):
+        xs, ts = x[a:a + step].double(), target[a:a + step]
+        keep = ts >= 0
+        z = xs @ w.double().t()
+        lse = torch.logsumexp(z, 1)
+        loss = torch.where(keep, lse - z.gather(1, ts.clamp(min=0)[:, None])[:, 0], torch.zeros_like(lse))
+        assert float((op.loss[a:a + step].double() - loss).abs().max()) <= 2.0 ** -16 * float(lse.abs().max())
+        p = torch.exp(z - lse[:, None])
+        p.scatter_add_(1, ts.clamp(min=0)[:, None], torch.full_like(lse, -1.0)[:, None])
+        p *= keep[:, None] / n
+        dx = p @ w.double()
+        assert float((op.dx[a:a + step].double() - dx).norm()) <= 2.0 ** -16 * float(dx.norm())
+        d_w += p.t() @ xs
+        total += float(loss.sum()) / n
+    assert abs(float(op.total) - total) <= 2.0 ** -16 * total
+    assert float((op.d_w.double() - d_w).norm()) <= 2.0 ** -12 * float(d_w.norm())
+    want = op.loss.clone()
+    op.loss.fill_(-1.0)
+    loss, _ = op.score(x, w, target.to(torch.int32))
+    assert torch.equal(loss, want)

@@ -30,6 +30,15 @@ int main() {
   CHECK(vocab_dx_tile(640, 1 << 23, 256) == 128, "tile");
   CHECK(vocab_dx_tile(256, 8400000, 1024) == 128, "tile");
   CHECK(vocab_dx_tile(8192, 32000, 4096) == 256, "tile");
+  // fp32: threads of the launches of a piece
+  for (int i = 0; i < 200000; ++i) {
+    const int T = 1 + std::rand() % (1 << (1 + i % 24)), V = 1 + std::rand() % (1 << (1 + i / 24 % 24)), d = 16 * (1 + std::rand() % (1 << (1 + i % 16)));
+    const int R = vocab_f32_rows(T, V, d);
+    CHECK(R >= 1 && R <= T, "%d of %d rows", R, T);
+    CHECK(R * 256L < 1L << 32, "%d rows", R);
+    for (int columns : {V, d}) CHECK((columns + 63L) / 64 * ((R + 63L) / 64 + 1) * 256 < 1L << 31, "%d rows, %d columns", R, columns);
+  }
+  CHECK(vocab_f32_rows(1 << 24, 16, 16) == 1 << 23 && vocab_f32_rows(16384, 131072, 4096) == 16384, "rows");
   std::printf("bad %d\n", bad);
   return bad != 0;
 }
@@ -65,3 +74,9 @@ def test_most_words(lib):
     at = [ctypes.c_void_p(i << 40) for i in range(1, 9)]
     # refused ahead of any launch
     assert lib.moe_vocab_loss(at[0], at[1], at[2], None, BF16, 8, 16, MOST - 63, 0, at[3], at[4], at[5], at[6], at[7], F32, 0, at[0], 1 << 50, None) == -2
+
+
+def test_most_rows(lib):
+    """fp32: not all of 2^24 rows in one piece, whose pass would have 2^32 threads."""
+    for gradients in (0, 1):
+        assert 0 < lib.moe_vocab_workspace_bytes(MOST, 16, 16, F32, F32, 0, gradients) < MOST * 64 * 4
