@@ -400,8 +400,9 @@ int moe_quant_fp8_tgroup(const void* src, moe_dtype src_dt, int rows, int cols,
  * moe_vocab_loss: with c[t] = token_w[t], or 1 / (number of tokens that count) where token_w is
  * NULL, also total[0] = sum_t c[t] loss[t] and its gradients: dx [T,d] in `dt`, written, and
  * d_w [V,d] in grad_dt (MOE_F32, or MOE_BF16 for bf16 data), written or with accumulate=1 added
- * to.  No token that counts: total 0, gradients 0.  dx and d_w share no memory with x, w or each
- * other.  Results do not depend on what ran before.
+ * to.  No token that counts: total 0, gradients 0.  T = 0: nothing is enqueued and no output is
+ * written, total and d_w neither (a caller that has no tokens keeps or clears them itself).  dx and
+ * d_w share no memory with x, w or each other.  Results do not depend on what ran before.
  * G = c (softmax(z) - onehot) is kept for piece_rows rows at a time (0: all), V elements of the
  * data's type each (fp32 data: also the logits, in the same place, and in the score as well).
  * More pieces cost launches and passes over d_w.  A power of two of at least 2048 rows, or all

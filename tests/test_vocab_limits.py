@@ -80,3 +80,13 @@ def test_most_rows(lib):
     """fp32: not all of 2^24 rows in one piece, whose pass would have 2^32 threads."""
     for gradients in (0, 1):
         assert 0 < lib.moe_vocab_workspace_bytes(MOST, 16, 16, F32, F32, 0, gradients) < MOST * 64 * 4
+
+
+def test_no_tokens_leave_the_outputs(lib):
+    """T = 0 returns without a launch: total, d_w and the rest stay as they were (host memory here, which no kernel could write)."""
+    out = (ctypes.c_float * 64)(*([7.0] * 64))
+    at = ctypes.cast(out, ctypes.c_void_p)
+    ws = ctypes.c_void_p(4096)
+    assert lib.moe_vocab_workspace_bytes(0, 16, 4, BF16, F32, 0, 1) > 0
+    assert lib.moe_vocab_loss(None, None, None, None, BF16, 0, 16, 4, 0, at, at, at, at, at, F32, 0, ws, 256, None) == 0
+    assert list(out) == [7.0] * 64
