@@ -377,6 +377,13 @@ class _List:
         return all(a < 0 or (a == b and t == (w if dtype is None else dtype)) for a, b, t, w in zip(mine, theirs, types, want))
 
 
+def _apart(written, read, in_place=False) -> bool:
+    """Whether no tensor of a list that is written shares memory with another one: the launch takes them in no order.  in_place: the tensors of the
+    first list read may be those of the first list written, each at its place."""
+    parts = [[(t.pointers, t.numel, t.types) for t in lists] for lists in (written, read)]
+    return _native.lists_apart(parts[0], parts[1], in_place)
+
+
 def _table(fn, tensors, size, fill):
     """Fills a table in host memory and copies it to the device of the tensors."""
     host = torch.zeros((size,), dtype=torch.uint8)
@@ -389,6 +396,7 @@ def moe_grad_clip_table(grads, outs=None):
     g = _List(grads)
     o = _List(outs) if outs is not None else None
     assert o is None or o.like(g), "an out for each gradient, of its size and type"
+    assert o is None or _apart([o], [g], in_place=True), "an out is its own gradient or shares no memory with any tensor"
     n = len(grads)
     return _table("moe_grad_clip_table", grads, _lib.moe_grad_clip_table_bytes(n), lambda host: _lib.moe_grad_clip_table(
         n, g.pointers, o.pointers if o else None, g.numel, g.types, host))
@@ -412,6 +420,7 @@ def moe_adamw_table(params, grads, m, v, weights=None):
     assert p.like(p, F32) and m1.like(p, F32) and v1.like(p, F32), "parameters and moments are fp32, of one size"
     assert g.like(p, grad_dt), "gradients have one type and their parameters' sizes"
     assert w is None or w.like(p, BF16), "weights are bf16, of their parameters' sizes"
+    assert _apart([p, m1, v1] + ([w] if w else []), [g]), "parameters, moments and weights share no memory with each other or with a gradient"
     return _table("moe_adamw_table", params, _lib.moe_adamw_table_bytes(n), lambda host: _lib.moe_adamw_table(
         n, p.pointers, g.pointers, m1.pointers, v1.pointers, w.pointers if w else None, p.numel, grad_dt, host))
 

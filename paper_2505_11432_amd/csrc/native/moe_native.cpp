@@ -9,9 +9,11 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <tuple>
 #include <type_traits>
 #include <utility>
+#include <vector>
 
 #include "../../../include/moe.h"
 
@@ -149,6 +151,62 @@ PyObject* tensor_list(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   return result;
 }
 
+// lists_apart(written, read, in_place) -> whether no byte of a list that is written belongs to another tensor of any of them: a launch over the lists writes
+// and reads them in no order.  written, read: sequences of what tensor_list gives; in_place: a tensor of read[0] may be the one of written[0] at its place.
+PyObject* lists_apart(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  if (n_args != 3) {
+    PyErr_SetString(PyExc_TypeError, "takes two sequences of lists and a truth value");
+    return nullptr;
+  }
+  struct Range { uintptr_t begin, end; bool written; };
+  struct List { const int64_t* pointers; const int64_t* numel; const int32_t* types; Py_ssize_t n; };
+  const int in_place = PyObject_IsTrue(args[2]);
+  if (in_place < 0) return nullptr;
+  PyObject* seq[2] = {PySequence_Fast(args[0], "takes sequences of lists"), nullptr};
+  if (seq[0]) seq[1] = PySequence_Fast(args[1], "takes sequences of lists");
+  bool ok = seq[1] != nullptr, apart = true;
+  try {
+    std::vector<List> lists[2];
+    for (int k = 0; ok && k < 2; ++k)
+      for (Py_ssize_t i = 0; ok && i < PySequence_Fast_GET_SIZE(seq[k]); ++i) {
+        PyObject* bytes[3];
+        ok = PyArg_ParseTuple(PySequence_Fast_GET_ITEM(seq[k], i), "SSS", &bytes[0], &bytes[1], &bytes[2]) != 0;
+        if (!ok) break;
+        const Py_ssize_t n = PyBytes_GET_SIZE(bytes[2]) / 4;
+        if (PyBytes_GET_SIZE(bytes[0]) != n * 8 || PyBytes_GET_SIZE(bytes[1]) != n * 8) {
+          PyErr_SetString(PyExc_ValueError, "lists of one length");
+          ok = false;
+          break;
+        }
+        lists[k].push_back({reinterpret_cast<const int64_t*>(PyBytes_AS_STRING(bytes[0])), reinterpret_cast<const int64_t*>(PyBytes_AS_STRING(bytes[1])),
+                            reinterpret_cast<const int32_t*>(PyBytes_AS_STRING(bytes[2])), n});
+      }
+    std::vector<Range> all;
+    for (int k = 0; ok && k < 2; ++k)
+      for (size_t j = 0; j < lists[k].size(); ++j) {
+        const List& l = lists[k][j];
+        for (Py_ssize_t i = 0; i < l.n; ++i) {
+          if (l.numel[i] <= 0 || !l.pointers[i]) continue;
+          if (k == 1 && j == 0 && in_place && !lists[0].empty() && i < lists[0][0].n && lists[0][0].pointers[i] == l.pointers[i]) continue;
+          const uintptr_t begin = static_cast<uintptr_t>(l.pointers[i]);
+          all.push_back({begin, begin + static_cast<uintptr_t>(l.numel[i]) * (l.types[i] == MOE_F32 ? 4 : 2), k == 0});
+        }
+      }
+    std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+    uintptr_t any = 0, written = 0;          // ends of what begins in front
+    for (const Range& r : all) {
+      apart = apart && r.begin >= (r.written ? any : written);
+      any = std::max(any, r.end);
+      if (r.written) written = std::max(written, r.end);
+    }
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    ok = false;
+  }
+  for (PyObject* s : seq) Py_XDECREF(s);
+  return ok ? PyBool_FromLong(apart) : nullptr;
+}
+
 #define MOE_BOUND(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&Bound<&name>::call)), METH_FASTCALL, nullptr}
 
 PyMethodDef methods[] = {
@@ -158,7 +216,8 @@ PyMethodDef methods[] = {
     MOE_BOUND(moe_expert_ffn_fwd), MOE_BOUND(moe_expert_ffn_bwd), MOE_BOUND(moe_row_map), MOE_BOUND(moe_expert_ffn_fused_fwd),
     MOE_BOUND(moe_expert_ffn_fused_bwd), MOE_BOUND(moe_quant_fp8), MOE_BOUND(moe_dequant_fp8), MOE_BOUND(moe_quant_fp8_tgroup),
     MOE_BOUND(moe_transpose), MOE_BOUND(moe_vocab_score), MOE_BOUND(moe_vocab_loss), MOE_BOUND(moe_grad_clip), MOE_BOUND(moe_adamw),
-    {"tensor_list", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&tensor_list)), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    {"tensor_list", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&tensor_list)), METH_FASTCALL, nullptr},
+    {"lists_apart", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&lists_apart)), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_moe_native", "Calls of the MoE library on torch tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -11,7 +11,8 @@ class GradClip:
     """norm = sqrt(sum of all gradients squared), coef = min(1, max_norm / (norm + 1e-6)), and out = coef * gradients where asked.
 
     grads: bf16 or fp32 tensors.  out: None (the norm and the factor only, for an update that takes the factor), or a tensor for each
-    gradient; the gradients themselves clip in place.  Buffers: norm, coef [1] fp32 on the device."""
+    gradient; the gradients themselves clip in place.  An out shares no memory with another tensor (the gradient of a shared weight comes once).
+    Buffers: norm, coef [1] fp32 on the device."""
 
     def __init__(self, grads, max_norm: float, out=None, device=None):
         self.grads, self.out, self.max_norm = list(grads), None if out is None else list(out), float(max_norm)
@@ -31,7 +32,8 @@ class GradClip:
 class AdamW:
     """In place: fp32 parameters and moments from bf16 or fp32 gradients, and the parameters rounded to bf16 into `weights`.
 
-    params, grads, m, v (and weights): lists of one length.  lr: a float, or a [1] fp32 device tensor that a schedule writes.
+    params, grads, m, v (and weights): lists of one length; what is written shares no memory (a shared weight comes once).
+    lr: a float, or a [1] fp32 device tensor that a schedule writes.
     step: a [1] int32 device tensor with the updates taken so far (made at 0 if not given)."""
 
     def __init__(self, params, grads, m, v, weights=None, lr=1e-3, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1, step=None, device=None):
