@@ -426,7 +426,8 @@ int moe_vocab_loss(const void* x, const void* w, const int32_t* target, const fl
 /* Gradient norm over n tensors and clipping: norm[0] = sqrt(sum of all squares), summed in 64
  * bits in a fixed order, coef[0] = min(1, max_norm / (norm + 1e-6)); write=1: outs = coef * grads
  * as well (an out may be its gradient and else shares no memory with any tensor; a NULL out is
- * skipped).  A norm that is infinite or NaN gives a factor of 0 or NaN: the caller looks at it.
+ * skipped).  A norm that is infinite or NaN gives a factor of 0 or NaN: the caller looks at it, or
+ * makes the factor NaN on the device, with which moe_adamw changes nothing.
  * The tensors are named by a table that is made once: moe_grad_clip_table fills
  * moe_grad_clip_table_bytes(n) bytes of HOST memory from the tensors' device pointers (aligned
  * to their elements, no more), element counts and types (MOE_F32 or MOE_BF16; an out has its
@@ -443,10 +444,12 @@ int moe_grad_clip(const void* table /*device*/, int n, int64_t total, double max
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
  * in fp32, the new p rounded to bf16 into weights (NULL, or a NULL entry: none), step[0] = t.
- * lr, step and coef are read on the device, so a captured step follows a schedule.  params, m, v
- * fp32; grads all in grad_dt (MOE_F32 or MOE_BF16).  What is written shares no memory with another
- * tensor of the lists (each is taken once).  The table as above.  Workspace:
- * MOE_ADAMW_WS_BYTES that the caller has cleared once; every call leaves them cleared. */
+ * lr, step and coef are read on the device, so a captured step follows a schedule.  Where coef[0]
+ * is NaN the call changes nothing, step[0] neither: a step whose gradients are bad can be left out
+ * without the host.  params, m, v fp32; grads all in grad_dt (MOE_F32 or
+ * MOE_BF16).  What is written shares no memory with another tensor of the lists (each is taken
+ * once).  The table as above.  Workspace: MOE_ADAMW_WS_BYTES that the caller has cleared once;
+ * every call leaves them cleared. */
 #define MOE_ADAMW_WS_BYTES ((size_t)4096)
 size_t moe_adamw_table_bytes(int n);
 int moe_adamw_table(int n, void* const* params, const void* const* grads, void* const* m,

@@ -295,10 +295,13 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwEntry* __res
   a.r1 = (float)(1.0 / (1.0 - power(h.beta1, (unsigned)t)));
   a.r2 = (float)(1.0 / (1.0 - power(h.beta2, (unsigned)t)));
   a.eps = (float)h.eps;
+  const bool left_out = a.coef != a.coef;      // (looked at behind the table, whose reads do not wait for the factor then)
   for_parts(table, n, per, [&](const AdamwEntry& q, long first, long k) __attribute__((always_inline)) {
+    if (left_out) return;
     adamw_range(static_cast<float*>(q.p) + first, static_cast<const TG*>(q.g) + first, static_cast<float*>(q.m) + first, static_cast<float*>(q.v) + first,
                 q.w ? static_cast<bf16*>(q.w) + first : nullptr, k, a);
   });
+  if (left_out) return;                        // (every workgroup: the counters stay cleared)
   __syncthreads();
   if (threadIdx.x == 0) {
     // (no fence: what counts is that this workgroup has read the step, which the values above have needed; a fence would write back its L2)

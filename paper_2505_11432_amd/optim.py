@@ -51,7 +51,8 @@ class AdamW:
         self.workspace = torch.zeros((B.ADAMW_WS_BYTES,), dtype=torch.uint8, device=device)
 
     def step(self, coef=None):
-        """One update; coef: a [1] fp32 device tensor that every gradient is multiplied by (GradClip.coef)."""
+        """One update; coef: a [1] fp32 device tensor that every gradient is multiplied by (GradClip.coef).  A factor that is NaN leaves the update out:
+        nothing changes, the step count neither."""
         assert coef is None or (coef.dtype == torch.float32 and coef.numel() == 1), "coef is one fp32 number"
         B.moe_adamw(self.table, len(self.params), self.total, self.grad_dt, self.lr, self.step_count, coef, self.betas[0], self.betas[1],
                     self.eps, self.weight_decay, self.workspace)

@@ -19,7 +19,8 @@ from .optim import AdamW, GradClip
 
 
 class TrainStep:
-    """hidden = x + MoE(x); loss over the vocabulary; gradients clipped to max_norm; one AdamW update.
+    """hidden = x + MoE(x); loss over the vocabulary; gradients clipped to max_norm; one AdamW update, left out where the norm is infinite or NaN (the
+    step count then stays, so the host can see it whenever it looks).
 
     Master parameters w_r [E, d], w1 [E, 2f, d], w2 [E, d, f] and w_vocab [V, d] are fp32; bf16 models multiply with the copies
     that the update rounds them to."""
@@ -37,6 +38,7 @@ class TrainStep:
         grads = [self.layer.d_w_r, self.layer.d_w1, self.layer.d_w2, self.head.d_w]
         moments = [[torch.zeros_like(p) for p in self.masters] for _ in range(2)]
         self.clip = GradClip(grads, max_norm)
+        self.left_out = torch.full((1,), float("nan"), dtype=torch.float32, device=device)
         self.lr = torch.full((1,), lr, device=device)
         self.adamw = AdamW(self.masters, grads, *moments, weights=None if dtype == torch.float32 else self.params, lr=self.lr,
                            weight_decay=weight_decay)
@@ -58,7 +60,7 @@ class TrainStep:
         self.head.step(self.hidden, w_vocab, self.target)
         self.layer.backward(self.x, w_r, w1, w2, self.head.dx)
         self.clip.clip()
-        self.adamw.step(coef=self.clip.coef)
+        self.adamw.step(coef=torch.where(torch.isfinite(self.clip.norm), self.clip.coef, self.left_out))
 
     def step(self):
         """Enqueues one step; returns the loss [1] and the gradient norm [1], on the device."""
