@@ -216,11 +216,14 @@ __global__ void __launch_bounds__(kThreads, 8) clip_kernel(const ClipEntry* __re
 
 struct AdamwScalars { float coef, b1, g1, b2, g2, keep, lr, r1, r2, eps; };
 
+// Which products are fused is written out, so that an element's bits do not depend on whether it is taken alone or with its neighbours (that is, on where its
+// tensor begins).
 __device__ __forceinline__ void adamw_one(float& p, float g, float& m, float& v, const AdamwScalars& a) {
+#pragma clang fp contract(off)
   g *= a.coef;
-  m = m * a.b1 + g * a.g1;
-  v = v * a.b2 + g * g * a.g2;
-  p = p * a.keep - a.lr * (m * a.r1) / (sqrtf(v * a.r2) + a.eps);
+  m = __builtin_fmaf(g, a.g1, m * a.b1);
+  v = __builtin_fmaf(v, a.b2, g * g * a.g2);
+  p = __builtin_fmaf(p, a.keep, -(a.lr * (m * a.r1) / (sqrtf(v * a.r2) + a.eps)));
 }
 
 template <typename TG>
