@@ -447,7 +447,7 @@ int moe_grad_clip(const void* table /*device*/, int n, int64_t total, double max
  * lr, step and coef are read on the device, so a captured step follows a schedule.  Where coef[0]
  * is NaN the call changes nothing, step[0] neither: a step whose gradients are bad can be left out
  * without the host.  params, m, v fp32; grads all in grad_dt (MOE_F32 or
- * MOE_BF16).  What is written shares no memory with another tensor of the lists (each is taken
+ * MOE_BF16), or see below.  What is written shares no memory with another tensor of the lists (each is taken
  * once).  The table as above.  Workspace: MOE_ADAMW_WS_BYTES that the caller has cleared once;
  * every call leaves them cleared. */
 #define MOE_ADAMW_WS_BYTES ((size_t)4096)
@@ -455,6 +455,12 @@ size_t moe_adamw_table_bytes(int n);
 int moe_adamw_table(int n, void* const* params, const void* const* grads, void* const* m,
                     void* const* v, void* const* weights, const int64_t* numel,
                     moe_dtype grad_dt, void* table);
+/* Gradients of both types in one list (the layer's own: bf16 of the experts, fp32 of the router):
+ * grad_dtypes [n] name them, and moe_adamw takes MOE_GRADS_MIXED with such a table. */
+#define MOE_GRADS_MIXED ((moe_dtype)3)
+int moe_adamw_table_mixed(int n, void* const* params, const void* const* grads,
+                          const int32_t* grad_dtypes, void* const* m, void* const* v,
+                          void* const* weights, const int64_t* numel, void* table);
 int moe_adamw(const void* table /*device*/, int n, int64_t total, moe_dtype grad_dt,
               const float* lr, int32_t* step, const float* coef, double beta1, double beta2,
               double eps, double weight_decay, void* workspace, size_t ws_bytes, void* stream);

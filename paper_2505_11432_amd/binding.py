@@ -32,7 +32,7 @@ EXPORTS = (
     "moe_route_noalloc", "moe_init", "moe_transpose",
     "moe_vocab_workspace_bytes", "moe_vocab_score", "moe_vocab_loss",
     "moe_grad_clip_table_bytes", "moe_grad_clip_table", "moe_grad_clip_workspace_bytes", "moe_grad_clip",
-    "moe_adamw_table_bytes", "moe_adamw_table", "moe_adamw",
+    "moe_adamw_table_bytes", "moe_adamw_table", "moe_adamw_table_mixed", "moe_adamw",
 )
 
 
@@ -89,6 +89,7 @@ def _load() -> ctypes.CDLL:
         "moe_grad_clip_workspace_bytes": (Z, []),
         "moe_adamw_table_bytes": (Z, [I]),
         "moe_adamw_table": (I, [I, P, P, P, P, P, P, I, P]),
+        "moe_adamw_table_mixed": (I, [I, P, P, P, P, P, P, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -376,6 +377,10 @@ class _List:
         types, want = memoryview(self.types).cast("i"), memoryview(other.types).cast("i")
         return all(a < 0 or (a == b and t == (w if dtype is None else dtype)) for a, b, t, w in zip(mine, theirs, types, want))
 
+    def sizes_like(self, other) -> bool:
+        """As many elements at every place, whatever the types."""
+        return self.numel == other.numel
+
 
 def _apart(written, read, in_place=False) -> bool:
     """Whether no tensor of a list that is written shares memory with another one: the launch takes them in no order.  in_place: the tensors of the
@@ -411,18 +416,31 @@ def moe_grad_clip(table, n, total, max_norm, write, norm, coef, workspace):
                                                   workspace.numel() * workspace.element_size()))
 
 
+GRADS_MIXED = 3
+
+
+def adamw_grad_type(grads) -> int:
+    """What moe_adamw is told of a list of gradients: their type, or that there are both."""
+    types = {dtype_code(g.dtype) for g in grads if g is not None}
+    return GRADS_MIXED if len(types) > 1 else types.pop() if types else F32
+
+
 def moe_adamw_table(params, grads, m, v, weights=None):
-    """The device table of moe_adamw; weights: None, or a bf16 tensor (or None) for each parameter."""
+    """The device table of moe_adamw; grads: bf16 or fp32 each; weights: None, or a bf16 tensor (or None) for each parameter."""
     n = len(params)
-    grad_dt = dtype_code(grads[0].dtype) if grads else F32
+    grad_dt = adamw_grad_type(grads)
     p, g, m1, v1 = _List(params), _List(grads), _List(m), _List(v)
     w = _List(weights) if weights is not None else None
     assert p.like(p, F32) and m1.like(p, F32) and v1.like(p, F32), "parameters and moments are fp32, of one size"
-    assert g.like(p, grad_dt), "gradients have one type and their parameters' sizes"
+    assert g.sizes_like(p), "gradients have their parameters' sizes"
     assert w is None or w.like(p, BF16), "weights are bf16, of their parameters' sizes"
     assert _apart([p, m1, v1] + ([w] if w else []), [g]), "parameters, moments and weights share no memory with each other or with a gradient"
+    w_pointers = w.pointers if w else None
+    if grad_dt == GRADS_MIXED:
+        return _table("moe_adamw_table_mixed", params, _lib.moe_adamw_table_bytes(n), lambda host: _lib.moe_adamw_table_mixed(
+            n, p.pointers, g.pointers, g.types, m1.pointers, v1.pointers, w_pointers, p.numel, host))
     return _table("moe_adamw_table", params, _lib.moe_adamw_table_bytes(n), lambda host: _lib.moe_adamw_table(
-        n, p.pointers, g.pointers, m1.pointers, v1.pointers, w.pointers if w else None, p.numel, grad_dt, host))
+        n, p.pointers, g.pointers, m1.pointers, v1.pointers, w_pointers, p.numel, grad_dt, host))
 
 
 def moe_adamw(table, n, total, grad_dt, lr, step, coef, beta1, beta2, eps, weight_decay, workspace):

@@ -48,6 +48,27 @@ template <typename Entry> bool number_entries(const int64_t* numel, int n, Entry
 
 bool at_elements(const void* p, size_t es) { return (reinterpret_cast<uintptr_t>(p) & (es - 1)) == 0; }
 
+bool adamw_lists_ok(int n, void* const* params, const void* const* grads, void* const* m, void* const* v, const int64_t* numel, const void* table) {
+  return n >= 0 && table && (n == 0 || (params && grads && m && v && numel));
+}
+// type(i): of gradient i; bf16_mark: what is set in the addresses of those in bf16
+template <typename Type>
+int adamw_table(int n, void* const* params, const void* const* grads, Type type, void* const* m, void* const* v, void* const* weights, const int64_t* numel,
+                uintptr_t bf16_mark, void* table) {
+  AdamwEntry* e = static_cast<AdamwEntry*>(table);
+  for (int i = 0; i < n; ++i) {
+    const moe_dtype dt = type(i);
+    if (dt != MOE_F32 && dt != MOE_BF16) return MOE_ERR_UNSUPPORTED;
+    if (numel[i] > 0 && (!params[i] || !grads[i] || !m[i] || !v[i])) return MOE_ERR_INVALID;
+    void* w = weights ? weights[i] : nullptr;
+    if (!at_elements(params[i], 4) || !at_elements(m[i], 4) || !at_elements(v[i], 4) || !at_elements(grads[i], dtype_size(dt)) || !at_elements(w, 2))
+      return MOE_ERR_UNSUPPORTED;
+    const uintptr_t g = reinterpret_cast<uintptr_t>(grads[i]) | (dt == MOE_BF16 ? bf16_mark : 0);
+    e[i] = AdamwEntry{params[i], reinterpret_cast<const void*>(g), m[i], v[i], w, 0};
+  }
+  return number_entries(numel, n, e) ? MOE_OK : MOE_ERR_INVALID;
+}
+
 }  // namespace
 }  // namespace moe
 
@@ -118,24 +139,22 @@ size_t moe_adamw_table_bytes(int n) { return n < 0 ? 0 : ((size_t)n + 1) * sizeo
 
 int moe_adamw_table(int n, void* const* params, const void* const* grads, void* const* m, void* const* v, void* const* weights, const int64_t* numel,
                     moe_dtype grad_dt, void* table) {
-  if (n < 0 || !table || (n > 0 && (!params || !grads || !m || !v || !numel))) return MOE_ERR_INVALID;
+  if (!adamw_lists_ok(n, params, grads, m, v, numel, table)) return MOE_ERR_INVALID;
   if (grad_dt != MOE_F32 && grad_dt != MOE_BF16) return MOE_ERR_UNSUPPORTED;
-  AdamwEntry* e = static_cast<AdamwEntry*>(table);
-  for (int i = 0; i < n; ++i) {
-    if (numel[i] > 0 && (!params[i] || !grads[i] || !m[i] || !v[i])) return MOE_ERR_INVALID;
-    void* w = weights ? weights[i] : nullptr;
-    if (!at_elements(params[i], 4) || !at_elements(m[i], 4) || !at_elements(v[i], 4) || !at_elements(grads[i], dtype_size(grad_dt)) || !at_elements(w, 2))
-      return MOE_ERR_UNSUPPORTED;
-    e[i] = AdamwEntry{params[i], grads[i], m[i], v[i], w, 0};
-  }
-  return number_entries(numel, n, e) ? MOE_OK : MOE_ERR_INVALID;
+  return adamw_table(n, params, grads, [=](int) { return grad_dt; }, m, v, weights, numel, 0, table);
+}
+
+int moe_adamw_table_mixed(int n, void* const* params, const void* const* grads, const int32_t* grad_dtypes, void* const* m, void* const* v,
+                          void* const* weights, const int64_t* numel, void* table) {
+  if (!adamw_lists_ok(n, params, grads, m, v, numel, table) || (n > 0 && !grad_dtypes)) return MOE_ERR_INVALID;
+  return adamw_table(n, params, grads, [=](int i) { return (moe_dtype)grad_dtypes[i]; }, m, v, weights, numel, kBf16Gradient, table);
 }
 
 int moe_adamw(const void* table, int n, int64_t total, moe_dtype grad_dt, const float* lr, int32_t* step, const float* coef, double beta1, double beta2,
               double eps, double weight_decay, void* workspace, size_t ws_bytes, void* stream) {
   if (n < 0 || total < 0 || !table || !lr || !step) return MOE_ERR_INVALID;
   if (!(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0) || !(weight_decay >= 0)) return MOE_ERR_INVALID;
-  if (grad_dt != MOE_F32 && grad_dt != MOE_BF16) return MOE_ERR_UNSUPPORTED;
+  if (grad_dt != MOE_F32 && grad_dt != MOE_BF16 && grad_dt != MOE_GRADS_MIXED) return MOE_ERR_UNSUPPORTED;
   if (!at_elements(table, 8) || !at_elements(lr, 4) || !at_elements(step, 4) || !at_elements(coef, 4)) return MOE_ERR_UNSUPPORTED;
   if (!workspace || !at_elements(workspace, 4) || ws_bytes < MOE_ADAMW_WS_BYTES) return MOE_ERR_WORKSPACE;
   return launch_adamw(static_cast<const AdamwEntry*>(table), n, total, grad_dt, lr, step, coef, AdamwHyper{beta1, beta2, eps, weight_decay},

@@ -8,6 +8,8 @@ namespace moe {
 constexpr int kChunkBytes = 2048, kAdamwChunk = 512;
 struct ClipEntry { const void* g; void* out; int64_t first; int32_t dt, chunk; };
 struct AdamwEntry { void* p; const void* g; void* m; void* v; void* w; int64_t first; };
+// In a list of both types bit 0 of g, which an address of either has clear, says that its gradient is bf16.
+constexpr uintptr_t kBf16Gradient = 1;
 __host__ __device__ inline long chunk_elements(const ClipEntry& e) { return kChunkBytes / (e.dt == MOE_F32 ? 4 : 2); }
 __host__ __device__ inline long chunk_elements(const AdamwEntry&) { return kAdamwChunk; }
 // first chunk of entry i (AdamW, whose lists have one type: at least one chunk more than a tensor fills)

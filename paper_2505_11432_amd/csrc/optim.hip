@@ -282,6 +282,8 @@ __device__ __forceinline__ double power(double base, unsigned t) {
 constexpr int kShards = 16, kShardWords = 32;              // a line each
 static_assert((kShards + 1) * kShardWords * 4 <= MOE_ADAMW_WS_BYTES, "the workspace holds the counters");
 
+struct Mixed {};                         // gradients of both types (optim.h)
+
 // Every workgroup reads the step count before any has changed it: the last one to finish writes the new one.
 template <typename TG>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwEntry* __restrict__ table, int n, int per, const float* __restrict__ lr, int32_t* step,
@@ -301,8 +303,17 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const AdamwEntry* __res
   const bool left_out = a.coef != a.coef;      // (looked at behind the table, whose reads do not wait for the factor then)
   for_parts(table, n, per, [&](const AdamwEntry& q, long first, long k) __attribute__((always_inline)) {
     if (left_out) return;
-    adamw_range(static_cast<float*>(q.p) + first, static_cast<const TG*>(q.g) + first, static_cast<float*>(q.m) + first, static_cast<float*>(q.v) + first,
-                q.w ? static_cast<bf16*>(q.w) + first : nullptr, k, a);
+    auto range = [&](auto* g) __attribute__((always_inline)) {
+      adamw_range(static_cast<float*>(q.p) + first, g + first, static_cast<float*>(q.m) + first, static_cast<float*>(q.v) + first,
+                  q.w ? static_cast<bf16*>(q.w) + first : nullptr, k, a);
+    };
+    if constexpr (std::is_same_v<TG, Mixed>) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(q.g);
+      if (at & kBf16Gradient) range(reinterpret_cast<const bf16*>(at - kBf16Gradient));
+      else range(static_cast<const float*>(q.g));
+    } else {
+      range(static_cast<const TG*>(q.g));
+    }
   });
   if (left_out) return;                        // (every workgroup: the counters stay cleared)
   __syncthreads();
@@ -352,7 +363,8 @@ int launch_adamw(const AdamwEntry* table, int n, long total, moe_dtype grad_dt, 
   // four chunks, 2048 elements, at a time, two pieces per thread: 400 M elements by 2, 4, 8, 16 chunks 1965, 1925, 2045, 2130 us, 20 M 102, 102, 112, 120
   const Cut c = cut(total / kAdamwChunk + 2L * n, 4, 1L << 20);
   if (grad_dt == MOE_F32) adamw_kernel<float><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, lr, step, coef, h, done);
-  else adamw_kernel<bf16><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, lr, step, coef, h, done);
+  else if (grad_dt == MOE_BF16) adamw_kernel<bf16><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, lr, step, coef, h, done);
+  else adamw_kernel<Mixed><<<dim3(c.blocks), dim3(kThreads), 0, s>>>(table, n, c.per, lr, step, coef, h, done);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }

@@ -30,7 +30,7 @@ class GradClip:
 
 
 class AdamW:
-    """In place: fp32 parameters and moments from bf16 or fp32 gradients, and the parameters rounded to bf16 into `weights`.
+    """In place: fp32 parameters and moments from bf16 or fp32 gradients (a list may have both), and the parameters rounded to bf16 into `weights`.
 
     params, grads, m, v (and weights): lists of one length; what is written shares no memory (a shared weight comes once).
     lr: a float, or a [1] fp32 device tensor that a schedule writes.
@@ -42,7 +42,7 @@ class AdamW:
         device = device or (self.params[0].device if self.params else "cuda:0")
         self.total = sum(p.numel() for p in self.params)
         self.table = B.moe_adamw_table(self.params, self.grads, self.m, self.v, self.weights)
-        self.grad_dt = B.dtype_code(self.grads[0].dtype) if self.grads else B.F32
+        self.grad_dt = B.adamw_grad_type(self.grads)
         self.lr = lr if isinstance(lr, torch.Tensor) else torch.full((1,), float(lr), device=device)
         self.step_count = step if step is not None else torch.zeros((1,), dtype=torch.int32, device=device)
         assert self.lr.dtype == torch.float32 and self.lr.numel() == 1, "lr is one fp32 number"

@@ -23,16 +23,17 @@ class TrainStep:
     step count then stays, so the host can see it whenever it looks).
 
     Master parameters w_r [E, d], w1 [E, 2f, d], w2 [E, d, f] and w_vocab [V, d] are fp32; bf16 models multiply with the copies
-    that the update rounds them to."""
+    that the update rounds them to.  grad_dtype: of the gradients of w1, w2 and w_vocab (that of w_r is fp32)."""
 
-    def __init__(self, T, d, E, k, f, V, dtype=torch.bfloat16, lr=3e-3, max_norm=1.0, weight_decay=0.0, seed=0, device="cuda:0"):
+    def __init__(self, T, d, E, k, f, V, dtype=torch.bfloat16, lr=3e-3, max_norm=1.0, weight_decay=0.0, seed=0, device="cuda:0",
+                 grad_dtype=torch.float32):
         g = torch.Generator(device=device).manual_seed(seed)
 
         def normal(*shape, std):
             return torch.randn(shape, device=device, generator=g) * std
 
-        self.layer = MoELayer(T, d, E, k, f, dtype=dtype, device=device)
-        self.head = VocabLoss(T, d, V, dtype=dtype, device=device)
+        self.layer = MoELayer(T, d, E, k, f, dtype=dtype, grad_dtype=grad_dtype, device=device)
+        self.head = VocabLoss(T, d, V, dtype=dtype, grad_dtype=grad_dtype, device=device)
         self.masters = [normal(E, d, std=0.1), normal(E, 2 * f, d, std=d ** -0.5), normal(E, d, f, std=f ** -0.5), normal(V, d, std=d ** -0.5)]
         self.params = self.masters if dtype == torch.float32 else [p.to(dtype) for p in self.masters]
         grads = [self.layer.d_w_r, self.layer.d_w1, self.layer.d_w2, self.head.d_w]
