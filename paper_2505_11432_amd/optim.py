@@ -43,7 +43,7 @@ class AdamW:
         self.total = sum(p.numel() for p in self.params)
         self.table = B.moe_adamw_table(self.params, self.grads, self.m, self.v, self.weights)
         self.grad_dt = B.adamw_grad_type(self.grads)
-        self.lr = lr if isinstance(lr, torch.Tensor) else torch.full((1,), float(lr), device=device)
+        self.lr = lr if isinstance(lr, torch.Tensor) else torch.full((1,), float(lr), dtype=torch.float32, device=device)
         self.step_count = step if step is not None else torch.zeros((1,), dtype=torch.int32, device=device)
         assert self.lr.dtype == torch.float32 and self.lr.numel() == 1, "lr is one fp32 number"
         assert self.step_count.dtype == torch.int32 and self.step_count.numel() == 1, "step is one int32 number"

@@ -30,7 +30,7 @@ class TrainStep:
         g = torch.Generator(device=device).manual_seed(seed)
 
         def normal(*shape, std):
-            return torch.randn(shape, device=device, generator=g) * std
+            return torch.randn(shape, dtype=torch.float32, device=device, generator=g) * std
 
         self.layer = MoELayer(T, d, E, k, f, dtype=dtype, grad_dtype=grad_dtype, device=device)
         self.head = VocabLoss(T, d, V, dtype=dtype, grad_dtype=grad_dtype, device=device)
@@ -40,7 +40,7 @@ class TrainStep:
         moments = [[torch.zeros_like(p) for p in self.masters] for _ in range(2)]
         self.clip = GradClip(grads, max_norm)
         self.left_out = torch.full((1,), float("nan"), dtype=torch.float32, device=device)
-        self.lr = torch.full((1,), lr, device=device)
+        self.lr = torch.full((1,), lr, dtype=torch.float32, device=device)
         self.adamw = AdamW(self.masters, grads, *moments, weights=None if dtype == torch.float32 else self.params, lr=self.lr,
                            weight_decay=weight_decay)
         self.embedding = normal(V, d, std=1.0).to(dtype)
