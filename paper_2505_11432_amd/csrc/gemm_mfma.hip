@@ -351,11 +351,6 @@ int mfma_vocab_softmax(const VocabRows& x, const void* w, const int32_t* rows, c
   return P ? launch_softmax<EPI_CE>(a, tile, s) : launch_softmax<EPI_LSE>(a, tile, s);
 }
 
-// Costs of d_w's tiles (row_plan.h): on 256 x 256 and on 128 x 128 in pairs of workgroups, whose parts take a launch.
-namespace {
-constexpr CutCost kDwFull = {13000, 1500, 105, 4000}, kDwPair = {11000, 750, 26, 4000};
-}  // namespace
-
 VocabDxPlan mfma_vocab_dx_plan(int R, int V, int d) {
   VocabDxPlan p{};
   p.tile = vocab_dx_tile(R, V, d);
@@ -384,12 +379,6 @@ int mfma_vocab_dx(const void* G, long ldg, const void* w, const int32_t* rows, c
 
 // d_w (+)= G^T x over *rows rows (device; at most R).  G [R, ldg] with ldg a multiple of 8, V <= ldg.
 namespace {
-bool vocab_dw_pairs(int R, int V, int d) {
-  const int steps = cdiv(R, 64);
-  const long full = (long)cdiv(V, 256) * cdiv(d, 256), small = (long)cdiv(V, 128) * cdiv(d, 128);
-  // (in long lists the estimate is too near to go by: 102400 words, 2048 wide, 8200 rows in pairs 4270 us, else 2760)
-  return full <= 2 * kPlanGroups && dense_ns(small, 2 * kPlanGroups, steps, kDwPair) < dense_ns(full, kPlanGroups, steps, kDwFull);
-}
 template <int BM, typename TC> int launch_dense_dw(const Args& a, int groups, int most_tiles, hipStream_t s) {
   int rc;
   if constexpr (BM == 256) rc = launch<256, 256, 64, 2, 2, 4, MNMAJOR, MNMAJOR, DENSE, EPI_STORE, TC>(a, 1, s);

@@ -221,6 +221,16 @@ inline int vocab_dx_tile(int R, int V, int d) {
   return dense_ns(mid, kPlanGroups, steps, kDxMid) < dense_ns(full, kPlanGroups, steps, kDxFull) ? 128 : 256;
 }
 
+// d_w, G^T x: on 256 x 256, or on 128 x 128 in pairs of workgroups; the parts take a launch.
+constexpr CutCost kDwFull = {13000, 1500, 105, 4000}, kDwPair = {11000, 750, 26, 4000};
+inline bool vocab_dw_pairs(int R, int V, int d) {
+  auto up = [](long a, long b) { return (a + b - 1) / b; };
+  const int steps = (int)up(R, 64);
+  const long full = up(V, 256) * up(d, 256), small = up(V, 128) * up(d, 128);
+  // (in long lists the estimate is too near to go by: 102400 words, 2048 wide, 8200 rows in pairs 4270 us, else 2760)
+  return full <= 2 * kPlanGroups && dense_ns(small, 2 * kPlanGroups, steps, kDwPair) < dense_ns(full, kPlanGroups, steps, kDwFull);
+}
+
 // ---- fp32 expert products (gemm_f32_split.hip): the split into bf16 parts or the fp32 instruction, 64 x 64 or 128 x 128 tiles.
 constexpr int kF32SplitStep = 32;        // contraction per step
 struct F32Product { bool rows; int M, N, K, E; };      // rows: the segments lie along M (forward, dgrad), else along K (weight gradients)
