@@ -360,6 +360,11 @@ inline F32Plan f32_parts(const F32Product& p, long room) {
   if (n > room) n = room;
   return {F32_64, n > 1 ? (int)n : 1};
 }
+// Words per panel of the fp32 logits.  The split products take rows of less than 2^20 elements; what is longer would go to the fp32 instruction in one chain of
+// V products, so logits of more words are kept, and multiplied, panel by panel.  2^20 + 77 words (one chain, panels): dx 1.1e-4, 1.1e-6 off; 70 tokens, 512
+// wide 13.6, 3.5 ms; 2^21 words 2.1e-4, 1.0e-6, 300 tokens, 256 wide 30.1, 10.0 ms.
+constexpr int kF32Panel = 1 << 19;
+inline long vocab_f32_panel(long ld) { return ld < 1 << 20 ? ld : kF32Panel; }
 // Rows of a piece of the fp32 vocabulary loss, at most R: a launch holds less than 2^32 threads, 256 per row in the pass over the logits (2^24 rows of 16 words
 // are 4 GB of them) and per tile of x w^T and G w, one row of tiles more than R fills; the tiles stay below 2^31, as f32_blocks is asked for.
 inline int vocab_f32_rows(int R, int V, int d) {

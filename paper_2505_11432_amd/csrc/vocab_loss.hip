@@ -15,6 +15,7 @@
 // the whole row, and the results of few tokens would carry its rounding error undivided, so what the rounding took off (`rest`) is kept in fp32:
 // dx gets rest * w[target] when its parts are added, d_w one more row per token with rest in the target's column where the tokens are few
 // (kFewRows) and that is free.
+#include <algorithm>
 #include <type_traits>
 
 #include "dense_plan.h"
@@ -364,21 +365,24 @@ __global__ void __launch_bounds__(THREADS) vocab_grad_rows_kernel(const f32x2* _
   }
 }
 
-// fp32: the logits of a piece are in Z, in n_parts parts; loss and lse, and with GRAD G in the place of the first part.
-template <bool GRAD, int THREADS>
+// fp32: the logits of a piece are in Z, in n_parts parts; loss and lse, and with GRAD G in the place of the first part.  PANELS: each panel of kF32Panel
+// words has its rows together (then one part).
+template <bool GRAD, int THREADS, bool PANELS>
 __global__ void __launch_bounds__(THREADS) vocab_rows_f32_kernel(float* __restrict__ Z, int n_parts, long part_stride, int V, long ld, RowOut o) {
   __shared__ f32x2 lds[THREADS / 64];
   const int r = blockIdx.x;
   if (r >= o.range[1]) return;
   float* row = Z + (long)r * ld;
-  const int t = o.token[r], tg = o.target_of[r];
-  float zt = row[tg];
-  for (int p = 1; p < n_parts; ++p) zt += row[p * part_stride + tg];
-  if (n_parts > 1) __syncthreads();        // (the sums go over the first part)
+  auto at = [&](int v) __attribute__((always_inline)) { return PANELS ? row + (v / kF32Panel * part_stride + v % kF32Panel) : row + v; };
+  const int t = o.token[r], tg = o.target_of[r], width = (V + 63) / 64 * 64;
+  float zt = *at(tg);
+  if constexpr (!PANELS)
+    for (int p = 1; p < n_parts; ++p) zt += row[p * part_stride + tg];
+  if (!PANELS && n_parts > 1) __syncthreads();        // (the sums go over the first part)
   float m = kLowest, s = 0.f;
   for (int v = threadIdx.x * 4; v < V; v += THREADS * 4) {
-    f32x4 z = *reinterpret_cast<const f32x4*>(row + v);
-    if (n_parts > 1) {
+    f32x4 z = *reinterpret_cast<const f32x4*>(at(v));
+    if (!PANELS && n_parts > 1) {
       for (int p = 1; p < n_parts; ++p) z += *reinterpret_cast<const f32x4*>(row + p * part_stride + v);
       if (GRAD) *reinterpret_cast<f32x4*>(row + v) = z;
     }
@@ -398,11 +402,11 @@ __global__ void __launch_bounds__(THREADS) vocab_rows_f32_kernel(float* __restri
   if constexpr (GRAD) {                    // (every thread has read the target's logit and its share of the row: join_block waits for all)
     const float c = row_weight(o, t), g_target = -c * l.miss;
     if (threadIdx.x == 0) o.weighted[r] = c * l.loss;
-    for (int v = threadIdx.x * 4; v < ld; v += THREADS * 4) {
-      f32x4 z = *reinterpret_cast<const f32x4*>(row + v);
+    for (int v = threadIdx.x * 4; v < width; v += THREADS * 4) {
+      f32x4 z = *reinterpret_cast<const f32x4*>(at(v));
 #pragma unroll
       for (int i = 0; i < 4; ++i) z[i] = v + i >= V ? 0.f : v + i == tg ? g_target : c * exp_f32((z[i] - l.top) - l.log_sum);
-      *reinterpret_cast<f32x4*>(row + v) = z;
+      *reinterpret_cast<f32x4*>(at(v)) = z;
     }
   }
 }
@@ -482,13 +486,13 @@ __global__ void __launch_bounds__(256) vocab_dx_f32_kernel(const float* __restri
     *reinterpret_cast<f32x4*>(dx + (long)o.token[r] * d + c) = a;
   }
 }
-// d_w (+)= the sum of its parts
-__global__ void __launch_bounds__(256) vocab_dw_f32_kernel(const float* __restrict__ parts, int n_parts, long part_stride, long vecs, int accumulate,
-                                                           float* __restrict__ d_w) {
+// out (+)= the sum of its parts
+__global__ void __launch_bounds__(256) vocab_add_f32_kernel(const float* __restrict__ parts, int n_parts, long part_stride, long vecs, int accumulate,
+                                                            float* __restrict__ out) {
   for (long i = blockIdx.x * 256L + threadIdx.x; i < vecs; i += gridDim.x * 256L) {
     f32x4 a = *reinterpret_cast<const f32x4*>(parts + 4 * i);
     for (int p = 1; p < n_parts; ++p) a += *reinterpret_cast<const f32x4*>(parts + p * part_stride + 4 * i);
-    f32x4* dst = reinterpret_cast<f32x4*>(d_w + 4 * i);
+    f32x4* dst = reinterpret_cast<f32x4*>(out + 4 * i);
     *dst = accumulate ? a + *dst : a;
   }
 }
@@ -550,7 +554,7 @@ GemmProblem f32_dx(const VocabPlan& p, const float* G, const void* w, const int3
 }
 GemmProblem f32_dw(const VocabPlan& p, const float* G, const void* x, const int32_t* range, int d, int V, float* out) {
   GemmProblem g{};
-  g.offsets = range; g.E = 1; g.mode = 1; g.M = (int)p.ld; g.c_rows = V;
+  g.offsets = range; g.E = 1; g.mode = 1; g.M = (int)align_up((size_t)V, 64); g.c_rows = V;
   g.A = G; g.a_rs = 1; g.a_cs = p.ld;
   g.B = x; g.b_rs = d; g.b_cs = 1;
   g.C = out; g.ldc = d; g.N = d; g.K = p.R;
@@ -577,7 +581,9 @@ VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int p
   if (!grad && !f32) p.R = T < kScorePiece ? T : kScorePiece;          // nothing is kept per element
   if (f32) p.R = vocab_f32_rows(p.R, V, d);
   p.pieces = (T + p.R - 1) / p.R;
-  p.ld = (long)align_up((size_t)V, 64);
+  const long ld = (long)align_up((size_t)V, 64);
+  p.ld = f32 ? vocab_f32_panel(ld) : ld;
+  p.panels = (int)((ld + p.ld - 1) / p.ld);
   p.gather = grad || f32 || T > kScoreAsIs;
   p.twice = grad && !f32 && T <= kFewRows && p.pieces == 1;
   const size_t R = (size_t)p.R, rows = R * p.pieces, copies = p.twice ? 2 : 1;
@@ -590,8 +596,17 @@ VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int p
     p.xc = take(at, copies * R * d * es);
   }
   if (f32) {
-    p.z = plan_f32(f32_logits(p, nullptr, nullptr, nullptr, d, V, nullptr));
-    p.G = take(at, (size_t)p.z.parts * R * p.ld * 4);
+    auto products = [&](int words) {
+      VocabPlan::Products q{};
+      q.z = plan_f32(f32_logits(p, nullptr, nullptr, nullptr, d, words, nullptr));
+      if (p.panels > 1) q.z.parts = 1;                  // (the row pass knows panels or parts)
+      q.dx = plan_f32(f32_dx(p, nullptr, nullptr, nullptr, d, words, nullptr));
+      q.dw = plan_f32(f32_dw(p, nullptr, nullptr, nullptr, d, words, nullptr));
+      return q;
+    };
+    p.last = products(V - (p.panels - 1) * (int)p.ld);
+    p.whole = p.panels > 1 ? products((int)p.ld) : p.last;
+    p.G = take(at, (size_t)p.whole.z.parts * p.panels * R * p.ld * 4);
   } else {
     p.tiles = mfma_vocab_tiles(p.R, V, d, grad);
     p.stats = take(at, R * p.tiles.parts * 8);
@@ -603,10 +618,15 @@ VocabPlan vocab_plan(int T, int d, int V, moe_dtype dt, moe_dtype grad_dt, int p
     p.rest = take(at, R * 4);
     size_t part_floats;
     if (f32) {
-      p.dx = plan_f32(f32_dx(p, nullptr, nullptr, nullptr, d, V, nullptr));
-      p.dw = plan_f32(f32_dw(p, nullptr, nullptr, nullptr, d, V, nullptr));
-      p.dxc = take(at, (size_t)p.dx.parts * R * d * 4);
-      part_floats = p.dw.parts > 1 ? (size_t)p.dw.parts * p.ld * d : 0;
+      // dx's parts are added where its rows are placed, or panel by panel into the sum of those before; d_w's into d_w
+      p.dxc = take(at, (size_t)(p.panels > 1 ? 1 : p.last.dx.parts) * R * d * 4);
+      part_floats = 0;
+      for (const VocabPlan::Products* q : {&p.whole, &p.last}) {
+        const size_t words = q == &p.last ? (size_t)V - (p.panels - 1) * p.ld : (size_t)p.ld;
+        const size_t dx_floats = p.panels > 1 && q->dx.parts > 1 ? (size_t)q->dx.parts * R * d : 0;
+        const size_t dw_floats = q->dw.parts > 1 ? (size_t)q->dw.parts * align_up(words, 64) * d : 0;
+        part_floats = std::max({part_floats, dx_floats, dw_floats});
+      }
     } else {
       const size_t dx_floats = mfma_vocab_dx_plan(p.R, V, d).part_floats, dw_floats = mfma_vocab_dw_part_floats(p.twice ? 2 * p.R : p.R, V, d);
       p.dxc = take(at, R * d * 4);
@@ -661,35 +681,68 @@ int score_rows(const VocabProblem& q, const VocabPlan& p, const float* stats, co
 int f32_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, const RowOut& o, hipStream_t s) {
   const int R = p.R, d = q.d, V = q.V;
   float* Z = reinterpret_cast<float*>(ws + p.G);
+  float* parts = reinterpret_cast<float*>(ws + p.parts);
+  const float* w = static_cast<const float*>(q.w);
   const void* xc = ws + p.xc;
-  int rc = launch_f32(f32_logits(p, xc, q.w, o.range, d, V, Z), p.z, s);
-  if (rc != MOE_OK) return rc;
-  if (!q.grad) {
-    if (R <= kFewGroups) vocab_rows_f32_kernel<false, 1024><<<dim3(R), dim3(1024), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
-    else vocab_rows_f32_kernel<false, 256><<<dim3(R), dim3(256), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
+  const long panel_floats = (long)R * p.ld;
+  // f(words of the panel, its first word, its logits, its products)
+  auto each_panel = [&](auto f) {
+    for (int i = 0; i < p.panels; ++i) {
+      const bool last = i + 1 == p.panels;
+      const long v0 = i * p.ld;
+      const int rc = f(last ? V - (int)v0 : (int)p.ld, v0, Z + i * panel_floats, last ? p.last : p.whole);
+      if (rc != MOE_OK) return rc;
+    }
+    return (int)MOE_OK;
+  };
+  auto add = [&](int n, long stride, long floats, int accumulate, float* out) {
+    vocab_add_f32_kernel<<<dim3(blocks_for(floats / 4)), dim3(256), 0, s>>>(parts, n, stride, floats / 4, accumulate, out);
     MOE_LAUNCH_CHECK();
-    return MOE_OK;
-  }
-  if (R <= kFewGroups) vocab_rows_f32_kernel<true, 1024><<<dim3(R), dim3(1024), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
-  else vocab_rows_f32_kernel<true, 256><<<dim3(R), dim3(256), 0, s>>>(Z, p.z.parts, (long)R * p.ld, V, p.ld, o);
+    return (int)MOE_OK;
+  };
+  int rc = each_panel([&](int words, long v0, float* z, const VocabPlan::Products& plan) {
+    return launch_f32(f32_logits(p, xc, w + v0 * d, o.range, d, words, z), plan.z, s);
+  });
+  if (rc != MOE_OK) return rc;
+  const int n_parts = p.last.z.parts;
+  auto rows = [&](auto grad, auto threads, auto panels) {
+    constexpr int N = decltype(threads)::value;
+    vocab_rows_f32_kernel<decltype(grad)::value, N, decltype(panels)::value><<<dim3(R), dim3(N), 0, s>>>(Z, n_parts, panel_floats, V, p.ld, o);
+  };
+  auto rows_in = [&](auto grad, auto panels) {
+    if (R <= kFewGroups) rows(grad, std::integral_constant<int, 1024>(), panels);
+    else rows(grad, std::integral_constant<int, 256>(), panels);
+  };
+  if (q.grad && p.panels > 1) rows_in(std::true_type(), std::true_type());
+  else if (q.grad) rows_in(std::true_type(), std::false_type());
+  else if (p.panels > 1) rows_in(std::false_type(), std::true_type());
+  else rows_in(std::false_type(), std::false_type());
   MOE_LAUNCH_CHECK();
+  if (!q.grad) return MOE_OK;
   float* dxc = reinterpret_cast<float*>(ws + p.dxc);
-  rc = launch_f32(f32_dx(p, Z, q.w, o.range, d, V, dxc), p.dx, s);
+  rc = each_panel([&](int words, long v0, float* g, const VocabPlan::Products& plan) {
+    if (p.panels == 1) return launch_f32(f32_dx(p, g, w, o.range, d, words, dxc), plan.dx, s);
+    const int accumulate = v0 > 0, cut = plan.dx.parts > 1;
+    GemmProblem product = f32_dx(p, g, w + v0 * d, o.range, d, words, cut ? parts : dxc);
+    product.accumulate = cut ? 0 : accumulate;
+    const int made = launch_f32(product, plan.dx, s);
+    return made != MOE_OK || !cut ? made : add(plan.dx.parts, (long)R * d, (long)R * d, accumulate, dxc);
+  });
   if (rc != MOE_OK) return rc;
   const bool last = piece + 1 == p.pieces;
-  vocab_dx_f32_kernel<<<dim3(blocks_for((long)R * d / 4) + last), dim3(256), 0, s>>>(dxc, p.dx.parts, (long)R * d, d, o, static_cast<float*>(q.dx),
-                                                                                    reinterpret_cast<float*>(ws + p.weighted), last ? q.total : nullptr);
+  vocab_dx_f32_kernel<<<dim3(blocks_for((long)R * d / 4) + last), dim3(256), 0, s>>>(dxc, p.panels > 1 ? 1 : p.last.dx.parts, (long)R * d, d, o,
+                                                                                    static_cast<float*>(q.dx), reinterpret_cast<float*>(ws + p.weighted),
+                                                                                    last ? q.total : nullptr);
   MOE_LAUNCH_CHECK();
   const int accumulate = q.accumulate || piece > 0;
-  float* dw_parts = reinterpret_cast<float*>(ws + p.parts);
-  GemmProblem g = f32_dw(p, Z, xc, o.range, d, V, p.dw.parts > 1 ? dw_parts : static_cast<float*>(q.d_w));
-  g.accumulate = p.dw.parts > 1 ? 0 : accumulate;
-  rc = launch_f32(g, p.dw, s);
-  if (rc != MOE_OK || p.dw.parts == 1) return rc;
-  const long vecs = (long)V * d / 4;
-  vocab_dw_f32_kernel<<<dim3(blocks_for(vecs)), dim3(256), 0, s>>>(dw_parts, p.dw.parts, p.ld * d, vecs, accumulate, static_cast<float*>(q.d_w));
-  MOE_LAUNCH_CHECK();
-  return MOE_OK;
+  return each_panel([&](int words, long v0, float* g, const VocabPlan::Products& plan) {
+    float* d_w = static_cast<float*>(q.d_w) + v0 * d;
+    const int cut = plan.dw.parts > 1;
+    GemmProblem product = f32_dw(p, g, xc, o.range, d, words, cut ? parts : d_w);
+    product.accumulate = cut ? 0 : accumulate;
+    const int made = launch_f32(product, plan.dw, s);
+    return made != MOE_OK || !cut ? made : add(plan.dw.parts, (long)product.M * d, (long)words * d, accumulate, d_w);
+  });
 }
 
 int bf16_piece(const VocabProblem& q, const VocabPlan& p, char* ws, int piece, const RowOut& o, hipStream_t s) {

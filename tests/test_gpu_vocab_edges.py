@@ -160,3 +160,38 @@ def test_most_rows():
     op.loss.fill_(-1.0)
     loss, _ = op.score(x, w, target.to(torch.int32))
     assert torch.equal(loss, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,V,piece", [(70, 32, 2 ** 20 + 77, 0), (20000, 32, 120_000, 0), (300, 16, 2 ** 21, 100)])
+def test_large_in_fp32(T, d, V, piece):
+    """fp32: rows of 2^20 logits and more, which the split products leave to the fp32 instruction, and more than 2^31 logits in one piece.  Reference in 64
+    bits on the GPU, some rows at a time.  As in the tests of smaller sizes 2^-16, and 2^-24 per step of a random walk of V (dx) or T (d_w) terms."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    w = torch.randn((V, d), device=DEV, generator=g) * (1.28 / math.sqrt(d))
+    target = torch.randint(0, V, (T,), device=DEV, generator=g)
+    target[0], target[1] = V - 1, 0
+    x = torch.randn((T, d), device=DEV, generator=g) + 5.0 * w[target]
+    from paper_2505_11432_amd.head import VocabLoss
+    op = VocabLoss(T, d, V, dtype=torch.float32, piece_bytes=1 << 40)
+    if piece:
+        op.piece_rows = piece                       # (fewer rows than the workspace is for)
+    op.step(x, w, target.to(torch.int32))
+    wd, d_w, total = w.double(), torch.zeros((V, d), dtype=torch.float64, device=DEV), 0.0
+    step = max(1, 2 ** 28 // V)
+    for a in range(0, T, step):
+        xd, tg = x[a:a + step].double(), target[a:a + step]
+        p = xd @ wd.t()
+        lse = torch.logsumexp(p, 1)
+        loss = lse - p.gather(1, tg[:, None])[:, 0]
+        tol = 2.0 ** -16 * float(lse.abs().max())
+        assert float((op.loss[a:a + step].double() - loss).abs().max()) <= tol and float((op.lse[a:a + step].double() - lse).abs().max()) <= tol
+        p = torch.exp(p - lse[:, None])
+        p.scatter_add_(1, tg[:, None], torch.full_like(lse, -1.0)[:, None])
+        p /= T
+        dx = p @ wd
+        assert float((op.dx[a:a + step].double() - dx).norm()) <= max(2.0 ** -16, 2.0 ** -24 * math.sqrt(V)) * float(dx.norm())
+        d_w += p.t() @ xd
+        total += float(loss.sum()) / T
+    assert abs(float(op.total) - total) <= 2.0 ** -16 * total
+    assert float((op.d_w.double() - d_w).norm()) <= max(2.0 ** -16, 2.0 ** -24 * math.sqrt(T)) * float(d_w.norm())
