@@ -54,6 +54,13 @@ def label(name: str) -> str:
             return (f"grouped_gemm<{bm}x{bn}x{bk} s{ns} w{wm}x{wn} {_LAYOUT.get((la, lb), '??')} {_MODE.get(mode, '?')} "
                     f"{_EPI.get(epi, '?')} out={'f32' if out_f32 else 'bf16'} in={'e4m3' if in_fp8 else 'bf16'}>")
         return "grouped_gemm<?> " + tail[:80]
+    if name.startswith("_ZN"):                                                # nested name: lengths in front of its parts
+        at, parts = 3, []
+        while (m := re.match(r"\d+", name[at:])):
+            at += m.end() + int(m.group())
+            parts.append(name[at - int(m.group()):at])
+        if parts and parts[-1].endswith("_kernel"):
+            return parts[-1]
     m = re.search(r"([a-z][a-z0-9_]*_kernel)", name)
     if m:
         return m.group(1)
