@@ -403,6 +403,8 @@ int moe_quant_fp8_tgroup(const void* src, moe_dtype src_dt, int rows, int cols,
  * to.  No token that counts: total 0, gradients 0.  T = 0: nothing is enqueued and no output is
  * written, total and d_w neither (a caller that has no tokens keeps or clears them itself).  dx and
  * d_w share no memory with x, w or each other.  Results do not depend on what ran before.
+ * bf16 data: G is rounded to bf16 for the matrix cores, so dx and d_w, one in fp32 as well, carry up
+ * to 2^-8 of its elements.
  * G = c (softmax(z) - onehot) is kept for piece_rows rows at a time (0: all), V elements of the
  * data's type each (fp32 data: also the logits, in the same place, and in the score as well).
  * More pieces cost launches and passes over d_w.  A power of two of at least 2048 rows, or all
