@@ -170,7 +170,9 @@ PyObject* lists_apart(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     for (int k = 0; ok && k < 2; ++k)
       for (Py_ssize_t i = 0; ok && i < PySequence_Fast_GET_SIZE(seq[k]); ++i) {
         PyObject* bytes[3];
-        ok = PyArg_ParseTuple(PySequence_Fast_GET_ITEM(seq[k], i), "SSS", &bytes[0], &bytes[1], &bytes[2]) != 0;
+        PyObject* list = PySequence_Fast_GET_ITEM(seq[k], i);
+        if (!PyTuple_Check(list)) PyErr_SetString(PyExc_TypeError, "a list is what tensor_list gives");
+        ok = PyTuple_Check(list) && PyArg_ParseTuple(list, "SSS", &bytes[0], &bytes[1], &bytes[2]);
         if (!ok) break;
         const Py_ssize_t n = PyBytes_GET_SIZE(bytes[2]) / 4;
         if (PyBytes_GET_SIZE(bytes[0]) != n * 8 || PyBytes_GET_SIZE(bytes[1]) != n * 8) {

@@ -41,9 +41,12 @@ def test_in_place():
 
 
 def test_refused_calls():
-    for bad in (([], []), ([], [], True, 1), (None, [], True), ([b"x"], [], True), ([(b"1", b"2", b"3")], [], True), ([(b"", b"", 3)], [], True)):
-        with pytest.raises((TypeError, ValueError, SystemError)):
-            apart(*bad) if len(bad) == 3 else __import__("paper_2505_11432_amd.binding", fromlist=["_native"])._native.lists_apart(*bad)
+    from paper_2505_11432_amd import binding as B
+    for bad in (([], []), ([], [], True, 1), (None, [], True), ([], 3, True), ([b"x"], [], True), ([(b"", b"", 3)], [], True), ([(b"", b"")], [], True)):
+        with pytest.raises(TypeError):
+            B._native.lists_apart(*bad)
+    with pytest.raises(ValueError, match="one length"):
+        B._native.lists_apart([(b"12345678", b"", b"")], [], True)
 
 
 @pytest.mark.gpu
