@@ -167,7 +167,7 @@ def _matrix_inputs(c, seed):
     grad = torch.randn(shape, device=DEV, generator=g).mul_(1e-4).add_(m, alpha=0.1).to(_dtype(c["dtype"]))
     if c["kind"] == "orth":
         return (m.to(_dtype(c["dtype"])),)
-    p = torch.randn(shape, device=DEV, generator=g).mul_(cols ** -0.5)
+    p = torch.randn(shape, device=DEV, generator=g).mul_(0.02)              # (the layers' w_std)
     return p, grad, m
 
 
