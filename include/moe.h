@@ -467,6 +467,81 @@ int moe_adamw(const void* table /*device*/, int n, int64_t total, moe_dtype grad
               const float* lr, int32_t* step, const float* coef, double beta1, double beta2,
               double eps, double weight_decay, void* workspace, size_t ws_bytes, void* stream);
 
+/* ---- around the layer: embedding, norms --------------------------------------------------------
+ * (Section 2.1's transformer block around the MoE layer; Section 4.1 names the norms, the paper gives no formula.)
+ *
+ * Embedding: out[t,:] = scale * table[tokens[t],:], rounded once; a token outside 0..V-1 (padding)
+ * gives a row of zeros.  table [V,d] and out [T,d] in `dt` (MOE_F32 or MOE_BF16); d a multiple of 16.
+ * out shares no memory with table.  T = 0: nothing is enqueued.
+ * moe_embedding_bwd: d_table[v,:] = scale * sum of dy[t,:] over the tokens t that are v, summed in fp32
+ * in an order that only the tokens and the sizes decide (reproducible), rounded once to grad_dt
+ * (MOE_F32, or MOE_BF16 for bf16 data); rows without a token get zeros.  accumulate=1: added to what
+ * is there (a matrix shared with the vocabulary loss, a micro-batch after the first), rows without a
+ * token are not touched.  T = 0 is an empty batch: zeros, or nothing with accumulate=1.  d_table shares
+ * no memory with dy.  Workspace: moe_embedding_workspace_bytes (0 on invalid sizes). */
+size_t moe_embedding_workspace_bytes(int T, int d, int V);
+int moe_embedding_fwd(const void* table, const int32_t* tokens /*[T]*/, moe_dtype dt, int T, int d,
+                      int V, double scale, void* out, void* stream);
+int moe_embedding_bwd(const int32_t* tokens, const void* dy /*[T,d]*/, moe_dtype dt, int T, int d,
+                      int V, double scale, void* d_table /*[V,d]*/, moe_dtype grad_dt, int accumulate,
+                      void* workspace, size_t ws_bytes, void* stream);
+
+/* Norms around a block F on the residual stream, h = norm(x) w_before in front of it and
+ * alpha x + gate norm(F(h)) w_after behind it: one call ends a block and starts the next.
+ *   rms(v) = sqrt(mean of v^2 over the row + eps),  n = y / rms(y) * w_after  (y where w_after is NULL)
+ *   out = alpha x + gate[t / gate_rows,:] * n  (alpha x + n where gate is NULL), rounded to dt
+ *   h = out / rms(out) * w_before  of the rounded out, rounded to dt  (none where w_before is NULL)
+ * x, y, out, h [T,d] in `dt` (MOE_F32 or MOE_BF16), w_after, w_before [d] and gate
+ * [ceil(T/gate_rows),d] fp32: gate_rows = T (or more) one vector, 1 a row per token, a sequence's length
+ * a row per sequence.  y = NULL: no block ends here (the first one starts): out = x is not written and
+ * h is made from x; w_after, gate and out are NULL then and alpha is 1.  d is a multiple of 16, at most
+ * MOE_NORM_MAX_WIDTH.  out may be x or y; else outputs share no memory with inputs or each other.
+ * T = 0: nothing is enqueued.
+ *
+ * moe_block_norm_bwd: all gradients, from `out` as the forward pass wrote it (x where y is NULL), d_out,
+ * the gradient that comes down the stream (NULL: none), and d_h (with w_before, not without).  dx, dy
+ * [T,d] in dt; d_w_after, d_w_before [d] and d_gate [ceil(T/gate_rows),d] fp32, summed in a fixed order,
+ * written or with accumulate=1 added to.  Where there is no y: no dy, d_w_after, d_gate.  y is read only
+ * where w_after or gate is given.  d_w_after, d_gate and d_w_before are given where their parameter is.  dx may be
+ * d_out or d_h, dy may be y or the other of d_out and d_h; else outputs share no memory with inputs or each other.  T = 0: nothing is
+ * enqueued and nothing written.  Workspace: moe_block_norm_workspace_bytes (after, gate, before: whether there is one). */
+#define MOE_NORM_MAX_WIDTH 16384
+int moe_block_norm_fwd(const void* x, const void* y, const float* w_after, const float* gate,
+                       const float* w_before, moe_dtype dt, int T, int d, int gate_rows, double alpha,
+                       double eps, void* out, void* h, void* stream);
+size_t moe_block_norm_workspace_bytes(int T, int d, moe_dtype dt, int after, int gate, int before);
+int moe_block_norm_bwd(const void* out, const void* y, const float* w_after, const float* gate,
+                       const float* w_before, const void* d_out, const void* d_h, moe_dtype dt, int T,
+                       int d, int gate_rows, double alpha, double eps, void* dx, void* dy,
+                       float* d_w_after, float* d_gate, float* d_w_before, int accumulate,
+                       void* workspace, size_t ws_bytes, void* stream);
+
+/* Orthogonalised updates (Muon) for a batch of matrices [rows,cols], one after another in memory:
+ * O(u) = the matrix that `steps` Newton-Schulz steps X <- a X + b (X X^T) X + c (X X^T)^2 X make from
+ * X = u / |u|_F (2-norm of all elements; a matrix of zeros stays one).  coefficients: steps rows (a, b, c) in HOST memory, read
+ * before the call returns; NULL: (3.4445, -4.7750, 2.0315) in every step.  Coefficients with which some
+ * product on the way may pass 15.5 are refused (MOE_ERR_UNSUPPORTED): operands are 16-bit numbers with
+ * fp32 accumulation, X carries 22 bits from step to step; relative error (2-norm) about 2e-3.
+ * moe_orthogonalize: out = O(x); x in dt, out in out_dt (MOE_F32 or MOE_BF16 each); out may be x.
+ * moe_muon, in place, with f = coef[0] (coef NULL: 1):
+ *   m = momentum m + f grad,  u = f grad + momentum m  (nesterov=0: u = m),
+ *   p = p (1 - lr weight_decay) - lr scale O(u)
+ * p and m fp32, grad in grad_dt, the new p rounded to bf16 into weights (NULL: none).  lr and coef are read on the
+ * device.  Where coef[0] is NaN the call changes nothing.  An infinite or NaN gradient spoils its matrix.
+ * Pointers are aligned to their elements, no more; what is written shares no memory with another argument.
+ * piece matrices are taken at a time (0: all of them, 32768 at most), which bounds the workspace:
+ * moe_orthogonal_workspace_bytes with the same sizes (0 on invalid sizes).  batch = 0: nothing is enqueued. */
+#define MOE_ORTH_MAX_STEPS 16
+#define MOE_ORTH_MAX_SIDE (1 << 20)
+size_t moe_orthogonal_workspace_bytes(int batch, int rows, int cols, int piece);
+int moe_orthogonalize(const void* x, moe_dtype dt, int batch, int rows, int cols, int steps,
+                      const double* coefficients, int piece, void* out, moe_dtype out_dt,
+                      void* workspace, size_t ws_bytes, void* stream);
+int moe_muon(float* p, const void* grad, moe_dtype grad_dt, float* m, void* weights, int batch,
+             int rows, int cols, const float* lr, const float* coef, double momentum, int nesterov,
+             double weight_decay, double scale, int steps, const double* coefficients, int piece,
+             void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import c_char_p, c_int, c_size_t, c_void_p
 
 import torch
@@ -33,6 +34,9 @@ EXPORTS = (
     "moe_vocab_workspace_bytes", "moe_vocab_score", "moe_vocab_loss",
     "moe_grad_clip_table_bytes", "moe_grad_clip_table", "moe_grad_clip_workspace_bytes", "moe_grad_clip",
     "moe_adamw_table_bytes", "moe_adamw_table", "moe_adamw_table_mixed", "moe_adamw",
+    "moe_embedding_workspace_bytes", "moe_embedding_fwd", "moe_embedding_bwd",
+    "moe_block_norm_fwd", "moe_block_norm_workspace_bytes", "moe_block_norm_bwd",
+    "moe_orthogonal_workspace_bytes", "moe_orthogonalize", "moe_muon",
 )
 
 
@@ -90,6 +94,9 @@ def _load() -> ctypes.CDLL:
         "moe_adamw_table_bytes": (Z, [I]),
         "moe_adamw_table": (I, [I, P, P, P, P, P, P, I, P]),
         "moe_adamw_table_mixed": (I, [I, P, P, P, P, P, P, P, P]),
+        "moe_embedding_workspace_bytes": (Z, [I, I, I]),
+        "moe_block_norm_workspace_bytes": (Z, [I, I, I, I, I, I]),
+        "moe_orthogonal_workspace_bytes": (Z, [I, I, I, I]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -446,3 +453,94 @@ def moe_adamw_table(params, grads, m, v, weights=None):
 def moe_adamw(table, n, total, grad_dt, lr, step, coef, beta1, beta2, eps, weight_decay, workspace):
     _check("moe_adamw", _native.moe_adamw(table, n, total, grad_dt, lr, step, coef, beta1, beta2, eps, weight_decay,
                                           workspace, workspace.numel() * workspace.element_size()))
+
+
+# ---- around the layer: embedding, norms, orthogonalised updates --------------------------------------------------------
+NORM_MAX_WIDTH, ORTH_MAX_STEPS = 16384, 16
+COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5            # of the quintic Newton-Schulz steps
+
+
+def _embedding_shapes(matrix, tokens, rows):
+    V, d = matrix.shape
+    T, = tokens.shape
+    assert tokens.dtype == torch.int32, "tokens [T] int32"
+    assert tuple(rows.shape) == (T, d), "a row of the matrix's width for each token"
+    return T, d, V
+
+
+def moe_embedding_workspace_bytes(T, d, V) -> int:
+    return _lib.moe_embedding_workspace_bytes(T, d, V)
+
+
+def moe_embedding_fwd(table, tokens, scale, out):
+    T, d, V = _embedding_shapes(table, tokens, out)
+    assert out.dtype == table.dtype, "out like table"
+    _check("moe_embedding_fwd", _native.moe_embedding_fwd(table, tokens, dtype_code(table.dtype), T, d, V, scale, out))
+
+
+def moe_embedding_bwd(tokens, dy, scale, d_table, accumulate, workspace):
+    T, d, V = _embedding_shapes(d_table, tokens, dy)
+    _check("moe_embedding_bwd", _native.moe_embedding_bwd(
+        tokens, dy, dtype_code(dy.dtype), T, d, V, scale, d_table, dtype_code(d_table.dtype), int(accumulate), workspace,
+        workspace.numel() * workspace.element_size()))
+
+
+def _norm_shapes(x, rows, vectors, gates, gate_rows):
+    T, d = x.shape
+    for t in rows:
+        assert t is None or (t.shape == x.shape and t.dtype == x.dtype), "rows [T, d] of one type"
+    for t in vectors:
+        assert t is None or (tuple(t.shape) == (d,) and t.dtype == torch.float32), "weights [d] fp32"
+    for t in gates:
+        assert t is None or (gate_rows > 0 and tuple(t.shape) == (-(-T // gate_rows), d) and t.dtype == torch.float32), \
+            "gate [ceil(T / gate_rows), d] fp32"
+    return T, d
+
+
+def moe_block_norm_fwd(x, y, w_after, gate, w_before, gate_rows, alpha, eps, out, h):
+    T, d = _norm_shapes(x, (y, out, h), (w_after, w_before), (gate,), gate_rows)
+    _check("moe_block_norm_fwd", _native.moe_block_norm_fwd(
+        x, y, w_after, gate, w_before, dtype_code(x.dtype), T, d, gate_rows, alpha, eps, out, h))
+
+
+def moe_block_norm_workspace_bytes(T, d, dt, after, gate, before) -> int:
+    return _lib.moe_block_norm_workspace_bytes(T, d, dt, int(after), int(gate), int(before))
+
+
+def moe_block_norm_bwd(out, y, w_after, gate, w_before, d_out, d_h, gate_rows, alpha, eps, dx, dy, d_w_after, d_gate, d_w_before,
+                       accumulate, workspace):
+    T, d = _norm_shapes(dx, (out, y, d_out, d_h, dy), (w_after, w_before, d_w_after, d_w_before), (gate, d_gate), gate_rows)
+    _check("moe_block_norm_bwd", _native.moe_block_norm_bwd(
+        out, y, w_after, gate, w_before, d_out, d_h, dtype_code(dx.dtype), T, d, gate_rows, alpha, eps, dx, dy, d_w_after, d_gate,
+        d_w_before, int(accumulate), workspace, workspace.numel() * workspace.element_size()))
+
+
+def _coefficients(c):
+    """(number of steps, the bytes of their doubles)."""
+    rows = [tuple(float(v) for v in row) for row in c]
+    assert 1 <= len(rows) <= ORTH_MAX_STEPS and all(len(r) == 3 for r in rows), "1 to 16 rows of three coefficients"
+    return len(rows), struct.pack(f"{3 * len(rows)}d", *(v for r in rows for v in r))
+
+
+def moe_orthogonal_workspace_bytes(batch, rows, cols, piece=0) -> int:
+    return _lib.moe_orthogonal_workspace_bytes(batch, rows, cols, piece)
+
+
+def moe_orthogonalize(x, out, workspace, coefficients=COEFFICIENTS, piece=0):
+    batch, rows, cols = x.shape
+    assert out.shape == x.shape, "out like x"
+    steps, packed = coefficients if isinstance(coefficients[-1], bytes) else _coefficients(coefficients)
+    _check("moe_orthogonalize", _native.moe_orthogonalize(
+        x, dtype_code(x.dtype), batch, rows, cols, steps, packed, piece, out, dtype_code(out.dtype), workspace,
+        workspace.numel() * workspace.element_size()))
+
+
+def moe_muon(p, grad, m, weights, lr, coef, momentum, nesterov, weight_decay, scale, workspace, coefficients=COEFFICIENTS, piece=0):
+    batch, rows, cols = p.shape
+    assert p.dtype == m.dtype == torch.float32 and m.shape == p.shape, "parameters and momentum are fp32, of one size"
+    assert grad.shape == p.shape, "gradients have their parameters' sizes"
+    assert weights is None or (weights.shape == p.shape and weights.dtype == torch.bfloat16), "weights are bf16, of their parameters' sizes"
+    steps, packed = coefficients if isinstance(coefficients[-1], bytes) else _coefficients(coefficients)
+    _check("moe_muon", _native.moe_muon(
+        p, grad, dtype_code(grad.dtype), m, weights, batch, rows, cols, lr, coef, momentum, int(nesterov), weight_decay, scale, steps,
+        packed, piece, workspace, workspace.numel() * workspace.element_size()))

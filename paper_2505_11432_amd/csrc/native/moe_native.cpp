@@ -53,7 +53,14 @@ bool to_pointer(PyObject* o, void** out) {
 }
 
 template <typename A> bool convert(PyObject* o, A* out) {
-  if constexpr (std::is_pointer_v<A>) {
+  if constexpr (std::is_same_v<A, const double*>) {   // host memory (the coefficients of a call): a bytes object, or None
+    if (o != Py_None && (!PyBytes_Check(o) || PyBytes_GET_SIZE(o) % sizeof(double) != 0)) {
+      PyErr_SetString(PyExc_TypeError, "coefficients are a bytes object of doubles");
+      return false;
+    }
+    *out = o == Py_None ? nullptr : reinterpret_cast<const double*>(PyBytes_AS_STRING(o));
+    return true;
+  } else if constexpr (std::is_pointer_v<A>) {
     void* p = nullptr;
     if (!to_pointer(o, &p)) return false;
     *out = static_cast<A>(p);
@@ -218,6 +225,8 @@ PyMethodDef methods[] = {
     MOE_BOUND(moe_expert_ffn_fwd), MOE_BOUND(moe_expert_ffn_bwd), MOE_BOUND(moe_row_map), MOE_BOUND(moe_expert_ffn_fused_fwd),
     MOE_BOUND(moe_expert_ffn_fused_bwd), MOE_BOUND(moe_quant_fp8), MOE_BOUND(moe_dequant_fp8), MOE_BOUND(moe_quant_fp8_tgroup),
     MOE_BOUND(moe_transpose), MOE_BOUND(moe_vocab_score), MOE_BOUND(moe_vocab_loss), MOE_BOUND(moe_grad_clip), MOE_BOUND(moe_adamw),
+    MOE_BOUND(moe_embedding_fwd), MOE_BOUND(moe_embedding_bwd), MOE_BOUND(moe_block_norm_fwd), MOE_BOUND(moe_block_norm_bwd),
+    MOE_BOUND(moe_orthogonalize), MOE_BOUND(moe_muon),
     {"tensor_list", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&tensor_list)), METH_FASTCALL, nullptr},
     {"lists_apart", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&lists_apart)), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 

@@ -1,0 +1,34 @@
+// What the entry points (api_muon.hip) and the kernels (newton_schulz.hip) of orthogonalised updates share.
+#pragma once
+#include "moe_common.h"
+
+namespace moe {
+
+constexpr int kOrthPad = 128;                // rows and columns of a matrix in the workspace are multiples of this
+constexpr int kNormBlocks = 64;              // sums of squares per matrix, at most
+struct OrthCoef { double a, b, c; };
+
+struct MuonProblem {
+  const void* u; moe_dtype u_dt;             // matrices to orthogonalise; Muon: their gradients
+  int batch, rows, cols, piece;              // piece: matrices at a time
+  OrthCoef coef[MOE_ORTH_MAX_STEPS]; int steps;
+  void* out; moe_dtype out_dt;               // orthogonalised matrices, or NULL: Muon
+  float* p; float* m; void* w;
+  const float* lr; const float* factor;
+  float momentum, scale; bool nesterov;
+  double decay;
+};
+struct OrthPlan {
+  int R, C, S;                               // padded rows, columns, and the smaller of them
+  int count;                                 // matrices at a time
+  int norm_blocks;
+  size_t hi, lo, t, other, gram, sums;       // offsets of a piece's buffers
+  size_t gram_one;                           // bytes of one list of Gram matrices
+  size_t bytes;
+};
+bool orth_takes(int batch, int rows, int cols, int piece);
+OrthPlan orth_plan(int batch, int rows, int cols, int piece);
+bool orth_coefficients_ok(const OrthCoef* c, int steps);        // every matrix that is kept fits 16 bits
+int launch_orth(const MuonProblem& q, const OrthPlan& p, char* ws, hipStream_t s);
+
+}  // namespace moe
