@@ -23,9 +23,10 @@ typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 // eight elements as floats, from and to memory that is 16-byte aligned
 __device__ __forceinline__ f32x8 load8(const float* p) { return *reinterpret_cast<const f32x8 __attribute__((aligned(16)))*>(p); }
 __device__ __forceinline__ f32x8 load8(const bf16* p) { return __builtin_convertvector(*reinterpret_cast<const bf16x8*>(p), f32x8); }
+// (eight fp32 lie in two stores that fill a line together: they are left to the L2)
 __device__ __forceinline__ void store8(float* p, f32x8 v) {
-  __builtin_nontemporal_store(__builtin_shufflevector(v, v, 0, 1, 2, 3), reinterpret_cast<f32x4*>(p));
-  __builtin_nontemporal_store(__builtin_shufflevector(v, v, 4, 5, 6, 7), reinterpret_cast<f32x4*>(p) + 1);
+  *reinterpret_cast<f32x4*>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+  *(reinterpret_cast<f32x4*>(p) + 1) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
 }
 __device__ __forceinline__ void store8(bf16* p, f32x8 v) { __builtin_nontemporal_store(__builtin_convertvector(v, bf16x8), reinterpret_cast<bf16x8*>(p)); }
 
@@ -248,6 +249,12 @@ template <typename TG> __device__ __forceinline__ void write_sum(TG* p, f32x8 su
   store8(p, sum);
 }
 
+// zeros past the caches, by 256 threads
+template <typename TG> __device__ __forceinline__ void zero_row(TG* row, int d) {
+  constexpr int N = 16 / sizeof(TG);
+  for (int c = threadIdx.x * N; c < d; c += 256 * N) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>(row + c));
+}
+
 template <typename T, typename TG>
 __global__ void __launch_bounds__(256) sum_kernel(const uint2* __restrict__ pairs, const T* __restrict__ dy, int n, int d, int V, float scale, TG* __restrict__ d_table,
                                                   int accumulate, int chunk, int chunks, int slabs, int sum_groups, float* __restrict__ parts) {
@@ -268,7 +275,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const uint2* __restrict__ pair
     __syncthreads();
     for (int r = 0; r < rows; ++r)
       if (empty >> r & 1)
-        for (int c = threadIdx.x * 8; c < d; c += 256 * 8) store8(d_table + (long)(row0 + r) * d + c, f32x8{});
+        zero_row(d_table + (long)(row0 + r) * d, d);
     return;
   }
   const long task = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
@@ -276,6 +283,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const uint2* __restrict__ pair
   if (c >= chunks) return;
   const int first = c * chunk, count = min(chunk, n - first), col = slab * kSlab + lane * 8;
   const bool live = col < d;
+  if (pairs[first].x >= (unsigned)V) return;                             // padding, to the end
   // (lanes past the width go along with the last columns and write nothing)
   const T* src = dy + min(col, d - 8);
   const uint2 mine = pairs[first + min(lane, count - 1)];

@@ -5,7 +5,7 @@
 namespace moe {
 
 constexpr int kOrthPad = 128;                // rows and columns of a matrix in the workspace are multiples of this
-constexpr int kNormBlocks = 64;              // sums of squares per matrix, at most
+constexpr int kNormBlocks = 1024;             // sums of squares per matrix, at most
 struct OrthCoef { double a, b, c; };
 
 struct MuonProblem {

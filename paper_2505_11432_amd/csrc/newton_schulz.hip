@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(256) norm_kernel(MuonProblem q, int first, dou
     for (int c = 0; c < 4; ++c) s = fma((double)v[c], (double)v[c], s);
   }
   s = block_sum(s, lds);
-  if (threadIdx.x == 0) sums[(long)blockIdx.y * kNormBlocks + blockIdx.x] = s;
+  if (threadIdx.x == 0) sums[(long)blockIdx.y * gridDim.x + blockIdx.x] = s;
 }
 
 // X = u / |u| in both orientations, 64 x 64 elements per workgroup; padding is zeros.
@@ -111,8 +111,10 @@ __global__ void __launch_bounds__(256) start_kernel(MuonProblem q, OrthPlan p, i
   const TG* g = static_cast<const TG*>(q.u) + base;
   const float* m = MUON ? q.m + base : nullptr;
   const float factor = MUON ? factor_of(q.factor) : 1.0f;
+  __shared__ double lds[4];
   double sum = 0;
-  for (int i = 0; i < p.norm_blocks; ++i) sum += sums[(long)blockIdx.z * kNormBlocks + i];
+  for (int i = threadIdx.x; i < p.norm_blocks; i += 256) sum += sums[(long)blockIdx.z * p.norm_blocks + i];
+  sum = block_sum(sum, lds);
   const double scale = sum > 0 ? (double)kScale / sqrt(sum) : sum;      // (no number stays none)
   const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
 #pragma unroll
@@ -380,8 +382,10 @@ OrthPlan orth_plan(int batch, int rows, int cols, int piece) {
   p.C = (int)align_up(cols, kOrthPad);
   p.S = p.R < p.C ? p.R : p.C;
   const long size = (long)rows * cols;
-  long blocks = (size + 4095) / 4096, share = 2048 / count + 1;
-  p.norm_blocks = (int)(blocks < 1 ? 1 : blocks < kNormBlocks ? (blocks < share ? blocks : share) : (share < kNormBlocks ? share : kNormBlocks));
+  long blocks = (size + 4095) / 4096;
+  const long share = 4096 / count + 1;
+  if (blocks > share) blocks = share;
+  p.norm_blocks = (int)(blocks < kNormBlocks ? blocks : kNormBlocks);
   const size_t x = (size_t)count * p.R * p.C * 2;
   p.gram_one = (size_t)count * p.S * p.S * 2;
   p.hi = 0;
@@ -390,7 +394,7 @@ OrthPlan orth_plan(int batch, int rows, int cols, int piece) {
   p.other = 3 * x;
   p.gram = 4 * x;
   p.sums = p.gram + 2 * p.gram_one;
-  p.bytes = p.sums + (size_t)count * kNormBlocks * 8 + 256;
+  p.bytes = p.sums + (size_t)count * p.norm_blocks * 8 + 256;
   return p;
 }
 

@@ -292,44 +292,50 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_bwd_kernel(NormProblem
     }
 }
 
-// Sums over the teams: 64 columns and one list (a weight, or a row of the gate that several teams share) per workgroup.
-__global__ void __launch_bounds__(1024) norm_join_kernel(NormProblem q, int teams, int rows, const float* __restrict__ parts) {
-  __shared__ float lds[16][64];
+// Sums over the teams: 64 columns of one list (a weight, or a row of the gate that several teams share) per workgroup, four columns and every 64th team
+// per thread.  blockIdx.y: the weights, then the gate's rows, or where those are more than the teams, the ends of teams.
+__global__ void __launch_bounds__(1024) norm_join_kernel(NormProblem q, int teams, int rows, int gates, const float* __restrict__ parts) {
+  __shared__ f32x4 lds[64][17];
   const Parts lists = parts_of(q.w_after, q.gate, q.w_before);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+  const int part = threadIdx.x >> 4, col = blockIdx.x * 64 + (threadIdx.x & 15) * 4;
   const long team_stride = (long)lists.lists * q.d;
-  int list = blockIdx.y, first = 0, last = teams - 1;
-  const int weights = (q.w_before ? 1 : 0) + (q.w_after ? 1 : 0);
+  int first = 0, last = teams - 1;
+  const int weights = (q.w_before ? 1 : 0) + (q.w_after ? 1 : 0), list = blockIdx.y;
+  const bool is_gate = list >= weights;
   float* to;
   const float* from;
-  if (list < weights) {
+  if (!is_gate) {
     const bool is_before = q.w_before && list == 0;
     to = is_before ? q.d_w_before : q.d_w_after;
     from = parts + (long)(is_before ? lists.wb : lists.wa) * q.d;
   } else {
-    // the row of the gate that is open where a team ends and goes on with the next one: the team where it begins adds it up
-    const int team = list - weights, at = (team + 1) * rows;             // (rows of the teams in front)
-    if (at >= q.T) return;
-    const int group = (at - 1) / q.gate_rows;
+    const int n = list - weights;
+    const int group = gates < teams ? n : (int)(((long)(n + 1) * rows - 1) / q.gate_rows);       // the row of the gate that is open where team n ends
     const long begin = (long)group * q.gate_rows, end = min(begin + q.gate_rows, (long)q.T);
-    if (end <= at || begin < (long)team * rows) return;                  // it ends here, or began in front
-    first = team;
+    first = (int)(begin / rows);
     last = (int)((end - 1) / rows);
+    if (first == last || (gates >= teams && first != n)) return;          // written by its team, or another workgroup's
     to = q.d_gate + (long)group * q.d;
-    from = parts + (long)lists.gate * q.d;                               // (the first team's is its last row, one list on)
+    from = parts + (long)lists.gate * q.d;
   }
-  float sum = 0.f;
+  f32x4 sum = {};
   if (col < q.d) {
-    const bool is_gate = list >= weights;
-    for (int t = first + wave; t <= last; t += 16) sum += from[(long)t * team_stride + (is_gate && t == first ? q.d : 0) + col];
+    // (a row of the gate begins in its first team's second list)
+#pragma unroll 4
+    for (int t = first + part; t <= last; t += 64) sum += *reinterpret_cast<const f32x4*>(from + (long)t * team_stride + (is_gate && t == first ? q.d : 0) + col);
   }
-  lds[wave][lane] = sum;
+  lds[part][threadIdx.x & 15] = sum;
   __syncthreads();
-  if (wave == 0 && col < q.d) {
-    float s = 0.f;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) s += lds[w][lane];
-    to[col] = q.accumulate ? to[col] + s : s;
+  if (part < 16) {                                  // (a quarter each, then all of them)
+    sum = lds[part][threadIdx.x & 15] + lds[part + 16][threadIdx.x & 15] + lds[part + 32][threadIdx.x & 15] + lds[part + 48][threadIdx.x & 15];
+  }
+  __syncthreads();
+  if (part < 16) lds[part][threadIdx.x & 15] = sum;
+  __syncthreads();
+  if (part == 0 && col < q.d) {
+    for (int w = 1; w < 16; ++w) sum += lds[w][threadIdx.x & 15];
+    f32x4* at = reinterpret_cast<f32x4*>(to + col);
+    *at = q.accumulate ? *at + sum : sum;
   }
 }
 
@@ -347,7 +353,7 @@ template <typename F> int with_team(int d, F f) {
 
 NormPlan norm_bwd_plan(int T, int d, moe_dtype dt, bool after, bool gate, bool before) {
   NormPlan p{};
-  const int most = d <= 1024 ? 2048 : d <= 4096 ? 1024 : 512;
+  const int most = d <= 1024 ? 2048 : 512;
   p.rows = cdiv(T, most);
   if (p.rows < 4) p.rows = T < 4 ? (T < 1 ? 1 : T) : 4;
   p.teams = cdiv(T, p.rows);
@@ -379,9 +385,10 @@ int launch_norm_bwd(const NormProblem& q, const NormPlan& p, float* ws, hipStrea
   });
   if (rc != MOE_OK) return rc;
   const int weights = (q.w_before ? 1 : 0) + (q.w_after ? 1 : 0);
-  const int spans = q.gate && q.gate_rows > 1 ? p.teams - 1 : 0;        // (a row of the gate for each token never spans teams)
+  const int gates = q.gate ? (int)(((long)q.T + q.gate_rows - 1) / q.gate_rows) : 0;
+  const int spans = !q.gate || q.gate_rows == 1 || p.teams == 1 ? 0 : gates < p.teams ? gates : p.teams - 1;      // (a token's own row never spans teams)
   if (weights + spans > 0) {
-    norm_join_kernel<<<dim3((unsigned)cdiv(q.d, 64), (unsigned)(weights + spans)), dim3(1024), 0, s>>>(q, p.teams, p.rows, ws);
+    norm_join_kernel<<<dim3((unsigned)cdiv(q.d, 64), (unsigned)(weights + spans)), dim3(1024), 0, s>>>(q, p.teams, p.rows, gates, ws);
     MOE_LAUNCH_CHECK();
   }
   return MOE_OK;
