@@ -1,6 +1,5 @@
 // extern "C" entry points: argument validation (before any HIP call), workspace carving and the
 // sequencing of kernels for each call.  Declarations and contracts are in include/moe.h.
-#include "block.h"
 #include "moe_common.h"
 
 namespace moe {
@@ -171,8 +170,6 @@ int moe_init(void) {
   int rc = mfma_configure_all();
   if (rc != MOE_OK) return rc;
   rc = gemm_f32_split_configure();
-  if (rc != MOE_OK) return rc;
-  rc = embedding_configure();
   if (rc != MOE_OK) return rc;
   return route_noalloc_prepare();
 }

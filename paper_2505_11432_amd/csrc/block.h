@@ -7,14 +7,16 @@ namespace moe {
 // ---- embedding -----------------------------------------------------------------------------
 constexpr int kSortTile = 4096;             // tokens that a workgroup sorts at a time (twice as many where one workgroup sorts all)
 constexpr int kSortOne = 2 * kSortTile;
+constexpr int kOneBits = 19;                // bits of a word where one workgroup sorts all
 constexpr int kMaxDigit = 9;                // bits of a sorting pass
+constexpr int kFewTokens = 2048;            // up to so many are not sorted
 struct EmbeddingPlan {
+  bool few, zero_first;                     // no sort; the gradient is zeroed beside the sort
   int chunk, chunks;                        // sorted tokens that one wave adds up
   int tiles, passes, bits;                  // of the sort: workgroups, passes and bits of each
   size_t pairs, counts, parts, bytes;       // offsets in the workspace; what it takes
 };
 EmbeddingPlan embedding_plan(int T, int d, int V);
-int embedding_configure();                // per-device set-up (moe_init)
 int launch_embedding_fwd(const void* table, const int32_t* tokens, moe_dtype dt, int T, int d, int V, float scale, void* out, hipStream_t s);
 int launch_embedding_bwd(const int32_t* tokens, const void* dy, moe_dtype dt, int T, int d, int V, float scale, void* d_table, moe_dtype grad_dt,
                          int accumulate, const EmbeddingPlan& p, char* ws, hipStream_t s);

@@ -8,8 +8,6 @@
 // written to its row at once, the first and last run of a chunk may go on in the next one and leave a partial sum, which a second launch
 // adds up in order.  No atomic addition: the bits depend on the tokens and the sizes alone.  Rows without a token are zeroed by
 // other workgroups of the same launch, which find them by binary search, a lane per row.
-#include <atomic>
-
 #include "block.h"
 
 namespace moe {
@@ -58,8 +56,8 @@ __global__ void __launch_bounds__(256) lookup_kernel(const T* __restrict__ table
 // ---- sort ----------------------------------------------------------------------------------------
 // One pass over BITS bits of the keys of a tile, the items of a wave lying one after another: wave w of NW, round r, lane l holds item
 // (w * ROUNDS + r) * 64 + l.  rank: how many items with the same digit lie in front of it in its wave; counts[digit][wave].
-template <int ROUNDS>
-__device__ __forceinline__ void rank_items(const unsigned (&digit)[ROUNDS], const bool (&there)[ROUNDS], int bits, unsigned* counts, unsigned (&rank)[ROUNDS]) {
+template <int ROUNDS, typename Count>
+__device__ __forceinline__ void rank_items(const unsigned (&digit)[ROUNDS], const bool (&there)[ROUNDS], int bits, Count* counts, unsigned (&rank)[ROUNDS]) {
   const int lane = threadIdx.x & 63;
   const unsigned long long below = (1ull << lane) - 1;
 #pragma unroll
@@ -76,7 +74,7 @@ __device__ __forceinline__ void rank_items(const unsigned (&digit)[ROUNDS], cons
       rank[r] = before + (unsigned)__popcll(same & below);
     }
     __builtin_amdgcn_wave_barrier();
-    if (there[r] && (same & below) == 0) counts[digit[r]] += (unsigned)__popcll(same);
+    if (there[r] && (same & below) == 0) counts[digit[r]] += (Count)__popcll(same);
     __builtin_amdgcn_wave_barrier();
   }
 }
@@ -103,31 +101,39 @@ __device__ __forceinline__ unsigned key_of(int32_t token, int V) { return (unsig
 constexpr int kBins = 1 << kMaxDigit, kWaves = 16;
 constexpr int kStride = kBins + 1;      // (counts of the waves in different banks)
 
-constexpr int kSortOneBytes = kSortOne * 8 + kWaves * kStride * 4;
-static_assert(kSortOneBytes <= 150 * 1024, "keys, places and counts fit the LDS");
-
-// All passes over at most kSortOne tokens in one workgroup; keys and places in LDS.
-__global__ void __launch_bounds__(1024) sort_one_kernel(const int32_t* __restrict__ tokens, int T, int V, int passes, int bits, uint2* __restrict__ pairs) {
-  constexpr int ROUNDS = kSortOne / 1024;
-  extern __shared__ __attribute__((aligned(16))) unsigned smem[];
-  uint2* items = reinterpret_cast<uint2*>(smem);                 // [kSortOne]
-  unsigned* counts = smem + 2 * kSortOne;                        // [kWaves][kStride]
+// All passes over at most kSortOne tokens in one workgroup, word and place packed into one number in LDS (the words take at most kOneBits bits).  The
+// other workgroups zero `zero_units` pieces of 16 bytes.
+__global__ void __launch_bounds__(1024) sort_one_kernel(const int32_t* __restrict__ tokens, int T, int V, int passes, int bits, uint2* __restrict__ pairs,
+                                                        u32x4* __restrict__ zero, long zero_units) {
+  constexpr int ROUNDS = kSortOne / 1024, PLACE = 32 - kOneBits;
+  static_assert(kSortOne <= 1 << PLACE, "a place fits beside the word");
+  __shared__ unsigned items[kSortOne];
+  __shared__ unsigned short counts[kWaves * kStride];
   __shared__ unsigned sums[16];
+  if (blockIdx.x > 0) {
+    const long step = ((long)gridDim.x - 1) * 1024;
+    long i = ((long)blockIdx.x - 1) * 1024 + threadIdx.x;
+    for (; i + 3 * step < zero_units; i += 4 * step)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) zero[i + u * step] = u32x4{0, 0, 0, 0};
+    for (; i < zero_units; i += step) zero[i] = u32x4{0, 0, 0, 0};
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rounds = (T + 1023) / 1024;
-  uint2 item[ROUNDS];
+  unsigned item[ROUNDS];
   bool there[ROUNDS];
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
     const int i = (wave * rounds + r) * 64 + lane;
     there[r] = r < rounds && i < T;
-    item[r] = there[r] ? uint2{key_of(tokens[i], V), (unsigned)i} : uint2{0, 0};
+    item[r] = there[r] ? key_of(tokens[i], V) << PLACE | (unsigned)i : 0u;
   }
   for (int pass = 0; pass < passes; ++pass) {
     for (int i = tid; i < kWaves * kStride; i += 1024) counts[i] = 0;
     __syncthreads();
     unsigned digit[ROUNDS], rank[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) digit[r] = item[r].x >> (pass * bits) & ((1u << bits) - 1);
+    for (int r = 0; r < ROUNDS; ++r) digit[r] = item[r] >> (PLACE + pass * bits) & ((1u << bits) - 1);
     rank_items<ROUNDS>(digit, there, bits, counts + wave * kStride, rank);
     __syncthreads();
     // thread t: digit t; its counts become where each wave's items begin
@@ -138,7 +144,7 @@ __global__ void __launch_bounds__(1024) sort_one_kernel(const int32_t* __restric
     if (tid < kBins)
       for (int w = 0; w < kWaves; ++w) {
         const unsigned n = counts[w * kStride + tid];
-        counts[w * kStride + tid] = at;
+        counts[w * kStride + tid] = (unsigned short)at;
         at += n;
       }
     __syncthreads();
@@ -146,7 +152,8 @@ __global__ void __launch_bounds__(1024) sort_one_kernel(const int32_t* __restric
     for (int r = 0; r < ROUNDS; ++r)
       if (there[r]) {
         const unsigned to = counts[wave * kStride + digit[r]] + rank[r];
-        if (pass + 1 < passes) items[to] = item[r]; else pairs[to] = item[r];
+        if (pass + 1 < passes) items[to] = item[r];
+        else pairs[to] = uint2{item[r] >> PLACE, item[r] & ((1u << PLACE) - 1)};
       }
     __syncthreads();
     if (pass + 1 < passes) {
@@ -249,10 +256,76 @@ template <typename TG> __device__ __forceinline__ void write_sum(TG* p, f32x8 su
   store8(p, sum);
 }
 
-// zeros past the caches, by 256 threads
+// zeros, by 256 threads
 template <typename TG> __device__ __forceinline__ void zero_row(TG* row, int d) {
   constexpr int N = 16 / sizeof(TG);
-  for (int c = threadIdx.x * N; c < d; c += 256 * N) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4*>(row + c));
+  for (int c = threadIdx.x * N; c < d; c += 256 * N) *reinterpret_cast<u32x4*>(row + c) = u32x4{0, 0, 0, 0};
+}
+
+// Few tokens: the whole gradient in one launch, without a sort.  A workgroup per token and slab of columns looks through all tokens; if its own is the
+// first of its word it adds them up, wave w the w-th quarter of the batch, in order.
+template <typename T, typename TG>
+__global__ void __launch_bounds__(256) few_kernel(const int32_t* __restrict__ tokens, const T* __restrict__ dy, int n, int d, int V, float scale,
+                                                  TG* __restrict__ d_table, int accumulate, int slabs, int sum_groups) {
+  constexpr int B = 8;                      // rows in flight
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  if ((int)blockIdx.x >= sum_groups) {      // rows without a token
+    __shared__ unsigned seen[kZeroRows];
+    const int row0 = ((int)blockIdx.x - sum_groups) * kZeroRows, rows = min(kZeroRows, V - row0);
+    if (threadIdx.x < kZeroRows) seen[threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += 256) {
+      const unsigned r = (unsigned)tokens[i] - (unsigned)row0;
+      if (r < (unsigned)rows) seen[r] = 1;
+    }
+    __syncthreads();
+    for (int r = 0; r < rows; ++r)
+      if (!seen[r]) zero_row(d_table + (long)(row0 + r) * d, d);
+    return;
+  }
+  __shared__ f32x8 others[3][64];
+  const int t = blockIdx.x / slabs, slab = blockIdx.x - t * slabs, col = slab * kSlab + lane * 8;
+  const int token = tokens[t];
+  if ((unsigned)token >= (unsigned)V) return;
+  int found = 0;
+  for (int i = threadIdx.x; i < t; i += 256) found |= tokens[i] == token;
+  if (__syncthreads_or(found)) return;
+  // places of the word in this wave's quarter of what is left, in order
+  constexpr int ROUNDS = kFewTokens / 4 / 64;
+  __shared__ unsigned short list[4][ROUNDS * 64];
+  const int quarter = (n - t + 3) / 4, begin = t + wave * quarter, end = min(begin + quarter, n);
+  int count = 0;
+  bool same[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int i = begin + r * 64 + lane;
+    same[r] = i < end && tokens[min(i, n - 1)] == token;
+  }
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const unsigned long long mask = __ballot(same[r]);
+    if (same[r]) list[wave][count + __popcll(mask & ((1ull << lane) - 1))] = (unsigned short)(begin + r * 64 + lane);
+    count += __popcll(mask);
+  }
+  __builtin_amdgcn_wave_barrier();
+  const T* src = dy + min(col, d - 8);
+  f32x8 sum = {};
+  for (int k = 0; k < count; k += B) {
+    f32x8 v[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      v[b] = f32x8{};
+      if (k + b < count) v[b] = load8(src + (long)list[wave][k + b] * d);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) sum += v[b];
+  }
+  if (wave > 0) others[wave - 1][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && col < d) {
+    sum = sum + others[0][lane] + others[1][lane] + others[2][lane];
+    write_sum(d_table + (long)token * d + col, sum, scale, accumulate);
+  }
 }
 
 template <typename T, typename TG>
@@ -274,8 +347,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const uint2* __restrict__ pair
     }
     __syncthreads();
     for (int r = 0; r < rows; ++r)
-      if (empty >> r & 1)
-        zero_row(d_table + (long)(row0 + r) * d, d);
+      if (empty >> r & 1) zero_row(d_table + (long)(row0 + r) * d, d);
     return;
   }
   const long task = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
@@ -351,9 +423,19 @@ __global__ void __launch_bounds__(256) join_kernel(const uint2* __restrict__ pai
 }
 
 template <typename T, typename TG>
-int sums(const uint2* pairs, const T* dy, int n, int d, int V, float scale, TG* d_table, int accumulate, const EmbeddingPlan& p, float* parts, hipStream_t s) {
+int sums(const int32_t* tokens, const T* dy, int n, int d, int V, float scale, TG* d_table, int accumulate, const EmbeddingPlan& p, char* ws, hipStream_t s) {
   const int slabs = cdiv(d, kSlab);
-  const int sum_groups = cdiv(p.chunks * slabs, 4), zero_groups = accumulate ? 0 : cdiv(V, kZeroRows);
+  if (p.few) {
+    const int sum_groups = n * slabs, zero_groups = accumulate ? 0 : cdiv(V, kZeroRows);
+    if (sum_groups + zero_groups > 0) {
+      few_kernel<T, TG><<<dim3(sum_groups + zero_groups), dim3(256), 0, s>>>(tokens, dy, n, d, V, scale, d_table, accumulate, slabs, sum_groups);
+      MOE_LAUNCH_CHECK();
+    }
+    return MOE_OK;
+  }
+  const uint2* pairs = reinterpret_cast<const uint2*>(ws + p.pairs);
+  float* parts = reinterpret_cast<float*>(ws + p.parts);
+  const int sum_groups = cdiv(p.chunks * slabs, 4), zero_groups = accumulate || p.zero_first ? 0 : cdiv(V, kZeroRows);
   if (sum_groups + zero_groups > 0) {
     sum_kernel<T, TG><<<dim3(sum_groups + zero_groups), dim3(256), 0, s>>>(pairs, dy, n, d, V, scale, d_table, accumulate, p.chunk, p.chunks, slabs, sum_groups, parts);
     MOE_LAUNCH_CHECK();
@@ -377,25 +459,15 @@ EmbeddingPlan embedding_plan(int T, int d, int V) {
   while (key_bits < 31 && (V >> key_bits) != 0) ++key_bits;      // keys 0..V
   p.passes = cdiv(key_bits, kMaxDigit);
   p.bits = cdiv(key_bits, p.passes);
-  p.tiles = T <= kSortOne ? 0 : cdiv(T, kSortTile);
+  p.tiles = T <= kSortOne && key_bits <= kOneBits ? 0 : cdiv(T, kSortTile);
+  p.few = T <= kFewTokens;
+  p.zero_first = p.tiles == 0 && T <= V / 2;
   const size_t list = align_up((size_t)T * sizeof(uint2), 256);
   p.pairs = 0;
   p.counts = p.tiles ? 2 * list : list;
   p.parts = p.counts + align_up((size_t)p.tiles * kBins * 4, 256);
   p.bytes = p.parts + (p.chunks > 1 ? (size_t)p.chunks * 2 * d * 4 : 0) + 256;
   return p;
-}
-
-// The sort in one workgroup needs its dynamic-LDS limit raised once per device; moe_init does it ahead of a graph capture.
-int embedding_configure() {
-  static std::atomic<unsigned long long> done{0};
-  int dev = 0;
-  MOE_HIP_TRY(hipGetDevice(&dev));
-  if (dev < 0 || dev >= 64) return MOE_ERR_UNSUPPORTED;
-  if (done.load(std::memory_order_acquire) >> dev & 1) return MOE_OK;
-  MOE_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&sort_one_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kSortOneBytes));
-  done.fetch_or(1ull << dev, std::memory_order_release);
-  return MOE_OK;
 }
 
 int launch_embedding_fwd(const void* table, const int32_t* tokens, moe_dtype dt, int T, int d, int V, float scale, void* out, hipStream_t s) {
@@ -410,11 +482,13 @@ int launch_embedding_fwd(const void* table, const int32_t* tokens, moe_dtype dt,
 int launch_embedding_bwd(const int32_t* tokens, const void* dy, moe_dtype dt, int T, int d, int V, float scale, void* d_table, moe_dtype grad_dt,
                          int accumulate, const EmbeddingPlan& p, char* ws, hipStream_t s) {
   uint2* pairs = reinterpret_cast<uint2*>(ws + p.pairs);
-  if (T > 0 && p.tiles == 0) {
-    if (const int rc = embedding_configure()) return rc;
-    sort_one_kernel<<<dim3(1), dim3(1024), kSortOneBytes, s>>>(tokens, T, V, p.passes, p.bits, pairs);
+  if (!p.few && p.tiles == 0) {
+    const long units = accumulate || !p.zero_first ? 0 : (long)V * d * (long)dtype_size(grad_dt) / 16;
+    const long groups = (units + 4095) / 4096;
+    sort_one_kernel<<<dim3((unsigned)(1 + (groups < 2048 ? groups : 2048))), dim3(1024), 0, s>>>(tokens, T, V, p.passes, p.bits, pairs,
+                                                                                              static_cast<u32x4*>(d_table), units);
     MOE_LAUNCH_CHECK();
-  } else if (T > 0) {
+  } else if (!p.few) {
     uint2* lists[2] = {pairs, reinterpret_cast<uint2*>(ws + p.counts / 2)};
     unsigned* counts = reinterpret_cast<unsigned*>(ws + p.counts);
     const uint2* from = nullptr;
@@ -427,10 +501,9 @@ int launch_embedding_bwd(const int32_t* tokens, const void* dy, moe_dtype dt, in
       from = to;
     }
   }
-  float* parts = reinterpret_cast<float*>(ws + p.parts);
-  if (dt == MOE_F32) return sums(pairs, static_cast<const float*>(dy), T, d, V, scale, static_cast<float*>(d_table), accumulate, p, parts, s);
-  if (grad_dt == MOE_F32) return sums(pairs, static_cast<const bf16*>(dy), T, d, V, scale, static_cast<float*>(d_table), accumulate, p, parts, s);
-  return sums(pairs, static_cast<const bf16*>(dy), T, d, V, scale, static_cast<bf16*>(d_table), accumulate, p, parts, s);
+  if (dt == MOE_F32) return sums(tokens, static_cast<const float*>(dy), T, d, V, scale, static_cast<float*>(d_table), accumulate, p, ws, s);
+  if (grad_dt == MOE_F32) return sums(tokens, static_cast<const bf16*>(dy), T, d, V, scale, static_cast<float*>(d_table), accumulate, p, ws, s);
+  return sums(tokens, static_cast<const bf16*>(dy), T, d, V, scale, static_cast<bf16*>(d_table), accumulate, p, ws, s);
 }
 
 }  // namespace moe

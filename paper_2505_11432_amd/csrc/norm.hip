@@ -7,71 +7,100 @@
 // Bound by memory: a row is read once into registers, its statistics are made again in the backward pass from the row that it needs
 // anyway (a sum more in a round of sums that is made anyway, instead of kept numbers).
 //
-// A team of 64, 256 or 1024 threads has a row, eight elements of it per thread and step; sums in fp32.  In the backward pass a team takes rows one
-// after another and keeps its share of the weights' gradients in registers; they go to memory once per team and a second launch adds
-// them up in order.  A row of the gate whose tokens lie with one team is written at once.
+// A team of 64 to 1024 threads has a row, eight elements of it per thread and step.  What it holds per column (weights, gate, sums of gradients) is most of its
+// registers, so few teams fit a CU and the rows in flight come from within them: the forward pass takes several rows at a time (one round of barriers serves all
+// of them), the backward pass loads the next row while it works on one.  Sums in fp32.  In the backward pass a team's rows lie one after another; its share
+// of the weights' gradients goes to memory once and a second launch adds the teams up in order.  A row of the gate whose tokens lie with one team is
+// written at once.
 #include "block.h"
 
 namespace moe {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(8))) float f32x8;
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 
-template <typename T> struct Row8;                  // eight elements as they lie in memory
-template <> struct Row8<float> {
-  f32x8 v;
-  __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const f32x8 __attribute__((aligned(16)))*>(p); }
-  __device__ __forceinline__ f32x8 get() const { return v; }
+template <int W> using vec = float __attribute__((ext_vector_type(W)));
+
+// W elements as they lie in memory, read and written past the caches (a row is used once)
+template <typename T, int W> struct Piece;
+template <int W> struct Piece<float, W> {
+  vec<W> v;
+  __device__ __forceinline__ void load(const float* p) {
+    const f32x4 a = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+    if constexpr (W == 4) v = a;
+    else v = __builtin_shufflevector(a, __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p) + 1), 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  __device__ __forceinline__ vec<W> get() const { return v; }
 };
-template <> struct Row8<bf16> {
-  bf16x8 v;
-  __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const bf16x8*>(p); }
-  __device__ __forceinline__ f32x8 get() const { return __builtin_convertvector(v, f32x8); }
+template <int W> struct Piece<bf16, W> {
+  typedef __bf16 raw __attribute__((ext_vector_type(W)));
+  raw v;
+  __device__ __forceinline__ void load(const bf16* p) { v = __builtin_nontemporal_load(reinterpret_cast<const raw*>(p)); }
+  __device__ __forceinline__ vec<W> get() const { return __builtin_convertvector(v, vec<W>); }
 };
-__device__ __forceinline__ f32x8 load8(const float* p) { return *reinterpret_cast<const f32x8 __attribute__((aligned(16)))*>(p); }
-__device__ __forceinline__ void store8(float* p, f32x8 v) {
-  *reinterpret_cast<f32x4*>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-  *(reinterpret_cast<f32x4*>(p) + 1) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+template <int W> __device__ __forceinline__ vec<W> load_f32(const float* p) {
+  if constexpr (W == 4) return *reinterpret_cast<const f32x4*>(p);
+  else return __builtin_shufflevector(*reinterpret_cast<const f32x4*>(p), *(reinterpret_cast<const f32x4*>(p) + 1), 0, 1, 2, 3, 4, 5, 6, 7);
 }
-__device__ __forceinline__ void store8(bf16* p, f32x8 v) { *reinterpret_cast<bf16x8*>(p) = __builtin_convertvector(v, bf16x8); }
+template <int W> __device__ __forceinline__ void store(float* p, vec<W> v) {
+  if constexpr (W == 4) {
+    *reinterpret_cast<f32x4*>(p) = v;
+  } else {
+    *reinterpret_cast<f32x4*>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+    *(reinterpret_cast<f32x4*>(p) + 1) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+  }
+}
+template <int W> __device__ __forceinline__ void store(bf16* p, vec<W> v) {
+  typedef __bf16 raw __attribute__((ext_vector_type(W)));
+  __builtin_nontemporal_store(__builtin_convertvector(v, raw), reinterpret_cast<raw*>(p));
+}
 // v as T keeps it
-template <typename T> __device__ __forceinline__ f32x8 rounded(f32x8 v);
-template <> __device__ __forceinline__ f32x8 rounded<float>(f32x8 v) { return v; }
-template <> __device__ __forceinline__ f32x8 rounded<bf16>(f32x8 v) { return __builtin_convertvector(__builtin_convertvector(v, bf16x8), f32x8); }
-
-__device__ __forceinline__ float sum8(f32x8 v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
+template <typename T, int W> __device__ __forceinline__ vec<W> rounded(vec<W> v) {
+  typedef T raw __attribute__((ext_vector_type(W)));
+  return __builtin_convertvector(__builtin_convertvector(v, raw), vec<W>);
+}
+template <int W> __device__ __forceinline__ float sum_of(vec<W> v) {
+  float s = (v[0] + v[1]) + (v[2] + v[3]);
+  if constexpr (W == 8) s += (v[4] + v[5]) + (v[6] + v[7]);
+  return s;
+}
 
 // Sums of N values over a team, the same in every thread; `lds` holds two rounds, told apart by `turn`, so one barrier a round is enough.
+constexpr int kMostSums = 8;
 template <int TS, int N> __device__ __forceinline__ void team_sum(float (&v)[N], float* lds, int& turn) {
+  static_assert(N <= kMostSums, "the sums of a round");
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1)
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], off);
   if constexpr (TS > 64) {
     constexpr int WAVES = TS / 64;
-    float* at = lds + turn * (2 * WAVES);
+    float* at = lds + turn * (kMostSums * WAVES);
     turn ^= 1;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-      for (int i = 0; i < N; ++i) at[(threadIdx.x >> 6) * N + i] = v[i];
+      for (int i = 0; i < N; ++i) at[i * WAVES + (threadIdx.x >> 6)] = v[i];
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float s = 0.f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) s += at[w * N + i];
+      for (int w = 0; w < WAVES; w += 4) {
+        const f32x4 four = *reinterpret_cast<const f32x4*>(at + i * WAVES + w);
+        s += (four[0] + four[1]) + (four[2] + four[3]);
+      }
       v[i] = s;
     }
   }
 }
 
 constexpr int block_threads(int ts) { return ts < 256 ? 256 : ts; }
+template <int TS> constexpr int lds_floats() { return 2 * kMostSums * (TS / 64); }
 
-template <typename T, int TS, int K>
+// Teams of the forward pass take groups of R rows in turn.
+template <typename T, int TS, int W, int K, int R>
 __global__ void __launch_bounds__(block_threads(TS)) norm_fwd_kernel(NormProblem q, int teams) {
-  __shared__ float lds[2 * 2 * (TS / 64)];
+  __shared__ __attribute__((aligned(16))) float lds[lds_floats<TS>()];
   const int lane = threadIdx.x % TS, team = blockIdx.x * (block_threads(TS) / TS) + threadIdx.x / TS;
   if (team >= teams) return;                        // (whole waves; teams of more than one wave are blocks of their own)
   const T* x = static_cast<const T*>(q.x);
@@ -80,73 +109,91 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_fwd_kernel(NormProblem
   T* h = static_cast<T*>(q.h);
   const float inv_d = 1.0f / (float)q.d;
   int turn = 0;
-  f32x8 wa[K], wb[K], gate[K];
+  vec<W> wa[K], wb[K], gate[K];
   int col[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    col[k] = (k * TS + lane) * 8;
-    wa[k] = wb[k] = gate[k] = f32x8{};
+    col[k] = (k * TS + lane) * W;
+    wa[k] = wb[k] = gate[k] = vec<W>{};
     if (col[k] < q.d) {
-      if (q.w_after) wa[k] = load8(q.w_after + col[k]);
-      if (q.w_before) wb[k] = load8(q.w_before + col[k]);
+      if (q.w_after) wa[k] = load_f32<W>(q.w_after + col[k]);
+      if (q.w_before) wb[k] = load_f32<W>(q.w_before + col[k]);
     }
   }
-  int open = -1;
-  for (int t = team; t < q.T; t += teams) {
-    const long row = (long)t * q.d;
-    Row8<T> xr[K], yr[K];
+  int open = -1;                                    // row of the gate in registers
+  for (long t0 = (long)team * R; t0 < q.T; t0 += (long)teams * R) {
+    const int rows = (int)min((long)R, q.T - t0);
+    Piece<T, W> xr[R][K], yr[R][K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      xr[k].v = {};
-      yr[k].v = {};
-      if (col[k] < q.d) {
-        xr[k].load(x + row + col[k]);
-        if (y) yr[k].load(y + row + col[k]);
-      }
-    }
-    if (q.gate) {
-      const int group = t / q.gate_rows;
-      if (group != open) {
-        open = group;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-          if (col[k] < q.d) gate[k] = load8(q.gate + (long)group * q.d + col[k]);
-      }
-    }
-    f32x8 o[K];
-    if (y) {
-      float r = 1.f;
-      if (q.w_after) {
-        float s[1] = {0.f};
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          const f32x8 v = yr[k].get();
-          s[0] += sum8(v * v);
-        }
-        team_sum<TS>(s, lds, turn);
-        r = 1.0f / sqrtf(s[0] * inv_d + q.eps);
-      }
+    for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        f32x8 n = yr[k].get();
-        if (q.w_after) n = n * r * wa[k];
-        if (q.gate) n = n * gate[k];
-        o[k] = rounded<T>(xr[k].get() * q.alpha + n);
-        if (col[k] < q.d) store8(out + row + col[k], o[k]);
+        const long at = (t0 + r) * q.d + col[k];
+        xr[r][k].v = {};
+        yr[r][k].v = {};
+        if (r < rows && col[k] < q.d) {
+          xr[r][k].load(x + at);
+          if (y) yr[r][k].load(y + at);
+        }
+      }
+    float inv[R];
+    vec<W> o[R][K];
+    if (y) {
+      if (q.w_after) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          inv[r] = 0.f;
+#pragma unroll
+          for (int k = 0; k < K; ++k) {
+            const vec<W> v = yr[r][k].get();
+            inv[r] += sum_of<W>(v * v);
+          }
+        }
+        team_sum<TS>(inv, lds, turn);
+#pragma unroll
+        for (int r = 0; r < R; ++r) inv[r] = 1.0f / sqrtf(inv[r] * inv_d + q.eps);
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (q.gate && r < rows) {
+          const int group = (int)((t0 + r) / q.gate_rows);
+          if (group != open) {
+            open = group;
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+              if (col[k] < q.d) gate[k] = load_f32<W>(q.gate + (long)group * q.d + col[k]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          vec<W> n = yr[r][k].get();
+          if (q.w_after) n = n * inv[r] * wa[k];
+          if (q.gate) n = n * gate[k];
+          o[r][k] = rounded<T, W>(xr[r][k].get() * q.alpha + n);
+          if (r < rows && col[k] < q.d) store<W>(out + (t0 + r) * q.d + col[k], o[r][k]);
+        }
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < K; ++k) o[k] = xr[k].get();
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int k = 0; k < K; ++k) o[r][k] = xr[r][k].get();
     }
     if (q.w_before) {
-      float s[1] = {0.f};
 #pragma unroll
-      for (int k = 0; k < K; ++k) s[0] += sum8(o[k] * o[k]);
-      team_sum<TS>(s, lds, turn);
-      const float r = 1.0f / sqrtf(s[0] * inv_d + q.eps);
+      for (int r = 0; r < R; ++r) {
+        inv[r] = 0.f;
 #pragma unroll
-      for (int k = 0; k < K; ++k)
-        if (col[k] < q.d) store8(h + row + col[k], o[k] * r * wb[k]);
+        for (int k = 0; k < K; ++k) inv[r] += sum_of<W>(o[r][k] * o[r][k]);
+      }
+      team_sum<TS>(inv, lds, turn);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float i = 1.0f / sqrtf(inv[r] * inv_d + q.eps);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+          if (r < rows && col[k] < q.d) store<W>(h + (t0 + r) * q.d + col[k], o[r][k] * i * wb[k]);
+      }
     }
   }
 }
@@ -162,9 +209,11 @@ __host__ __device__ inline Parts parts_of(bool after, bool gate, bool before) {
   return p;
 }
 
-template <typename T, int TS, int K>
+// TOKEN: every token has its own row of the gate.  HOLD: the weights stay in registers (the widest rows leave no room for them).  AHEAD: the next row is
+// on its way while one is worked on.
+template <typename T, int TS, int W, int K, bool HOLD, bool TOKEN, bool AHEAD>
 __global__ void __launch_bounds__(block_threads(TS)) norm_bwd_kernel(NormProblem q, int teams, int rows, float* __restrict__ parts) {
-  __shared__ float lds[2 * 2 * (TS / 64)];
+  __shared__ __attribute__((aligned(16))) float lds[lds_floats<TS>()];
   const int lane = threadIdx.x % TS, team = blockIdx.x * (block_threads(TS) / TS) + threadIdx.x / TS;
   if (team >= teams) return;
   const T* x = static_cast<const T*>(q.x);
@@ -176,119 +225,159 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_bwd_kernel(NormProblem
   const Parts lists = parts_of(q.w_after, q.gate, q.w_before);
   float* mine = parts + (long)team * lists.lists * q.d;
   const float inv_d = 1.0f / (float)q.d;
+  const bool grouped = q.gate && !TOKEN;
   int turn = 0;
-  f32x8 wa[K], wb[K], gate[K], sum_wa[K], sum_wb[K], sum_gate[K];
+  vec<W> wa_held[HOLD ? K : 1], wb_held[HOLD ? K : 1], gate_held[HOLD && !TOKEN ? K : 1], sum_wa[K], sum_wb[K], sum_gate[TOKEN ? 1 : K];
   int col[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    col[k] = (k * TS + lane) * 8;
-    wa[k] = wb[k] = gate[k] = sum_wa[k] = sum_wb[k] = sum_gate[k] = f32x8{};
-    if (col[k] < q.d) {
-      if (q.w_after) wa[k] = load8(q.w_after + col[k]);
-      if (q.w_before) wb[k] = load8(q.w_before + col[k]);
+    col[k] = (k * TS + lane) * W;
+    sum_wa[k] = sum_wb[k] = vec<W>{};
+    if constexpr (!TOKEN) sum_gate[k] = vec<W>{};
+    if constexpr (HOLD && !TOKEN) gate_held[k] = vec<W>{};
+    if constexpr (HOLD) {
+      wa_held[k] = wb_held[k] = vec<W>{};
+      if (col[k] < q.d) {
+        if (q.w_after) wa_held[k] = load_f32<W>(q.w_after + col[k]);
+        if (q.w_before) wb_held[k] = load_f32<W>(q.w_before + col[k]);
+      }
     }
   }
   const bool needs_y = q.dy && (q.w_after || q.gate);
-  const int t0 = team * rows, t1 = min(t0 + rows, q.T);
+  const int t_begin = team * rows, t_end = min(t_begin + rows, q.T);
   int open = -1;
+  auto at_col = [&](const float* w, int k) __attribute__((always_inline)) -> vec<W> { return col[k] < q.d ? load_f32<W>(w + col[k]) : vec<W>{}; };
+  auto wa = [&](int k) __attribute__((always_inline)) -> vec<W> { if constexpr (HOLD) return wa_held[k]; else return at_col(q.w_after, k); };
+  auto wb = [&](int k) __attribute__((always_inline)) -> vec<W> { if constexpr (HOLD) return wb_held[k]; else return at_col(q.w_before, k); };
   auto close_gate = [&](int group) __attribute__((always_inline)) {
-    const long begin = (long)group * q.gate_rows;
-    const bool begins = begin >= t0, ends = min(begin + q.gate_rows, (long)q.T) <= t1;
-    float* to = begins && ends ? q.d_gate + (long)group * q.d : mine + (long)(lists.gate + (begins ? 1 : 0)) * q.d;
-    const bool add = begins && ends && q.accumulate;
+    if constexpr (!TOKEN) {
+      const long begin = (long)group * q.gate_rows;
+      const bool begins = begin >= t_begin, ends = min(begin + q.gate_rows, (long)q.T) <= t_end;
+      float* to = begins && ends ? q.d_gate + (long)group * q.d : mine + (long)(lists.gate + (begins ? 1 : 0)) * q.d;
+      const bool add = begins && ends && q.accumulate;
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-      if (col[k] < q.d) {
-        store8(to + col[k], add ? sum_gate[k] + load8(to + col[k]) : sum_gate[k]);
-        sum_gate[k] = f32x8{};
-      }
+      for (int k = 0; k < K; ++k)
+        if (col[k] < q.d) {
+          store<W>(to + col[k], add ? sum_gate[k] + load_f32<W>(to + col[k]) : sum_gate[k]);
+          sum_gate[k] = vec<W>{};
+        }
+    }
   };
-  for (int t = t0; t < t1; ++t) {
-    const long row = (long)t * q.d;
-    Row8<T> xr[K], yr[K], gr[K], hr[K];
+  struct Row { Piece<T, W> x[K], y[K], g[K], h[K]; } now, next;
+  auto fetch = [&](Row& to, int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      xr[k].v = {};
-      yr[k].v = {};
-      gr[k].v = {};
-      hr[k].v = {};
+      const long at = (long)t * q.d + col[k];
+      to.x[k].v = {};
+      to.y[k].v = {};
+      to.g[k].v = {};
+      to.h[k].v = {};
       if (col[k] < q.d) {
         if (q.w_before) {
-          xr[k].load(x + row + col[k]);
-          hr[k].load(d_h + row + col[k]);
+          to.x[k].load(x + at);
+          to.h[k].load(d_h + at);
         }
-        if (d_out) gr[k].load(d_out + row + col[k]);
-        if (needs_y) yr[k].load(y + row + col[k]);
+        if (d_out) to.g[k].load(d_out + at);
+        if (needs_y) to.y[k].load(y + at);
       }
     }
-    if (q.gate) {
+  };
+  if constexpr (AHEAD) {
+    if (t_begin < t_end) fetch(next, t_begin);
+  }
+  for (int t = t_begin; t < t_end; ++t) {
+    if (grouped) {
       const int group = t / q.gate_rows;
       if (group != open) {
         if (open >= 0) close_gate(open);
         open = group;
+        if constexpr (HOLD && !TOKEN) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-          if (col[k] < q.d) gate[k] = load8(q.gate + (long)group * q.d + col[k]);
+          for (int k = 0; k < K; ++k) gate_held[k] = at_col(q.gate + (long)group * q.d, k);
+        }
       }
     }
-    f32x8 g[K];
+    const long row = (long)t * q.d;
+    if constexpr (AHEAD) {
+      now = next;
+      if (t + 1 < t_end) fetch(next, t + 1);
+    } else {
+      fetch(now, t);
+    }
+    vec<W> token_gate[TOKEN ? K : 1];
+    if constexpr (TOKEN) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) g[k] = gr[k].get();
+      for (int k = 0; k < K; ++k) token_gate[k] = at_col(q.gate + row, k);
+    }
+    auto gate = [&](int k) __attribute__((always_inline)) -> vec<W> {
+      if constexpr (TOKEN) return token_gate[k];
+      else if constexpr (HOLD) return gate_held[k];
+      else return at_col(q.gate + (long)open * q.d, k);
+    };
+    vec<W> g[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) g[k] = now.g[k].get();
     if (q.w_before) {
       float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const f32x8 v = xr[k].get();
-        s[0] += sum8(v * v);
-        s[1] += sum8(hr[k].get() * wb[k] * v);
+        const vec<W> v = now.x[k].get();
+        s[0] += sum_of<W>(v * v);
+        s[1] += sum_of<W>(now.h[k].get() * wb(k) * v);
       }
       team_sum<TS>(s, lds, turn);
-      const float r = 1.0f / sqrtf(s[0] * inv_d + q.eps), mean = s[1] * r * inv_d;
+      const float i = 1.0f / sqrtf(s[0] * inv_d + q.eps), mean = s[1] * i * inv_d;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const f32x8 unit = xr[k].get() * r, dh = hr[k].get();
+        const vec<W> unit = now.x[k].get() * i, dh = now.h[k].get();
         sum_wb[k] += dh * unit;
-        g[k] += (dh * wb[k] - unit * mean) * r;
+        g[k] += (dh * wb(k) - unit * mean) * i;
       }
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (col[k] < q.d) store8(dx + row + col[k], g[k] * q.alpha);
+      if (col[k] < q.d) store<W>(dx + row + col[k], g[k] * q.alpha);
     if (!q.dy) continue;
-    float r = 1.f, mean = 0.f;
+    float i = 1.f, mean = 0.f;
     if (q.w_after) {
       float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const f32x8 v = yr[k].get();
-        s[0] += sum8(v * v);
-        s[1] += sum8((q.gate ? g[k] * gate[k] : g[k]) * wa[k] * v);
+        const vec<W> v = now.y[k].get();
+        s[0] += sum_of<W>(v * v);
+        s[1] += sum_of<W>((q.gate ? g[k] * gate(k) : g[k]) * wa(k) * v);
       }
       team_sum<TS>(s, lds, turn);
-      r = 1.0f / sqrtf(s[0] * inv_d + q.eps);
-      mean = s[1] * r * inv_d;
+      i = 1.0f / sqrtf(s[0] * inv_d + q.eps);
+      mean = s[1] * i * inv_d;
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const f32x8 unit = yr[k].get() * r;
-      f32x8 u = g[k];
+      const vec<W> unit = now.y[k].get() * i;
+      vec<W> u = g[k];
       if (q.gate) {
-        sum_gate[k] += q.w_after ? u * unit * wa[k] : u * unit;
-        u = u * gate[k];
+        const vec<W> d_gate = q.w_after ? u * unit * wa(k) : u * unit;
+        if constexpr (TOKEN) {
+          float* to = q.d_gate + row + col[k];
+          if (col[k] < q.d) store<W>(to, q.accumulate ? d_gate + load_f32<W>(to) : d_gate);
+        } else {
+          sum_gate[k] += d_gate;
+        }
+        u = u * gate(k);
       }
       if (q.w_after) {
         sum_wa[k] += u * unit;
-        u = (u * wa[k] - unit * mean) * r;
+        u = (u * wa(k) - unit * mean) * i;
       }
-      if (col[k] < q.d) store8(dy + row + col[k], u);
+      if (col[k] < q.d) store<W>(dy + row + col[k], u);
     }
   }
-  if (q.gate && open >= 0) close_gate(open);
+  if (grouped && open >= 0) close_gate(open);
 #pragma unroll
   for (int k = 0; k < K; ++k)
     if (col[k] < q.d) {
-      if (q.w_before) store8(mine + (long)lists.wb * q.d + col[k], sum_wb[k]);
-      if (q.w_after) store8(mine + (long)lists.wa * q.d + col[k], sum_wa[k]);
+      if (q.w_before) store<W>(mine + (long)lists.wb * q.d + col[k], sum_wb[k]);
+      if (q.w_after) store<W>(mine + (long)lists.wa * q.d + col[k], sum_wa[k]);
     }
 }
 
@@ -339,47 +428,65 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(NormProblem q, int team
   }
 }
 
-// (threads of a team, steps of each)
-template <typename F> int with_team(int d, F f) {
-  if (d <= 512) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-  if (d <= 1024) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-  if (d <= 2048) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-  if (d <= 4096) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-  if (d <= 8192) return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
-  return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+// threads of a team, elements of each and steps of those, rows at a time
+template <int TS_, int W_, int K_, int R_, bool HOLD_ = true> struct Team { static constexpr int TS = TS_, W = W_, K = K_, R = R_; static constexpr bool HOLD = HOLD_; };
+template <typename F> int with_fwd_team(int d, F f) {
+  if (d <= 512) return f(Team<64, 8, 1, 4>());
+  if (d <= 1024) return f(Team<256, 4, 1, 4>());
+  if (d <= 2048) return f(Team<256, 8, 1, 4>());
+  if (d <= 4096) return f(Team<512, 8, 1, 4>());
+  if (d <= 8192) return f(Team<1024, 8, 1, 2>());
+  return f(Team<1024, 8, 2, 1>());
+}
+// Backward (8192 x 4096, bf16, all parts, 256 or 512 teams, us): 256 threads, 16 elements each 91, with the next row ahead 84; 512 threads, 8 elements, a row
+// ahead 82 (4.9 TB/s, what a copy takes); 1024 threads 109 to 127; two to four rows at a time instead of one ahead 103 to 141.
+template <typename F> int with_bwd_team(int d, F f) {
+  if (d <= 512) return f(Team<64, 8, 1, 1>());
+  if (d <= 1024) return f(Team<64, 8, 2, 1>());
+  if (d <= 2048) return f(Team<256, 8, 1, 1>());
+  if (d <= 4096) return f(Team<512, 8, 1, 1>());
+  if (d <= 8192) return f(Team<1024, 8, 1, 1>());
+  return f(Team<1024, 8, 2, 1, false>());
 }
 
 }  // namespace
 
 NormPlan norm_bwd_plan(int T, int d, moe_dtype dt, bool after, bool gate, bool before) {
   NormPlan p{};
-  const int most = d <= 1024 ? 2048 : 512;
-  p.rows = cdiv(T, most);
-  if (p.rows < 4) p.rows = T < 4 ? (T < 1 ? 1 : T) : 4;
+  // as many teams as run at a time; where a team would have a row or two, one each
+  const int most = d <= 1024 ? 2048 : d <= 2048 ? 512 : 256;
+  p.rows = T <= 1024 ? 1 : cdiv(T, most);
   p.teams = cdiv(T, p.rows);
   p.bytes = (size_t)p.teams * parts_of(after, gate, before).lists * d * 4 + 256;
   return p;
 }
 
 int launch_norm_fwd(const NormProblem& q, hipStream_t s) {
-  return with_team(q.d, [&](auto ts, auto k) {
-    constexpr int TS = decltype(ts)::value, K = decltype(k)::value, per = block_threads(TS) / TS;
-    const int most = 256 * 2048 / TS;
-    const int teams = q.T < most ? q.T : most;
-    const dim3 grid((unsigned)cdiv(teams, per)), block(block_threads(TS));
-    if (q.dt == MOE_F32) norm_fwd_kernel<float, TS, K><<<grid, block, 0, s>>>(q, teams);
-    else norm_fwd_kernel<bf16, TS, K><<<grid, block, 0, s>>>(q, teams);
+  return with_fwd_team(q.d, [&](auto team) {
+    typedef decltype(team) C;
+    constexpr int per = block_threads(C::TS) / C::TS;
+    const int most = 256 * 2048 / C::TS, groups = cdiv(q.T, C::R);
+    const int teams = groups < most ? groups : most;
+    const dim3 grid((unsigned)cdiv(teams, per)), block(block_threads(C::TS));
+    if (q.dt == MOE_F32) norm_fwd_kernel<float, C::TS, C::W, C::K, C::R><<<grid, block, 0, s>>>(q, teams);
+    else norm_fwd_kernel<bf16, C::TS, C::W, C::K, C::R><<<grid, block, 0, s>>>(q, teams);
     MOE_LAUNCH_CHECK();
     return (int)MOE_OK;
   });
 }
 
 int launch_norm_bwd(const NormProblem& q, const NormPlan& p, float* ws, hipStream_t s) {
-  const int rc = with_team(q.d, [&](auto ts, auto k) {
-    constexpr int TS = decltype(ts)::value, K = decltype(k)::value, per = block_threads(TS) / TS;
-    const dim3 grid((unsigned)cdiv(p.teams, per)), block(block_threads(TS));
-    if (q.dt == MOE_F32) norm_bwd_kernel<float, TS, K><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
-    else norm_bwd_kernel<bf16, TS, K><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
+  const int rc = with_bwd_team(q.d, [&](auto team) {
+    typedef decltype(team) C;
+    constexpr int per = block_threads(C::TS) / C::TS;
+    // (a row ahead takes registers: twice as many in fp32)
+    constexpr bool AHEAD16 = C::TS < 1024, AHEAD32 = AHEAD16 && C::K == 1;
+    const dim3 grid((unsigned)cdiv(p.teams, per)), block(block_threads(C::TS));
+    const bool token = q.gate && q.gate_rows == 1;
+    if (q.dt == MOE_F32 && !token) norm_bwd_kernel<float, C::TS, C::W, C::K, C::HOLD, false, AHEAD32><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
+    else if (q.dt == MOE_F32) norm_bwd_kernel<float, C::TS, C::W, C::K, C::HOLD, true, AHEAD32><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
+    else if (!token) norm_bwd_kernel<bf16, C::TS, C::W, C::K, C::HOLD, false, AHEAD16><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
+    else norm_bwd_kernel<bf16, C::TS, C::W, C::K, C::HOLD, true, AHEAD16><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
     MOE_LAUNCH_CHECK();
     return (int)MOE_OK;
   });
