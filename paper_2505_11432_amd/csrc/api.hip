@@ -1,6 +1,7 @@
 // extern "C" entry points: argument validation (before any HIP call), workspace carving and the
 // sequencing of kernels for each call.  Declarations and contracts are in include/moe.h.
 #include "moe_common.h"
+#include "newton_schulz.h"
 
 namespace moe {
 
@@ -170,6 +171,8 @@ int moe_init(void) {
   int rc = mfma_configure_all();
   if (rc != MOE_OK) return rc;
   rc = gemm_f32_split_configure();
+  if (rc != MOE_OK) return rc;
+  rc = orth_configure();
   if (rc != MOE_OK) return rc;
   return route_noalloc_prepare();
 }

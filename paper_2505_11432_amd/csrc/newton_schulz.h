@@ -22,12 +22,14 @@ struct OrthPlan {
   int R, C, S;                               // padded rows, columns, and the smaller of them
   int count;                                 // matrices at a time
   int norm_blocks;
-  size_t hi, lo, t, other, gram, sums;       // offsets of a piece's buffers
+  bool pairs;                                // steps taken two at a time
+  size_t hi, lo, t, other, gram, parts, sums;      // offsets of a piece's buffers
   size_t gram_one;                           // bytes of one list of Gram matrices
   size_t bytes;
 };
 bool orth_takes(int batch, int rows, int cols, int piece);
 OrthPlan orth_plan(int batch, int rows, int cols, int piece);
+int orth_configure();                        // per-device set-up (moe_init)
 bool orth_coefficients_ok(const OrthCoef* c, int steps);        // every matrix that is kept fits 16 bits
 int launch_orth(const MuonProblem& q, const OrthPlan& p, char* ws, hipStream_t s);
 

@@ -151,197 +151,398 @@ __global__ void __launch_bounds__(256) start_kernel(MuonProblem q, OrthPlan p, i
 }
 
 // ---- products --------------------------------------------------------------------------------
-// C = e1 E1 + e2 E2 + f L R^T, both operands [rows][K] of fp16; a list of matrices, `one` elements from each to the next.
+// C = e1 E1 + e2 E2 + f L R^T + diagonal I, both operands [rows][K] of fp16; a list of matrices, `one` elements from each to the next.
 struct Product {
   const half* l; const half* r; long l_one, r_one;
   int ldl, ldr, K;
-  int tiles_m, tiles_n;                     // SYMMETRIC: tiles_m of both, the lower ones are computed
-  const half* e1; const half* e2; float f1, f2, f;
-  half* c; half* c_lo; half* ct; long c_one; int ldc, ldt;      // ct: the transposed result
+  int M, N;                                 // multiples of 128; SYMMETRIC: M of both
+  const half* e1; const half* e2; float f1, f2, f, diagonal;
+  half* c; half* c_lo; half* ct; long c_one; int ldc, ldt;      // c_lo: what c leaves of the result; ct: the transposed result
+  int full, split;                          // the tiles from `full` on are cut into `split` parts along K, which go to
+  float* parts;
 };
 enum Result { SYMMETRIC, KEPT, MUON_UPDATE, OUT_F32, OUT_BF16 };
 
-constexpr int BM = 128, BN = 128, BK = 64, NW = 4;
-typedef KTile<BM, BK> Tile;
-constexpr int kStage = 2 * Tile::BYTES;
+// Tiles of 128 x 256, a wave has 64 x 128 of them; four waves, two workgroups per CU, so that one multiplies while the other stores its result or waits.
+constexpr int BM = 128, BN = 256, BK = 32, NW = 4, STAGES = 3;
+constexpr int FM = 4, FN = 8;               // 16 x 16 parts of a wave
+typedef KTile<BM, BK> TileL;
+typedef KTile<BN, BK> TileR;
+constexpr int kStage = TileL::BYTES + TileR::BYTES;
 constexpr int kPitch = BM + 8;              // of the transposed tile in LDS, elements
-static_assert(BN * kPitch * 2 <= 2 * kStage, "the transposed tile takes the place of the operands");
+constexpr int kProductLds = STAGES * kStage;
+static_assert(BN * kPitch * 2 <= kProductLds, "the transposed tile takes the place of the operands");
+static_assert(2 * kProductLds <= 160 * 1024, "two workgroups share a CU's LDS");
+constexpr int kPartFloats = BM * BN;
 
-template <Result RES>
-__global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProblem mu, int first) {
-  __shared__ __attribute__((aligned(256))) char smem[2 * kStage];
-  const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int wm = wave >> 1, wn = wave & 1;
-  const int per = RES == SYMMETRIC ? q.tiles_m * (q.tiles_m + 1) / 2 : q.tiles_m * q.tiles_n;
-  const int which = blockIdx.x / per;
-  int at = blockIdx.x - which * per, mt, nt;
+// Which tile: matrix, row and column.  Half tiles of the lower triangle of 256 x 256 squares (SYMMETRIC), or bands of eight rows of tiles, column by column.
+struct Place { int which, mt, nt; };
+template <Result RES> __host__ __device__ __forceinline__ int tiles_of(const Product& q) {
+  const int tm = (q.M + BM - 1) / BM, tn = (q.N + BN - 1) / BN;
+  return RES == SYMMETRIC ? tn * (tn + 1) : tm * tn;
+}
+template <Result RES> __device__ __forceinline__ Place place_of(const Product& q, int item) {
+  const int per = tiles_of<RES>(q), which = item / per;
+  int at = item - which * per;
   if constexpr (RES == SYMMETRIC) {
-    mt = (int)((sqrtf(8.f * (float)at + 1.f) - 1.f) * 0.5f);
-    while ((mt + 1) * (mt + 2) / 2 <= at) ++mt;
-    while (mt * (mt + 1) / 2 > at) --mt;
-    nt = at - mt * (mt + 1) / 2;
+    const int pair = at >> 1;
+    int p = (int)((sqrtf(8.f * (float)pair + 1.f) - 1.f) * 0.5f);
+    while ((p + 1) * (p + 2) / 2 <= pair) ++p;
+    while (p * (p + 1) / 2 > pair) --p;
+    return {which, p * 2 + (at & 1), pair - p * (p + 1) / 2};
   } else {
-    mt = at / q.tiles_n;
-    nt = at - mt * q.tiles_n;
+    const int tm = (q.M + BM - 1) / BM, tn = (q.N + BN - 1) / BN, band = at / (8 * tn), rows = min(8, tm - band * 8);
+    at -= band * 8 * tn;
+    return {which, band * 8 + at % rows, at / rows};
   }
-  const char* l = uniform_ptr(reinterpret_cast<const char*>(q.l + which * q.l_one + (long)mt * BM * q.ldl));
-  const char* r = uniform_ptr(reinterpret_cast<const char*>(q.r + which * q.r_one + (long)nt * BN * q.ldr));
-  // loads: 16 slots of 1 KB per operand tile, four per wave
-  constexpr int SLOTS = Tile::BYTES / 1024 / NW;
-  unsigned offl[SLOTS], offr[SLOTS];
-#pragma unroll
-  for (int j = 0; j < SLOTS; ++j) {
-    const int row = (wave + j * NW) * Tile::ROWS_PER_DMA + lane / Tile::CPR, chunk = (lane % Tile::CPR) ^ Tile::swz(row);
-    offl[j] = (unsigned)row * (unsigned)q.ldl * 2u + (unsigned)chunk * 16u;
-    offr[j] = (unsigned)row * (unsigned)q.ldr * 2u + (unsigned)chunk * 16u;
-  }
-  auto issue = [&](int s) __attribute__((always_inline)) {
-    const unsigned to = lds + (unsigned)(s & 1) * kStage + (unsigned)wave * 1024u;
-#pragma unroll
-    for (int j = 0; j < SLOTS; ++j) {
-      dma16s(l + (long)s * BK * 2, offl[j], to + (unsigned)j * NW * 1024u);
-      dma16s(r + (long)s * BK * 2, offr[j], to + Tile::BYTES + (unsigned)j * NW * 1024u);
-    }
-  };
-  f32x4 acc[4][4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int steps = q.K / BK;
-  const unsigned fa = mfma::frag_origin<mfma::KMAJOR, BM, BK>(wm * 64, lane), fb = Tile::BYTES + mfma::frag_origin<mfma::KMAJOR, BN, BK>(wn * 64, lane);
-  issue(0);
-  for (int s = 0; s < steps; ++s) {
-    wait_vmcnt<0>();
-    __syncthreads();
-    if (s + 1 < steps) issue(s + 1);
-    const unsigned base = lds + (unsigned)(s & 1) * kStage;
-#pragma unroll
-    for (int kk = 0; kk < BK / 32; ++kk) {
-      f16x8 a[4], b[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, BM, BK>(base + fa, i, kk));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, BN, BK>(base + fb, j, kk));
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], a[i], acc[i][j], 0, 0, 0);
-    }
-  }
-  __syncthreads();                          // the operands' LDS is free
-  // a lane holds row lane % 16 and columns 4 (lane / 16) .. + 3 of every 16 x 16 part
+}
+
+// The result of FI x FN parts of a wave, its rows from part i0 on: a lane holds row lane % 16 and columns 4 (lane / 16) .. + 3 of every 16 x 16 part.
+template <Result RES, int FI>
+__device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, int first, Place at, const f32x4 (&acc)[FI][FN], int i0, char* smem) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+  const int row0 = at.mt * BM, col0 = at.nt * BN;
   half* turned = reinterpret_cast<half*>(smem);
-  const int row0 = mt * BM, col0 = nt * BN;
+  if (col0 + wn * 128 < q.N) {              // (the last tile's second half may lie outside)
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < FI; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int lr = wm * 64 + i * 16 + (lane & 15), lc = wn * 64 + j * 16 + (lane >> 4) * 4;
-      const long to = which * q.c_one + (long)(row0 + lr) * q.ldc + col0 + lc;
-      f32x4 v = acc[i][j] * q.f;
-      if (q.e1) v += __builtin_convertvector(*reinterpret_cast<const f16x4*>(q.e1 + to), f32x4) * q.f1;
-      if (q.e2) v += __builtin_convertvector(*reinterpret_cast<const f16x4*>(q.e2 + to), f32x4) * q.f2;
-      if constexpr (RES == SYMMETRIC || RES == KEPT) {
-        const f16x4 h = __builtin_convertvector(v, f16x4);
-        *reinterpret_cast<f16x4*>(q.c + to) = h;
-        if constexpr (RES == KEPT) {
-          const f16x4 low = __builtin_convertvector((v - __builtin_convertvector(h, f32x4)) * kLow, f16x4);
-          *reinterpret_cast<f16x4*>(q.c_lo + to) = low;
+      for (int j = 0; j < FN; ++j) {
+        const int lr = wm * 64 + (i0 + i) * 16 + (lane & 15), lc = wn * 128 + j * 16 + (lane >> 4) * 4;
+        const int row = row0 + lr, col = col0 + lc;
+        const long to = at.which * q.c_one + (long)row * q.ldc + col;
+        f32x4 v = acc[i][j] * q.f;
+        if (q.e1) v += __builtin_convertvector(*reinterpret_cast<const f16x4*>(q.e1 + to), f32x4) * q.f1;
+        if (q.e2) v += __builtin_convertvector(*reinterpret_cast<const f16x4*>(q.e2 + to), f32x4) * q.f2;
+        if constexpr (RES == SYMMETRIC) {
+          const unsigned k = (unsigned)(row - col);
+          if (k < 4u) {                     // (no dynamic index into a vector)
+            v[0] += k == 0 ? q.diagonal : 0.f;
+            v[1] += k == 1 ? q.diagonal : 0.f;
+            v[2] += k == 2 ? q.diagonal : 0.f;
+            v[3] += k == 3 ? q.diagonal : 0.f;
+          }
         }
+        if constexpr (RES == SYMMETRIC || RES == KEPT) {
+          const f16x4 h = __builtin_convertvector(v, f16x4);
+          *reinterpret_cast<f16x4*>(q.c + to) = h;
+          if constexpr (RES == KEPT) {
+            const f16x4 low = __builtin_convertvector((v - __builtin_convertvector(h, f32x4)) * kLow, f16x4);
+            *reinterpret_cast<f16x4*>(q.c_lo + to) = low;
+          }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) turned[(lc + k) * kPitch + lr] = h[k];
-      } else {
-        const int row = row0 + lr, n = min(mu.cols - col0 - lc, 4);
-        if (row < mu.rows && n > 0) {
-          const long o = ((first + (long)which) * mu.rows + row) * mu.cols + col0 + lc;
-          if constexpr (RES == MUON_UPDATE) {
-            const float factor = factor_of(mu.factor), lr_now = *mu.lr;
-            if (factor == factor) {
-              const float keep = (float)(1.0 - (double)lr_now * mu.decay), step = lr_now * mu.scale * (1.0f / kScale);
-              const f32x4 x = load4(mu.p + o, n) * keep - v * step;
-              store4(mu.p + o, n, x);
-              if (mu.w) store4(static_cast<bf16*>(mu.w) + o, n, x);
+          for (int k = 0; k < 4; ++k) turned[(lc + k) * kPitch + lr] = h[k];
+        } else {
+          const int n = min(mu.cols - col, 4);
+          if (row < mu.rows && n > 0) {
+            const long o = ((first + (long)at.which) * mu.rows + row) * mu.cols + col;
+            if constexpr (RES == MUON_UPDATE) {
+              const float factor = factor_of(mu.factor), lr_now = *mu.lr;
+              if (factor == factor) {
+                const float keep = (float)(1.0 - (double)lr_now * mu.decay), step = lr_now * mu.scale * (1.0f / kScale);
+                const f32x4 x = load4(mu.p + o, n) * keep - v * step;
+                store4(mu.p + o, n, x);
+                if (mu.w) store4(static_cast<bf16*>(mu.w) + o, n, x);
+              }
+            } else {
+              v *= 1.0f / kScale;
+              if constexpr (RES == OUT_F32) store4(static_cast<float*>(mu.out) + o, n, v);
+              else store4(static_cast<bf16*>(mu.out) + o, n, v);
             }
-          } else {
-            v *= 1.0f / kScale;
-            if constexpr (RES == OUT_F32) store4(static_cast<float*>(mu.out) + o, n, v);
-            else store4(static_cast<bf16*>(mu.out) + o, n, v);
           }
         }
       }
-    }
+  }
   if constexpr (RES == SYMMETRIC || RES == KEPT) {
+    // the transposed result, eight rows of the tile at a time; a square on the diagonal holds both halves
     half* t = RES == SYMMETRIC ? q.c : q.ct;
     const int ldt = RES == SYMMETRIC ? q.ldc : q.ldt;
-    if (RES == SYMMETRIC && mt == nt) return;          // (the tile holds both halves)
+    if (RES == SYMMETRIC && (at.mt >> 1) == at.nt) return;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < BM * BN / 8 / (NW * 64); ++i) {
-      const int unit = threadIdx.x + i * NW * 64, c = unit / (BM / 8), x = unit % (BM / 8) * 8;
-      *reinterpret_cast<f16x8*>(t + which * q.c_one + (long)(col0 + c) * ldt + row0 + x) = *reinterpret_cast<const f16x8*>(&turned[c * kPitch + x]);
+    const int cols = min(BN, q.N - col0);
+    constexpr int GROUPS = FI * 2 * 2;      // of eight rows
+    for (int unit = threadIdx.x; unit < cols * GROUPS; unit += NW * 64) {
+      const int c = unit / GROUPS, g = unit % GROUPS;
+      const int x = FI == FM ? g * 8 : (g >> 1) * 64 + i0 * 16 + (g & 1) * 8;
+      *reinterpret_cast<f16x8*>(t + at.which * q.c_one + (long)(col0 + c) * ldt + row0 + x) = *reinterpret_cast<const f16x8*>(&turned[c * kPitch + x]);
     }
   }
 }
 
-template <Result RES> int product(const Product& q, const MuonProblem& mu, int first, int count, hipStream_t s) {
-  const long per = RES == SYMMETRIC ? (long)q.tiles_m * (q.tiles_m + 1) / 2 : (long)q.tiles_m * q.tiles_n;
-  product_kernel<RES><<<dim3((unsigned)(per * count)), dim3(NW * 64), 0, s>>>(q, mu, first);
+template <Result RES>
+__global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProblem mu, int first) {
+  extern __shared__ __attribute__((aligned(256))) char smem[];
+  const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+  int item = blockIdx.x, part = -1;
+  int step0 = 0, steps = q.K / BK;
+  if (item >= q.full) {
+    part = item - q.full;
+    item = q.full + part / q.split;
+    const int n = part % q.split;
+    step0 = n * steps / q.split;
+    steps = (n + 1) * steps / q.split - step0;
+  } else {
+    // Workgroup b runs on XCD b % 8: 64 tiles that are neighbours go to the 64 places of an XCD at a time.
+    const int round = item / 512, in_round = item % 512, size = min(512, q.full - round * 512), share = size / 8;
+    if (in_round < share * 8) item = round * 512 + in_round % 8 * share + in_round / 8;
+  }
+  const Place at = place_of<RES>(q, item);
+  if (RES == SYMMETRIC && at.mt * BM >= q.M) return;                     // (the second half of the last square)
+  const char* l = uniform_ptr(reinterpret_cast<const char*>(q.l + at.which * q.l_one + (long)at.mt * BM * q.ldl + (long)step0 * BK));
+  const char* r = uniform_ptr(reinterpret_cast<const char*>(q.r + at.which * q.r_one + (long)at.nt * BN * q.ldr + (long)step0 * BK));
+  // loads: slots of 1 KB, two of the left and four of the right operand per wave and step
+  constexpr int SL = TileL::BYTES / 1024 / NW, SR = TileR::BYTES / 1024 / NW;
+  unsigned offl[SL], offr[SR];
+  const int rows_r = (RES == SYMMETRIC ? q.M : q.N) - at.nt * BN;        // rows past the last one repeat it
+#pragma unroll
+  for (int j = 0; j < SL; ++j) {
+    const int row = (wave + j * NW) * TileL::ROWS_PER_DMA + lane / TileL::CPR, chunk = (lane % TileL::CPR) ^ TileL::swz(row);
+    offl[j] = (unsigned)row * (unsigned)q.ldl * 2u + (unsigned)chunk * 16u;
+  }
+#pragma unroll
+  for (int j = 0; j < SR; ++j) {
+    const int row = (wave + j * NW) * TileR::ROWS_PER_DMA + lane / TileR::CPR, chunk = (lane % TileR::CPR) ^ TileR::swz(row);
+    offr[j] = (unsigned)min(row, rows_r - 1) * (unsigned)q.ldr * 2u + (unsigned)chunk * 16u;
+  }
+  auto issue = [&](int s, int slot) __attribute__((always_inline)) {
+    const unsigned to = lds + (unsigned)slot * kStage + (unsigned)wave * 1024u;
+    const char* lk = l + (long)s * BK * 2;
+    const char* rk = r + (long)s * BK * 2;
+#pragma unroll
+    for (int j = 0; j < SL; ++j) dma16s(lk, offl[j], to + (unsigned)j * NW * 1024u);
+#pragma unroll
+    for (int j = 0; j < SR; ++j) dma16s(rk, offr[j], to + TileL::BYTES + (unsigned)j * NW * 1024u);
+  };
+  constexpr int LOADS = SL + SR;
+  f32x4 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const unsigned fa = mfma::frag_origin<mfma::KMAJOR, BM, BK>(wm * 64, lane), fb = TileL::BYTES + mfma::frag_origin<mfma::KMAJOR, BN, BK>(wn * 128, lane);
+  // A step has two phases: the wave's left fragments are held for both, its right ones pass through four at a time, and each phase's are read while the one
+  // before multiplies.  The barrier in between: every wave's loads of step s + 1 have landed, and every wave has read all of step s, whose slot
+  // the loads of step s + STAGES then fill.
+  f16x8 held[2][FM], strm[2][FN / 2];
+  auto read_held = [&](unsigned base, int set) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) held[set][i] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, BM, BK>(base + fa, i, 0));
+  };
+  auto read_strm = [&](unsigned base, int which) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < FN / 2; ++j) strm[which][j] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, BN, BK>(base + fb, which * (FN / 2) + j, 0));
+  };
+  auto multiply = [&](int set, int which) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < FN / 2; ++j)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+        acc[i][which * (FN / 2) + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(strm[which][j], held[set][i], acc[i][which * (FN / 2) + j], 0, 0, 0);
+  };
+  auto open = [&](int s) __attribute__((always_inline)) {      // step s can be read
+    if (s + 1 < steps) wait_vmcnt<LOADS>(); else wait_vmcnt<0>();
+    __syncthreads();
+  };
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s)
+    if (s < steps) issue(s, s);
+  open(0);
+  if (STAGES - 1 < steps) issue(STAGES - 1, STAGES - 1);
+  unsigned at_lds = lds;                    // slot of the step
+  int slot = 0;
+  read_held(at_lds, 0);
+  read_strm(at_lds, 0);
+  auto step = [&](int s, auto parity) __attribute__((always_inline)) {
+    constexpr int P = decltype(parity)::value;
+    read_strm(at_lds, 1);
+    multiply(P, 0);
+    if (s + 1 < steps) {
+      open(s + 1);
+      if (s + STAGES < steps) issue(s + STAGES, slot);
+      slot = slot + 1 == STAGES ? 0 : slot + 1;
+      at_lds = lds + (unsigned)slot * kStage;
+      read_held(at_lds, P ^ 1);
+      read_strm(at_lds, 0);
+    }
+    multiply(P, 1);
+  };
+  int s = 0;
+  for (; s + 1 < steps; s += 2) {
+    step(s, std::integral_constant<int, 0>());
+    step(s + 1, std::integral_constant<int, 1>());
+  }
+  if (s < steps) step(s, std::integral_constant<int, 0>());
+  if (part >= 0) {
+    f32x4* to = reinterpret_cast<f32x4*>(q.parts + (long)part * kPartFloats) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) to[(i * FN + j) * (NW * 64)] = acc[i][j];
+    return;
+  }
+  __syncthreads();                          // the operands' LDS is free
+  finish<RES, FM>(q, mu, first, at, acc, 0, smem);
+}
+
+// Adds the parts of the cut tiles and finishes them: four workgroups per tile, a quarter of each wave's rows each.
+template <Result RES>
+__global__ void __launch_bounds__(NW * 64) join_kernel(Product q, MuonProblem mu, int first) {
+  extern __shared__ __attribute__((aligned(256))) char smem[];
+  const int cut = blockIdx.x / FM, i0 = blockIdx.x % FM;
+  const Place at = place_of<RES>(q, q.full + cut);
+  if (RES == SYMMETRIC && at.mt * BM >= q.M) return;
+  f32x4 acc[1][FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) acc[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const f32x4* from = reinterpret_cast<const f32x4*>(q.parts + (long)cut * q.split * kPartFloats) + threadIdx.x + i0 * FN * (NW * 64);
+#pragma unroll 2
+  for (int n = 0; n < q.split; ++n, from += kPartFloats / 4)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[0][j] += from[j * (NW * 64)];
+  finish<RES, 1>(q, mu, first, at, acc, i0, smem);
+}
+
+// Which tiles are cut along K: those behind the last whole round of workgroups, where that is the faster way.  In units of a step's time (two workgroups per
+// CU, 0.4 us): a round takes its steps, adding parts up a launch and a read of 128 KB per part.
+struct Cut { int full, split; };
+Cut cut_of(long tiles, int steps, long most_parts) {
+  const int places = 512;
+  Cut best{(int)tiles, 1};
+  const int full = (int)(tiles / places * places), rem = (int)(tiles - full);
+  if (rem == 0) return best;
+  // (workgroups alone on their CU take about 0.6 of the time)
+  auto round = [&](long n, double s) { return n <= 256 ? 0.6 * s : s; };
+  double least = round(rem, steps);
+  for (int split = 2; split <= 16; ++split) {
+    const long parts = (long)rem * split;
+    if (steps / split < 4 || parts > most_parts) break;
+    const double each = (double)steps / split;
+    const double time = (parts / places) * each + round(parts % places, parts % places ? each : 0) + 14 + 0.8 * split;
+    if (time < least) {
+      least = time;
+      best = {full, split};
+    }
+  }
+  return best;
+}
+constexpr int kMostParts = 1024;            // of a launch: 128 MB
+
+template <Result RES> int product(Product q, const MuonProblem& mu, int first, int count, float* parts, hipStream_t s) {
+  const long tiles = (long)tiles_of<RES>(q) * count;
+  const Cut cut = cut_of(tiles, q.K / BK, kMostParts);
+  q.full = cut.full;
+  q.split = cut.split;
+  q.parts = parts;
+  const int rem = (int)(tiles - cut.full);
+  product_kernel<RES><<<dim3((unsigned)(cut.full + (long)rem * cut.split)), dim3(NW * 64), kProductLds, s>>>(q, mu, first);
   MOE_LAUNCH_CHECK();
+  if (rem > 0) {
+    join_kernel<RES><<<dim3((unsigned)rem * FM), dim3(NW * 64), BN * kPitch * 2, s>>>(q, mu, first);
+    MOE_LAUNCH_CHECK();
+  }
   return MOE_OK;
 }
 
-// the products of the steps on `count` matrices from `first` on, whose X is in the workspace
-int run_steps(const MuonProblem& mu, const OrthPlan& p, int first, int count, char* ws, hipStream_t s) {
+// Every product's dynamic-LDS limit is raised once per device; moe_init does it ahead of a graph capture.
+}  // namespace
+int orth_configure() {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  MOE_HIP_TRY(hipGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return MOE_ERR_UNSUPPORTED;
+  if (done.load(std::memory_order_acquire) >> dev & 1) return MOE_OK;
+  for (const void* k : {(const void*)product_kernel<SYMMETRIC>, (const void*)product_kernel<KEPT>, (const void*)product_kernel<MUON_UPDATE>,
+                        (const void*)product_kernel<OUT_F32>, (const void*)product_kernel<OUT_BF16>, (const void*)join_kernel<SYMMETRIC>,
+                        (const void*)join_kernel<KEPT>, (const void*)join_kernel<MUON_UPDATE>, (const void*)join_kernel<OUT_F32>,
+                        (const void*)join_kernel<OUT_BF16>})
+    MOE_HIP_TRY(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kProductLds));
+  done.fetch_or(1ull << dev, std::memory_order_release);
+  return MOE_OK;
+}
+namespace {
+
+// The steps of a piece, each alone or two on the powers of one A.  With A' = A - c I a step's polynomial is
+//   p(A) = s I + R,  s = p(c),  R = (b + 2 c2 c) A' + c2 A'^2
+// The centre c is 0 at first and near the singular values' squares in late steps, where what is kept of A and R is then small (512 x 512, flat
+// spectrum: error 1.5e-3 -> 8e-4).  Two steps share one A and one product with X, which pays where X is large against A; A of the second one is
+//   A2' = (s I + R)^2 (c I + A') - c' I,  made as  T = s A' + c R + R A',  A2' = s T + s c R + R T + (s^2 c - c') I
+// and both together multiply X with s s' I + (s R' + s' R + R' R).  The first two and the last two are taken so: an error of A2' passes through one
+// polynomial more, which matters least there (steps 0 1, 2, 3 4: errors up to 2.6e-3 for singular values that fall as i^-1.5).
+double centre_of(int k, int steps) { return k < 3 ? 0.0 : k + 1 == steps ? 0.8 : 0.5; }
+bool pair_at(int k, int steps) { return k + 1 < steps && (k == 0 || k + 2 == steps); }
+
+int run_steps(const MuonProblem& mu, const OrthPlan& p, int first, int count, char* ws, hipStream_t stream) {
   half* hi = reinterpret_cast<half*>(ws + p.hi);
   half* t = reinterpret_cast<half*>(ws + p.t);
   half* lo = reinterpret_cast<half*>(ws + p.lo);
   half* other = reinterpret_cast<half*>(ws + p.other);          // the next one of the orientation that a step reads
-  half* gram[2] = {reinterpret_cast<half*>(ws + p.gram), reinterpret_cast<half*>(ws + p.gram + p.gram_one)};
+  half* gram[4];
+  for (int i = 0; i < 4; ++i) gram[i] = reinterpret_cast<half*>(ws + p.gram + i * p.gram_one);
+  float* parts = reinterpret_cast<float*>(ws + p.parts);
   const bool tall = mu.rows > mu.cols;
   const long one = (long)p.R * p.C, gram_size = (long)p.S * p.S;
+  // C = f1 E1 + f2 E2 + f L R + diagonal I of symmetric matrices, in units of what is kept
+  auto symmetric = [&](int to, int l, int r, double f, int e1, double f1, int e2, double f2, double diagonal) -> int {
+    Product q{};
+    q.l = gram[l]; q.r = gram[r];
+    q.l_one = q.r_one = q.c_one = gram_size;
+    q.ldl = q.ldr = q.K = q.ldc = q.M = q.N = p.S;
+    q.f = (float)(f / kScale);
+    if (e1 >= 0) { q.e1 = gram[e1]; q.f1 = (float)f1; }
+    if (e2 >= 0) { q.e2 = gram[e2]; q.f2 = (float)f2; }
+    q.diagonal = (float)(diagonal * kScale);
+    q.c = gram[to];
+    return product<SYMMETRIC>(q, mu, first, count, parts, stream);
+  };
   for (int k = 0; k < mu.steps; ++k) {
-    const OrthCoef c = mu.coef[k];
+    OrthCoef c = mu.coef[k];
+    double mid = centre_of(k, mu.steps), s = c.a + c.b * mid + c.c * mid * mid;
     Product a{};
     a.l = a.r = tall ? t : hi;
     a.l_one = a.r_one = one;
     a.ldl = a.ldr = a.K = tall ? p.R : p.C;
-    a.tiles_m = a.tiles_n = p.S / BM;
+    a.M = a.N = p.S;
     a.f = 1.0f / kScale;
+    a.diagonal = (float)(-mid * kScale);
     a.c = gram[0]; a.c_one = gram_size; a.ldc = p.S;
-    if (const int rc = product<SYMMETRIC>(a, mu, first, count, s)) return rc;
-    Product b = a;
-    b.l = b.r = gram[0];
-    b.l_one = b.r_one = gram_size;
-    b.ldl = b.ldr = b.K = p.S;
-    b.e1 = gram[0]; b.f1 = (float)c.b;
-    b.f = (float)c.c / kScale;
-    b.c = gram[1];
-    if (const int rc = product<SYMMETRIC>(b, mu, first, count, s)) return rc;
+    if (const int rc = product<SYMMETRIC>(a, mu, first, count, parts, stream)) return rc;
+    if (const int rc = symmetric(1, 0, 0, c.c, 0, c.b + 2 * c.c * mid, -1, 0, 0)) return rc;
+    int r = 1;
+    if (p.pairs && pair_at(k, mu.steps)) {
+      const double mid2 = centre_of(++k, mu.steps);
+      if (const int rc = symmetric(2, 1, 0, 1, 0, s, mid != 0 ? 1 : -1, mid, 0)) return rc;
+      if (const int rc = symmetric(3, 1, 2, 1, 2, s, mid != 0 ? 1 : -1, s * mid, s * s * mid - mid2)) return rc;
+      c = mu.coef[k];
+      const double s2 = c.a + c.b * mid2 + c.c * mid2 * mid2;
+      if (const int rc = symmetric(2, 3, 3, c.c, 3, c.b + 2 * c.c * mid2, -1, 0, 0)) return rc;
+      if (const int rc = symmetric(0, 2, 1, 1, 2, s, 1, s2, 0)) return rc;
+      s *= s2;
+      r = 0;
+    }
     Product x{};
-    x.l = tall ? hi : gram[1];
+    x.l = tall ? hi : gram[r];
     x.l_one = tall ? one : gram_size;
-    x.r = tall ? gram[1] : t;
+    x.r = tall ? gram[r] : t;
     x.r_one = tall ? gram_size : one;
     x.ldl = x.ldr = x.K = p.S;
-    x.tiles_m = p.R / BM; x.tiles_n = p.C / BN;
-    x.e1 = hi; x.f1 = (float)c.a;
-    x.e2 = lo; x.f2 = (float)c.a / kLow;
+    x.M = p.R; x.N = p.C;
+    x.e1 = hi; x.f1 = (float)s;
+    x.e2 = lo; x.f2 = (float)(s / kLow);
     x.f = 1.0f / kScale;
     x.c_one = one; x.ldc = p.C; x.ldt = p.R;
     if (k + 1 < mu.steps) {
       x.c = tall ? other : hi;
       x.c_lo = lo;
       x.ct = tall ? t : other;
-      if (const int rc = product<KEPT>(x, mu, first, count, s)) return rc;
+      if (const int rc = product<KEPT>(x, mu, first, count, parts, stream)) return rc;
       half*& read = tall ? hi : t;
       half* was = read;
       read = other;
       other = was;
     } else {
-      const int rc = !mu.out ? product<MUON_UPDATE>(x, mu, first, count, s)
-                             : mu.out_dt == MOE_F32 ? product<OUT_F32>(x, mu, first, count, s) : product<OUT_BF16>(x, mu, first, count, s);
+      const int rc = !mu.out ? product<MUON_UPDATE>(x, mu, first, count, parts, stream)
+                             : mu.out_dt == MOE_F32 ? product<OUT_F32>(x, mu, first, count, parts, stream) : product<OUT_BF16>(x, mu, first, count, parts, stream);
       if (rc) return rc;
     }
   }
@@ -393,20 +594,34 @@ OrthPlan orth_plan(int batch, int rows, int cols, int piece) {
   p.t = 2 * x;
   p.other = 3 * x;
   p.gram = 4 * x;
-  p.sums = p.gram + 2 * p.gram_one;
+  // Two steps on one A: 3 n + 5 m instead of 6 n + 2 m products of m^2, and one rewriting of X instead of two, but a launch more: where a product takes
+  // longer than a launch
+  p.pairs = (double)count * p.S * p.S * p.S > 5e9;
+  p.parts = p.gram + (p.pairs ? 4 : 2) * p.gram_one;
+  p.sums = p.parts + (size_t)kMostParts * kPartFloats * 4;
   p.bytes = p.sums + (size_t)count * p.norm_blocks * 8 + 256;
   return p;
 }
 
 bool orth_coefficients_ok(const OrthCoef* c, int steps) {
-  // singular values from 0 to `top` go to the polynomial's values there; what is kept on the way are values of polynomials in them
+  for (int k = 0; k < steps; ++k)
+    if (!(fabs(c[k].a) <= 1e3 && fabs(c[k].b) <= 1e3 && fabs(c[k].c) <= 1e3)) return false;
+  // singular values from 0 to `top` go to the polynomial's values there; what is kept on the way, with steps alone and in pairs, are values of
+  // polynomials in them
   double top = 1.0;
   for (int k = 0; k < steps; ++k) {
     double next = 0;
-    if (!(fabs(c[k].a) <= 1e3 && fabs(c[k].b) <= 1e3 && fabs(c[k].c) <= 1e3)) return false;
+    const double mid = centre_of(k, steps), s = c[k].a + c[k].b * mid + c[k].c * mid * mid;
     for (int i = 0; i <= 4096; ++i) {
-      const double x = top * 1.01 * i / 4096, l = x * x, r = c[k].b * l + c[k].c * l * l, v = fabs(x * (c[k].a + r));
-      if (l > kLimit || fabs(r) > kLimit || v > kLimit) return false;
+      const double x = top * 1.01 * i / 4096, a = x * x - mid, r = (c[k].b + 2 * c[k].c * mid) * a + c[k].c * a * a, v = fabs(x * (s + r));
+      double most = fmax(fmax(fabs(a), fabs(r)), v);
+      if (pair_at(k, steps)) {
+        const OrthCoef d = c[k + 1];
+        const double mid2 = centre_of(k + 1, steps), s2 = d.a + d.b * mid2 + d.c * mid2 * mid2, t = s * a + mid * r + r * a,
+                     a2 = s * t + s * mid * r + r * t + s * s * mid - mid2, r2 = (d.b + 2 * d.c * mid2) * a2 + d.c * a2 * a2, both = s * r2 + s2 * r + r2 * r;
+        most = fmax(fmax(fmax(most, fabs(t)), fmax(fabs(a2), fabs(r2))), fabs(both));
+      }
+      if (!(most <= kLimit)) return false;
       if (v > next) next = v;
     }
     top = next;
@@ -415,6 +630,7 @@ bool orth_coefficients_ok(const OrthCoef* c, int steps) {
 }
 
 int launch_orth(const MuonProblem& mu, const OrthPlan& p, char* ws, hipStream_t s) {
+  if (const int rc = orth_configure()) return rc;
   for (int first = 0; first < mu.batch; first += p.count) {
     const int count = mu.batch - first < p.count ? mu.batch - first : p.count;
     int rc;
