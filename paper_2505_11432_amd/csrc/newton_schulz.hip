@@ -158,113 +158,155 @@ struct Product {
   int M, N;                                 // multiples of 128; SYMMETRIC: M of both
   const half* e1; const half* e2; float f1, f2, f, diagonal;
   half* c; half* c_lo; half* ct; long c_one; int ldc, ldt;      // c_lo: what c leaves of the result; ct: the transposed result
-  int full, split;                          // the tiles from `full` on are cut into `split` parts along K, which go to
+  int full, split, items;                   // the tiles from `full` on are cut into `split` parts along K, which go to
   float* parts;
 };
 enum Result { SYMMETRIC, KEPT, MUON_UPDATE, OUT_F32, OUT_BF16 };
 
-// Tiles of 128 x 256, a wave has 64 x 128 of them; four waves, two workgroups per CU, so that one multiplies while the other stores its result or waits.
-constexpr int BM = 128, BN = 256, BK = 32, NW = 4, STAGES = 3;
-constexpr int FM = 4, FN = 8;               // 16 x 16 parts of a wave
-typedef KTile<BM, BK> TileL;
-typedef KTile<BN, BK> TileR;
-constexpr int kStage = TileL::BYTES + TileR::BYTES;
-constexpr int kPitch = BM + 8;              // of the transposed tile in LDS, elements
-constexpr int kProductLds = STAGES * kStage;
-static_assert(BN * kPitch * 2 <= kProductLds, "the transposed tile takes the place of the operands");
-static_assert(2 * kProductLds <= 160 * 1024, "two workgroups share a CU's LDS");
+// Tiles of 256 x 256 by eight waves, 128 x 64 each, one workgroup per CU that walks a list of tiles.  Operands go from memory to an LDS ring of two steps of
+// 64 directly; the lower four waves, one per SIMD, issue the loads while the others multiply.  The loads of a tile's first step are issued before the results
+// of the tile in front are stored.
+constexpr int BM = 256, BN = 256, BK = 64, NW = 8, LOADERS = 4;
+constexpr int WTM = 128, WTN = 64, FM = WTM / 16, FN = WTN / 16, TM = WTM / 32, TN = WTN / 32;
+typedef KTile<BM, BK> Tile;
+constexpr int kStage = 2 * Tile::BYTES;
+constexpr int kRing = 2 * kStage;
+constexpr int kProductLds = kRing + NW * mfma::STG_BYTES;
+static_assert(kProductLds <= 160 * 1024, "LDS of a CU");
 constexpr int kPartFloats = BM * BN;
+constexpr int kGroups = 256;                // workgroups: a CU each
 
-// Which tile: matrix, row and column.  Half tiles of the lower triangle of 256 x 256 squares (SYMMETRIC), or bands of eight rows of tiles, column by column.
+// Which tile: matrix, row and column.  Squares of the lower triangle (SYMMETRIC), or bands of four rows of tiles, column by column.
 struct Place { int which, mt, nt; };
 template <Result RES> __host__ __device__ __forceinline__ int tiles_of(const Product& q) {
   const int tm = (q.M + BM - 1) / BM, tn = (q.N + BN - 1) / BN;
-  return RES == SYMMETRIC ? tn * (tn + 1) : tm * tn;
+  return RES == SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn;
 }
 template <Result RES> __device__ __forceinline__ Place place_of(const Product& q, int item) {
   const int per = tiles_of<RES>(q), which = item / per;
   int at = item - which * per;
   if constexpr (RES == SYMMETRIC) {
-    const int pair = at >> 1;
-    int p = (int)((sqrtf(8.f * (float)pair + 1.f) - 1.f) * 0.5f);
-    while ((p + 1) * (p + 2) / 2 <= pair) ++p;
-    while (p * (p + 1) / 2 > pair) --p;
-    return {which, p * 2 + (at & 1), pair - p * (p + 1) / 2};
+    int p = (int)((sqrtf(8.f * (float)at + 1.f) - 1.f) * 0.5f);
+    while ((p + 1) * (p + 2) / 2 <= at) ++p;
+    while (p * (p + 1) / 2 > at) --p;
+    p = __builtin_amdgcn_readfirstlane(p);
+    return {which, p, at - p * (p + 1) / 2};
   } else {
-    const int tm = (q.M + BM - 1) / BM, tn = (q.N + BN - 1) / BN, band = at / (8 * tn), rows = min(8, tm - band * 8);
-    at -= band * 8 * tn;
-    return {which, band * 8 + at % rows, at / rows};
+    const int tm = (q.M + BM - 1) / BM, tn = (q.N + BN - 1) / BN, band = at / (4 * tn), rows = min(4, tm - band * 4);
+    at -= band * 4 * tn;
+    return {which, band * 4 + at % rows, at / rows};
   }
 }
 
-// The result of FI x FN parts of a wave, its rows from part i0 on: a lane holds row lane % 16 and columns 4 (lane / 16) .. + 3 of every 16 x 16 part.
-template <Result RES, int FI>
-__device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, int first, Place at, const f32x4 (&acc)[FI][FN], int i0, char* smem) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-  const int row0 = at.mt * BM, col0 = at.nt * BN;
-  half* turned = reinterpret_cast<half*>(smem);
-  if (col0 + wn * 128 < q.N) {              // (the last tile's second half may lie outside)
+struct Fetch { mfma::u32x4v v[2]; };        // 32 x 32 fp16 on the way: lane l has 8 columns of rows l / 4 and 16 + l / 4
+__device__ __forceinline__ Fetch fetch_block(const half* g, int ld, int lane) {
+  Fetch f;
 #pragma unroll
-    for (int i = 0; i < FI; ++i)
+  for (int pass = 0; pass < 2; ++pass)
+    f.v[pass] = *reinterpret_cast<const mfma::u32x4v*>(g + (long)(pass * 16 + (lane >> 2)) * ld + (lane & 3) * 8);
+  return f;
+}
+// to the lanes that hold the sums: group q of a lane is row 16 (q / 2) + lane % 16, columns 16 (q % 2) + 4 (lane / 16) .. + 3
+__device__ __forceinline__ void unpack_block(char* stg, const Fetch& f, f16x4 (&v)[4], int lane) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int lr = wm * 64 + (i0 + i) * 16 + (lane & 15), lc = wn * 128 + j * 16 + (lane >> 4) * 4;
-        const int row = row0 + lr, col = col0 + lc;
-        const long to = at.which * q.c_one + (long)row * q.ldc + col;
-        f32x4 v = acc[i][j] * q.f;
-        if (q.e1) v += __builtin_convertvector(*reinterpret_cast<const f16x4*>(q.e1 + to), f32x4) * q.f1;
-        if (q.e2) v += __builtin_convertvector(*reinterpret_cast<const f16x4*>(q.e2 + to), f32x4) * q.f2;
-        if constexpr (RES == SYMMETRIC) {
-          const unsigned k = (unsigned)(row - col);
-          if (k < 4u) {                     // (no dynamic index into a vector)
-            v[0] += k == 0 ? q.diagonal : 0.f;
-            v[1] += k == 1 ? q.diagonal : 0.f;
-            v[2] += k == 2 ? q.diagonal : 0.f;
-            v[3] += k == 3 ? q.diagonal : 0.f;
-          }
-        }
-        if constexpr (RES == SYMMETRIC || RES == KEPT) {
-          const f16x4 h = __builtin_convertvector(v, f16x4);
-          *reinterpret_cast<f16x4*>(q.c + to) = h;
-          if constexpr (RES == KEPT) {
-            const f16x4 low = __builtin_convertvector((v - __builtin_convertvector(h, f32x4)) * kLow, f16x4);
-            *reinterpret_cast<f16x4*>(q.c_lo + to) = low;
-          }
+  for (int pass = 0; pass < 2; ++pass)
+    *reinterpret_cast<mfma::u32x4v*>(stg + (pass * 16 + (lane >> 2)) * mfma::STG_STRIDE + (lane & 3) * 16) = f.v[pass];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) turned[(lc + k) * kPitch + lr] = h[k];
-        } else {
-          const int n = min(mu.cols - col, 4);
-          if (row < mu.rows && n > 0) {
-            const long o = ((first + (long)at.which) * mu.rows + row) * mu.cols + col;
-            if constexpr (RES == MUON_UPDATE) {
-              const float factor = factor_of(mu.factor), lr_now = *mu.lr;
-              if (factor == factor) {
-                const float keep = (float)(1.0 - (double)lr_now * mu.decay), step = lr_now * mu.scale * (1.0f / kScale);
-                const f32x4 x = load4(mu.p + o, n) * keep - v * step;
-                store4(mu.p + o, n, x);
-                if (mu.w) store4(static_cast<bf16*>(mu.w) + o, n, x);
-              }
-            } else {
-              v *= 1.0f / kScale;
-              if constexpr (RES == OUT_F32) store4(static_cast<float*>(mu.out) + o, n, v);
-              else store4(static_cast<bf16*>(mu.out) + o, n, v);
+  for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const f16x4*>(stg + mfma::patch_row(q, lane) * mfma::STG_STRIDE + mfma::patch_col(q, lane) * 2);
+}
+__device__ __forceinline__ void store_patch(const char* stg, half* g, int ld, int lane) {
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass)
+    *reinterpret_cast<mfma::u32x4v*>(g + (long)(pass * 16 + (lane >> 2)) * ld + (lane & 3) * 8) =
+        *reinterpret_cast<const mfma::u32x4v*>(stg + (pass * 16 + (lane >> 2)) * mfma::STG_STRIDE + (lane & 3) * 16);
+}
+__device__ __forceinline__ void store_block(char* stg, const f16x4 (&v)[4], half* g, int ld, int lane) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) *reinterpret_cast<f16x4*>(stg + mfma::patch_row(q, lane) * mfma::STG_STRIDE + mfma::patch_col(q, lane) * 2) = v[q];
+  store_patch(stg, g, ld, lane);
+}
+__device__ __forceinline__ void store_turned(char* stg, const f16x4 (&v)[4], half* g, int ld, int lane) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<half*>(stg + (mfma::patch_col(q, lane) + c) * mfma::STG_STRIDE + mfma::patch_row(q, lane) * 2) = v[q][c];
+  store_patch(stg, g, ld, lane);
+}
+
+// The results of TI rows of 32 x 32 blocks of a wave, whose first one is row b0.  A wave's 128 x 64 lie inside the matrix or outside.
+template <Result RES, int TI>
+__device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, int first, Place at, const f32x4 (&acc)[2 * TI][FN], int b0, int wave, char* stg) {
+  const int lane = threadIdx.x & 63, row0 = at.mt * BM + (wave >> 2) * WTM, col0 = at.nt * BN + (wave & 3) * WTN;
+  const int rows = q.M, cols = RES == SYMMETRIC ? q.M : q.N;
+  if (row0 >= rows || col0 >= cols) return;
+  constexpr int NB = TI * TN;
+  auto origin = [&](int b) __attribute__((always_inline)) -> long {
+    return at.which * q.c_one + (long)(row0 + (b0 + b / TN) * 32) * q.ldc + col0 + b % TN * 32;
+  };
+  Fetch f1, f2;
+  if (q.e1) f1 = fetch_block(q.e1 + origin(0), q.ldc, lane);
+  if (q.e2) f2 = fetch_block(q.e2 + origin(0), q.ldc, lane);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int i = b / TN, j = b % TN;
+    f32x4 v[4] = {acc[2 * i][2 * j] * q.f, acc[2 * i][2 * j + 1] * q.f, acc[2 * i + 1][2 * j] * q.f, acc[2 * i + 1][2 * j + 1] * q.f};
+    f16x4 h[4];
+    if (q.e1) {
+      unpack_block(stg, f1, h, lane);
+      if (b + 1 < NB) f1 = fetch_block(q.e1 + origin(b + 1), q.ldc, lane);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) v[n] += __builtin_convertvector(h[n], f32x4) * q.f1;
+    }
+    if (q.e2) {
+      unpack_block(stg, f2, h, lane);
+      if (b + 1 < NB) f2 = fetch_block(q.e2 + origin(b + 1), q.ldc, lane);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) v[n] += __builtin_convertvector(h[n], f32x4) * q.f2;
+    }
+    const int br = row0 + (b0 + i) * 32, bc = col0 + j * 32;
+    if constexpr (RES == SYMMETRIC) {
+      if (br == bc && q.diagonal != 0.f) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[n][c] += mfma::patch_row(n, lane) == mfma::patch_col(n, lane) + c ? q.diagonal : 0.f;
+      }
+    }
+    if constexpr (RES == SYMMETRIC || RES == KEPT) {
+      const long o = at.which * q.c_one;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) h[n] = __builtin_convertvector(v[n], f16x4);
+      store_block(stg, h, q.c + origin(b), q.ldc, lane);
+      // (a square on the diagonal holds both halves)
+      if (RES == KEPT) store_turned(stg, h, q.ct + o + (long)bc * q.ldt + br, q.ldt, lane);
+      else if (at.mt != at.nt) store_turned(stg, h, q.c + o + (long)bc * q.ldc + br, q.ldc, lane);
+      if constexpr (RES == KEPT) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) h[n] = __builtin_convertvector((v[n] - __builtin_convertvector(h[n], f32x4)) * kLow, f16x4);
+        store_block(stg, h, q.c_lo + origin(b), q.ldc, lane);
+      }
+    } else {
+#pragma unroll
+      for (int n4 = 0; n4 < 4; ++n4) {
+        const int row = br + mfma::patch_row(n4, lane), col = bc + mfma::patch_col(n4, lane), n = min(mu.cols - col, 4);
+        if (row < mu.rows && n > 0) {
+          const long o = ((first + (long)at.which) * mu.rows + row) * mu.cols + col;
+          if constexpr (RES == MUON_UPDATE) {
+            const float factor = factor_of(mu.factor), lr_now = *mu.lr;
+            if (factor == factor) {
+              const float keep = (float)(1.0 - (double)lr_now * mu.decay), step = lr_now * mu.scale * (1.0f / kScale);
+              const f32x4 x = load4(mu.p + o, n) * keep - v[n4] * step;
+              store4(mu.p + o, n, x);
+              if (mu.w) store4(static_cast<bf16*>(mu.w) + o, n, x);
             }
+          } else {
+            v[n4] *= 1.0f / kScale;
+            if constexpr (RES == OUT_F32) store4(static_cast<float*>(mu.out) + o, n, v[n4]);
+            else store4(static_cast<bf16*>(mu.out) + o, n, v[n4]);
           }
         }
       }
-  }
-  if constexpr (RES == SYMMETRIC || RES == KEPT) {
-    // the transposed result, eight rows of the tile at a time; a square on the diagonal holds both halves
-    half* t = RES == SYMMETRIC ? q.c : q.ct;
-    const int ldt = RES == SYMMETRIC ? q.ldc : q.ldt;
-    if (RES == SYMMETRIC && (at.mt >> 1) == at.nt) return;
-    __syncthreads();
-    const int cols = min(BN, q.N - col0);
-    constexpr int GROUPS = FI * 2 * 2;      // of eight rows
-    for (int unit = threadIdx.x; unit < cols * GROUPS; unit += NW * 64) {
-      const int c = unit / GROUPS, g = unit % GROUPS;
-      const int x = FI == FM ? g * 8 : (g >> 1) * 64 + i0 * 16 + (g & 1) * 8;
-      *reinterpret_cast<f16x8*>(t + at.which * q.c_one + (long)(col0 + c) * ldt + row0 + x) = *reinterpret_cast<const f16x8*>(&turned[c * kPitch + x]);
     }
   }
 }
@@ -273,152 +315,153 @@ template <Result RES>
 __global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProblem mu, int first) {
   extern __shared__ __attribute__((aligned(256))) char smem[];
   const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-  int item = blockIdx.x, part = -1;
-  int step0 = 0, steps = q.K / BK;
-  if (item >= q.full) {
-    part = item - q.full;
-    item = q.full + part / q.split;
-    const int n = part % q.split;
-    step0 = n * steps / q.split;
-    steps = (n + 1) * steps / q.split - step0;
-  } else {
-    // Workgroup b runs on XCD b % 8: 64 tiles that are neighbours go to the 64 places of an XCD at a time.
-    const int round = item / 512, in_round = item % 512, size = min(512, q.full - round * 512), share = size / 8;
-    if (in_round < share * 8) item = round * 512 + in_round % 8 * share + in_round / 8;
-  }
-  const Place at = place_of<RES>(q, item);
-  if (RES == SYMMETRIC && at.mt * BM >= q.M) return;                     // (the second half of the last square)
-  const char* l = uniform_ptr(reinterpret_cast<const char*>(q.l + at.which * q.l_one + (long)at.mt * BM * q.ldl + (long)step0 * BK));
-  const char* r = uniform_ptr(reinterpret_cast<const char*>(q.r + at.which * q.r_one + (long)at.nt * BN * q.ldr + (long)step0 * BK));
-  // loads: slots of 1 KB, two of the left and four of the right operand per wave and step
-  constexpr int SL = TileL::BYTES / 1024 / NW, SR = TileR::BYTES / 1024 / NW;
-  unsigned offl[SL], offr[SR];
-  const int rows_r = (RES == SYMMETRIC ? q.M : q.N) - at.nt * BN;        // rows past the last one repeat it
-#pragma unroll
-  for (int j = 0; j < SL; ++j) {
-    const int row = (wave + j * NW) * TileL::ROWS_PER_DMA + lane / TileL::CPR, chunk = (lane % TileL::CPR) ^ TileL::swz(row);
-    offl[j] = (unsigned)row * (unsigned)q.ldl * 2u + (unsigned)chunk * 16u;
-  }
-#pragma unroll
-  for (int j = 0; j < SR; ++j) {
-    const int row = (wave + j * NW) * TileR::ROWS_PER_DMA + lane / TileR::CPR, chunk = (lane % TileR::CPR) ^ TileR::swz(row);
-    offr[j] = (unsigned)min(row, rows_r - 1) * (unsigned)q.ldr * 2u + (unsigned)chunk * 16u;
-  }
-  auto issue = [&](int s, int slot) __attribute__((always_inline)) {
-    const unsigned to = lds + (unsigned)slot * kStage + (unsigned)wave * 1024u;
-    const char* lk = l + (long)s * BK * 2;
-    const char* rk = r + (long)s * BK * 2;
-#pragma unroll
-    for (int j = 0; j < SL; ++j) dma16s(lk, offl[j], to + (unsigned)j * NW * 1024u);
-#pragma unroll
-    for (int j = 0; j < SR; ++j) dma16s(rk, offr[j], to + TileL::BYTES + (unsigned)j * NW * 1024u);
-  };
-  constexpr int LOADS = SL + SR;
-  f32x4 acc[FM][FN];
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const unsigned fa = mfma::frag_origin<mfma::KMAJOR, BM, BK>(wm * 64, lane), fb = TileL::BYTES + mfma::frag_origin<mfma::KMAJOR, BN, BK>(wn * 128, lane);
-  // A step has two phases: the wave's left fragments are held for both, its right ones pass through four at a time, and each phase's are read while the one
-  // before multiplies.  The barrier in between: every wave's loads of step s + 1 have landed, and every wave has read all of step s, whose slot
-  // the loads of step s + STAGES then fill.
-  f16x8 held[2][FM], strm[2][FN / 2];
-  auto read_held = [&](unsigned base, int set) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < FM; ++i) held[set][i] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, BM, BK>(base + fa, i, 0));
-  };
-  auto read_strm = [&](unsigned base, int which) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < FN / 2; ++j) strm[which][j] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, BN, BK>(base + fb, which * (FN / 2) + j, 0));
-  };
-  auto multiply = [&](int set, int which) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < FN / 2; ++j)
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-        acc[i][which * (FN / 2) + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(strm[which][j], held[set][i], acc[i][which * (FN / 2) + j], 0, 0, 0);
-  };
-  auto open = [&](int s) __attribute__((always_inline)) {      // step s can be read
-    if (s + 1 < steps) wait_vmcnt<LOADS>(); else wait_vmcnt<0>();
-    __syncthreads();
-  };
-#pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s)
-    if (s < steps) issue(s, s);
-  open(0);
-  if (STAGES - 1 < steps) issue(STAGES - 1, STAGES - 1);
-  unsigned at_lds = lds;                    // slot of the step
-  int slot = 0;
-  read_held(at_lds, 0);
-  read_strm(at_lds, 0);
-  auto step = [&](int s, auto parity) __attribute__((always_inline)) {
-    constexpr int P = decltype(parity)::value;
-    read_strm(at_lds, 1);
-    multiply(P, 0);
-    if (s + 1 < steps) {
-      open(s + 1);
-      if (s + STAGES < steps) issue(s + STAGES, slot);
-      slot = slot + 1 == STAGES ? 0 : slot + 1;
-      at_lds = lds + (unsigned)slot * kStage;
-      read_held(at_lds, P ^ 1);
-      read_strm(at_lds, 0);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  const bool is_loader = wave < LOADERS;
+  char* stg = smem + kRing + wave * mfma::STG_BYTES;
+  const unsigned fa = mfma::frag_origin<mfma::KMAJOR, BM, BK>(wm * WTM, lane), fb = Tile::BYTES + mfma::frag_origin<mfma::KMAJOR, BN, BK>(wn * WTN, lane);
+  // a tile, or a part of one
+  Place at{};
+  int part = -1, steps = 0;
+  const char* l = nullptr;
+  const char* r = nullptr;
+  unsigned offl[8], offr[8];
+  auto open_tile = [&](int slot) __attribute__((always_inline)) -> bool {
+    // Workgroup b runs on XCD b % 8: neighbouring tiles, which share operands, go to the CUs of one XCD.
+    const int round = slot * kGroups, size = min(kGroups, q.items - round), share = size / 8, b = blockIdx.x;
+    if (b >= size) return false;
+    int item = round + (b < share * 8 ? b % 8 * share + b / 8 : b);
+    part = -1;
+    int step0 = 0;
+    steps = q.K / BK;
+    if (item >= q.full) {
+      part = item - q.full;
+      item = q.full + part / q.split;
+      const int n = part % q.split, all = steps;
+      step0 = n * all / q.split;
+      steps = (n + 1) * all / q.split - step0;
     }
-    multiply(P, 1);
+    at = place_of<RES>(q, item);
+    l = uniform_ptr(reinterpret_cast<const char*>(q.l + at.which * q.l_one + (long)at.mt * BM * q.ldl + (long)step0 * BK));
+    r = uniform_ptr(reinterpret_cast<const char*>(q.r + at.which * q.r_one + (long)at.nt * BN * q.ldr + (long)step0 * BK));
+    if (is_loader) {
+      // slot j of a loader: 1 KB, eight rows of the tile; rows past the last one repeat it
+      const int left_l = q.M - at.mt * BM - 1, left_r = (RES == SYMMETRIC ? q.M : q.N) - at.nt * BN - 1;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int row = (wave + j * LOADERS) * Tile::ROWS_PER_DMA + lane / Tile::CPR, chunk = (lane % Tile::CPR) ^ Tile::swz(row);
+        offl[j] = (unsigned)min(row, left_l) * (unsigned)q.ldl * 2u + (unsigned)chunk * 16u;
+        offr[j] = (unsigned)min(row, left_r) * (unsigned)q.ldr * 2u + (unsigned)chunk * 16u;
+      }
+    }
+    return true;
   };
-  int s = 0;
-  for (; s + 1 < steps; s += 2) {
-    step(s, std::integral_constant<int, 0>());
-    step(s + 1, std::integral_constant<int, 1>());
-  }
-  if (s < steps) step(s, std::integral_constant<int, 0>());
-  if (part >= 0) {
-    f32x4* to = reinterpret_cast<f32x4*>(q.parts + (long)part * kPartFloats) + threadIdx.x;
+  static_assert(Tile::BYTES / 1024 / LOADERS == 8 && Tile::BYTES == 0x8000, "sixteen loads per loader and step, an operand after the other");
+  auto issue = [&](int s) __attribute__((always_inline)) {
+    if (is_loader) mfma::dma16s_x16(l + (long)s * BK * 2, r + (long)s * BK * 2, offl, offr, lds + (unsigned)(s & 1) * kStage + (unsigned)wave * 1024u);
+  };
+  int slot = 0;
+  if (!open_tile(slot)) return;
+  issue(0);
+  for (;;) {
+    f32x4 acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) to[(i * FN + j) * (NW * 64)] = acc[i][j];
-    return;
+      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // A step has four phases, two for each half of its 64: the wave's right fragments are held for two, the left ones pass through four at a time, and the
+    // fragments of each phase are read while the one before multiplies.  The barrier that opens step s + 1, whose loads have landed then, lies before the
+    // last phase of step s, whose fragments are in registers: the slot of s is free for the loads of s + 2.
+    f16x8 held[2][FN], strm[2][FM / 2];
+    auto read_phase = [&](unsigned base, int p) __attribute__((always_inline)) {
+      const int kk = p >> 1, ph = p & 1;
+      if (ph == 0) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) held[kk][j] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, BN, BK>(base + fb, j, kk));
+      }
+#pragma unroll
+      for (int i = 0; i < FM / 2; ++i) strm[p & 1][i] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, BM, BK>(base + fa, ph * (FM / 2) + i, kk));
+    };
+    auto open_step = [&](int s) __attribute__((always_inline)) {
+      if (is_loader) wait_vmcnt<0>();
+      __syncthreads();
+      if (s + 1 < steps) issue(s + 1);
+    };
+    open_step(0);
+    read_phase(lds, 0);
+    for (int s = 0; s < steps; ++s) {
+      const unsigned base = lds + (unsigned)(s & 1) * kStage;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        if (p < 3) {
+          read_phase(base, p + 1);
+        } else {
+          mfma::wait_lgkmcnt0();
+          if (s + 1 < steps) {
+            open_step(s + 1);
+            read_phase(lds + (unsigned)((s + 1) & 1) * kStage, 0);
+          }
+        }
+        const int kk = p >> 1, ph = p & 1;
+#pragma unroll
+        for (int i = 0; i < FM / 2; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+            acc[ph * (FM / 2) + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(held[kk][j], strm[p & 1][i], acc[ph * (FM / 2) + i][j], 0, 0, 0);
+      }
+    }
+    const Place was = at;
+    const int was_part = part;
+    ++slot;
+    __syncthreads();                        // every wave has read its last fragments: the ring is free
+    const bool more = open_tile(slot);
+    if (more) issue(0);
+    if (was_part >= 0) {
+      f32x4* to = reinterpret_cast<f32x4*>(q.parts + (long)was_part * kPartFloats) + threadIdx.x;
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) to[(i * FN + j) * (NW * 64)] = acc[i][j];
+    } else {
+      finish<RES, TM>(q, mu, first, was, acc, 0, wave, stg);
+    }
+    if (!more) break;
   }
-  __syncthreads();                          // the operands' LDS is free
-  finish<RES, FM>(q, mu, first, at, acc, 0, smem);
 }
 
-// Adds the parts of the cut tiles and finishes them: four workgroups per tile, a quarter of each wave's rows each.
+// Adds the parts of the cut tiles and finishes them: four workgroups per tile, a row of blocks of each wave each.
 template <Result RES>
 __global__ void __launch_bounds__(NW * 64) join_kernel(Product q, MuonProblem mu, int first) {
-  extern __shared__ __attribute__((aligned(256))) char smem[];
-  const int cut = blockIdx.x / FM, i0 = blockIdx.x % FM;
+  __shared__ __attribute__((aligned(16))) char smem[NW * mfma::STG_BYTES];
+  const int cut = blockIdx.x / TM, b0 = blockIdx.x % TM, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const Place at = place_of<RES>(q, q.full + cut);
-  if (RES == SYMMETRIC && at.mt * BM >= q.M) return;
-  f32x4 acc[1][FN];
+  f32x4 acc[2][FN];
 #pragma unroll
-  for (int j = 0; j < FN; ++j) acc[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const f32x4* from = reinterpret_cast<const f32x4*>(q.parts + (long)cut * q.split * kPartFloats) + threadIdx.x + i0 * FN * (NW * 64);
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const f32x4* from = reinterpret_cast<const f32x4*>(q.parts + (long)cut * q.split * kPartFloats) + threadIdx.x + 2 * b0 * FN * (NW * 64);
 #pragma unroll 2
   for (int n = 0; n < q.split; ++n, from += kPartFloats / 4)
 #pragma unroll
-    for (int j = 0; j < FN; ++j) acc[0][j] += from[j * (NW * 64)];
-  finish<RES, 1>(q, mu, first, at, acc, i0, smem);
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] += from[(i * FN + j) * (NW * 64)];
+  finish<RES, 1>(q, mu, first, at, acc, b0, wave, smem + wave * mfma::STG_BYTES);
 }
 
-// Which tiles are cut along K: those behind the last whole round of workgroups, where that is the faster way.  In units of a step's time (two workgroups per
-// CU, 0.4 us): a round takes its steps, adding parts up a launch and a read of 128 KB per part.
+// Which tiles are cut along K: those behind the last whole round of workgroups, where that is the faster way.  In units of a step's time (1 us): a round takes
+// its steps and about four for its results, adding parts up a launch (5 us) and a read of 256 KB per part.
 struct Cut { int full, split; };
 Cut cut_of(long tiles, int steps, long most_parts) {
-  const int places = 512;
+  const int full = (int)(tiles / kGroups * kGroups), rem = (int)(tiles - full);
   Cut best{(int)tiles, 1};
-  const int full = (int)(tiles / places * places), rem = (int)(tiles - full);
   if (rem == 0) return best;
-  // (workgroups alone on their CU take about 0.6 of the time)
-  auto round = [&](long n, double s) { return n <= 256 ? 0.6 * s : s; };
-  double least = round(rem, steps);
-  for (int split = 2; split <= 16; ++split) {
+  double least = steps + 4;
+  for (int split = 2; split <= 32; ++split) {
     const long parts = (long)rem * split;
-    if (steps / split < 4 || parts > most_parts) break;
-    const double each = (double)steps / split;
-    const double time = (parts / places) * each + round(parts % places, parts % places ? each : 0) + 14 + 0.8 * split;
+    if (steps / split < 2 || parts > most_parts) break;
+    const double time = (double)((parts + kGroups - 1) / kGroups) * ((double)steps / split + 2) + 6 + 0.6 * split;
     if (time < least) {
       least = time;
       best = {full, split};
@@ -426,19 +469,20 @@ Cut cut_of(long tiles, int steps, long most_parts) {
   }
   return best;
 }
-constexpr int kMostParts = 1024;            // of a launch: 128 MB
+constexpr int kMostParts = 512;             // of a launch: 128 MB
 
 template <Result RES> int product(Product q, const MuonProblem& mu, int first, int count, float* parts, hipStream_t s) {
   const long tiles = (long)tiles_of<RES>(q) * count;
   const Cut cut = cut_of(tiles, q.K / BK, kMostParts);
+  const int rem = (int)(tiles - cut.full);
   q.full = cut.full;
   q.split = cut.split;
+  q.items = cut.full + rem * cut.split;
   q.parts = parts;
-  const int rem = (int)(tiles - cut.full);
-  product_kernel<RES><<<dim3((unsigned)(cut.full + (long)rem * cut.split)), dim3(NW * 64), kProductLds, s>>>(q, mu, first);
+  product_kernel<RES><<<dim3(q.items < kGroups ? q.items : kGroups), dim3(NW * 64), kProductLds, s>>>(q, mu, first);
   MOE_LAUNCH_CHECK();
   if (rem > 0) {
-    join_kernel<RES><<<dim3((unsigned)rem * FM), dim3(NW * 64), BN * kPitch * 2, s>>>(q, mu, first);
+    join_kernel<RES><<<dim3((unsigned)rem * TM), dim3(NW * 64), 0, s>>>(q, mu, first);
     MOE_LAUNCH_CHECK();
   }
   return MOE_OK;
@@ -453,9 +497,7 @@ int orth_configure() {
   if (dev < 0 || dev >= 64) return MOE_ERR_UNSUPPORTED;
   if (done.load(std::memory_order_acquire) >> dev & 1) return MOE_OK;
   for (const void* k : {(const void*)product_kernel<SYMMETRIC>, (const void*)product_kernel<KEPT>, (const void*)product_kernel<MUON_UPDATE>,
-                        (const void*)product_kernel<OUT_F32>, (const void*)product_kernel<OUT_BF16>, (const void*)join_kernel<SYMMETRIC>,
-                        (const void*)join_kernel<KEPT>, (const void*)join_kernel<MUON_UPDATE>, (const void*)join_kernel<OUT_F32>,
-                        (const void*)join_kernel<OUT_BF16>})
+                        (const void*)product_kernel<OUT_F32>, (const void*)product_kernel<OUT_BF16>})
     MOE_HIP_TRY(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kProductLds));
   done.fetch_or(1ull << dev, std::memory_order_release);
   return MOE_OK;
