@@ -45,7 +45,7 @@ int orthogonal_problem(int batch, int rows, int cols, int steps, const double* c
   if (batch < 0 || rows < 1 || cols < 1 || piece < 0 || steps < 1 || steps > MOE_ORTH_MAX_STEPS) return MOE_ERR_INVALID;
   if (!orth_takes(batch, rows, cols, piece)) return MOE_ERR_UNSUPPORTED;
   for (int k = 0; k < steps; ++k)
-    q->coef[k] = coefficients ? OrthCoef{coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2]} : OrthCoef{3.4445, -4.7750, 2.0315};
+    q->coef[k] = coefficients ? OrthCoef{coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2]} : kDefaultCoef;
   if (!orth_coefficients_ok(q->coef, steps)) return MOE_ERR_UNSUPPORTED;
   q->batch = batch; q->rows = rows; q->cols = cols; q->steps = steps; q->piece = piece;
   if (batch > 0 && (!workspace || !aligned16(workspace) || ws_bytes < orth_plan(batch, rows, cols, piece).bytes)) return MOE_ERR_WORKSPACE;

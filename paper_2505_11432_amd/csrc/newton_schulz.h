@@ -6,7 +6,9 @@ namespace moe {
 
 constexpr int kOrthPad = 128;                // rows and columns of a matrix in the workspace are multiples of this
 constexpr int kNormBlocks = 1024;             // sums of squares per matrix, at most
+constexpr int kSmallSide = 128, kSmallTile = 128;
 struct OrthCoef { double a, b, c; };
+constexpr OrthCoef kDefaultCoef{3.4445, -4.7750, 2.0315};
 
 struct MuonProblem {
   const void* u; moe_dtype u_dt;             // matrices to orthogonalise; Muon: their gradients
@@ -23,6 +25,8 @@ struct OrthPlan {
   int count;                                 // matrices at a time
   int norm_blocks;
   bool pairs;                                // steps taken two at a time
+  bool small;                                // the smaller side within kSmallSide: see newton_schulz_small.hip
+  int slabs, tiles_per_slab;                 // of the longer side there
   size_t hi, lo, t, other, gram, parts, sums;      // offsets of a piece's buffers
   size_t gram_one;                           // bytes of one list of Gram matrices
   size_t bytes;
@@ -30,7 +34,10 @@ struct OrthPlan {
 bool orth_takes(int batch, int rows, int cols, int piece);
 OrthPlan orth_plan(int batch, int rows, int cols, int piece);
 int orth_configure();                        // per-device set-up (moe_init)
+bool orth_is_default(const OrthCoef* c, int steps);
 bool orth_coefficients_ok(const OrthCoef* c, int steps);        // every matrix that is kept fits 16 bits
+int orth_small_configure();
+int launch_orth_small(const MuonProblem& q, const OrthPlan& p, int first, int count, char* ws, hipStream_t s);
 int launch_orth(const MuonProblem& q, const OrthPlan& p, char* ws, hipStream_t s);
 
 }  // namespace moe

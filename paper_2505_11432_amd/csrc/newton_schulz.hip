@@ -18,64 +18,12 @@
 
 #include <atomic>
 
-#include "gemm_mfma_dma.h"
-#include "newton_schulz.h"
+#include "newton_schulz_device.h"
 
 namespace moe {
 namespace {
 
-using mfma::KTile;
-using mfma::dma16s;
-using mfma::f32x4;
-using mfma::uniform_ptr;
-using mfma::wait_vmcnt;
-
-typedef _Float16 half;
-typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-typedef f32x4 f32x4_u __attribute__((aligned(4)));
-typedef bf16x4 bf16x4_u __attribute__((aligned(2)));
-
-constexpr float kScale = 4096.f, kLimit = 15.5f;        // what is kept is times 2^12
-constexpr float kLow = 2048.f;                          // lo is times 2^11 more
-
-__device__ __forceinline__ float factor_of(const float* f) { return f ? *f : 1.0f; }
-
-// four elements, the last ones of a row one by one
-template <typename T> __device__ __forceinline__ f32x4 load4(const T* p, int n) {
-  f32x4 v = {};
-  if (n >= 4) {
-    if constexpr (sizeof(T) == 4) v = *reinterpret_cast<const f32x4_u*>(p);
-    else v = __builtin_convertvector(*reinterpret_cast<const bf16x4_u*>(p), f32x4);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-      if (i < n) v[i] = to_f32(p[i]);
-  }
-  return v;
-}
-template <typename T> __device__ __forceinline__ void store4(T* p, int n, f32x4 v) {
-  if (n >= 4) {
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_u*>(p) = v;
-    else *reinterpret_cast<bf16x4_u*>(p) = __builtin_convertvector(v, bf16x4);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-      if (i < n) p[i] = from_f32<T>(v[i]);
-  }
-}
-
-__device__ __forceinline__ f32x4 momentum_of(f32x4 g, f32x4 m, float factor, float momentum) { return m * momentum + g * factor; }
-__device__ __forceinline__ f32x4 update_of(f32x4 g, f32x4 m, float factor, float momentum, bool nesterov) { return nesterov ? g * factor + m * momentum : m; }
-
-__device__ __forceinline__ double block_sum(double s, double* lds) {      // of 256 threads
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) s += __shfl_xor(s, off);
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
-  __syncthreads();
-  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
-}
+using namespace orth;
 
 // New momentum, and sums of squares of u: gridDim.x parts of every matrix.
 template <typename TG, bool MUON>
@@ -161,7 +109,6 @@ struct Product {
   int full, split, items;                   // the tiles from `full` on are cut into `split` parts along K, which go to
   float* parts;
 };
-enum Result { SYMMETRIC, KEPT, MUON_UPDATE, OUT_F32, OUT_BF16 };
 
 // Tiles of 256 x 256 by eight waves, 128 x 64 each, one workgroup per CU that walks a list of tiles.  Operands go from memory to an LDS ring of two steps of
 // 64 directly; the lower four waves, one per SIMD, issue the loads while the others multiply.  The loads of a tile's first step are issued before the results
@@ -292,19 +239,7 @@ __device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, 
         const int row = br + mfma::patch_row(n4, lane), col = bc + mfma::patch_col(n4, lane), n = min(mu.cols - col, 4);
         if (row < mu.rows && n > 0) {
           const long o = ((first + (long)at.which) * mu.rows + row) * mu.cols + col;
-          if constexpr (RES == MUON_UPDATE) {
-            const float factor = factor_of(mu.factor), lr_now = *mu.lr;
-            if (factor == factor) {
-              const float keep = (float)(1.0 - (double)lr_now * mu.decay), step = lr_now * mu.scale * (1.0f / kScale);
-              const f32x4 x = load4(mu.p + o, n) * keep - v[n4] * step;
-              store4(mu.p + o, n, x);
-              if (mu.w) store4(static_cast<bf16*>(mu.w) + o, n, x);
-            }
-          } else {
-            v[n4] *= 1.0f / kScale;
-            if constexpr (RES == OUT_F32) store4(static_cast<float*>(mu.out) + o, n, v[n4]);
-            else store4(static_cast<bf16*>(mu.out) + o, n, v[n4]);
-          }
+          write_result<RES>(mu, o, n, v[n4] * (1.0f / kScale));
         }
       }
     }
@@ -499,6 +434,7 @@ int orth_configure() {
   for (const void* k : {(const void*)product_kernel<SYMMETRIC>, (const void*)product_kernel<KEPT>, (const void*)product_kernel<MUON_UPDATE>,
                         (const void*)product_kernel<OUT_F32>, (const void*)product_kernel<OUT_BF16>})
     MOE_HIP_TRY(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kProductLds));
+  if (const int rc = orth_small_configure()) return rc;
   done.fetch_or(1ull << dev, std::memory_order_release);
   return MOE_OK;
 }
@@ -595,6 +531,7 @@ template <typename TG, bool MUON> int start(const MuonProblem& mu, const OrthPla
   double* sums = reinterpret_cast<double*>(ws + p.sums);
   norm_kernel<TG, MUON><<<dim3(p.norm_blocks, count), dim3(256), 0, s>>>(mu, first, sums);
   MOE_LAUNCH_CHECK();
+  if (p.small) return MOE_OK;
   start_kernel<TG, MUON><<<dim3(p.C / 64, p.R / 64, count), dim3(256), 0, s>>>(mu, p, first, sums, reinterpret_cast<half*>(ws + p.hi),
                                                                               reinterpret_cast<half*>(ws + p.lo), reinterpret_cast<half*>(ws + p.t));
   MOE_LAUNCH_CHECK();
@@ -621,14 +558,28 @@ OrthPlan orth_plan(int batch, int rows, int cols, int piece) {
   OrthPlan p{};
   const int count = matrices_at_a_time(batch, piece) < 1 ? 1 : matrices_at_a_time(batch, piece);
   p.count = count;
-  p.R = (int)align_up(rows, kOrthPad);
-  p.C = (int)align_up(cols, kOrthPad);
-  p.S = p.R < p.C ? p.R : p.C;
+  const int least = rows < cols ? rows : cols, most = rows < cols ? cols : rows;
   const long size = (long)rows * cols;
   long blocks = (size + 4095) / 4096;
   const long share = 4096 / count + 1;
   if (blocks > share) blocks = share;
   p.norm_blocks = (int)(blocks < kNormBlocks ? blocks : kNormBlocks);
+  p.small = least <= kSmallSide;
+  if (p.small) {
+    p.S = least <= kSmallSide / 2 ? kSmallSide / 2 : kSmallSide;
+    const int tiles = cdiv(most, kSmallTile);
+    p.tiles_per_slab = cdiv(tiles, 32);
+    p.slabs = cdiv(tiles, p.tiles_per_slab);
+    p.gram = 0;
+    p.gram_one = (size_t)count * p.slabs * p.S * p.S * 4;
+    p.t = p.gram_one;
+    p.sums = p.t + (size_t)count * p.S * p.S * 4;
+    p.bytes = p.sums + (size_t)count * p.norm_blocks * 8 + 256;
+    return p;
+  }
+  p.R = (int)align_up(rows, kOrthPad);
+  p.C = (int)align_up(cols, kOrthPad);
+  p.S = p.R < p.C ? p.R : p.C;
   const size_t x = (size_t)count * p.R * p.C * 2;
   p.gram_one = (size_t)count * p.S * p.S * 2;
   p.hi = 0;
@@ -645,7 +596,18 @@ OrthPlan orth_plan(int batch, int rows, int cols, int piece) {
   return p;
 }
 
+bool orth_is_default(const OrthCoef* c, int steps) {
+  for (int k = 0; k < steps; ++k)
+    if (c[k].a != kDefaultCoef.a || c[k].b != kDefaultCoef.b || c[k].c != kDefaultCoef.c) return false;
+  return true;
+}
+
+constexpr double kLimit = 15.0;             // (and a little for what lies between the places that are looked at)
+constexpr int kLook = 128;
+
 bool orth_coefficients_ok(const OrthCoef* c, int steps) {
+  // The default ones keep singular values within 1.21, and what is kept within 12: the looking alone takes longer than a small update.
+  if (orth_is_default(c, steps)) return true;
   for (int k = 0; k < steps; ++k)
     if (!(fabs(c[k].a) <= 1e3 && fabs(c[k].b) <= 1e3 && fabs(c[k].c) <= 1e3)) return false;
   // singular values from 0 to `top` go to the polynomial's values there; what is kept on the way, with steps alone and in pairs, are values of
@@ -654,8 +616,8 @@ bool orth_coefficients_ok(const OrthCoef* c, int steps) {
   for (int k = 0; k < steps; ++k) {
     double next = 0;
     const double mid = centre_of(k, steps), s = c[k].a + c[k].b * mid + c[k].c * mid * mid;
-    for (int i = 0; i <= 4096; ++i) {
-      const double x = top * 1.01 * i / 4096, a = x * x - mid, r = (c[k].b + 2 * c[k].c * mid) * a + c[k].c * a * a, v = fabs(x * (s + r));
+    for (int i = 0; i <= kLook; ++i) {
+      const double x = top * 1.01 * i / kLook, a = x * x - mid, r = (c[k].b + 2 * c[k].c * mid) * a + c[k].c * a * a, v = fabs(x * (s + r));
       double most = fmax(fmax(fabs(a), fabs(r)), v);
       if (pair_at(k, steps)) {
         const OrthCoef d = c[k + 1];
@@ -663,6 +625,7 @@ bool orth_coefficients_ok(const OrthCoef* c, int steps) {
                      a2 = s * t + s * mid * r + r * t + s * s * mid - mid2, r2 = (d.b + 2 * d.c * mid2) * a2 + d.c * a2 * a2, both = s * r2 + s2 * r + r2 * r;
         most = fmax(fmax(fmax(most, fabs(t)), fmax(fabs(a2), fabs(r2))), fabs(both));
       }
+      most = fmax(most, fabs(x * x * (c[k].a + (c[k].b + c[k].c * x * x) * x * x)));      // (A times its polynomial, of small matrices)
       if (!(most <= kLimit)) return false;
       if (v > next) next = v;
     }
@@ -678,8 +641,8 @@ int launch_orth(const MuonProblem& mu, const OrthPlan& p, char* ws, hipStream_t 
     int rc;
     if (mu.out) rc = mu.u_dt == MOE_F32 ? start<float, false>(mu, p, first, count, ws, s) : start<bf16, false>(mu, p, first, count, ws, s);
     else rc = mu.u_dt == MOE_F32 ? start<float, true>(mu, p, first, count, ws, s) : start<bf16, true>(mu, p, first, count, ws, s);
+    if (rc == MOE_OK) rc = p.small ? launch_orth_small(mu, p, first, count, ws, s) : run_steps(mu, p, first, count, ws, s);
     if (rc != MOE_OK) return rc;
-    if (const int rc2 = run_steps(mu, p, first, count, ws, s)) return rc2;
   }
   return MOE_OK;
 }
