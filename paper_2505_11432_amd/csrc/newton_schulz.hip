@@ -123,6 +123,11 @@ static_assert(kProductLds <= 160 * 1024, "LDS of a CU");
 constexpr int kPartFloats = BM * BN;
 constexpr int kGroups = 256;                // workgroups: a CU each
 
+// A wave's rows and columns in the tile.  Waves w and w + 4 share a SIMD: they lie in opposite halves along both sides, so that of a tile that is half
+// outside each SIMD has one wave to multiply for (the others skip their products).
+__device__ __forceinline__ int wave_row(int wave) { return (wave >> 2) * WTM; }
+__device__ __forceinline__ int wave_col(int wave) { return ((wave & 3) ^ (wave >> 2) * 2) * WTN; }
+
 // Which tile: matrix, row and column.  Squares of the lower triangle (SYMMETRIC), or bands of four rows of tiles, column by column.
 struct Place { int which, mt, nt; };
 template <Result RES> __host__ __device__ __forceinline__ int tiles_of(const Product& q) {
@@ -145,12 +150,15 @@ template <Result RES> __device__ __forceinline__ Place place_of(const Product& q
   }
 }
 
-struct Fetch { mfma::u32x4v v[2]; };        // 32 x 32 fp16 on the way: lane l has 8 columns of rows l / 4 and 16 + l / 4
-__device__ __forceinline__ Fetch fetch_block(const half* g, int ld, int lane) {
+// Blocks of 32 x 32 fp16 in memory: the block's place is the same for the wave and goes into a buffer descriptor, a lane has 8 columns of rows l / 4 and
+// 16 + l / 4, at an offset that is the same in every block.
+__device__ __forceinline__ int lane_offset(int ld, int lane) { return ((lane >> 2) * ld + (lane & 3) * 8) * 2; }
+struct Fetch { mfma::u32x4v v[2]; };
+__device__ __forceinline__ Fetch fetch_block(const half* g, int ld, int off) {
+  const __amdgpu_buffer_rsrc_t rs = mfma::block_rsrc(g);
   Fetch f;
 #pragma unroll
-  for (int pass = 0; pass < 2; ++pass)
-    f.v[pass] = *reinterpret_cast<const mfma::u32x4v*>(g + (long)(pass * 16 + (lane >> 2)) * ld + (lane & 3) * 8);
+  for (int pass = 0; pass < 2; ++pass) f.v[pass] = __builtin_amdgcn_raw_buffer_load_b128(rs, off, pass * 32 * ld, 0);
   return f;
 }
 // to the lanes that hold the sums: group q of a lane is row 16 (q / 2) + lane % 16, columns 16 (q % 2) + 4 (lane / 16) .. + 3
@@ -161,57 +169,81 @@ __device__ __forceinline__ void unpack_block(char* stg, const Fetch& f, f16x4 (&
 #pragma unroll
   for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const f16x4*>(stg + mfma::patch_row(q, lane) * mfma::STG_STRIDE + mfma::patch_col(q, lane) * 2);
 }
-__device__ __forceinline__ void store_patch(const char* stg, half* g, int ld, int lane) {
+__device__ __forceinline__ void store_patch(const char* stg, half* g, int ld, int off, int lane) {
+  const __amdgpu_buffer_rsrc_t rs = mfma::block_rsrc(g);
 #pragma unroll
   for (int pass = 0; pass < 2; ++pass)
-    *reinterpret_cast<mfma::u32x4v*>(g + (long)(pass * 16 + (lane >> 2)) * ld + (lane & 3) * 8) =
-        *reinterpret_cast<const mfma::u32x4v*>(stg + (pass * 16 + (lane >> 2)) * mfma::STG_STRIDE + (lane & 3) * 16);
+    __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const mfma::u32x4v*>(stg + (pass * 16 + (lane >> 2)) * mfma::STG_STRIDE + (lane & 3) * 16), rs, off,
+                                           pass * 32 * ld, 0);
 }
-__device__ __forceinline__ void store_block(char* stg, const f16x4 (&v)[4], half* g, int ld, int lane) {
+__device__ __forceinline__ void store_block(char* stg, const f16x4 (&v)[4], half* g, int ld, int off, int lane) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) *reinterpret_cast<f16x4*>(stg + mfma::patch_row(q, lane) * mfma::STG_STRIDE + mfma::patch_col(q, lane) * 2) = v[q];
-  store_patch(stg, g, ld, lane);
+  store_patch(stg, g, ld, off, lane);
 }
-__device__ __forceinline__ void store_turned(char* stg, const f16x4 (&v)[4], half* g, int ld, int lane) {
+__device__ __forceinline__ void store_turned(char* stg, const f16x4 (&v)[4], half* g, int ld, int off, int lane) {
 #pragma unroll
   for (int q = 0; q < 4; ++q)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
       *reinterpret_cast<half*>(stg + (mfma::patch_col(q, lane) + c) * mfma::STG_STRIDE + mfma::patch_row(q, lane) * 2) = v[q][c];
-  store_patch(stg, g, ld, lane);
+  store_patch(stg, g, ld, off, lane);
 }
 
-// The results of TI rows of 32 x 32 blocks of a wave, whose first one is row b0.  A wave's 128 x 64 lie inside the matrix or outside.
-template <Result RES, int TI>
-__device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, int first, Place at, const f32x4 (&acc)[2 * TI][FN], int b0, int wave, char* stg) {
-  const int lane = threadIdx.x & 63, row0 = at.mt * BM + (wave >> 2) * WTM, col0 = at.nt * BN + (wave & 3) * WTN;
+// The results of TI x TJ blocks of 32 x 32 of a wave, from row b0 and column j0 of them on.  A wave's 128 x 64 lie inside the matrix or outside.
+template <Result RES, int TI, int TJ>
+__device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, int first, Place at, const f32x4 (&acc)[2 * TI][2 * TJ], int b0, int j0, int wave, char* stg) {
+  const int lane = threadIdx.x & 63, row0 = at.mt * BM + wave_row(wave), col0 = at.nt * BN + wave_col(wave);
   const int rows = q.M, cols = RES == SYMMETRIC ? q.M : q.N;
   if (row0 >= rows || col0 >= cols) return;
-  constexpr int NB = TI * TN;
+  constexpr int NB = TI * TJ;
   auto origin = [&](int b) __attribute__((always_inline)) -> long {
-    return at.which * q.c_one + (long)(row0 + (b0 + b / TN) * 32) * q.ldc + col0 + b % TN * 32;
+    return at.which * q.c_one + (long)(row0 + (b0 + b / TJ) * 32) * q.ldc + col0 + (j0 + b % TJ) * 32;
   };
-  Fetch f1, f2;
-  if (q.e1) f1 = fetch_block(q.e1 + origin(0), q.ldc, lane);
-  if (q.e2) f2 = fetch_block(q.e2 + origin(0), q.ldc, lane);
+  // What is read lies AHEAD blocks ahead of what is stored: a block takes a fraction of the time that a read does.
+  constexpr int AHEAD = NB < 2 ? NB : 2;
+  const int off = lane_offset(q.ldc, lane), off_t = lane_offset(q.ldt, lane);
+  Fetch f1[AHEAD], f2[AHEAD];
+  f32x4 old[4];
+  auto ask = [&](int b) __attribute__((always_inline)) {
+    if (q.e1) f1[b % AHEAD] = fetch_block(q.e1 + origin(b), q.ldc, off);
+    if (q.e2) f2[b % AHEAD] = fetch_block(q.e2 + origin(b), q.ldc, off);
+  };
+  auto place = [&](int b, int n4, int& n) __attribute__((always_inline)) -> long {      // four elements of the result: where, and how many there are
+    const int row = row0 + (b0 + b / TJ) * 32 + mfma::patch_row(n4, lane), col = col0 + (j0 + b % TJ) * 32 + mfma::patch_col(n4, lane);
+    n = row < mu.rows ? min(mu.cols - col, 4) : 0;
+    return ((first + (long)at.which) * mu.rows + row) * mu.cols + col;
+  };
+  auto ask_old = [&](int b) __attribute__((always_inline)) {
+    if constexpr (RES == MUON_UPDATE) {
+#pragma unroll
+      for (int n4 = 0; n4 < 4; ++n4) {
+        int n;
+        const long o = place(b, n4, n);
+        old[n4] = n > 0 ? load4(mu.p + o, n) : f32x4{};
+      }
+    }
+  };
+#pragma unroll
+  for (int b = 0; b < AHEAD; ++b) ask(b);
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
-    const int i = b / TN, j = b % TN;
+    const int i = b / TJ, j = b % TJ;
+    ask_old(b);
     f32x4 v[4] = {acc[2 * i][2 * j] * q.f, acc[2 * i][2 * j + 1] * q.f, acc[2 * i + 1][2 * j] * q.f, acc[2 * i + 1][2 * j + 1] * q.f};
     f16x4 h[4];
     if (q.e1) {
-      unpack_block(stg, f1, h, lane);
-      if (b + 1 < NB) f1 = fetch_block(q.e1 + origin(b + 1), q.ldc, lane);
+      unpack_block(stg, f1[b % AHEAD], h, lane);
 #pragma unroll
       for (int n = 0; n < 4; ++n) v[n] += __builtin_convertvector(h[n], f32x4) * q.f1;
     }
     if (q.e2) {
-      unpack_block(stg, f2, h, lane);
-      if (b + 1 < NB) f2 = fetch_block(q.e2 + origin(b + 1), q.ldc, lane);
+      unpack_block(stg, f2[b % AHEAD], h, lane);
 #pragma unroll
       for (int n = 0; n < 4; ++n) v[n] += __builtin_convertvector(h[n], f32x4) * q.f2;
     }
-    const int br = row0 + (b0 + i) * 32, bc = col0 + j * 32;
+    if (b + AHEAD < NB) ask(b + AHEAD);
+    const int br = row0 + (b0 + i) * 32, bc = col0 + (j0 + j) * 32;
     if constexpr (RES == SYMMETRIC) {
       if (br == bc && q.diagonal != 0.f) {
 #pragma unroll
@@ -224,23 +256,21 @@ __device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, 
       const long o = at.which * q.c_one;
 #pragma unroll
       for (int n = 0; n < 4; ++n) h[n] = __builtin_convertvector(v[n], f16x4);
-      store_block(stg, h, q.c + origin(b), q.ldc, lane);
+      store_block(stg, h, q.c + origin(b), q.ldc, off, lane);
       // (a square on the diagonal holds both halves)
-      if (RES == KEPT) store_turned(stg, h, q.ct + o + (long)bc * q.ldt + br, q.ldt, lane);
-      else if (at.mt != at.nt) store_turned(stg, h, q.c + o + (long)bc * q.ldc + br, q.ldc, lane);
+      if (RES == KEPT) store_turned(stg, h, q.ct + o + (long)bc * q.ldt + br, q.ldt, off_t, lane);
+      else if (at.mt != at.nt) store_turned(stg, h, q.c + o + (long)bc * q.ldc + br, q.ldc, off, lane);
       if constexpr (RES == KEPT) {
 #pragma unroll
         for (int n = 0; n < 4; ++n) h[n] = __builtin_convertvector((v[n] - __builtin_convertvector(h[n], f32x4)) * kLow, f16x4);
-        store_block(stg, h, q.c_lo + origin(b), q.ldc, lane);
+        store_block(stg, h, q.c_lo + origin(b), q.ldc, off, lane);
       }
     } else {
 #pragma unroll
       for (int n4 = 0; n4 < 4; ++n4) {
-        const int row = br + mfma::patch_row(n4, lane), col = bc + mfma::patch_col(n4, lane), n = min(mu.cols - col, 4);
-        if (row < mu.rows && n > 0) {
-          const long o = ((first + (long)at.which) * mu.rows + row) * mu.cols + col;
-          write_result<RES>(mu, o, n, v[n4] * (1.0f / kScale));
-        }
+        int n;
+        const long o = place(b, n4, n);
+        if (n > 0) write_result<RES>(mu, o, n, v[n4] * (1.0f / kScale), old[n4]);
       }
     }
   }
@@ -251,10 +281,9 @@ __global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProb
   extern __shared__ __attribute__((aligned(256))) char smem[];
   const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int wm = wave >> 2, wn = wave & 3;
   const bool is_loader = wave < LOADERS;
   char* stg = smem + kRing + wave * mfma::STG_BYTES;
-  const unsigned fa = mfma::frag_origin<mfma::KMAJOR, BM, BK>(wm * WTM, lane), fb = Tile::BYTES + mfma::frag_origin<mfma::KMAJOR, BN, BK>(wn * WTN, lane);
+  const unsigned fa = mfma::frag_origin<mfma::KMAJOR, BM, BK>(wave_row(wave), lane), fb = Tile::BYTES + mfma::frag_origin<mfma::KMAJOR, BN, BK>(wave_col(wave), lane);
   // a tile, or a part of one
   Place at{};
   int part = -1, steps = 0;
@@ -322,7 +351,11 @@ __global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProb
       __syncthreads();
       if (s + 1 < steps) issue(s + 1);
     };
+    const bool active = at.mt * BM + wave_row(wave) < q.M && at.nt * BN + wave_col(wave) < (RES == SYMMETRIC ? q.M : q.N);
     open_step(0);
+    if (!active) {
+      for (int s = 1; s < steps; ++s) open_step(s);
+    } else {
     read_phase(lds, 0);
     for (int s = 0; s < steps; ++s) {
       const unsigned base = lds + (unsigned)(s & 1) * kStage;
@@ -337,6 +370,7 @@ __global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProb
             read_phase(lds + (unsigned)((s + 1) & 1) * kStage, 0);
           }
         }
+        __builtin_amdgcn_sched_barrier(0);        // (the compiler would move the reads behind the products, to where they are used)
         const int kk = p >> 1, ph = p & 1;
 #pragma unroll
         for (int i = 0; i < FM / 2; ++i)
@@ -344,6 +378,7 @@ __global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProb
           for (int j = 0; j < FN; ++j)
             acc[ph * (FM / 2) + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(held[kk][j], strm[p & 1][i], acc[ph * (FM / 2) + i][j], 0, 0, 0);
       }
+    }
     }
     const Place was = at;
     const int was_part = part;
@@ -358,31 +393,31 @@ __global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProb
 #pragma unroll
         for (int j = 0; j < FN; ++j) to[(i * FN + j) * (NW * 64)] = acc[i][j];
     } else {
-      finish<RES, TM>(q, mu, first, was, acc, 0, wave, stg);
+      finish<RES, TM, TN>(q, mu, first, was, acc, 0, 0, wave, stg);
     }
     if (!more) break;
   }
 }
 
-// Adds the parts of the cut tiles and finishes them: four workgroups per tile, a row of blocks of each wave each.
+// Adds the parts of the cut tiles and finishes them: eight workgroups per tile, a block of each wave each.
 template <Result RES>
 __global__ void __launch_bounds__(NW * 64) join_kernel(Product q, MuonProblem mu, int first) {
   __shared__ __attribute__((aligned(16))) char smem[NW * mfma::STG_BYTES];
-  const int cut = blockIdx.x / TM, b0 = blockIdx.x % TM, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int cut = blockIdx.x / (TM * TN), b0 = blockIdx.x / TN % TM, j0 = blockIdx.x % TN, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const Place at = place_of<RES>(q, q.full + cut);
-  f32x4 acc[2][FN];
+  f32x4 acc[2][2];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const f32x4* from = reinterpret_cast<const f32x4*>(q.parts + (long)cut * q.split * kPartFloats) + threadIdx.x + 2 * b0 * FN * (NW * 64);
-#pragma unroll 2
+    for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const f32x4* from = reinterpret_cast<const f32x4*>(q.parts + (long)cut * q.split * kPartFloats) + threadIdx.x + (2 * b0 * FN + 2 * j0) * (NW * 64);
+#pragma unroll 4
   for (int n = 0; n < q.split; ++n, from += kPartFloats / 4)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] += from[(i * FN + j) * (NW * 64)];
-  finish<RES, 1>(q, mu, first, at, acc, b0, wave, smem + wave * mfma::STG_BYTES);
+      for (int j = 0; j < 2; ++j) acc[i][j] += from[(i * FN + j) * (NW * 64)];
+  finish<RES, 1, 1>(q, mu, first, at, acc, b0, j0, wave, smem + wave * mfma::STG_BYTES);
 }
 
 // Which tiles are cut along K: those behind the last whole round of workgroups, where that is the faster way.  In units of a step's time (1 us): a round takes
@@ -417,7 +452,7 @@ template <Result RES> int product(Product q, const MuonProblem& mu, int first, i
   product_kernel<RES><<<dim3(q.items < kGroups ? q.items : kGroups), dim3(NW * 64), kProductLds, s>>>(q, mu, first);
   MOE_LAUNCH_CHECK();
   if (rem > 0) {
-    join_kernel<RES><<<dim3((unsigned)rem * TM), dim3(NW * 64), 0, s>>>(q, mu, first);
+    join_kernel<RES><<<dim3((unsigned)rem * TM * TN), dim3(NW * 64), 0, s>>>(q, mu, first);
     MOE_LAUNCH_CHECK();
   }
   return MOE_OK;

@@ -59,14 +59,14 @@ __device__ __forceinline__ double block_sum(double s, double* lds) {      // of 
   return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// One block of 4 elements of an update: new parameters and weights, or the orthogonalised matrix.  v: the result, n of its elements exist.
+// Four elements of the outcome: new parameters and weights, or the orthogonalised matrix.  v: the result, of which n elements exist; old: the parameters.
 enum Result { SYMMETRIC, KEPT, MUON_UPDATE, OUT_F32, OUT_BF16 };
-template <Result RES> __device__ __forceinline__ void write_result(const MuonProblem& mu, long o, int n, f32x4 v) {
+template <Result RES> __device__ __forceinline__ void write_result(const MuonProblem& mu, long o, int n, f32x4 v, f32x4 old) {
   if constexpr (RES == MUON_UPDATE) {
     const float factor = factor_of(mu.factor), lr_now = *mu.lr;
     if (factor == factor) {
       const float keep = (float)(1.0 - (double)lr_now * mu.decay), step = lr_now * mu.scale;
-      const f32x4 x = load4(mu.p + o, n) * keep - v * step;
+      const f32x4 x = old * keep - v * step;
       store4(mu.p + o, n, x);
       if (mu.w) store4(static_cast<bf16*>(mu.w) + o, n, x);
     }

@@ -280,8 +280,12 @@ __global__ void __launch_bounds__(threads_of<SP>(), 2) small_apply_kernel(MuonPr
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int row = r0 + row0 + i * 16 + (lane & 15), col = c0 + col0 + j * 16 + (lane >> 4) * 4, n = min(mu.cols - col, 4);
-      if (row < mu.rows && n > 0)
-        write_result<RES>(mu, base + (long)row * mu.cols + col, n, (acc[i][j] + low[i][j] * (1.0f / kLow)) * (unit / (kScale * kScale)));
+      if (row < mu.rows && n > 0) {
+        const long o = base + (long)row * mu.cols + col;
+        f32x4 old = {};
+        if constexpr (MUON) old = load4(mu.p + o, n);
+        write_result<RES>(mu, o, n, (acc[i][j] + low[i][j] * (1.0f / kLow)) * (unit / (kScale * kScale)), old);
+      }
     }
 }
 
