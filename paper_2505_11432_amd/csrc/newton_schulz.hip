@@ -169,12 +169,14 @@ __device__ __forceinline__ void unpack_block(char* stg, const Fetch& f, f16x4 (&
 #pragma unroll
   for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const f16x4*>(stg + mfma::patch_row(q, lane) * mfma::STG_STRIDE + mfma::patch_col(q, lane) * 2);
 }
+// (The offset of the second half is added to the lane's.  With it in the store's scalar offset the compiler puts no wait state between the store and a write of
+// its data registers, and the last of a lane's four words has been stored as what was written behind it.)
 __device__ __forceinline__ void store_patch(const char* stg, half* g, int ld, int off, int lane) {
   const __amdgpu_buffer_rsrc_t rs = mfma::block_rsrc(g);
 #pragma unroll
   for (int pass = 0; pass < 2; ++pass)
-    __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const mfma::u32x4v*>(stg + (pass * 16 + (lane >> 2)) * mfma::STG_STRIDE + (lane & 3) * 16), rs, off,
-                                           pass * 32 * ld, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const mfma::u32x4v*>(stg + (pass * 16 + (lane >> 2)) * mfma::STG_STRIDE + (lane & 3) * 16), rs,
+                                           off + pass * 32 * ld, 0, 0);
 }
 __device__ __forceinline__ void store_block(char* stg, const f16x4 (&v)[4], half* g, int ld, int off, int lane) {
 #pragma unroll
