@@ -192,15 +192,14 @@ __device__ __forceinline__ void store_turned(char* stg, const f16x4 (&v)[4], hal
   store_patch(stg, g, ld, off, lane);
 }
 
-// The results of TI x TJ blocks of 32 x 32 of a wave, from row b0 and column j0 of them on.  A wave's 128 x 64 lie inside the matrix or outside.
+// The results of TI x TJ blocks of 32 x 32 of a wave, which begin at row0 and col0 of matrix `which`; mirrored: the transposed ones as well (SYMMETRIC, off the
+// diagonal tiles, which hold both halves).
 template <Result RES, int TI, int TJ>
-__device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, int first, Place at, const f32x4 (&acc)[2 * TI][2 * TJ], int b0, int j0, int wave, char* stg) {
-  const int lane = threadIdx.x & 63, row0 = at.mt * BM + wave_row(wave), col0 = at.nt * BN + wave_col(wave);
-  const int rows = q.M, cols = RES == SYMMETRIC ? q.M : q.N;
-  if (row0 >= rows || col0 >= cols) return;
+__device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, int first, int which, int row0, int col0, bool mirrored, const f32x4 (&acc)[2 * TI][2 * TJ], char* stg) {
+  const int lane = threadIdx.x & 63;
   constexpr int NB = TI * TJ;
   auto origin = [&](int b) __attribute__((always_inline)) -> long {
-    return at.which * q.c_one + (long)(row0 + (b0 + b / TJ) * 32) * q.ldc + col0 + (j0 + b % TJ) * 32;
+    return which * q.c_one + (long)(row0 + b / TJ * 32) * q.ldc + col0 + b % TJ * 32;
   };
   // What is read lies AHEAD blocks ahead of what is stored: a block takes a fraction of the time that a read does.
   constexpr int AHEAD = NB < 2 ? NB : 2;
@@ -212,9 +211,9 @@ __device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, 
     if (q.e2) f2[b % AHEAD] = fetch_block(q.e2 + origin(b), q.ldc, off);
   };
   auto place = [&](int b, int n4, int& n) __attribute__((always_inline)) -> long {      // four elements of the result: where, and how many there are
-    const int row = row0 + (b0 + b / TJ) * 32 + mfma::patch_row(n4, lane), col = col0 + (j0 + b % TJ) * 32 + mfma::patch_col(n4, lane);
+    const int row = row0 + b / TJ * 32 + mfma::patch_row(n4, lane), col = col0 + b % TJ * 32 + mfma::patch_col(n4, lane);
     n = row < mu.rows ? min(mu.cols - col, 4) : 0;
-    return ((first + (long)at.which) * mu.rows + row) * mu.cols + col;
+    return ((first + (long)which) * mu.rows + row) * mu.cols + col;
   };
   auto ask_old = [&](int b) __attribute__((always_inline)) {
     if constexpr (RES == MUON_UPDATE) {
@@ -245,7 +244,7 @@ __device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, 
       for (int n = 0; n < 4; ++n) v[n] += __builtin_convertvector(h[n], f32x4) * q.f2;
     }
     if (b + AHEAD < NB) ask(b + AHEAD);
-    const int br = row0 + (b0 + i) * 32, bc = col0 + (j0 + j) * 32;
+    const int br = row0 + i * 32, bc = col0 + j * 32;
     if constexpr (RES == SYMMETRIC) {
       if (br == bc && q.diagonal != 0.f) {
 #pragma unroll
@@ -255,13 +254,12 @@ __device__ __forceinline__ void finish(const Product& q, const MuonProblem& mu, 
       }
     }
     if constexpr (RES == SYMMETRIC || RES == KEPT) {
-      const long o = at.which * q.c_one;
+      const long o = which * q.c_one;
 #pragma unroll
       for (int n = 0; n < 4; ++n) h[n] = __builtin_convertvector(v[n], f16x4);
       store_block(stg, h, q.c + origin(b), q.ldc, off, lane);
-      // (a square on the diagonal holds both halves)
       if (RES == KEPT) store_turned(stg, h, q.ct + o + (long)bc * q.ldt + br, q.ldt, off_t, lane);
-      else if (at.mt != at.nt) store_turned(stg, h, q.c + o + (long)bc * q.ldc + br, q.ldc, off, lane);
+      else if (mirrored) store_turned(stg, h, q.c + o + (long)bc * q.ldc + br, q.ldc, off, lane);
       if constexpr (RES == KEPT) {
 #pragma unroll
         for (int n = 0; n < 4; ++n) h[n] = __builtin_convertvector((v[n] - __builtin_convertvector(h[n], f32x4)) * kLow, f16x4);
@@ -395,7 +393,8 @@ __global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProb
 #pragma unroll
         for (int j = 0; j < FN; ++j) to[(i * FN + j) * (NW * 64)] = acc[i][j];
     } else {
-      finish<RES, TM, TN>(q, mu, first, was, acc, 0, 0, wave, stg);
+      const int row0 = was.mt * BM + wave_row(wave), col0 = was.nt * BN + wave_col(wave);
+      if (active) finish<RES, TM, TN>(q, mu, first, was.which, row0, col0, was.mt != was.nt, acc, stg);
     }
     if (!more) break;
   }
@@ -419,33 +418,122 @@ __global__ void __launch_bounds__(NW * 64) join_kernel(Product q, MuonProblem mu
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j) acc[i][j] += from[(i * FN + j) * (NW * 64)];
-  finish<RES, 1, 1>(q, mu, first, at, acc, b0, j0, wave, smem + wave * mfma::STG_BYTES);
+  const int row0 = at.mt * BM + wave_row(wave), col0 = at.nt * BN + wave_col(wave);
+  if (row0 < q.M && col0 < (RES == SYMMETRIC ? q.M : q.N))
+    finish<RES, 1, 1>(q, mu, first, at.which, row0 + b0 * 32, col0 + j0 * 32, at.mt != at.nt, acc, smem + wave * mfma::STG_BYTES);
 }
 
-// Which tiles are cut along K: those behind the last whole round of workgroups, where that is the faster way.  In units of a step's time (1 us): a round takes
-// its steps and about four for its results, adding parts up a launch (5 us) and a read of 256 KB per part.
-struct Cut { int full, split; };
+// The same on tiles of 64 x 64 by four waves, 32 x 32 each, a workgroup per tile: where there are too few large tiles to fill the CUs, a product is
+// bound by how long a tile takes from start to end.  (Sides are multiples of 128: no tile lies half outside.)  Four steps of operands are in LDS or on the way.
+constexpr int SB = 64, STAGES = 4, SNW = 4;
+typedef KTile<SB, BK> SmallTile;
+constexpr int kSmallStage = 2 * SmallTile::BYTES;
+constexpr int kSmallLds = STAGES * kSmallStage + SNW * mfma::STG_BYTES;
+static_assert(2 * kSmallLds <= 160 * 1024, "two workgroups share a CU's LDS");
+
+template <Result RES>
+__global__ void __launch_bounds__(SNW * 64, 2) small_product_kernel(Product q, MuonProblem mu, int first) {
+  extern __shared__ __attribute__((aligned(256))) char smem[];
+  const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wrow = (wave >> 1) * 32, wcol = (wave & 1) * 32;
+  const int tm = q.M / SB, tn = q.N / SB, per = RES == SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn, which = blockIdx.x / per;
+  int at = blockIdx.x - which * per, mt, nt;
+  if constexpr (RES == SYMMETRIC) {
+    mt = (int)((sqrtf(8.f * (float)at + 1.f) - 1.f) * 0.5f);
+    while ((mt + 1) * (mt + 2) / 2 <= at) ++mt;
+    while (mt * (mt + 1) / 2 > at) --mt;
+    mt = __builtin_amdgcn_readfirstlane(mt);
+    nt = at - mt * (mt + 1) / 2;
+  } else {
+    mt = at / tn;
+    nt = at - mt * tn;
+  }
+  const char* l = uniform_ptr(reinterpret_cast<const char*>(q.l + which * q.l_one + (long)mt * SB * q.ldl));
+  const char* r = uniform_ptr(reinterpret_cast<const char*>(q.r + which * q.r_one + (long)nt * SB * q.ldr));
+  constexpr int SLOTS = SmallTile::BYTES / 1024 / SNW;
+  unsigned offl[SLOTS], offr[SLOTS];
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j) {
+    const int row = (wave + j * SNW) * SmallTile::ROWS_PER_DMA + lane / SmallTile::CPR, chunk = (lane % SmallTile::CPR) ^ SmallTile::swz(row);
+    offl[j] = (unsigned)row * (unsigned)q.ldl * 2u + (unsigned)chunk * 16u;
+    offr[j] = (unsigned)row * (unsigned)q.ldr * 2u + (unsigned)chunk * 16u;
+  }
+  auto issue = [&](int s) __attribute__((always_inline)) {
+    const unsigned to = lds + (unsigned)(s % STAGES) * kSmallStage + (unsigned)wave * 1024u;
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      dma16s(l + (long)s * BK * 2, offl[j], to + (unsigned)j * SNW * 1024u);
+      dma16s(r + (long)s * BK * 2, offr[j], to + SmallTile::BYTES + (unsigned)j * SNW * 1024u);
+    }
+  };
+  constexpr int LOADS = 2 * SLOTS;
+  const unsigned fa = mfma::frag_origin<mfma::KMAJOR, SB, BK>(wrow, lane), fb = SmallTile::BYTES + mfma::frag_origin<mfma::KMAJOR, SB, BK>(wcol, lane);
+  f32x4 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int steps = q.K / BK;
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s)
+    if (s < steps) issue(s);
+  for (int s = 0; s < steps; ++s) {
+    // at most the loads of the steps behind this one are on their way
+    if (s + 2 < steps) wait_vmcnt<2 * LOADS>();
+    else if (s + 1 < steps) wait_vmcnt<LOADS>();
+    else wait_vmcnt<0>();
+    __syncthreads();                        // ... and every wave has read step s - 1, whose slot is filled next
+    if (s + STAGES - 1 < steps) issue(s + STAGES - 1);
+    const unsigned base = lds + (unsigned)(s % STAGES) * kSmallStage;
+    f16x8 a[2][2], b[2][2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        a[kk][i] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, SB, BK>(base + fa, i, kk));
+        b[kk][i] = __builtin_bit_cast(f16x8, mfma::read_frag_dma<mfma::KMAJOR, SB, BK>(base + fb, i, kk));
+      }
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[kk][j], a[kk][i], acc[i][j], 0, 0, 0);
+  }
+  finish<RES, 1, 1>(q, mu, first, which, mt * SB + wrow, nt * SB + wcol, mt != nt, acc, smem + STAGES * kSmallStage + wave * mfma::STG_BYTES);
+}
+
+// Which tiles are cut along K: those behind the last whole round of workgroups, where that is the faster way.  By measured times (us): a step 1.9, a tile's
+// results 12, adding parts up a launch, and each of them 256 KB written and read.
+struct Cut { int full, split; double time; };
 Cut cut_of(long tiles, int steps, long most_parts) {
   const int full = (int)(tiles / kGroups * kGroups), rem = (int)(tiles - full);
-  Cut best{(int)tiles, 1};
+  const double rounds = (double)(full / kGroups) * (1.9 * steps + 12);
+  Cut best{(int)tiles, 1, rounds + (rem ? 1.9 * steps + 12 : 0)};
   if (rem == 0) return best;
-  double least = steps + 4;
   for (int split = 2; split <= 32; ++split) {
     const long parts = (long)rem * split;
     if (steps / split < 2 || parts > most_parts) break;
-    const double time = (double)((parts + kGroups - 1) / kGroups) * ((double)steps / split + 2) + 6 + 0.6 * split;
-    if (time < least) {
-      least = time;
-      best = {full, split};
-    }
+    const double time = rounds + (double)((parts + kGroups - 1) / kGroups) * (1.9 * steps / split + 2) + 8 + 0.3 * split + 0.1 * parts;
+    if (time < best.time) best = {full, split, time};
   }
   return best;
 }
+// Small tiles: alone on its CU a workgroup takes 0.35 us a step, 512 of them together 0.65.  (us, all products on small tiles and on large ones: 512 x 512 87, 235;
+// 1024 x 1024 122, 391, 8 of them 593, 799, 16 of them 1239, 697; 2048 x 2048 490, 757; 8 of 512 x 2048 321, 590; 512 x 16384 488, 516.)
+double small_tiles_time(long tiles, int steps) { return fmax(0.35 * steps + 3, (double)tiles / (2 * kGroups) * (0.65 * steps + 4)) + 1.5; }
 constexpr int kMostParts = 512;             // of a launch: 128 MB
 
 template <Result RES> int product(Product q, const MuonProblem& mu, int first, int count, float* parts, hipStream_t s) {
   const long tiles = (long)tiles_of<RES>(q) * count;
   const Cut cut = cut_of(tiles, q.K / BK, kMostParts);
+  const long tm = q.M / SB, tn = q.N / SB, small_tiles = (RES == SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn) * count;
+  if (small_tiles_time(small_tiles, q.K / BK) < cut.time) {
+    small_product_kernel<RES><<<dim3((unsigned)small_tiles), dim3(SNW * 64), kSmallLds, s>>>(q, mu, first);
+    MOE_LAUNCH_CHECK();
+    return MOE_OK;
+  }
   const int rem = (int)(tiles - cut.full);
   q.full = cut.full;
   q.split = cut.split;
@@ -471,6 +559,9 @@ int orth_configure() {
   for (const void* k : {(const void*)product_kernel<SYMMETRIC>, (const void*)product_kernel<KEPT>, (const void*)product_kernel<MUON_UPDATE>,
                         (const void*)product_kernel<OUT_F32>, (const void*)product_kernel<OUT_BF16>})
     MOE_HIP_TRY(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kProductLds));
+  for (const void* k : {(const void*)small_product_kernel<SYMMETRIC>, (const void*)small_product_kernel<KEPT>, (const void*)small_product_kernel<MUON_UPDATE>,
+                        (const void*)small_product_kernel<OUT_F32>, (const void*)small_product_kernel<OUT_BF16>})
+    MOE_HIP_TRY(hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kSmallLds));
   if (const int rc = orth_small_configure()) return rc;
   done.fetch_or(1ull << dev, std::memory_order_release);
   return MOE_OK;
