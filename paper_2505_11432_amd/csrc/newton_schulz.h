@@ -6,7 +6,7 @@ namespace moe {
 
 constexpr int kOrthPad = 128;                // rows and columns of a matrix in the workspace are multiples of this
 constexpr int kNormBlocks = 1024;             // sums of squares per matrix, at most
-constexpr int kSmallSide = 128, kSmallTile = 128;
+constexpr int kSmallSide = 64, kSmallTile = 128;
 struct OrthCoef { double a, b, c; };
 constexpr OrthCoef kDefaultCoef{3.4445, -4.7750, 2.0315};
 

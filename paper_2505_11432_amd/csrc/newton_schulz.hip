@@ -694,12 +694,12 @@ OrthPlan orth_plan(int batch, int rows, int cols, int piece) {
   p.norm_blocks = (int)(blocks < kNormBlocks ? blocks : kNormBlocks);
   p.small = least <= kSmallSide;
   if (p.small) {
-    p.S = least <= kSmallSide / 2 ? kSmallSide / 2 : kSmallSide;
+    p.S = kSmallSide;
     const int tiles = cdiv(most, kSmallTile);
     p.tiles_per_slab = cdiv(tiles, 32);
     p.slabs = cdiv(tiles, p.tiles_per_slab);
     p.gram = 0;
-    p.gram_one = (size_t)count * p.slabs * p.S * p.S * 4;
+    p.gram_one = (size_t)count * p.slabs * p.S * p.S * 8;
     p.t = p.gram_one;
     p.sums = p.t + (size_t)count * p.S * p.S * 4;
     p.bytes = p.sums + (size_t)count * p.norm_blocks * 8 + 256;

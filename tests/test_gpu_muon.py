@@ -1,14 +1,13 @@
 """Orthogonalised updates and Muon against their formulas in 64 bits.
 
-Tolerance of an orthogonalised matrix, in the 2-norm of all elements: what a step adds and what it multiplies earlier errors by.  A step keeps
-A = X X^T and R = b A + c A^2 in 11 bits: a rounding is at most half a step of 2^-11 of its element, 2^-11 / sqrt(3) in the root mean square over
-many elements that round independently.  With s the largest singular value of X and |.| the 2-norm of all elements:
-  dA <= r sqrt(|A|^2 + 2 s^2 |X|^2)  (A's own rounding, and that of the operand on either side),  r = 2^-11 / sqrt(3)
-  dR <= (|b| + 2 |c| s^2) dA + r |R|
-  added: s dR + r |R X| (the operand of R X) + 2^-21 |X| (X itself is carried in 22 bits)
-Earlier errors are multiplied by at most the largest slope of a s + b s^3 + c s^5 on the singular values' range (Lipschitz constant of the matrix function).
-Two adjacent steps may be taken on the powers of one A, whose error then passes through both polynomials: twice the above.  fp32
-accumulation adds up to 2^-24 sqrt(n) of the products' sizes, which a factor of 1.1 covers.  A result in bf16 adds half a step, 2^-8 of each element."""
+Tolerance of an orthogonalised matrix, in the 2-norm of all elements.  A step keeps A = X X^T and R = b A + c A^2 in 11 bits, multiplies with X in 11 bits and
+carries X itself in 22: roundings of at most half a step, 2^-11 or 2^-22 of the element.  What they do to the outcome is found by doing the same to the formula:
+`rounded` walks through the steps in 64 bits and changes every element that is kept by a random share of that size.  Over many elements such a change has
+nearly always the same 2-norm, so a correct kernel lies within it, give or take its few percent of chance; twice that is allowed, and 2^-22 sqrt(n) for sums in
+fp32.  From the fourth step on what is kept is A - m I, m = 0.5 and in the last step 0.8, and with p(A) = a I + b A + c A^2 the part of it that is left beside
+p(m) I: roundings are then shares of those, also in directions where A is nothing.  Large batches take two steps on the powers of one A (pairs).  `rounded` goes
+the same ways.  Matrices with a side of at most 64 are computed in 64 bits but for one product of 22-bit numbers, which is more exact than all that.  A result
+in bf16 adds half a step, 2^-8 of each element."""
 import math
 
 import pytest
@@ -16,28 +15,57 @@ import torch
 
 DEV = "cuda:0"
 STEPS = ((3.4445, -4.7750, 2.0315),) * 5
-R16 = 2.0 ** -11 / math.sqrt(3.0)
 
 
-def exact(u, steps=STEPS):
+def formula(x, steps):
+    for a, b, c in steps:
+        gram = x @ x.t()
+        x = a * x + (b * gram + c * gram @ gram) @ x
+    return x
+
+
+def rounded(x, steps, pairs, seed=5):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+
+    def off(t, bits):
+        return t * (1.0 + (2.0 * torch.rand(t.shape, dtype=torch.float64, device=DEV, generator=g) - 1.0) * 2.0 ** -bits)
+
+    def centre(k):
+        return 0.0 if k < 3 else 0.8 if k + 1 == len(steps) else 0.5
+
+    one = torch.eye(x.shape[0], dtype=torch.float64, device=DEV)
+    k = 0
+    while k < len(steps):
+        (a, b, c), m = steps[k], centre(k)
+        x = off(x, 22)
+        h = off(x, 11)
+        gram = off(h @ h.t() - m * one, 11)
+        r = off((b + 2 * c * m) * gram + c * gram @ gram, 11)
+        s = a + b * m + c * m * m
+        if pairs and k + 1 < len(steps) and (k == 0 or k + 2 == len(steps)):
+            k += 1
+            (a, b, c), m2 = steps[k], centre(k)
+            t = off(s * gram + m * r + r @ gram, 11)
+            gram = off(s * t + s * m * r + r @ t + (s * s * m - m2) * one, 11)
+            r2 = off((b + 2 * c * m2) * gram + c * gram @ gram, 11)
+            s2 = a + b * m2 + c * m2 * m2
+            r = off(s * r2 + s2 * r + r2 @ r, 11)
+            s *= s2
+        x = s * x + r @ h
+        k += 1
+    return x
+
+
+def exact(u, steps=STEPS, pairs=False):
     """(orthogonalised matrix, its tolerance) in 64 bits."""
     u = u.double()
     flip = u.shape[0] > u.shape[1]
-    x = u.t() if flip else u
+    x = u.t().contiguous() if flip else u
     size = x.norm()
     x = x / size if float(size) > 0 else x
-    off = 0.0
-    for a, b, c in steps:
-        s = float(torch.linalg.matrix_norm(x, 2)) if float(size) > 0 else 0.0
-        gram = x @ x.t()
-        r = b * gram + c * gram @ gram
-        d_gram = R16 * math.sqrt(float(gram.norm()) ** 2 + 2 * s ** 2 * float(x.norm()) ** 2)
-        d_r = (abs(b) + 2 * abs(c) * s ** 2) * d_gram + R16 * float(r.norm())
-        v = torch.linspace(0, max(s, 1e-3), 2001, dtype=torch.float64)
-        slope = float((a + 3 * b * v ** 2 + 5 * c * v ** 4).abs().max())
-        off = slope * off + s * d_r + R16 * float((r @ x).norm()) + 2.0 ** -21 * float(x.norm())
-        x = a * x + r @ x
-    return (x.t() if flip else x), 2.2 * off
+    want = formula(x, steps)
+    tol = 2.0 * float((rounded(x, steps, pairs) - want).norm()) + 2.0 ** -22 * math.sqrt(max(x.shape)) * float(want.norm())
+    return (want.t() if flip else want), tol
 
 
 def matrices(batch, rows, cols, kind, seed=0, dtype=torch.float32):
@@ -70,6 +98,42 @@ def test_orthogonal(batch, rows, cols, kind, dtype):
     assert torch.equal(short.apply(x), out.to(torch.bfloat16))
     op.workspace.zero_()
     assert torch.equal(op.apply(x), out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["flat", "falling", "steep", "low rank"])
+@pytest.mark.parametrize("batch,rows,cols", [(1, 1990, 2100), (1, 2100, 1990), (16, 1024, 1000), (9, 900, 1030), (1, 520, 9000), (1, 3000, 3200)])
+def test_large(batch, rows, cols, kind):
+    """Large tiles, in whole rounds and cut along the sums; all of them but the last but one take steps in pairs."""
+    from paper_2505_11432_amd.optim import Orthogonal
+    x = matrices(batch, rows, cols, kind)
+    op = Orthogonal(batch, rows, cols, out_dtype=torch.float32, device=DEV)
+    op.workspace.fill_(255)
+    out = op.apply(x).clone()
+    for i in (0, batch - 1):
+        want, tol = exact(x[i], pairs=min(rows, cols) > 600)
+        assert float((out[i].double() - want).norm()) <= tol, i
+    op.workspace.zero_()
+    assert torch.equal(op.apply(x), out)
+
+
+@pytest.mark.gpu
+def test_large_muon():
+    """An update of large matrices, whose last product writes the parameters: rows and columns that end inside a tile and inside four elements."""
+    from paper_2505_11432_amd.optim import Muon
+    for rows, cols in ((1901, 2503), (2503, 1901)):
+        g = torch.Generator(device=DEV).manual_seed(6)
+        p = torch.randn((2, rows, cols), device=DEV, generator=g) * 0.02
+        grad = (torch.randn((2, rows, cols), device=DEV, generator=g) * 1e-3).to(torch.bfloat16)
+        m, w = torch.zeros_like(p), torch.empty_like(p, dtype=torch.bfloat16)
+        p0 = p.double()
+        Muon([p], [grad], [m], weights=[w], lr=0.02, weight_decay=0.1).step()
+        lr, scale = float(torch.tensor(0.02)), 0.2 * 2503 ** 0.5
+        for i in range(2):
+            o, tol = exact(grad[i].double() * 1.95, pairs=True)
+            want = p0[i] * (1 - lr * 0.1) - lr * scale * o
+            assert float((p[i].double() - want).norm()) <= 2.0 ** -22 * float(p0[i].norm()) + lr * scale * tol
+        assert torch.equal(m, grad.float()) and torch.equal(w, p.to(torch.bfloat16))
 
 
 @pytest.mark.gpu
