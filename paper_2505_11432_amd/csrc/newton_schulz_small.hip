@@ -119,31 +119,30 @@ template <typename TG, bool MUON, typename F> __device__ __forceinline__ void fo
   }
 }
 
-// sums += L R^T of a wave's 32 x 32 (2 x 2 of 16 x 16): the fp64 matrix instruction takes four of k at a time, lane l has row (column) l % 16 and k = l / 16, and
+// sums += L R^T of a wave's 32 x 16 M (2 x M of 16 x 16): the fp64 matrix instruction takes four of k at a time, lane l has row (column) l % 16 and k = l / 16, and
 // of the sums column l % 16 and rows l / 16 + 4 i.
-template <int K, int PITCH, typename T> __device__ __forceinline__ void multiply64(const T* l, const T* r, f64x4 (&sums)[2][2]) {
+template <int K, int PITCH, int M, typename T> __device__ __forceinline__ void multiply64(const T* l, const T* r, f64x4 (&sums)[2][M]) {
   const int lane = threadIdx.x & 63, i = lane & 15, k0 = lane >> 4;
-#pragma unroll 4
+#pragma unroll 8
   for (int k = 0; k < K; k += 4) {
-    double a[2], b[2];
+    double a[2], b[M];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      a[n] = (double)l[(n * 16 + i) * PITCH + k + k0];
-      b[n] = (double)r[(n * 16 + i) * PITCH + k + k0];
-    }
+    for (int n = 0; n < 2; ++n) a[n] = (double)l[(n * 16 + i) * PITCH + k + k0];
+#pragma unroll
+    for (int m = 0; m < M; ++m) b[m] = (double)r[(m * 16 + i) * PITCH + k + k0];
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
-      for (int m = 0; m < 2; ++m) sums[n][m] = __builtin_amdgcn_mfma_f64_16x16x4f64(a[n], b[m], sums[n][m], 0, 0, 0);
+      for (int m = 0; m < M; ++m) sums[n][m] = __builtin_amdgcn_mfma_f64_16x16x4f64(a[n], b[m], sums[n][m], 0, 0, 0);
   }
 }
 // f(row, column, which of the sums) for a wave's sums; row0, col0: where they begin
-template <typename F> __device__ __forceinline__ void each64(int row0, int col0, F f) {
+template <int M, typename F> __device__ __forceinline__ void each64(int row0, int col0, F f) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int n = 0; n < 2; ++n)
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < M; ++m)
 #pragma unroll
       for (int i = 0; i < 4; ++i) f(row0 + n * 16 + (lane >> 4) + 4 * i, col0 + m * 16 + (lane & 15), n, m, i);
 }
@@ -169,34 +168,32 @@ __global__ void __launch_bounds__(kThreads) small_gram_kernel(MuonProblem q, Ort
       for (int k = 0; k < 4; ++k) tile[tall ? (c + k) * kTilePitch + r : r * kTilePitch + c + k] = v[k];
     });
     __syncthreads();
-    multiply64<kSmallTile, kTilePitch>(tile + row0 * kTilePitch, tile + col0 * kTilePitch, acc);
+    multiply64<kSmallTile, kTilePitch, 2>(tile + row0 * kTilePitch, tile + col0 * kTilePitch, acc);
   }
   double* to = parts + ((long)which * gridDim.x + blockIdx.x) * SP * SP;
-  each64(row0, col0, [&](int r, int c, int n, int m, int i) __attribute__((always_inline)) { to[r * SP + c] = acc[n][m][i] * (1.0 / ((double)kScale * kScale)); });
+  each64<2>(row0, col0, [&](int r, int c, int n, int m, int i) __attribute__((always_inline)) { to[r * SP + c] = acc[n][m][i] * (1.0 / ((double)kScale * kScale)); });
 }
 
 // All steps of a matrix: Q, hi and lo, in units of 2^12.  Two matrices in LDS, the others in the registers of the threads that made them.
-__global__ void __launch_bounds__(kThreads) small_steps_kernel(SmallSteps c, int slabs, const double* __restrict__ parts, half* __restrict__ out) {
+__global__ void __launch_bounds__(2 * kThreads) small_steps_kernel(SmallSteps c, int slabs, const double* __restrict__ parts, half* __restrict__ out) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   double* const buf0 = reinterpret_cast<double*>(smem);
   double* const buf1 = buf0 + SP * kGramPitch;
-  const int wave = threadIdx.x >> 6, row0 = (wave >> 1) * 32, col0 = (wave & 1) * 32;
-  f64x4 a[2][2] = {}, r[2][2], q[2][2];
+  const int wave = threadIdx.x >> 6, row0 = (wave >> 2) * 32, col0 = (wave & 3) * 16;
+  f64x4 a[2][1] = {}, r[2][1], q[2][1];
   for (int s = 0; s < slabs; ++s) {
     const double* from = parts + ((long)blockIdx.x * slabs + s) * SP * SP;
-    each64(row0, col0, [&](int y, int x, int n, int m, int i) __attribute__((always_inline)) { a[n][m][i] += from[y * SP + x]; });
+    each64<1>(row0, col0, [&](int y, int x, int n, int m, int i) __attribute__((always_inline)) { a[n][m][i] += from[y * SP + x]; });
   }
-  auto put = [&](double* buf, const f64x4 (&v)[2][2]) __attribute__((always_inline)) {
-    each64(row0, col0, [&](int y, int x, int n, int m, int i) __attribute__((always_inline)) { buf[y * kGramPitch + x] = v[n][m][i]; });
+  auto put = [&](double* buf, const f64x4 (&v)[2][1]) __attribute__((always_inline)) {
+    each64<1>(row0, col0, [&](int y, int x, int n, int m, int i) __attribute__((always_inline)) { buf[y * kGramPitch + x] = v[n][m][i]; });
   };
   // to = (e from + f L R) unit of symmetric matrices
-  auto product = [&](const double* l, const double* rr, double e, double f, double unit, const f64x4 (&from)[2][2], f64x4 (&to)[2][2]) __attribute__((always_inline)) {
-    f64x4 acc[2][2] = {};
-    multiply64<SP, kGramPitch>(l + row0 * kGramPitch, rr + col0 * kGramPitch, acc);
+  auto product = [&](const double* l, const double* rr, double e, double f, double unit, const f64x4 (&from)[2][1], f64x4 (&to)[2][1]) __attribute__((always_inline)) {
+    f64x4 acc[2][1] = {};
+    multiply64<SP, kGramPitch, 1>(l + row0 * kGramPitch, rr + col0 * kGramPitch, acc);
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int m = 0; m < 2; ++m) to[n][m] = (from[n][m] * e + acc[n][m] * f) * unit;
+    for (int n = 0; n < 2; ++n) to[n][0] = (from[n][0] * e + acc[n][0] * f) * unit;
   };
   put(buf0, a);
   __syncthreads();
@@ -206,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) small_steps_kernel(SmallSteps c, int
     put(buf1, r);
     __syncthreads();
     if (more) {
-      f64x4 t[2][2];
+      f64x4 t[2][1];
       product(buf1, buf0, c.a[k], 1.0, 1.0, a, t);
       __syncthreads();
       put(buf0, t);
@@ -215,7 +212,7 @@ __global__ void __launch_bounds__(kThreads) small_steps_kernel(SmallSteps c, int
       __syncthreads();
     }
     if (k == 0) {
-      each64(row0, col0, [&](int y, int x, int n, int m, int i) __attribute__((always_inline)) { q[n][m][i] = (r[n][m][i] + (y == x ? c.a[0] : 0.0)) * c.unit[0]; });
+      each64<1>(row0, col0, [&](int y, int x, int n, int m, int i) __attribute__((always_inline)) { q[n][m][i] = (r[n][m][i] + (y == x ? c.a[0] : 0.0)) * c.unit[0]; });
     } else {
       put(buf0, q);
       __syncthreads();
@@ -228,7 +225,7 @@ __global__ void __launch_bounds__(kThreads) small_steps_kernel(SmallSteps c, int
     }
   }
   half* hi = out + (long)blockIdx.x * 2 * SP * SP;
-  each64(row0, col0, [&](int y, int x, int n, int m, int i) __attribute__((always_inline)) {
+  each64<1>(row0, col0, [&](int y, int x, int n, int m, int i) __attribute__((always_inline)) {
     const double v = q[n][m][i] * (double)kScale;
     const half h = (half)(float)v;
     hi[y * SP + x] = h;
@@ -319,7 +316,7 @@ template <Result RES, typename TG> int run(const MuonProblem& mu, const OrthPlan
   }
   small_gram_kernel<TG, RES == MUON_UPDATE><<<dim3(p.slabs, count), dim3(kThreads), 0, s>>>(mu, p, first, sums, parts);
   MOE_LAUNCH_CHECK();
-  small_steps_kernel<<<dim3(count), dim3(kThreads), kStepsLds, s>>>(c, p.slabs, parts, q);
+  small_steps_kernel<<<dim3(count), dim3(2 * kThreads), kStepsLds, s>>>(c, p.slabs, parts, q);
   MOE_LAUNCH_CHECK();
   const int tiles = cdiv(mu.rows > mu.cols ? mu.rows : mu.cols, kSmallTile);
   small_apply_kernel<RES, TG><<<dim3(tiles, count), dim3(kThreads), 0, s>>>(mu, p, first, sums, q, (float)whole);
