@@ -520,8 +520,10 @@ int moe_block_norm_bwd(const void* out, const void* y, const float* w_after, con
  * O(u) = the matrix that `steps` Newton-Schulz steps X <- a X + b (X X^T) X + c (X X^T)^2 X make from
  * X = u / |u|_F (2-norm of all elements; a matrix of zeros stays one).  coefficients: steps rows (a, b, c) in HOST memory, read
  * before the call returns; NULL: (3.4445, -4.7750, 2.0315) in every step.  Coefficients with which some
- * product on the way may pass 15.5 are refused (MOE_ERR_UNSUPPORTED): operands are 16-bit numbers with
- * fp32 accumulation, X carries 22 bits from step to step; relative error (2-norm) about 2e-3.
+ * product on the way may pass 15 are refused (MOE_ERR_UNSUPPORTED): operands are 16-bit numbers with
+ * fp32 accumulation, X carries 22 bits from step to step.  Relative error (2-norm) for the default steps
+ * 1e-3, matrices of low rank 2e-3; 3e-3 and 6e-3 where piece * m^2 (n - m) > 1.2e10 (sides padded to 128, m < n),
+ * where steps share a Gram matrix, so that piece can change bits; 2e-5 where a side is at most 64.
  * moe_orthogonalize: out = O(x); x in dt, out in out_dt (MOE_F32 or MOE_BF16 each); out may be x.
  * moe_muon, in place, with f = coef[0] (coef NULL: 1):
  *   m = momentum m + f grad,  u = f grad + momentum m  (nesterov=0: u = m),

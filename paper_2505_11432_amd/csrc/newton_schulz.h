@@ -1,4 +1,4 @@
-// What the entry points (api_muon.hip) and the kernels (newton_schulz.hip) of orthogonalised updates share.
+// What the entry points (api_block.hip) and the kernels (newton_schulz.hip) of orthogonalised updates share.
 #pragma once
 #include "moe_common.h"
 

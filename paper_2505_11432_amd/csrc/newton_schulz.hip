@@ -9,8 +9,8 @@
 // coefficients) and are kept times 2^12, where entries down to 1.5e-8 have all their bits.  A rounding of X enters directions of small singular values
 // like a singular value of its own size and is multiplied by up to a = 3.4 in every later step, 485 in five.  X is therefore carried as two fp16, hi + 2^-11 lo
 // (22 bits), a step adds R X, whose operand is hi, to a (hi + lo): what is left out, R lo, has no part in directions that A does not have.  Relative error
-// (2-norm) of 512 x 1024 matrices with singular values falling as i^0, i^-0.5, i^-1, i^-1.5: 1.5e-3, 1.0e-3, 5e-4, 5e-4; with X in one fp16 1.2e-3,
-// 2.4e-3, 4.9e-3, 1.2e-2, in bf16 eight times that.
+// (2-norm) of matrices with singular values flat, falling as i^-0.5, as i^-1.5, and 64 of 512: 6e-4, 6e-4, 9e-4, 1.7e-3 measured; 9e-4, 8e-4, 1.1e-3, 2.3e-3 by a
+// model of these roundings in 64 bits, which gives 2.6e-3, 3.2e-3, 1.6e-2, 3.0e-2 for X in one fp16 and 2.1e-2, 2.6e-2, 0.13, 0.24 for bf16 throughout.
 //
 // Every product reads both operands along the contraction (rows of 128 bytes per step of 64), so X is kept in both orientations: as it lies (hi, lo) and
 // transposed (hi).  Matrices are padded with zeros to multiples of 128 in the workspace, which changes no value.
@@ -112,7 +112,9 @@ struct Product {
 
 // Tiles of 256 x 256 by eight waves, 128 x 64 each, one workgroup per CU that walks a list of tiles.  Operands go from memory to an LDS ring of two steps of
 // 64 directly; the lower four waves, one per SIMD, issue the loads while the others multiply.  The loads of a tile's first step are issued before the results
-// of the tile in front are stored.
+// of the tile in front are stored.  Two 4096 x 14336: the Gram matrices 392 us, 1.26 PFLOP/s of the tiles computed, R X with X rewritten 905 us, 1.06 PFLOP/s, matrix
+// cores 49 % busy at 2.06 GHz; of 64 times 2048 x 1408 787 us, 0.66 PFLOP/s: 22 steps of some 1.1 us and 40 us of results, 0.75 MB of memory per tile, which all CUs
+// move at once (half of the CUs begun half a tile later: 2 % slower).  128 x 256 by two workgroups per CU took 8.2 ms for that update, this 6.75.
 constexpr int BM = 256, BN = 256, BK = 64, NW = 8, LOADERS = 4;
 constexpr int WTM = 128, WTN = 64, FM = WTM / 16, FN = WTN / 16, TM = WTM / 32, TN = WTN / 32;
 typedef KTile<BM, BK> Tile;
@@ -356,29 +358,29 @@ __global__ void __launch_bounds__(NW * 64, 2) product_kernel(Product q, MuonProb
     if (!active) {
       for (int s = 1; s < steps; ++s) open_step(s);
     } else {
-    read_phase(lds, 0);
-    for (int s = 0; s < steps; ++s) {
-      const unsigned base = lds + (unsigned)(s & 1) * kStage;
+      read_phase(lds, 0);
+      for (int s = 0; s < steps; ++s) {
+        const unsigned base = lds + (unsigned)(s & 1) * kStage;
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        if (p < 3) {
-          read_phase(base, p + 1);
-        } else {
-          mfma::wait_lgkmcnt0();
-          if (s + 1 < steps) {
-            open_step(s + 1);
-            read_phase(lds + (unsigned)((s + 1) & 1) * kStage, 0);
+        for (int p = 0; p < 4; ++p) {
+          if (p < 3) {
+            read_phase(base, p + 1);
+          } else {
+            mfma::wait_lgkmcnt0();
+            if (s + 1 < steps) {
+              open_step(s + 1);
+              read_phase(lds + (unsigned)((s + 1) & 1) * kStage, 0);
+            }
           }
+          __builtin_amdgcn_sched_barrier(0);        // (the compiler would move the reads behind the products, to where they are used)
+          const int kk = p >> 1, ph = p & 1;
+#pragma unroll
+          for (int i = 0; i < FM / 2; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+              acc[ph * (FM / 2) + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(held[kk][j], strm[p & 1][i], acc[ph * (FM / 2) + i][j], 0, 0, 0);
         }
-        __builtin_amdgcn_sched_barrier(0);        // (the compiler would move the reads behind the products, to where they are used)
-        const int kk = p >> 1, ph = p & 1;
-#pragma unroll
-        for (int i = 0; i < FM / 2; ++i)
-#pragma unroll
-          for (int j = 0; j < FN; ++j)
-            acc[ph * (FM / 2) + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(held[kk][j], strm[p & 1][i], acc[ph * (FM / 2) + i][j], 0, 0, 0);
       }
-    }
     }
     const Place was = at;
     const int was_part = part;
@@ -571,10 +573,10 @@ namespace {
 // The steps of a piece, each alone or two on the powers of one A.  With A' = A - c I a step's polynomial is
 //   p(A) = s I + R,  s = p(c),  R = (b + 2 c2 c) A' + c2 A'^2
 // The centre c is 0 at first and near the singular values' squares in late steps, where what is kept of A and R is then small (512 x 512, flat
-// spectrum: error 1.5e-3 -> 8e-4).  Two steps share one A and one product with X, which pays where X is large against A; A of the second one is
+// spectrum: error 1.5e-3 -> 8e-4).  Two steps may share one A and one product with X; A of the second one is
 //   A2' = (s I + R)^2 (c I + A') - c' I,  made as  T = s A' + c R + R A',  A2' = s T + s c R + R T + (s^2 c - c') I
 // and both together multiply X with s s' I + (s R' + s' R + R' R).  The first two and the last two are taken so: an error of A2' passes through one
-// polynomial more, which matters least there (steps 0 1, 2, 3 4: errors up to 2.6e-3 for singular values that fall as i^-1.5).
+// polynomial more, which matters least there (steps 0 1, 2, 3 4: errors of 2.1e-3 to 2.6e-3, and 6e-3 of matrices of an eighth of their rank).
 double centre_of(int k, int steps) { return k < 3 ? 0.0 : k + 1 == steps ? 0.8 : 0.5; }
 bool pair_at(int k, int steps) { return k + 1 < steps && (k == 0 || k + 2 == steps); }
 
@@ -715,9 +717,10 @@ OrthPlan orth_plan(int batch, int rows, int cols, int piece) {
   p.t = 2 * x;
   p.other = 3 * x;
   p.gram = 4 * x;
-  // Two steps on one A: 3 n + 5 m instead of 6 n + 2 m products of m^2, and one rewriting of X instead of two, but a launch more: where a product takes
-  // longer than a launch
-  p.pairs = (double)count * p.S * p.S * p.S > 5e9;
+  // Steps in pairs leave out 6 (n - m) m^2 of a matrix's products and two of four rewritings of X, for two launches more and twice the error: where what they leave
+  // out is long (us, in pairs and alone: 64 of 2048 x 1408 6740, 7150; two 4096 x 6144 3460, 3730; 8 of 2048 x 4096 2750, 3070; 2048 x 6144 683, 738; 1536 x 8192
+  // 535, 651; below: 8 of 1024 x 2048 722, 704; 8 of 1024 x 1536 645, 586; 16 of 1024 x 1024 652, 610; 2048 x 2048 500, 441; 1024 x 4096 202, 229).
+  p.pairs = (double)count * p.S * p.S * ((p.R < p.C ? p.C : p.R) - p.S) > 1.2e10;
   p.parts = p.gram + (p.pairs ? 4 : 2) * p.gram_one;
   p.sums = p.parts + (size_t)kMostParts * kPartFloats * 4;
   p.bytes = p.sums + (size_t)count * p.norm_blocks * 8 + 256;

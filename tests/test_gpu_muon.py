@@ -5,7 +5,7 @@ carries X itself in 22: roundings of at most half a step, 2^-11 or 2^-22 of the 
 `rounded` walks through the steps in 64 bits and changes every element that is kept by a random share of that size.  Over many elements such a change has
 nearly always the same 2-norm, so a correct kernel lies within it, give or take its few percent of chance; twice that is allowed, and 2^-22 sqrt(n) for sums in
 fp32.  From the fourth step on what is kept is A - m I, m = 0.5 and in the last step 0.8, and with p(A) = a I + b A + c A^2 the part of it that is left beside
-p(m) I: roundings are then shares of those, also in directions where A is nothing.  Large batches take two steps on the powers of one A (pairs).  `rounded` goes
+p(m) I: roundings are then shares of those, also in directions where A is nothing.  Large batches of long matrices take two steps on the powers of one A (pairs).  `rounded` goes
 the same ways.  Matrices with a side of at most 64 are computed in 64 bits but for one product of 22-bit numbers, which is more exact than all that.  A result
 in bf16 adds half a step, 2^-8 of each element."""
 import math
@@ -77,6 +77,11 @@ def matrices(batch, rows, cols, kind, seed=0, dtype=torch.float32):
     return (x * 10.0 ** torch.randint(-7, 3, (batch, 1, 1), device=DEV, generator=g)).to(dtype)
 
 
+def in_pairs(batch, rows, cols):
+    rows, cols = (-(-n // 128) * 128 for n in (rows, cols))
+    return batch * min(rows, cols) ** 2 * abs(rows - cols) > 1.2e10
+
+
 SHAPES = [(1, 1, 1), (3, 1, 7), (2, 5, 1), (2, 16, 16), (1, 64, 2048), (5, 100, 131), (3, 257, 129), (2, 128, 128), (2, 384, 256), (1, 300, 1000), (1, 1030, 515),
           (9, 65, 64)]
 
@@ -102,16 +107,17 @@ def test_orthogonal(batch, rows, cols, kind, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["flat", "falling", "steep", "low rank"])
-@pytest.mark.parametrize("batch,rows,cols", [(1, 1990, 2100), (1, 2100, 1990), (16, 1024, 1000), (9, 900, 1030), (1, 520, 9000), (1, 3000, 3200)])
+@pytest.mark.parametrize("batch,rows,cols", [(1, 1990, 2100), (1, 2100, 1990), (16, 1024, 1000), (9, 900, 1030), (1, 520, 9000), (1, 3000, 3200),
+                                             (1, 1500, 7100), (1, 7100, 1500), (9, 900, 2500)])
 def test_large(batch, rows, cols, kind):
-    """Large tiles, in whole rounds and cut along the sums; all of them but the last but one take steps in pairs."""
+    """Large tiles, in whole rounds and cut along the sums; the last three take steps in pairs."""
     from paper_2505_11432_amd.optim import Orthogonal
     x = matrices(batch, rows, cols, kind)
     op = Orthogonal(batch, rows, cols, out_dtype=torch.float32, device=DEV)
     op.workspace.fill_(255)
     out = op.apply(x).clone()
     for i in (0, batch - 1):
-        want, tol = exact(x[i], pairs=min(rows, cols) > 600)
+        want, tol = exact(x[i], pairs=in_pairs(batch, rows, cols))
         assert float((out[i].double() - want).norm()) <= tol, i
     op.workspace.zero_()
     assert torch.equal(op.apply(x), out)
@@ -121,16 +127,16 @@ def test_large(batch, rows, cols, kind):
 def test_large_muon():
     """An update of large matrices, whose last product writes the parameters: rows and columns that end inside a tile and inside four elements."""
     from paper_2505_11432_amd.optim import Muon
-    for rows, cols in ((1901, 2503), (2503, 1901)):
+    for rows, cols in ((1901, 2503), (2503, 1901), (1501, 5003), (5003, 1501)):
         g = torch.Generator(device=DEV).manual_seed(6)
         p = torch.randn((2, rows, cols), device=DEV, generator=g) * 0.02
         grad = (torch.randn((2, rows, cols), device=DEV, generator=g) * 1e-3).to(torch.bfloat16)
         m, w = torch.zeros_like(p), torch.empty_like(p, dtype=torch.bfloat16)
         p0 = p.double()
         Muon([p], [grad], [m], weights=[w], lr=0.02, weight_decay=0.1).step()
-        lr, scale = float(torch.tensor(0.02)), 0.2 * 2503 ** 0.5
+        lr, scale = float(torch.tensor(0.02)), 0.2 * max(rows, cols) ** 0.5
         for i in range(2):
-            o, tol = exact(grad[i].double() * 1.95, pairs=True)
+            o, tol = exact(grad[i].double() * 1.95, pairs=in_pairs(2, rows, cols))
             want = p0[i] * (1 - lr * 0.1) - lr * scale * o
             assert float((p[i].double() - want).norm()) <= 2.0 ** -22 * float(p0[i].norm()) + lr * scale * tol
         assert torch.equal(m, grad.float()) and torch.equal(w, p.to(torch.bfloat16))
