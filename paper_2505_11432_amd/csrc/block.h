@@ -9,7 +9,8 @@ constexpr int kSortTile = 4096;             // tokens that a workgroup sorts at 
 constexpr int kSortOne = 2 * kSortTile;
 constexpr int kOneBits = 19;                // bits of a word where one workgroup sorts all
 constexpr int kMaxDigit = 9;                // bits of a sorting pass
-constexpr int kFewTokens = 2048;            // up to so many are not sorted
+constexpr int kFewTokens = 2048;            // up to so many are not sorted, if the workgroups that look through them
+constexpr long kFewLooks = 1L << 24;        // look at no more than so many
 struct EmbeddingPlan {
   bool few, zero_first;                     // no sort; the gradient is zeroed beside the sort
   int chunk, chunks;                        // sorted tokens that one wave adds up

@@ -7,9 +7,9 @@
 // Bound by memory: a row is read once into registers, its statistics are made again in the backward pass from the row that it needs
 // anyway (a sum more in a round of sums that is made anyway, instead of kept numbers).
 //
-// A team of 64 to 1024 threads has a row, eight elements of it per thread and step.  What it holds per column (weights, gate, sums of gradients) is most of its
-// registers, so few teams fit a CU and the rows in flight come from within them: the forward pass takes several rows at a time (one round of barriers serves all
-// of them), the backward pass loads the next row while it works on one.  Sums in fp32.  In the backward pass a team's rows lie one after another; its share
+// A team of 64 to 1024 threads has a row, eight elements of it per thread and step.  In the forward pass the rows in flight are those of the teams that share a
+// CU.  In the backward pass what a team holds per column (weights, gate, sums of gradients) is most of its registers, few teams fit a CU, and a team loads the next
+// row while it works on one.  Sums in fp32.  In the backward pass a team's rows lie one after another; its share
 // of the weights' gradients goes to memory once and a second launch adds the teams up in order.  A row of the gate whose tokens lie with one team is
 // written at once.
 #include "block.h"
@@ -97,8 +97,8 @@ template <int TS, int N> __device__ __forceinline__ void team_sum(float (&v)[N],
 constexpr int block_threads(int ts) { return ts < 256 ? 256 : ts; }
 template <int TS> constexpr int lds_floats() { return 2 * kMostSums * (TS / 64); }
 
-// Teams of the forward pass take groups of R rows in turn.
-template <typename T, int TS, int W, int K, int R>
+// Teams of the forward pass take rows in turn.
+template <typename T, int TS, int W, int K>
 __global__ void __launch_bounds__(block_threads(TS)) norm_fwd_kernel(NormProblem q, int teams) {
   __shared__ __attribute__((aligned(16))) float lds[lds_floats<TS>()];
   const int lane = threadIdx.x % TS, team = blockIdx.x * (block_threads(TS) / TS) + threadIdx.x / TS;
@@ -121,79 +121,61 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_fwd_kernel(NormProblem
     }
   }
   int open = -1;                                    // row of the gate in registers
-  for (long t0 = (long)team * R; t0 < q.T; t0 += (long)teams * R) {
-    const int rows = (int)min((long)R, q.T - t0);
-    Piece<T, W> xr[R][K], yr[R][K];
+  for (long t = team; t < q.T; t += teams) {
+    Piece<T, W> xr[K], yr[K];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const long at = (t0 + r) * q.d + col[k];
-        xr[r][k].v = {};
-        yr[r][k].v = {};
-        if (r < rows && col[k] < q.d) {
-          xr[r][k].load(x + at);
-          if (y) yr[r][k].load(y + at);
-        }
+    for (int k = 0; k < K; ++k) {
+      xr[k].v = {};
+      yr[k].v = {};
+      if (col[k] < q.d) {
+        xr[k].load(x + t * q.d + col[k]);
+        if (y) yr[k].load(y + t * q.d + col[k]);
       }
-    float inv[R];
-    vec<W> o[R][K];
+    }
+    float sum[1];
+    vec<W> o[K];
     if (y) {
+      float inv = 1.f;
       if (q.w_after) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          inv[r] = 0.f;
-#pragma unroll
-          for (int k = 0; k < K; ++k) {
-            const vec<W> v = yr[r][k].get();
-            inv[r] += sum_of<W>(v * v);
-          }
-        }
-        team_sum<TS>(inv, lds, turn);
-#pragma unroll
-        for (int r = 0; r < R; ++r) inv[r] = 1.0f / sqrtf(inv[r] * inv_d + q.eps);
-      }
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (q.gate && r < rows) {
-          const int group = (int)((t0 + r) / q.gate_rows);
-          if (group != open) {
-            open = group;
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-              if (col[k] < q.d) gate[k] = load_f32<W>(q.gate + (long)group * q.d + col[k]);
-          }
-        }
+        sum[0] = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-          vec<W> n = yr[r][k].get();
-          if (q.w_after) n = n * inv[r] * wa[k];
-          if (q.gate) n = n * gate[k];
-          o[r][k] = rounded<T, W>(xr[r][k].get() * q.alpha + n);
-          if (r < rows && col[k] < q.d) store<W>(out + (t0 + r) * q.d + col[k], o[r][k]);
+          const vec<W> v = yr[k].get();
+          sum[0] += sum_of<W>(v * v);
         }
+        team_sum<TS>(sum, lds, turn);
+        inv = 1.0f / sqrtf(sum[0] * inv_d + q.eps);
+      }
+      if (q.gate) {
+        const int group = (int)(t / q.gate_rows);
+        if (group != open) {
+          open = group;
+#pragma unroll
+          for (int k = 0; k < K; ++k)
+            if (col[k] < q.d) gate[k] = load_f32<W>(q.gate + (long)group * q.d + col[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        vec<W> n = yr[k].get();
+        if (q.w_after) n = n * inv * wa[k];
+        if (q.gate) n = n * gate[k];
+        o[k] = rounded<T, W>(xr[k].get() * q.alpha + n);
+        if (col[k] < q.d) store<W>(out + t * q.d + col[k], o[k]);
       }
     } else {
 #pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int k = 0; k < K; ++k) o[r][k] = xr[r][k].get();
+      for (int k = 0; k < K; ++k) o[k] = xr[k].get();
     }
     if (q.w_before) {
+      sum[0] = 0.f;
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        inv[r] = 0.f;
+      for (int k = 0; k < K; ++k) sum[0] += sum_of<W>(o[k] * o[k]);
+      team_sum<TS>(sum, lds, turn);
+      const float inv = 1.0f / sqrtf(sum[0] * inv_d + q.eps);
 #pragma unroll
-        for (int k = 0; k < K; ++k) inv[r] += sum_of<W>(o[r][k] * o[r][k]);
-      }
-      team_sum<TS>(inv, lds, turn);
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const float i = 1.0f / sqrtf(inv[r] * inv_d + q.eps);
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-          if (r < rows && col[k] < q.d) store<W>(h + (t0 + r) * q.d + col[k], o[r][k] * i * wb[k]);
-      }
+      for (int k = 0; k < K; ++k)
+        if (col[k] < q.d) store<W>(h + t * q.d + col[k], o[k] * inv * wb[k]);
     }
   }
 }
@@ -428,25 +410,27 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(NormProblem q, int team
   }
 }
 
-// threads of a team, elements of each and steps of those, rows at a time
-template <int TS_, int W_, int K_, int R_, bool HOLD_ = true> struct Team { static constexpr int TS = TS_, W = W_, K = K_, R = R_; static constexpr bool HOLD = HOLD_; };
+// Threads of a team, elements of each and steps of those; HOLD: see the backward pass.
+template <int TS_, int W_, int K_, bool HOLD_ = true> struct Team { static constexpr int TS = TS_, W = W_, K = K_; static constexpr bool HOLD = HOLD_; };
+// Forward (bf16, all parts, us): a row at a time 16384 x 2048 50 (5.4 TB/s), 8192 x 4096 49, 4096 x 8192 52; two or four rows at a time, which leave room for fewer
+// teams, 53 and 56, 56 and 64, 60; 32768 x 1024 by one wave with two steps 59, by 256 threads of four elements 66.
 template <typename F> int with_fwd_team(int d, F f) {
-  if (d <= 512) return f(Team<64, 8, 1, 4>());
-  if (d <= 1024) return f(Team<256, 4, 1, 4>());
-  if (d <= 2048) return f(Team<256, 8, 1, 4>());
-  if (d <= 4096) return f(Team<512, 8, 1, 4>());
-  if (d <= 8192) return f(Team<1024, 8, 1, 2>());
-  return f(Team<1024, 8, 2, 1>());
+  if (d <= 512) return f(Team<64, 8, 1>());
+  if (d <= 1024) return f(Team<64, 8, 2>());
+  if (d <= 2048) return f(Team<256, 8, 1>());
+  if (d <= 4096) return f(Team<512, 8, 1>());
+  if (d <= 8192) return f(Team<1024, 8, 1>());
+  return f(Team<1024, 8, 2>());
 }
 // Backward (8192 x 4096, bf16, all parts, 256 or 512 teams, us): 256 threads, 16 elements each 91, with the next row ahead 84; 512 threads, 8 elements, a row
 // ahead 82 (4.9 TB/s, what a copy takes); 1024 threads 109 to 127; two to four rows at a time instead of one ahead 103 to 141.
 template <typename F> int with_bwd_team(int d, F f) {
-  if (d <= 512) return f(Team<64, 8, 1, 1>());
-  if (d <= 1024) return f(Team<64, 8, 2, 1>());
-  if (d <= 2048) return f(Team<256, 8, 1, 1>());
-  if (d <= 4096) return f(Team<512, 8, 1, 1>());
-  if (d <= 8192) return f(Team<1024, 8, 1, 1>());
-  return f(Team<1024, 8, 2, 1, false>());
+  if (d <= 512) return f(Team<64, 8, 1>());
+  if (d <= 1024) return f(Team<64, 8, 2>());
+  if (d <= 2048) return f(Team<256, 8, 1>());
+  if (d <= 4096) return f(Team<512, 8, 1>());
+  if (d <= 8192) return f(Team<1024, 8, 1>());
+  return f(Team<1024, 8, 2, false>());
 }
 
 }  // namespace
@@ -466,11 +450,10 @@ int launch_norm_fwd(const NormProblem& q, hipStream_t s) {
   return with_fwd_team(q.d, [&](auto team) {
     typedef decltype(team) C;
     constexpr int per = block_threads(C::TS) / C::TS;
-    const int most = 256 * 2048 / C::TS, groups = cdiv(q.T, C::R);
-    const int teams = groups < most ? groups : most;
+    const int most = 256 * 2048 / C::TS, teams = q.T < most ? q.T : most;
     const dim3 grid((unsigned)cdiv(teams, per)), block(block_threads(C::TS));
-    if (q.dt == MOE_F32) norm_fwd_kernel<float, C::TS, C::W, C::K, C::R><<<grid, block, 0, s>>>(q, teams);
-    else norm_fwd_kernel<bf16, C::TS, C::W, C::K, C::R><<<grid, block, 0, s>>>(q, teams);
+    if (q.dt == MOE_F32) norm_fwd_kernel<float, C::TS, C::W, C::K><<<grid, block, 0, s>>>(q, teams);
+    else norm_fwd_kernel<bf16, C::TS, C::W, C::K><<<grid, block, 0, s>>>(q, teams);
     MOE_LAUNCH_CHECK();
     return (int)MOE_OK;
   });
