@@ -271,6 +271,46 @@ def test_captured_twice_and_replayed():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("batch,rows,cols", [(1, 520, 9000), (1, 1500, 7100), (5, 60, 300), (1, 300, 1000)])
+def test_each_way_from_a_graph(batch, rows, cols):
+    """Tiles cut along the sums, steps in pairs, small matrices, small tiles: replays with new matrices give the eager result's bits."""
+    from paper_2505_11432_amd.optim import Orthogonal
+    eager, replayed = (Orthogonal(batch, rows, cols, device=DEV) for _ in range(2))
+    x = matrices(batch, rows, cols, "falling")
+    replayed.apply(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        replayed.apply(x)
+    for r, kind in enumerate(("steep", "flat", "falling")):
+        x.copy_(matrices(batch, rows, cols, kind, seed=r + 1))
+        graph.replay()
+        assert torch.equal(replayed.out, eager.apply(x))
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once():
+    from paper_2505_11432_amd.optim import Orthogonal
+    shapes = [(1, 1990, 2100), (3, 50, 900), (2, 300, 1000)]
+    ops = [Orthogonal(*s, device=DEV) for s in shapes]
+    xs = [matrices(*s, "falling", seed=i) for i, s in enumerate(shapes)]
+    want = [op.apply(x).clone() for op, x in zip(ops, xs)]
+    late = [torch.zeros_like(x) for x in xs]
+    for op in ops:
+        op.out.zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ops]
+    for op, x, to, s in zip(ops, xs, late, streams):
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(2_000_000)
+            to.copy_(x)
+            op.apply(to)
+    torch.cuda.synchronize()
+    for op, w in zip(ops, want):
+        assert torch.equal(op.out, w)
+
+
+@pytest.mark.gpu
 def test_refused():
     from paper_2505_11432_amd import binding as B
     from paper_2505_11432_amd.optim import Muon, Orthogonal

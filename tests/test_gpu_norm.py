@@ -281,6 +281,34 @@ def test_captured_twice_and_replayed():
 
 
 @pytest.mark.gpu
+def test_on_another_stream():
+    from paper_2505_11432_amd.norm import BlockNorm
+    T, d = 900, 528
+    s = inputs(T, d, torch.bfloat16, True, True, 100, True, seed=3)
+    op = BlockNorm(T, d, gate_rows=100, device=DEV)
+    names = ("out", "h", "dx", "dy", "d_w_after", "d_gate", "d_w_before")
+
+    def both(y):
+        out, _ = op.forward(s["x"], y, s["w_after"], s["gate"], s["w_before"])
+        op.backward(out, y, s["w_after"], s["gate"], s["w_before"], s["d_out"], s["d_h"])
+
+    both(s["y"])
+    want = {k: getattr(op, k).clone() for k in names}
+    later = torch.zeros_like(s["y"])
+    for k in names:
+        getattr(op, k).zero_()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2_000_000)
+        later.copy_(s["y"])
+        both(later)
+    side.synchronize()
+    for k in names:
+        assert torch.equal(getattr(op, k), want[k]), k
+
+
+@pytest.mark.gpu
 def test_refused():
     from paper_2505_11432_amd import binding as B
     from paper_2505_11432_amd.norm import BlockNorm
