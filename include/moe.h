@@ -525,9 +525,12 @@ int moe_block_norm_bwd(const void* out, const void* y, const float* w_after, con
  * 1e-3, matrices of low rank 2e-3; 3e-3 and 6e-3 where piece * m^2 (n - m) > 1.2e10 (sides padded to 128, m < n),
  * where steps share a Gram matrix, so that piece can change bits; 2e-5 where a side is at most 64.
  * moe_orthogonalize: out = O(x); x in dt, out in out_dt (MOE_F32 or MOE_BF16 each); out may be x.
- * moe_muon, in place, with f = coef[0] (coef NULL: 1):
+ * moe_muon_eps, in place, with f = coef[0] (coef NULL: 1):
  *   m = momentum m + f grad,  u = f grad + momentum m  (nesterov=0: u = m),
  *   p = p (1 - lr weight_decay) - lr scale O(u)
+ * where O begins with X = u / max(|u|_F, eps), so that the updates of a matrix without gradients (an expert without tokens) fade with
+ * its momentum: 0.95 m rounds back to m in the smallest fp32 numbers, and a direction of those would be as long as any other.
+ * moe_muon: the same with eps = MOE_MUON_EPS.  (moe_orthogonalize has no such bound: of any matrix but zeros it takes the direction.)
  * p and m fp32, grad in grad_dt, the new p rounded to bf16 into weights (NULL: none).  lr and coef are read on the
  * device.  Where coef[0] is NaN the call changes nothing.  An infinite or NaN gradient spoils its matrix.
  * Pointers are aligned to their elements, no more; what is written shares no memory with another argument.
@@ -535,6 +538,7 @@ int moe_block_norm_bwd(const void* out, const void* y, const float* w_after, con
  * moe_orthogonal_workspace_bytes with the same sizes (0 on invalid sizes).  batch = 0: nothing is enqueued. */
 #define MOE_ORTH_MAX_STEPS 16
 #define MOE_ORTH_MAX_SIDE (1 << 20)
+#define MOE_MUON_EPS 1e-7
 size_t moe_orthogonal_workspace_bytes(int batch, int rows, int cols, int piece);
 int moe_orthogonalize(const void* x, moe_dtype dt, int batch, int rows, int cols, int steps,
                       const double* coefficients, int piece, void* out, moe_dtype out_dt,
@@ -543,6 +547,10 @@ int moe_muon(float* p, const void* grad, moe_dtype grad_dt, float* m, void* weig
              int rows, int cols, const float* lr, const float* coef, double momentum, int nesterov,
              double weight_decay, double scale, int steps, const double* coefficients, int piece,
              void* workspace, size_t ws_bytes, void* stream);
+int moe_muon_eps(float* p, const void* grad, moe_dtype grad_dt, float* m, void* weights, int batch,
+                 int rows, int cols, const float* lr, const float* coef, double momentum, int nesterov,
+                 double weight_decay, double scale, double eps, int steps, const double* coefficients,
+                 int piece, void* workspace, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

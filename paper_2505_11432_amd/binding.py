@@ -36,7 +36,7 @@ EXPORTS = (
     "moe_adamw_table_bytes", "moe_adamw_table", "moe_adamw_table_mixed", "moe_adamw",
     "moe_embedding_workspace_bytes", "moe_embedding_fwd", "moe_embedding_bwd",
     "moe_block_norm_fwd", "moe_block_norm_workspace_bytes", "moe_block_norm_bwd",
-    "moe_orthogonal_workspace_bytes", "moe_orthogonalize", "moe_muon",
+    "moe_orthogonal_workspace_bytes", "moe_orthogonalize", "moe_muon", "moe_muon_eps",
 )
 
 
@@ -457,6 +457,7 @@ def moe_adamw(table, n, total, grad_dt, lr, step, coef, beta1, beta2, eps, weigh
 
 # ---- around the layer: embedding, norms, orthogonalised updates --------------------------------------------------------
 NORM_MAX_WIDTH, ORTH_MAX_STEPS = 16384, 16
+MUON_EPS = 1e-7                                           # MOE_MUON_EPS
 COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5            # of the quintic Newton-Schulz steps
 
 
@@ -535,12 +536,12 @@ def moe_orthogonalize(x, out, workspace, coefficients=COEFFICIENTS, piece=0):
         workspace.numel() * workspace.element_size()))
 
 
-def moe_muon(p, grad, m, weights, lr, coef, momentum, nesterov, weight_decay, scale, workspace, coefficients=COEFFICIENTS, piece=0):
+def moe_muon(p, grad, m, weights, lr, coef, momentum, nesterov, weight_decay, scale, workspace, coefficients=COEFFICIENTS, piece=0, eps=MUON_EPS):
     batch, rows, cols = p.shape
     assert p.dtype == m.dtype == torch.float32 and m.shape == p.shape, "parameters and momentum are fp32, of one size"
     assert grad.shape == p.shape, "gradients have their parameters' sizes"
     assert weights is None or (weights.shape == p.shape and weights.dtype == torch.bfloat16), "weights are bf16, of their parameters' sizes"
     steps, packed = coefficients if isinstance(coefficients[-1], bytes) else _coefficients(coefficients)
-    _check("moe_muon", _native.moe_muon(
-        p, grad, dtype_code(grad.dtype), m, weights, batch, rows, cols, lr, coef, momentum, int(nesterov), weight_decay, scale, steps,
+    _check("moe_muon", _native.moe_muon_eps(
+        p, grad, dtype_code(grad.dtype), m, weights, batch, rows, cols, lr, coef, momentum, int(nesterov), weight_decay, scale, eps, steps,
         packed, piece, workspace, workspace.numel() * workspace.element_size()))

@@ -169,10 +169,17 @@ int moe_orthogonalize(const void* x, moe_dtype dt, int batch, int rows, int cols
 int moe_muon(float* p, const void* grad, moe_dtype grad_dt, float* m, void* weights, int batch, int rows, int cols, const float* lr, const float* coef,
              double momentum, int nesterov, double weight_decay, double scale, int steps, const double* coefficients, int piece, void* workspace,
              size_t ws_bytes, void* stream) {
+  return moe_muon_eps(p, grad, grad_dt, m, weights, batch, rows, cols, lr, coef, momentum, nesterov, weight_decay, scale, MOE_MUON_EPS, steps, coefficients,
+                      piece, workspace, ws_bytes, stream);
+}
+
+int moe_muon_eps(float* p, const void* grad, moe_dtype grad_dt, float* m, void* weights, int batch, int rows, int cols, const float* lr, const float* coef,
+                 double momentum, int nesterov, double weight_decay, double scale, double eps, int steps, const double* coefficients, int piece,
+                 void* workspace, size_t ws_bytes, void* stream) {
   MuonProblem q{};
   const int rc = orthogonal_problem(batch, rows, cols, steps, coefficients, piece, workspace, ws_bytes, &q);
   if (rc != MOE_OK && rc != MOE_ERR_WORKSPACE) return rc;
-  if (!(momentum >= 0 && momentum < 1) || !(weight_decay >= 0) || !(scale >= 0)) return MOE_ERR_INVALID;
+  if (!(momentum >= 0 && momentum < 1) || !(weight_decay >= 0) || !(scale >= 0) || !(eps >= 0)) return MOE_ERR_INVALID;
   if (grad_dt != MOE_F32 && grad_dt != MOE_BF16) return MOE_ERR_UNSUPPORTED;
   if (batch == 0) return MOE_OK;
   if (!p || !grad || !m || !lr) return MOE_ERR_INVALID;
@@ -183,7 +190,7 @@ int moe_muon(float* p, const void* grad, moe_dtype grad_dt, float* m, void* weig
   if (!outputs_apart({{p, n * 4}, {m, n * 4}, {weights, n * 2}}, {{grad, n * dtype_size(grad_dt)}, {lr, 4}, {coef, 4}}, {}, {})) return MOE_ERR_INVALID;
   if (rc != MOE_OK) return rc;
   q.u = grad; q.u_dt = grad_dt; q.p = p; q.m = m; q.w = weights; q.lr = lr; q.factor = coef;
-  q.momentum = (float)momentum; q.nesterov = nesterov != 0; q.decay = weight_decay; q.scale = (float)scale;
+  q.momentum = (float)momentum; q.nesterov = nesterov != 0; q.decay = weight_decay; q.scale = (float)scale; q.eps = eps;
   return launch_orth(q, orth_plan(batch, rows, cols, piece), static_cast<char*>(workspace), as_stream(stream));
 }
 

@@ -226,7 +226,7 @@ PyMethodDef methods[] = {
     MOE_BOUND(moe_expert_ffn_fused_bwd), MOE_BOUND(moe_quant_fp8), MOE_BOUND(moe_dequant_fp8), MOE_BOUND(moe_quant_fp8_tgroup),
     MOE_BOUND(moe_transpose), MOE_BOUND(moe_vocab_score), MOE_BOUND(moe_vocab_loss), MOE_BOUND(moe_grad_clip), MOE_BOUND(moe_adamw),
     MOE_BOUND(moe_embedding_fwd), MOE_BOUND(moe_embedding_bwd), MOE_BOUND(moe_block_norm_fwd), MOE_BOUND(moe_block_norm_bwd),
-    MOE_BOUND(moe_orthogonalize), MOE_BOUND(moe_muon),
+    MOE_BOUND(moe_orthogonalize), MOE_BOUND(moe_muon), MOE_BOUND(moe_muon_eps),
     {"tensor_list", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&tensor_list)), METH_FASTCALL, nullptr},
     {"lists_apart", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&lists_apart)), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 

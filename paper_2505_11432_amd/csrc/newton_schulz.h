@@ -19,6 +19,7 @@ struct MuonProblem {
   const float* lr; const float* factor;
   float momentum, scale; bool nesterov;
   double decay;
+  double eps;                                // least norm that a matrix is divided by
 };
 struct OrthPlan {
   int R, C, S;                               // padded rows, columns, and the smaller of them

@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(256) start_kernel(MuonProblem q, OrthPlan p, i
   double sum = 0;
   for (int i = threadIdx.x; i < p.norm_blocks; i += 256) sum += sums[(long)blockIdx.z * p.norm_blocks + i];
   sum = block_sum(sum, lds);
-  const double scale = sum > 0 ? (double)kScale / sqrt(sum) : sum;      // (no number stays none)
+  const double scale = scale_of_norm(sum, q.eps);
   const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {

@@ -22,6 +22,9 @@ typedef bf16x4 bf16x4_u __attribute__((aligned(2)));
 constexpr float kScale = 4096.f;                        // what is kept is times 2^12
 constexpr float kLow = 2048.f;                          // lo is times 2^11 more
 
+// What a matrix is multiplied by: 2^12 over its norm, or over eps where that is larger.  (No number stays none, zeros stay zeros.)
+__device__ __forceinline__ double scale_of_norm(double sum, double eps) { return sum > 0 ? (double)kScale / fmax(sqrt(sum), eps) : sum; }
+
 __device__ __forceinline__ float factor_of(const float* f) { return f ? *f : 1.0f; }
 
 // four elements, the last ones of a row one by one

@@ -84,8 +84,8 @@ template <int FM, int FN> __device__ __forceinline__ void clear(f32x4 (&v)[FM][F
     for (int j = 0; j < FN; ++j) v[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// 2^12 over the norm of the matrix
-__device__ __forceinline__ double scale_of(const double* sums, int n, double* lds) {
+// of 2^12 over the norm of the matrix
+__device__ __forceinline__ double scale_of(const double* sums, int n, double eps, double* lds) {
   double s = 0;
   for (int i = threadIdx.x; i < n; i += kThreads) s += sums[i];
 #pragma unroll
@@ -95,7 +95,7 @@ __device__ __forceinline__ double scale_of(const double* sums, int n, double* ld
   s = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) s += lds[w];
-  return s > 0 ? (double)kScale / sqrt(s) : s;
+  return scale_of_norm(s, eps);
 }
 
 // f(row, column, four elements) for a tile of X, 128 of the longer side and 64 of the other; zeros outside.
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kThreads) small_gram_kernel(MuonProblem q, Ort
   const int wave = threadIdx.x >> 6, row0 = (wave >> 1) * 32, col0 = (wave & 1) * 32;
   const int which = blockIdx.y, long_side = q.rows > q.cols ? q.rows : q.cols;
   const long base = (first + (long)which) * q.rows * q.cols;
-  const double scale = scale_of(sums + (long)which * p.norm_blocks, p.norm_blocks, lds);
+  const double scale = scale_of(sums + (long)which * p.norm_blocks, p.norm_blocks, q.eps, lds);
   f64x4 acc[2][2] = {};
   const int t1 = min(((int)blockIdx.x + 1) * p.tiles_per_slab, (long_side + kSmallTile - 1) / kSmallTile);
   for (int t = blockIdx.x * p.tiles_per_slab; t < t1; ++t) {
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kThreads) small_apply_kernel(MuonProblem mu, O
     *reinterpret_cast<f16x8*>(to + KTile<SP, SP>::BYTES) = *reinterpret_cast<const f16x8*>(hi + SP * SP + row * SP + chunk * 8);
   }
   const bool tall = mu.rows > mu.cols;
-  const double scale = scale_of(sums + (long)which * p.norm_blocks, p.norm_blocks, reinterpret_cast<double*>(xs));
+  const double scale = scale_of(sums + (long)which * p.norm_blocks, p.norm_blocks, mu.eps, reinterpret_cast<double*>(xs));
   __syncthreads();
   for_tile<TG, MUON>(mu, base, blockIdx.x, scale, [&](int r, int c, f32x4 v) __attribute__((always_inline)) {
     if (tall) Split<kSmallTile, SP>::put(xs, r, c, v);

@@ -96,15 +96,15 @@ class Orthogonal:
 class Muon:
     """In place, for lists of fp32 parameters [..., rows, cols] that are matrices, or batches of them:
     m = momentum m + coef grad,  u = coef grad + momentum m (nesterov; else m),  p = p (1 - lr weight_decay) - lr scale O(u),
-    O(u) as in `Orthogonal`, and the parameters rounded to bf16 into `weights`.
+    O(u) as in `Orthogonal` but of u / max(|u|, eps), and the parameters rounded to bf16 into `weights`.
 
     grads: bf16 or fp32 (a list may have both).  What is written shares no memory (a shared weight comes once).
     scale: None: 0.2 sqrt(max(rows, cols)), with which an update is as large as AdamW's (root mean square about 0.2) and both take one learning
-    rate; or a number for all of them.  lr: a float, or a [1] fp32 device tensor that a schedule writes.  coefficients, max_bytes: as in `Orthogonal`;
+    rate; or a number for all of them.  eps: norm below which an update fades, as that of an expert without tokens does.  lr: a float, or a [1] fp32 device tensor that a schedule writes.  coefficients, max_bytes: as in `Orthogonal`;
     the tensors share one workspace."""
 
     def __init__(self, params, grads, m, weights=None, lr=1e-3, momentum=0.95, nesterov=True, weight_decay=0.1, scale=None, coefficients=B.COEFFICIENTS,
-                 max_bytes: int = 8 << 30, device=None):
+                 max_bytes: int = 8 << 30, device=None, eps=B.MUON_EPS):
         self.params, self.grads, self.m = list(params), list(grads), list(m)
         self.weights = [None] * len(self.params) if weights is None else list(weights)
         assert len(self.params) == len(self.grads) == len(self.m) == len(self.weights), "lists of one length"
@@ -118,7 +118,7 @@ class Muon:
         assert B._apart(lists[:3], lists[3:]), "parameters, momentum and weights share no memory with each other or with a gradient"
         self.lr = lr if isinstance(lr, torch.Tensor) else torch.full((1,), float(lr), dtype=torch.float32, device=device)
         assert self.lr.dtype == torch.float32 and self.lr.numel() == 1, "lr is one fp32 number"
-        self.momentum, self.nesterov, self.weight_decay = momentum, nesterov, weight_decay
+        self.momentum, self.nesterov, self.weight_decay, self.eps = momentum, nesterov, weight_decay, eps
         self.coefficients = B._coefficients(coefficients)
         self.calls, size = [], 256
         for p, g, v, w in zip(self.params, self.grads, self.m, self.weights):
@@ -136,4 +136,4 @@ class Muon:
         """One update; coef: a [1] fp32 device tensor that every gradient is multiplied by (GradClip.coef).  A factor that is NaN leaves the update out."""
         assert coef is None or (coef.dtype == torch.float32 and coef.numel() == 1), "coef is one fp32 number"
         for p, g, m, w, scale, piece in self.calls:
-            B.moe_muon(p, g, m, w, self.lr, coef, self.momentum, self.nesterov, self.weight_decay, scale, self.workspace, self.coefficients, piece)
+            B.moe_muon(p, g, m, w, self.lr, coef, self.momentum, self.nesterov, self.weight_decay, scale, self.workspace, self.coefficients, piece, self.eps)
