@@ -519,11 +519,15 @@ int moe_block_norm_bwd(const void* out, const void* y, const float* w_after, con
 /* Orthogonalised updates (Muon) for a batch of matrices [rows,cols], one after another in memory:
  * O(u) = the matrix that `steps` Newton-Schulz steps X <- a X + b (X X^T) X + c (X X^T)^2 X make from
  * X = u / |u|_F (2-norm of all elements; a matrix of zeros stays one).  coefficients: steps rows (a, b, c) in HOST memory, read
- * before the call returns; NULL: (3.4445, -4.7750, 2.0315) in every step.  Coefficients with which some
- * product on the way may pass 15 are refused (MOE_ERR_UNSUPPORTED): operands are 16-bit numbers with
- * fp32 accumulation, X carries 22 bits from step to step.  Relative error (2-norm) for the default steps
+ * before the call returns; NULL: (3.4445, -4.7750, 2.0315) in every step.  Operands are 16-bit numbers
+ * with fp32 accumulation, X carries 22 bits from step to step.  Refused (MOE_ERR_UNSUPPORTED) are
+ *   - coefficients with which some product on the way may pass 15;
+ *   - lists whose gain G, the largest product of |a| over steps one after another, passes 8192 (of default steps 7 have 5753, 8 have 19800), or
+ *     262144 where a side is at most 64 (10 default steps).
+ * Relative error (2-norm) for the default steps
  * 1e-3, matrices of low rank 2e-3; 3e-3 and 6e-3 where piece * m^2 (n - m) > 1.2e10 (sides padded to 128, m < n),
- * where steps share a Gram matrix, so that piece can change bits; 2e-5 where a side is at most 64.
+ * where steps share a Gram matrix, so that piece can change bits; 2e-5 where a side is at most 64.  What a step rounds off in a direction that the matrix does not have is multiplied by
+ * the later ones: in other lists low rank costs up to 3.5e-5 G (default steps 6e-6 G), with a side of at most 64 4e-7 G.
  * moe_orthogonalize: out = O(x); x in dt, out in out_dt (MOE_F32 or MOE_BF16 each); out may be x.
  * moe_muon_eps, in place, with f = coef[0] (coef NULL: 1):
  *   m = momentum m + f grad,  u = f grad + momentum m  (nesterov=0: u = m),

@@ -46,7 +46,7 @@ int orthogonal_problem(int batch, int rows, int cols, int steps, const double* c
   if (!orth_takes(batch, rows, cols, piece)) return MOE_ERR_UNSUPPORTED;
   for (int k = 0; k < steps; ++k)
     q->coef[k] = coefficients ? OrthCoef{coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2]} : kDefaultCoef;
-  if (!orth_coefficients_ok(q->coef, steps)) return MOE_ERR_UNSUPPORTED;
+  if (!orth_coefficients_ok(q->coef, steps, rows, cols)) return MOE_ERR_UNSUPPORTED;
   q->batch = batch; q->rows = rows; q->cols = cols; q->steps = steps; q->piece = piece;
   if (batch > 0 && (!workspace || !aligned16(workspace) || ws_bytes < orth_plan(batch, rows, cols, piece).bytes)) return MOE_ERR_WORKSPACE;
   return MOE_OK;

@@ -36,7 +36,7 @@ bool orth_takes(int batch, int rows, int cols, int piece);
 OrthPlan orth_plan(int batch, int rows, int cols, int piece);
 int orth_configure();                        // per-device set-up (moe_init)
 bool orth_is_default(const OrthCoef* c, int steps);
-bool orth_coefficients_ok(const OrthCoef* c, int steps);        // every matrix that is kept fits 16 bits
+bool orth_coefficients_ok(const OrthCoef* c, int steps, int rows, int cols);      // every matrix that is kept fits 16 bits, and what it leaves out stays small
 int orth_small_configure();
 int launch_orth_small(const MuonProblem& q, const OrthPlan& p, int first, int count, char* ws, hipStream_t s);
 int launch_orth(const MuonProblem& q, const OrthPlan& p, char* ws, hipStream_t s);
