@@ -524,9 +524,9 @@ int moe_block_norm_bwd(const void* out, const void* y, const float* w_after, con
  *   - coefficients with which some product on the way may pass 15;
  *   - lists whose gain G, the largest product of |a| over steps one after another, passes 8192 (of default steps 7 have 5753, 8 have 19800), or
  *     262144 where a side is at most 64 (10 default steps).
- * Relative error (2-norm) for the default steps
- * 1e-3, matrices of low rank 2e-3; 3e-3 and 6e-3 where piece * m^2 (n - m) > 1.2e10 (sides padded to 128, m < n),
- * where steps share a Gram matrix, so that piece can change bits; 2e-5 where a side is at most 64.  What a step rounds off in a direction that the matrix does not have is multiplied by
+ * Relative error (2-norm) of O for the five default steps: 2e-3, matrices of low rank 3e-3; 3e-3 and 7e-3 where
+ * piece * m^2 (n - m) > 1.2e10 (sides padded to 128, m < n), where steps share a Gram matrix; 2e-5 where a
+ * side is at most 64, of low rank 2e-4.  What a step rounds off in a direction that the matrix does not have is multiplied by
  * the later ones: in other lists low rank costs up to 3.5e-5 G (default steps 6e-6 G), with a side of at most 64 4e-7 G.
  * moe_orthogonalize: out = O(x); x in dt, out in out_dt (MOE_F32 or MOE_BF16 each); out may be x.
  * moe_muon_eps, in place, with f = coef[0] (coef NULL: 1):

@@ -9,8 +9,8 @@
 // coefficients) and are kept times 2^12, where entries down to 1.5e-8 have all their bits.  A rounding of X enters directions of small singular values
 // like a singular value of its own size and is multiplied by up to a = 3.4 in every later step, 485 in five.  X is therefore carried as two fp16, hi + 2^-11 lo
 // (22 bits), a step adds R X, whose operand is hi, to a (hi + lo): what is left out, R lo, has no part in directions that A does not have.  Relative error
-// (2-norm) of matrices with singular values flat, falling as i^-0.5, as i^-1.5, and 64 of 512: 6e-4, 6e-4, 9e-4, 1.7e-3 measured; 9e-4, 8e-4, 1.1e-3, 2.3e-3 by a
-// model of these roundings in 64 bits, which gives 2.6e-3, 3.2e-3, 1.6e-2, 3.0e-2 for X in one fp16 and 2.1e-2, 2.6e-2, 0.13, 0.24 for bf16 throughout.
+// (2-norm) of matrices with singular values flat, falling as i^-0.5, as i^-1.5, and 64 of 512: 6e-4, 6e-4, 9e-4, 1.7e-3 measured (of rank 1 1.9e-3, of small full ones,
+// 65 x 512, 1.2e-3); 9e-4, 8e-4, 1.1e-3, 2.3e-3 by a model of these roundings in 64 bits, which gives 2.6e-3, 3.2e-3, 1.6e-2, 3.0e-2 for X in one fp16 and 2.1e-2, 2.6e-2, 0.13, 0.24 for bf16 throughout.
 //
 // Every product reads both operands along the contraction (rows of 128 bytes per step of 64), so X is kept in both orientations: as it lies (hi, lo) and
 // transposed (hi).  Matrices are padded with zeros to multiples of 128 in the workspace, which changes no value.
