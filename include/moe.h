@@ -539,7 +539,9 @@ int moe_block_norm_bwd(const void* out, const void* y, const float* w_after, con
  * device.  Where coef[0] is NaN the call changes nothing.  An infinite or NaN gradient spoils its matrix.
  * Pointers are aligned to their elements, no more; what is written shares no memory with another argument.
  * piece matrices are taken at a time (0: all of them, 32768 at most), which bounds the workspace:
- * moe_orthogonal_workspace_bytes with the same sizes (0 on invalid sizes).  batch = 0: nothing is enqueued. */
+ * moe_orthogonal_workspace_bytes with the same sizes (0 on invalid sizes).  batch = 0: nothing is enqueued.
+ * The same sizes, batch and piece give the same bits.  How sums are cut depends on the number of matrices that are taken together, so
+ * another batch or piece can change a matrix's bits, within the errors above, and of equal matrices those of a last, smaller piece can differ. */
 #define MOE_ORTH_MAX_STEPS 16
 #define MOE_ORTH_MAX_SIDE (1 << 20)
 #define MOE_MUON_EPS 1e-7

@@ -76,7 +76,8 @@ class Orthogonal:
     vectors as they are.
 
     coefficients: a row (a, b, c) per step X <- a X + b (X X^T) X + c (X X^T)^2 X.  Roundings of matrices of low rank grow by |a| a step: lists with a product of
-    |a| above 8192 (with a side of at most 64: 262144) are refused, as are those that leave the range of 16 bits.  max_bytes bounds the workspace: matrices are taken in pieces.
+    |a| above 8192 (with a side of at most 64: 262144) are refused, as are those that leave the range of 16 bits.
+    max_bytes bounds the workspace: matrices are taken in pieces (how many at a time can change the bits of the sums, not their exactness).
     Buffer: out [batch, rows, cols] in out_dtype (bf16 or fp32)."""
 
     def __init__(self, batch: int, rows: int, cols: int, out_dtype=torch.bfloat16, coefficients=B.COEFFICIENTS, max_bytes: int = 8 << 30, device="cuda:0"):
