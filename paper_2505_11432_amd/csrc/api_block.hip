@@ -40,15 +40,17 @@ bool outputs_apart(std::initializer_list<Range> outputs, std::initializer_list<R
   return true;
 }
 
-// sizes, steps and workspace of a batch of matrices; fills in the problem
-int orthogonal_problem(int batch, int rows, int cols, int steps, const double* coefficients, int piece, const void* workspace, size_t ws_bytes, MuonProblem* q) {
+// sizes, steps and workspace of a batch of matrices; fills in the problem and how it is taken
+int orthogonal_problem(int batch, int rows, int cols, int steps, const double* coefficients, int piece, const void* workspace, size_t ws_bytes, MuonProblem* q,
+                       OrthPlan* plan) {
   if (batch < 0 || rows < 1 || cols < 1 || piece < 0 || steps < 1 || steps > MOE_ORTH_MAX_STEPS) return MOE_ERR_INVALID;
   if (!orth_takes(batch, rows, cols, piece)) return MOE_ERR_UNSUPPORTED;
   for (int k = 0; k < steps; ++k)
     q->coef[k] = coefficients ? OrthCoef{coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2]} : kDefaultCoef;
   if (!orth_coefficients_ok(q->coef, steps, rows, cols)) return MOE_ERR_UNSUPPORTED;
   q->batch = batch; q->rows = rows; q->cols = cols; q->steps = steps; q->piece = piece;
-  if (batch > 0 && (!workspace || !aligned16(workspace) || ws_bytes < orth_plan(batch, rows, cols, piece).bytes)) return MOE_ERR_WORKSPACE;
+  *plan = orth_plan(batch, rows, cols, piece);
+  if (batch > 0 && (!workspace || !aligned16(workspace) || ws_bytes < plan->bytes)) return MOE_ERR_WORKSPACE;
   return MOE_OK;
 }
 
@@ -152,7 +154,8 @@ size_t moe_orthogonal_workspace_bytes(int batch, int rows, int cols, int piece) 
 int moe_orthogonalize(const void* x, moe_dtype dt, int batch, int rows, int cols, int steps, const double* coefficients, int piece, void* out,
                       moe_dtype out_dt, void* workspace, size_t ws_bytes, void* stream) {
   MuonProblem q{};
-  const int rc = orthogonal_problem(batch, rows, cols, steps, coefficients, piece, workspace, ws_bytes, &q);
+  OrthPlan plan{};
+  const int rc = orthogonal_problem(batch, rows, cols, steps, coefficients, piece, workspace, ws_bytes, &q, &plan);
   if (rc != MOE_OK && rc != MOE_ERR_WORKSPACE) return rc;
   if ((dt != MOE_F32 && dt != MOE_BF16) || (out_dt != MOE_F32 && out_dt != MOE_BF16)) return MOE_ERR_UNSUPPORTED;
   if (batch == 0) return MOE_OK;
@@ -163,7 +166,7 @@ int moe_orthogonalize(const void* x, moe_dtype dt, int batch, int rows, int cols
   if (!(out == x && dt == out_dt) && !apart(out, n * dtype_size(out_dt), x, n * dtype_size(dt))) return MOE_ERR_INVALID;
   if (rc != MOE_OK) return rc;
   q.u = x; q.u_dt = dt; q.out = out; q.out_dt = out_dt;
-  return launch_orth(q, orth_plan(batch, rows, cols, piece), static_cast<char*>(workspace), as_stream(stream));
+  return launch_orth(q, plan, static_cast<char*>(workspace), as_stream(stream));
 }
 
 int moe_muon(float* p, const void* grad, moe_dtype grad_dt, float* m, void* weights, int batch, int rows, int cols, const float* lr, const float* coef,
@@ -177,7 +180,8 @@ int moe_muon_eps(float* p, const void* grad, moe_dtype grad_dt, float* m, void* 
                  double momentum, int nesterov, double weight_decay, double scale, double eps, int steps, const double* coefficients, int piece,
                  void* workspace, size_t ws_bytes, void* stream) {
   MuonProblem q{};
-  const int rc = orthogonal_problem(batch, rows, cols, steps, coefficients, piece, workspace, ws_bytes, &q);
+  OrthPlan plan{};
+  const int rc = orthogonal_problem(batch, rows, cols, steps, coefficients, piece, workspace, ws_bytes, &q, &plan);
   if (rc != MOE_OK && rc != MOE_ERR_WORKSPACE) return rc;
   if (!(momentum >= 0 && momentum < 1) || !(weight_decay >= 0) || !(scale >= 0) || !(eps >= 0)) return MOE_ERR_INVALID;
   if (grad_dt != MOE_F32 && grad_dt != MOE_BF16) return MOE_ERR_UNSUPPORTED;
@@ -191,7 +195,7 @@ int moe_muon_eps(float* p, const void* grad, moe_dtype grad_dt, float* m, void* 
   if (rc != MOE_OK) return rc;
   q.u = grad; q.u_dt = grad_dt; q.p = p; q.m = m; q.w = weights; q.lr = lr; q.factor = coef;
   q.momentum = (float)momentum; q.nesterov = nesterov != 0; q.decay = weight_decay; q.scale = (float)scale; q.eps = eps;
-  return launch_orth(q, orth_plan(batch, rows, cols, piece), static_cast<char*>(workspace), as_stream(stream));
+  return launch_orth(q, plan, static_cast<char*>(workspace), as_stream(stream));
 }
 
 }  // extern "C"

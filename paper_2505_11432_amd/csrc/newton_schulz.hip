@@ -16,9 +16,11 @@
 // transposed (hi).  Matrices are padded with zeros to multiples of 128 in the workspace, which changes no value.
 #include <math.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "newton_schulz_device.h"
+#include "orth_tiles.h"
 
 namespace moe {
 namespace {
@@ -123,7 +125,7 @@ constexpr int kRing = 2 * kStage;
 constexpr int kProductLds = kRing + NW * mfma::STG_BYTES;
 static_assert(kProductLds <= 160 * 1024, "LDS of a CU");
 constexpr int kPartFloats = BM * BN;
-constexpr int kGroups = 256;                // workgroups: a CU each
+static_assert(kPartFloats == kOrthPartFloats && BM == kOrthTile && BK == kOrthStep, "what the choice of tiles goes by");
 
 // A wave's rows and columns in the tile.  Waves w and w + 4 share a SIMD: they lie in opposite halves along both sides, so that of a tile that is half
 // outside each SIMD has one wave to multiply for (the others skip their products).
@@ -427,7 +429,7 @@ __global__ void __launch_bounds__(NW * 64) join_kernel(Product q, MuonProblem mu
 
 // The same on tiles of 64 x 64 by four waves, 32 x 32 each, a workgroup per tile: where there are too few large tiles to fill the CUs, a product is
 // bound by how long a tile takes from start to end.  (Sides are multiples of 128: no tile lies half outside.)  Four steps of operands are in LDS or on the way.
-constexpr int SB = 64, STAGES = 4, SNW = 4;
+constexpr int SB = kOrthSmallTile, STAGES = 4, SNW = 4;
 typedef KTile<SB, BK> SmallTile;
 constexpr int kSmallStage = 2 * SmallTile::BYTES;
 constexpr int kSmallLds = STAGES * kSmallStage + SNW * mfma::STG_BYTES;
@@ -506,31 +508,10 @@ __global__ void __launch_bounds__(SNW * 64, 2) small_product_kernel(Product q, M
   finish<RES, 1, 1>(q, mu, first, which, mt * SB + wrow, nt * SB + wcol, mt != nt, acc, smem + STAGES * kSmallStage + wave * mfma::STG_BYTES);
 }
 
-// Which tiles are cut along K: those behind the last whole round of workgroups, where that is the faster way.  By measured times (us): a step 1.9, a tile's
-// results 12, adding parts up a launch, and each of them 256 KB written and read.
-struct Cut { int full, split; double time; };
-Cut cut_of(long tiles, int steps, long most_parts) {
-  const int full = (int)(tiles / kGroups * kGroups), rem = (int)(tiles - full);
-  const double rounds = (double)(full / kGroups) * (1.9 * steps + 12);
-  Cut best{(int)tiles, 1, rounds + (rem ? 1.9 * steps + 12 : 0)};
-  if (rem == 0) return best;
-  for (int split = 2; split <= 32; ++split) {
-    const long parts = (long)rem * split;
-    if (steps / split < 2 || parts > most_parts) break;
-    const double time = rounds + (double)((parts + kGroups - 1) / kGroups) * (1.9 * steps / split + 2) + 8 + 0.3 * split + 0.1 * parts;
-    if (time < best.time) best = {full, split, time};
-  }
-  return best;
-}
-// Small tiles: alone on its CU a workgroup takes 0.35 us a step, 512 of them together 0.65.  (us, all products on small tiles and on large ones: 512 x 512 87, 235;
-// 1024 x 1024 122, 391, 8 of them 593, 799, 16 of them 1239, 697; 2048 x 2048 490, 757; 8 of 512 x 2048 321, 590; 512 x 16384 488, 516.)
-double small_tiles_time(long tiles, int steps) { return fmax(0.35 * steps + 3, (double)tiles / (2 * kGroups) * (0.65 * steps + 4)) + 1.5; }
-constexpr int kMostParts = 512;             // of a launch: 128 MB
-
 template <Result RES> int product(Product q, const MuonProblem& mu, int first, int count, float* parts, hipStream_t s) {
-  const long tiles = (long)tiles_of<RES>(q) * count;
-  const Cut cut = cut_of(tiles, q.K / BK, kMostParts);
-  const long tm = q.M / SB, tn = q.N / SB, small_tiles = (RES == SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn) * count;
+  const OrthTiles t = orth_tiles(RES == SYMMETRIC, q.M, q.N);
+  const long tiles = t.large * count, small_tiles = t.small * count;
+  const Cut cut = cut_of(tiles, q.K / BK);
   if (small_tiles_time(small_tiles, q.K / BK) < cut.time) {
     small_product_kernel<RES><<<dim3((unsigned)small_tiles), dim3(SNW * 64), kSmallLds, s>>>(q, mu, first);
     MOE_LAUNCH_CHECK();
@@ -722,7 +703,10 @@ OrthPlan orth_plan(int batch, int rows, int cols, int piece) {
   // 535, 651; below: 8 of 1024 x 2048 722, 704; 8 of 1024 x 1536 645, 586; 16 of 1024 x 1024 652, 610; 2048 x 2048 500, 441; 1024 x 4096 202, 229).
   p.pairs = (double)count * p.S * p.S * ((p.R < p.C ? p.C : p.R) - p.S) > 1.2e10;
   p.parts = p.gram + (p.pairs ? 4 : 2) * p.gram_one;
-  p.sums = p.parts + (size_t)kMostParts * kPartFloats * 4;
+  const int contracted = p.R < p.C ? p.C : p.R;
+  const long gram_parts = orth_most_parts(true, p.S, p.S, contracted, count), square_parts = orth_most_parts(true, p.S, p.S, p.S, count),
+             x_parts = orth_most_parts(false, p.R, p.C, p.S, count);
+  p.sums = p.parts + (size_t)std::max(gram_parts, std::max(square_parts, x_parts)) * kOrthPartFloats * 4;
   p.bytes = p.sums + (size_t)count * p.norm_blocks * 8 + 256;
   return p;
 }

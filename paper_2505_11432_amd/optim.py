@@ -63,11 +63,10 @@ class AdamW:
 def _piece(batch: int, rows: int, cols: int, max_bytes: int) -> int:
     """Matrices at a time whose workspace stays within max_bytes (one at least)."""
     assert batch >= 0 and rows > 0 and cols > 0, "matrices have rows and columns"
-    one, two = (B.moe_orthogonal_workspace_bytes(n, rows, cols) for n in (1, 2))
-    assert one > 0, f"unsupported matrices: {rows} x {cols}"
-    piece = max(1, min(batch, 1 + max(0, max_bytes - one) // max(1, two - one), 32768)) if two > 0 else 1
+    assert B.moe_orthogonal_workspace_bytes(1, rows, cols) > 0, f"unsupported matrices: {rows} x {cols}"
+    piece = max(1, min(batch, 32768))
     while piece > 1 and not 0 < B.moe_orthogonal_workspace_bytes(batch, rows, cols, piece) <= max_bytes:
-        piece -= (piece + 7) // 8           # (what is kept per matrix depends a little on their number)
+        piece -= (piece + 15) // 16
     return piece
 
 

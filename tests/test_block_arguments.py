@@ -1,5 +1,7 @@
 """Host-only checks of arguments of the calls around the layer, beside those of test_block_abi.  Nothing here reaches a stream."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 
@@ -54,3 +56,67 @@ def test_gain_of_the_steps(lib):
     assert both(100, 100, 15, [slow] * 14 + [still]) == -2
     assert both(100, 100, 14, [still] + [slow] * 13) == -3 and both(100, 100, 15, [still] + [slow] * 14) == -2
     assert both(100, 100, 16, [(1.5, -0.5, 0.0)] * 16) == -3
+
+
+def test_orthogonal_workspace(lib):
+    """What is asked for beside the matrices: nothing for parts of tiles where no tile is cut; more matrices never need less."""
+    size = lib.moe_orthogonal_workspace_bytes
+    assert size(1, 65, 65, 0) < MB and size(1, 300, 1000, 0) < 8 * MB and size(1, 1, 1, 0) < MB
+    for rows, cols in ((65, 65), (300, 1000), (520, 9000), (2000, 2000), (128, 16384), (1500, 7100)):
+        sizes = [size(n, rows, cols, 0) for n in range(1, 40)]
+        assert sizes == sorted(sizes)
+        x, gram = 2 * (-(-rows // 128) * 128) * (-(-cols // 128) * 128), 2 * (-(-min(rows, cols) // 128) * 128) ** 2
+        for n, s in enumerate(sizes, 1):
+            assert n * (4 * x + 2 * gram) < s <= n * (4 * x + 4 * gram) + 128 * MB + 64 * 1024
+
+
+def test_matrices_at_a_time():
+    from paper_2505_11432_amd import binding as B
+    from paper_2505_11432_amd.optim import _piece
+    assert _piece(4096, 100, 100, 64 * MB) > 300 and _piece(100, 300, 1000, 64 * MB) > 4
+    assert _piece(0, 100, 100, MB) == _piece(1, 100, 100, 1) == _piece(9, 100, 100, 1) == 1
+    for batch, rows, cols, most in ((64, 2048, 1408, 8 << 30), (64, 2048, 1408, 1 << 30), (50000, 16, 16, 1 << 30), (7, 4096, 14336, 2 << 30)):
+        piece = _piece(batch, rows, cols, most)
+        assert 1 <= piece <= min(batch, 32768) and 0 < B.moe_orthogonal_workspace_bytes(batch, rows, cols, piece)
+        assert piece == 1 or B.moe_orthogonal_workspace_bytes(batch, rows, cols, piece) <= most
+    with pytest.raises(AssertionError):
+        _piece(1, (1 << 20) + 1, 8, MB)
+
+
+PROGRAM = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "orth_tiles.h"
+using namespace moe;
+int main() {
+  std::srand(3);
+  long bad = 0, cut = 0;
+  for (int i = 0; i < 3000; ++i) {
+    const bool symmetric = i & 1;
+    const int M = 128 * (1 + std::rand() % (i % 3 ? 12 : 60)), N = symmetric ? M : 128 * (1 + std::rand() % (i % 3 ? 12 : 60)), K = 128 * (1 + std::rand() % (i % 5 ? 20 : 130));
+    const OrthTiles t = orth_tiles(symmetric, M, N);
+    long before = 0;
+    for (int n = 1; n <= 300; ++n) {
+      const long bound = orth_most_parts(symmetric, M, N, K, n);
+      bad += bound < before || bound > kMostParts;
+      before = bound;
+      const Cut c = cut_of(t.large * n, K / kOrthStep);
+      const long parts = small_tiles_time(t.small * n, K / kOrthStep) < c.time || c.split == 1 ? 0 : (t.large * n - c.full) * c.split;
+      cut += parts > 0;
+      if (parts > bound && bad++ < 10) std::printf("%d x %d x %d, %d: %ld parts, bound %ld\n", M, N, K, n, parts, bound);
+    }
+  }
+  std::printf("bad %ld, cut %ld\n", bad, cut);
+  return bad != 0 || cut < 1000;
+}
+"""
+
+
+def test_parts_fit(tmp_path):
+    """The parts of cut tiles, for the chosen tiles of every number of matrices, lie within what the workspace holds (orth_tiles.h is host code without HIP)."""
+    src, exe = tmp_path / "p.cpp", tmp_path / "p"
+    src.write_text(PROGRAM)
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2505_11432_amd", "csrc")
+    subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-I", csrc, str(src), "-o", str(exe)], check=True)
+    res = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert res.returncode == 0, res.stdout

@@ -34,3 +34,19 @@ def test_in_place(batch, rows, cols, piece, dtype):
     B.moe_orthogonalize(x, want, workspace, piece=piece)
     B.moe_orthogonalize(x, x, workspace, piece=piece)
     assert torch.equal(x, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,rows,cols,piece", [(1, 65, 65, 0), (1, 300, 1000, 0), (1, 520, 9000, 0), (2, 520, 9000, 0), (3, 520, 9000, 2), (8, 128, 16384, 0), (1, 1990, 2100, 0),
+                                                   (9, 900, 1030, 0), (9, 900, 2500, 4), (1, 1500, 7100, 0), (3, 50, 900, 0)])
+def test_nothing_behind_the_workspace(batch, rows, cols, piece):
+    """A workspace of exactly the size that is asked for: what lies behind it stays as it was."""
+    from paper_2505_11432_amd import binding as B
+    size = B.moe_orthogonal_workspace_bytes(batch, rows, cols, piece)
+    buffer = torch.full((size + (32 << 20),), 77, dtype=torch.uint8, device=DEV)
+    x = matrices(batch, rows, cols, "falling")
+    out = torch.empty_like(x)
+    B.moe_orthogonalize(x, out, buffer[:size], piece=piece)
+    assert bool((buffer[size:] == 77).all())
+    want, tol = exact(x[-1], pairs=in_pairs(piece or batch, rows, cols))
+    assert float((out[-1].double() - want).norm()) <= tol
