@@ -137,7 +137,8 @@ int moe_block_norm_bwd(const void* out, const void* y, const float* w_after, con
   const void* read_out = w_before ? out : nullptr;
   const void* read_y = w_after || gate ? y : nullptr;
   if (!outputs_apart({{dx, rows}, {dy, rows}, {d_w_after, vec}, {d_gate, gates}, {d_w_before, vec}},
-                     {{read_out, rows}, {read_y, rows}, {d_out, rows}, {d_h, rows}, {w_after, vec}, {gate, gates}, {w_before, vec}}, {dx, dy}, {d_out, d_h, read_y}))
+                     {{read_out, rows}, {read_y, rows}, {d_out, rows}, {d_h, rows}, {w_after, vec}, {gate, gates}, {w_before, vec}}, {dx, dy}, {d_out, d_h, read_y}) ||
+      (dx == read_y && dx != d_out && dx != d_h))
     return MOE_ERR_INVALID;
   NormProblem q{};
   q.x = read_out; q.y = read_y; q.w_after = w_after; q.gate = gate; q.w_before = w_before; q.dt = dt; q.T = T; q.d = d; q.gate_rows = gate ? gate_rows : 1;

@@ -120,3 +120,20 @@ def test_parts_fit(tmp_path):
     subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-I", csrc, str(src), "-o", str(exe)], check=True)
     res = subprocess.run([str(exe)], capture_output=True, text=True)
     assert res.returncode == 0, res.stdout
+
+
+def test_norm_gradients_in_place(lib):
+    """dx may be d_out or d_h, dy y or the other of them: what is allowed goes on to the workspace, which is too small here (-3), y for dx is not."""
+    lib.moe_block_norm_bwd.argtypes = [P] * 7 + [I, I, I, I, D, D] + [P] * 5 + [I, P, Z, P]
+    need = lib.moe_block_norm_workspace_bytes(8, 64, BF16, 1, 1, 1)
+
+    def bwd(dx, dy, y=P(2 * MB), n=need):
+        return lib.moe_block_norm_bwd(P(MB), y, P(3 * MB), P(4 * MB), P(5 * MB), P(6 * MB), P(7 * MB), BF16, 8, 64, 4, 1.0, 1e-6, dx, dy, P(10 * MB), P(11 * MB),
+                                      P(12 * MB), 0, P(13 * MB), n, None)
+
+    y, d_out, d_h = P(2 * MB), P(6 * MB), P(7 * MB)
+    for dy in (P(9 * MB), d_out, d_h):
+        assert bwd(y, dy) == -1
+    assert bwd(d_out, d_out) == bwd(d_h, d_h) == -1
+    for dx in (P(8 * MB), d_out, d_h):
+        assert bwd(dx, y, n=need - 1) == bwd(dx, P(9 * MB), n=need - 1) == -3
