@@ -471,7 +471,7 @@ int moe_adamw(const void* table /*device*/, int n, int64_t total, moe_dtype grad
  * (Section 2.1's transformer block around the MoE layer; Section 4.1 names the norms, the paper gives no formula.)
  *
  * Embedding: out[t,:] = scale * table[tokens[t],:], rounded once; a token outside 0..V-1 (padding)
- * gives a row of zeros.  table [V,d] and out [T,d] in `dt` (MOE_F32 or MOE_BF16); d a multiple of 16.
+ * gives a row of zeros.  scale is finite in fp32.  table [V,d] and out [T,d] in `dt` (MOE_F32 or MOE_BF16); d a multiple of 16.
  * out shares no memory with table.  T = 0: nothing is enqueued.
  * moe_embedding_bwd: d_table[v,:] = scale * sum of dy[t,:] over the tokens t that are v, summed in fp32
  * in an order that only the tokens and the sizes decide (reproducible), rounded once to grad_dt

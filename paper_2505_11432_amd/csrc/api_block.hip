@@ -1,5 +1,6 @@
 // extern "C" entry points of the parts around the layer: the embedding, the norms before and after a block, orthogonalised updates.  Arguments are
 // checked before any HIP call; declarations and contracts are in include/moe.h.
+#include <cmath>
 #include <initializer_list>
 
 #include "block.h"
@@ -10,6 +11,8 @@ namespace {
 
 bool at_elements(const void* p, size_t es) { return (reinterpret_cast<uintptr_t>(p) & (es - 1)) == 0; }
 
+// (a product with an infinity or no number would leave something in the rows of zeros)
+bool scale_ok(double scale) { return std::isfinite((float)scale); }
 bool embedding_sizes_ok(int T, int d, int V) { return T >= 0 && d > 0 && V > 0; }
 // (the sort's keys are words, a launch holds less than 2^32 threads)
 bool embedding_takes(int T, int d, int V) {
@@ -66,7 +69,7 @@ size_t moe_embedding_workspace_bytes(int T, int d, int V) {
 }
 
 int moe_embedding_fwd(const void* table, const int32_t* tokens, moe_dtype dt, int T, int d, int V, double scale, void* out, void* stream) {
-  if (!embedding_sizes_ok(T, d, V)) return MOE_ERR_INVALID;
+  if (!embedding_sizes_ok(T, d, V) || !scale_ok(scale)) return MOE_ERR_INVALID;
   if (!embedding_takes(T, d, V) || !grad_types_ok(dt, dt)) return MOE_ERR_UNSUPPORTED;
   if (T == 0) return MOE_OK;
   if (!table || !tokens || !out) return MOE_ERR_INVALID;
@@ -78,7 +81,7 @@ int moe_embedding_fwd(const void* table, const int32_t* tokens, moe_dtype dt, in
 
 int moe_embedding_bwd(const int32_t* tokens, const void* dy, moe_dtype dt, int T, int d, int V, double scale, void* d_table, moe_dtype grad_dt,
                       int accumulate, void* workspace, size_t ws_bytes, void* stream) {
-  if (!embedding_sizes_ok(T, d, V)) return MOE_ERR_INVALID;
+  if (!embedding_sizes_ok(T, d, V) || !scale_ok(scale)) return MOE_ERR_INVALID;
   if (!embedding_takes(T, d, V) || !grad_types_ok(dt, grad_dt)) return MOE_ERR_UNSUPPORTED;
   if (T == 0 && accumulate) return MOE_OK;
   if (!d_table || (T > 0 && (!tokens || !dy))) return MOE_ERR_INVALID;

@@ -137,3 +137,15 @@ def test_norm_gradients_in_place(lib):
     assert bwd(d_out, d_out) == bwd(d_h, d_h) == -1
     for dx in (P(8 * MB), d_out, d_h):
         assert bwd(dx, y, n=need - 1) == bwd(dx, P(9 * MB), n=need - 1) == -3
+
+
+def test_embedding_scale(lib):
+    """A scale that is no finite number in fp32 would make NaN of padding's rows of zeros: -1.  (A batch of none does nothing; a workspace of none is refused.)"""
+    lib.moe_embedding_fwd.argtypes = [P, P, I, I, I, I, D, P, P]
+    lib.moe_embedding_bwd.argtypes = [P, P, I, I, I, I, D, P, I, I, P, Z, P]
+    for scale in (float("nan"), float("inf"), -float("inf"), 1e39):
+        assert lib.moe_embedding_fwd(P(MB), P(2 * MB), BF16, 8, 64, 100, scale, P(3 * MB), None) == -1
+        assert lib.moe_embedding_bwd(P(2 * MB), P(MB), BF16, 8, 64, 100, scale, P(3 * MB), F32, 0, P(4 * MB), MB, None) == -1
+    for scale in (0.0, -0.5, 3e38):
+        assert lib.moe_embedding_fwd(NULL, NULL, BF16, 0, 64, 100, scale, NULL, None) == 0
+        assert lib.moe_embedding_bwd(P(2 * MB), P(MB), BF16, 8, 64, 100, scale, P(3 * MB), F32, 0, NULL, 0, None) == -3
