@@ -495,7 +495,8 @@ int moe_embedding_bwd(const int32_t* tokens, const void* dy /*[T,d]*/, moe_dtype
  * [ceil(T/gate_rows),d] fp32: gate_rows = T (or more) one vector, 1 a row per token, a sequence's length
  * a row per sequence.  y = NULL: no block ends here (the first one starts): out = x is not written and
  * h is made from x; w_after, gate and out are NULL then and alpha is 1.  d is a multiple of 16, at most
- * MOE_NORM_MAX_WIDTH.  out may be x or y; else outputs share no memory with inputs or each other.
+ * MOE_NORM_MAX_WIDTH, T at most MOE_NORM_MAX_ROWS.  The squares of a row are summed in fp32: elements of some 1e18 are too large.
+ * out may be x or y; else outputs share no memory with inputs or each other.
  * T = 0: nothing is enqueued.
  *
  * moe_block_norm_bwd: all gradients, from `out` as the forward pass wrote it (x where y is NULL), d_out,
@@ -506,6 +507,7 @@ int moe_embedding_bwd(const int32_t* tokens, const void* dy /*[T,d]*/, moe_dtype
  * d_out or d_h, dy may be y or the other of d_out and d_h; else outputs share no memory with inputs or each other.  T = 0: nothing is
  * enqueued and nothing written.  Workspace: moe_block_norm_workspace_bytes (after, gate, before: whether there is one). */
 #define MOE_NORM_MAX_WIDTH 16384
+#define MOE_NORM_MAX_ROWS 0x7f000000
 int moe_block_norm_fwd(const void* x, const void* y, const float* w_after, const float* gate,
                        const float* w_before, moe_dtype dt, int T, int d, int gate_rows, double alpha,
                        double eps, void* out, void* h, void* stream);

@@ -94,10 +94,10 @@ int moe_embedding_bwd(const int32_t* tokens, const void* dy, moe_dtype dt, int T
                               as_stream(stream));
 }
 
-// (an empty batch's rows may be NULL whatever is asked for)
+// (an empty batch's rows may be NULL whatever is asked for; places of rows, to the end of the last team's share, are counted in 31 bits)
 static int norm_arguments(const void* y, const float* w_after, const float* gate, moe_dtype dt, int T, int d, int gate_rows, double alpha, double eps) {
   if (T < 0 || d <= 0 || !(eps >= 0) || alpha != alpha || (gate && gate_rows < 1)) return MOE_ERR_INVALID;
-  if ((dt != MOE_F32 && dt != MOE_BF16) || d % 16 != 0 || d > MOE_NORM_MAX_WIDTH) return MOE_ERR_UNSUPPORTED;
+  if ((dt != MOE_F32 && dt != MOE_BF16) || d % 16 != 0 || d > MOE_NORM_MAX_WIDTH || T > MOE_NORM_MAX_ROWS) return MOE_ERR_UNSUPPORTED;
   return T > 0 && !y && (w_after || gate || alpha != 1.0) ? MOE_ERR_INVALID : MOE_OK;
 }
 
@@ -117,7 +117,7 @@ int moe_block_norm_fwd(const void* x, const void* y, const float* w_after, const
 }
 
 size_t moe_block_norm_workspace_bytes(int T, int d, moe_dtype dt, int after, int gate, int before) {
-  if (T < 0 || d <= 0 || d % 16 != 0 || d > MOE_NORM_MAX_WIDTH || (dt != MOE_F32 && dt != MOE_BF16)) return 0;
+  if (T < 0 || T > MOE_NORM_MAX_ROWS || d <= 0 || d % 16 != 0 || d > MOE_NORM_MAX_WIDTH || (dt != MOE_F32 && dt != MOE_BF16)) return 0;
   return norm_bwd_plan(T, d, dt, after != 0, gate != 0, before != 0).bytes;
 }
 

@@ -149,3 +149,17 @@ def test_embedding_scale(lib):
     for scale in (0.0, -0.5, 3e38):
         assert lib.moe_embedding_fwd(NULL, NULL, BF16, 0, 64, 100, scale, NULL, None) == 0
         assert lib.moe_embedding_bwd(P(2 * MB), P(MB), BF16, 8, 64, 100, scale, P(3 * MB), F32, 0, NULL, 0, None) == -3
+
+
+def test_norm_rows(lib):
+    """A team's share of the rows ends within 31 bits."""
+    lib.moe_block_norm_fwd.argtypes = [P, P, P, P, P, I, I, I, I, D, D, P, P, P]
+    lib.moe_block_norm_bwd.argtypes = [P] * 7 + [I, I, I, I, D, D] + [P] * 5 + [I, P, Z, P]
+    most = 0x7f000000
+    for T in (most + 1, 2 ** 31 - 2048, 2 ** 31 - 1):
+        assert lib.moe_block_norm_workspace_bytes(T, 16, BF16, 0, 0, 1) == 0
+        assert lib.moe_block_norm_fwd(P(MB), NULL, NULL, NULL, P(5 * MB), BF16, T, 16, 1, 1.0, 1e-6, NULL, P(7 * MB), None) == -2
+        assert lib.moe_block_norm_bwd(P(MB), NULL, NULL, NULL, P(5 * MB), NULL, P(7 * MB), BF16, T, 16, 1, 1.0, 1e-6, P(8 * MB), NULL, NULL, NULL, P(12 * MB), 0, P(13 * MB),
+                                      Z(1 << 40), None) == -2
+    # one list of sums for each of at most 2048 teams
+    assert 0 < lib.moe_block_norm_workspace_bytes(most, 16, BF16, 0, 0, 1) <= 2048 * 16 * 4 + 256
