@@ -517,7 +517,10 @@ def moe_block_norm_bwd(out, y, w_after, gate, w_before, d_out, d_h, gate_rows, a
 
 
 def _coefficients(c):
-    """(number of steps, the bytes of their doubles)."""
+    """(number of steps, the bytes of their doubles), or what this has made already."""
+    if len(c) == 2 and isinstance(c[1], bytes):
+        assert 1 <= c[0] <= ORTH_MAX_STEPS and len(c[1]) == 24 * c[0], "the bytes of three coefficients a step"
+        return c
     rows = [tuple(float(v) for v in row) for row in c]
     assert 1 <= len(rows) <= ORTH_MAX_STEPS and all(len(r) == 3 for r in rows), "1 to 16 rows of three coefficients"
     return len(rows), struct.pack(f"{3 * len(rows)}d", *(v for r in rows for v in r))
@@ -530,7 +533,7 @@ def moe_orthogonal_workspace_bytes(batch, rows, cols, piece=0) -> int:
 def moe_orthogonalize(x, out, workspace, coefficients=COEFFICIENTS, piece=0):
     batch, rows, cols = x.shape
     assert out.shape == x.shape, "out like x"
-    steps, packed = coefficients if isinstance(coefficients[-1], bytes) else _coefficients(coefficients)
+    steps, packed = _coefficients(coefficients)
     _check("moe_orthogonalize", _native.moe_orthogonalize(
         x, dtype_code(x.dtype), batch, rows, cols, steps, packed, piece, out, dtype_code(out.dtype), workspace,
         workspace.numel() * workspace.element_size()))
@@ -541,7 +544,7 @@ def moe_muon(p, grad, m, weights, lr, coef, momentum, nesterov, weight_decay, sc
     assert p.dtype == m.dtype == torch.float32 and m.shape == p.shape, "parameters and momentum are fp32, of one size"
     assert grad.shape == p.shape, "gradients have their parameters' sizes"
     assert weights is None or (weights.shape == p.shape and weights.dtype == torch.bfloat16), "weights are bf16, of their parameters' sizes"
-    steps, packed = coefficients if isinstance(coefficients[-1], bytes) else _coefficients(coefficients)
+    steps, packed = _coefficients(coefficients)
     _check("moe_muon", _native.moe_muon_eps(
         p, grad, dtype_code(grad.dtype), m, weights, batch, rows, cols, lr, coef, momentum, int(nesterov), weight_decay, scale, eps, steps,
         packed, piece, workspace, workspace.numel() * workspace.element_size()))

@@ -163,3 +163,19 @@ def test_norm_rows(lib):
                                       Z(1 << 40), None) == -2
     # one list of sums for each of at most 2048 teams
     assert 0 < lib.moe_block_norm_workspace_bytes(most, 16, BF16, 0, 0, 1) <= 2048 * 16 * 4 + 256
+
+
+def test_coefficients():
+    """Steps that are made into bytes once are used as they are; a number of steps beyond their bytes, which would be read past their end, is none."""
+    import torch
+
+    from paper_2505_11432_amd import binding as B
+    steps, packed = made = B._coefficients(B.COEFFICIENTS)
+    assert steps == 5 and len(packed) == 120 and B._coefficients(made) == made
+    x = torch.zeros((1, 8, 8))
+    w = torch.zeros((16,), dtype=torch.uint8)
+    for bad in ((), ((1.0, 2.0),), ((1.0, 0.0, 0.0),) * 17, (16, packed), (5, packed[:-8]), (0, b"")):
+        with pytest.raises(AssertionError, match="coefficients"):
+            B.moe_orthogonalize(x, x, w, coefficients=bad)
+        with pytest.raises(AssertionError, match="coefficients"):
+            B.moe_muon(x, x, x, None, w, None, 0.9, True, 0.0, 1.0, w, coefficients=bad)
