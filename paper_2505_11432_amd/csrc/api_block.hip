@@ -51,7 +51,7 @@ int orthogonal_problem(int batch, int rows, int cols, int steps, const double* c
   for (int k = 0; k < steps; ++k)
     q->coef[k] = coefficients ? OrthCoef{coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2]} : kDefaultCoef;
   if (!orth_coefficients_ok(q->coef, steps, rows, cols)) return MOE_ERR_UNSUPPORTED;
-  q->batch = batch; q->rows = rows; q->cols = cols; q->steps = steps; q->piece = piece;
+  q->batch = batch; q->rows = rows; q->cols = cols; q->steps = steps;
   *plan = orth_plan(batch, rows, cols, piece);
   if (batch > 0 && (!workspace || !aligned16(workspace) || ws_bytes < plan->bytes)) return MOE_ERR_WORKSPACE;
   return MOE_OK;

@@ -12,7 +12,7 @@ constexpr OrthCoef kDefaultCoef{3.4445, -4.7750, 2.0315};
 
 struct MuonProblem {
   const void* u; moe_dtype u_dt;             // matrices to orthogonalise; Muon: their gradients
-  int batch, rows, cols, piece;              // piece: matrices at a time
+  int batch, rows, cols;
   OrthCoef coef[MOE_ORTH_MAX_STEPS]; int steps;
   void* out; moe_dtype out_dt;               // orthogonalised matrices, or NULL: Muon
   float* p; float* m; void* w;

@@ -19,54 +19,48 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-template <int W> using vec = float __attribute__((ext_vector_type(W)));
+constexpr int W = 8;                        // elements of a thread's piece of a row
+typedef float vec __attribute__((ext_vector_type(W)));
 
-// W elements as they lie in memory, read and written past the caches (a row is used once)
-template <typename T, int W> struct Piece;
-template <int W> struct Piece<float, W> {
-  vec<W> v;
+// A piece as it lies in memory, read and written past the caches (a row is used once)
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+  vec v;
   __device__ __forceinline__ void load(const float* p) {
     const f32x4 a = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
-    if constexpr (W == 4) v = a;
-    else v = __builtin_shufflevector(a, __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p) + 1), 0, 1, 2, 3, 4, 5, 6, 7);
+    v = __builtin_shufflevector(a, __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p) + 1), 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  __device__ __forceinline__ vec<W> get() const { return v; }
+  __device__ __forceinline__ vec get() const { return v; }
 };
-template <int W> struct Piece<bf16, W> {
+template <> struct Piece<bf16> {
   typedef __bf16 raw __attribute__((ext_vector_type(W)));
   raw v;
   __device__ __forceinline__ void load(const bf16* p) { v = __builtin_nontemporal_load(reinterpret_cast<const raw*>(p)); }
-  __device__ __forceinline__ vec<W> get() const { return __builtin_convertvector(v, vec<W>); }
+  __device__ __forceinline__ vec get() const { return __builtin_convertvector(v, vec); }
 };
-template <int W> __device__ __forceinline__ vec<W> load_f32(const float* p) {
-  if constexpr (W == 4) return *reinterpret_cast<const f32x4*>(p);
-  else return __builtin_shufflevector(*reinterpret_cast<const f32x4*>(p), *(reinterpret_cast<const f32x4*>(p) + 1), 0, 1, 2, 3, 4, 5, 6, 7);
+__device__ __forceinline__ vec load_f32(const float* p) {
+  return __builtin_shufflevector(*reinterpret_cast<const f32x4*>(p), *(reinterpret_cast<const f32x4*>(p) + 1), 0, 1, 2, 3, 4, 5, 6, 7);
 }
-template <int W> __device__ __forceinline__ void store(float* p, vec<W> v) {
-  if constexpr (W == 4) {
-    *reinterpret_cast<f32x4*>(p) = v;
-  } else {
-    *reinterpret_cast<f32x4*>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-    *(reinterpret_cast<f32x4*>(p) + 1) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
-  }
+__device__ __forceinline__ void store(float* p, vec v) {
+  *reinterpret_cast<f32x4*>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+  *(reinterpret_cast<f32x4*>(p) + 1) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
 }
-template <int W> __device__ __forceinline__ void store(bf16* p, vec<W> v) {
+__device__ __forceinline__ void store(bf16* p, vec v) {
   typedef __bf16 raw __attribute__((ext_vector_type(W)));
   __builtin_nontemporal_store(__builtin_convertvector(v, raw), reinterpret_cast<raw*>(p));
 }
 // v as T keeps it
-template <typename T, int W> __device__ __forceinline__ vec<W> rounded(vec<W> v) {
+template <typename T> __device__ __forceinline__ vec rounded(vec v) {
   typedef T raw __attribute__((ext_vector_type(W)));
-  return __builtin_convertvector(__builtin_convertvector(v, raw), vec<W>);
+  return __builtin_convertvector(__builtin_convertvector(v, raw), vec);
 }
-template <int W> __device__ __forceinline__ float sum_of(vec<W> v) {
-  float s = (v[0] + v[1]) + (v[2] + v[3]);
-  if constexpr (W == 8) s += (v[4] + v[5]) + (v[6] + v[7]);
-  return s;
+__device__ __forceinline__ float sum_of(vec v) {
+  const float s = (v[0] + v[1]) + (v[2] + v[3]);
+  return s + ((v[4] + v[5]) + (v[6] + v[7]));
 }
 
 // Sums of N values over a team, the same in every thread; `lds` holds two rounds, told apart by `turn`, so one barrier a round is enough.
-constexpr int kMostSums = 8;
+constexpr int kMostSums = 2;
 template <int TS, int N> __device__ __forceinline__ void team_sum(float (&v)[N], float* lds, int& turn) {
   static_assert(N <= kMostSums, "the sums of a round");
 #pragma unroll
@@ -98,7 +92,7 @@ constexpr int block_threads(int ts) { return ts < 256 ? 256 : ts; }
 template <int TS> constexpr int lds_floats() { return 2 * kMostSums * (TS / 64); }
 
 // Teams of the forward pass take rows in turn.
-template <typename T, int TS, int W, int K>
+template <typename T, int TS, int K>
 __global__ void __launch_bounds__(block_threads(TS)) norm_fwd_kernel(NormProblem q, int teams) {
   __shared__ __attribute__((aligned(16))) float lds[lds_floats<TS>()];
   const int lane = threadIdx.x % TS, team = blockIdx.x * (block_threads(TS) / TS) + threadIdx.x / TS;
@@ -109,20 +103,20 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_fwd_kernel(NormProblem
   T* h = static_cast<T*>(q.h);
   const float inv_d = 1.0f / (float)q.d;
   int turn = 0;
-  vec<W> wa[K], wb[K], gate[K];
+  vec wa[K], wb[K], gate[K];
   int col[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     col[k] = (k * TS + lane) * W;
-    wa[k] = wb[k] = gate[k] = vec<W>{};
+    wa[k] = wb[k] = gate[k] = vec{};
     if (col[k] < q.d) {
-      if (q.w_after) wa[k] = load_f32<W>(q.w_after + col[k]);
-      if (q.w_before) wb[k] = load_f32<W>(q.w_before + col[k]);
+      if (q.w_after) wa[k] = load_f32(q.w_after + col[k]);
+      if (q.w_before) wb[k] = load_f32(q.w_before + col[k]);
     }
   }
   int open = -1;                                    // row of the gate in registers
   for (long t = team; t < q.T; t += teams) {
-    Piece<T, W> xr[K], yr[K];
+    Piece<T> xr[K], yr[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       xr[k].v = {};
@@ -133,15 +127,15 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_fwd_kernel(NormProblem
       }
     }
     float sum[1];
-    vec<W> o[K];
+    vec o[K];
     if (y) {
       float inv = 1.f;
       if (q.w_after) {
         sum[0] = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-          const vec<W> v = yr[k].get();
-          sum[0] += sum_of<W>(v * v);
+          const vec v = yr[k].get();
+          sum[0] += sum_of(v * v);
         }
         team_sum<TS>(sum, lds, turn);
         inv = 1.0f / sqrtf(sum[0] * inv_d + q.eps);
@@ -152,16 +146,16 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_fwd_kernel(NormProblem
           open = group;
 #pragma unroll
           for (int k = 0; k < K; ++k)
-            if (col[k] < q.d) gate[k] = load_f32<W>(q.gate + (long)group * q.d + col[k]);
+            if (col[k] < q.d) gate[k] = load_f32(q.gate + (long)group * q.d + col[k]);
         }
       }
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        vec<W> n = yr[k].get();
+        vec n = yr[k].get();
         if (q.w_after) n = n * inv * wa[k];
         if (q.gate) n = n * gate[k];
-        o[k] = rounded<T, W>(xr[k].get() * q.alpha + n);
-        if (col[k] < q.d) store<W>(out + t * q.d + col[k], o[k]);
+        o[k] = rounded<T>(xr[k].get() * q.alpha + n);
+        if (col[k] < q.d) store(out + t * q.d + col[k], o[k]);
       }
     } else {
 #pragma unroll
@@ -170,12 +164,12 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_fwd_kernel(NormProblem
     if (q.w_before) {
       sum[0] = 0.f;
 #pragma unroll
-      for (int k = 0; k < K; ++k) sum[0] += sum_of<W>(o[k] * o[k]);
+      for (int k = 0; k < K; ++k) sum[0] += sum_of(o[k] * o[k]);
       team_sum<TS>(sum, lds, turn);
       const float inv = 1.0f / sqrtf(sum[0] * inv_d + q.eps);
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (col[k] < q.d) store<W>(h + t * q.d + col[k], o[k] * inv * wb[k]);
+        if (col[k] < q.d) store(h + t * q.d + col[k], o[k] * inv * wb[k]);
     }
   }
 }
@@ -193,7 +187,7 @@ __host__ __device__ inline Parts parts_of(bool after, bool gate, bool before) {
 
 // TOKEN: every token has its own row of the gate.  HOLD: the weights stay in registers (the widest rows leave no room for them).  AHEAD: the next row is
 // on its way while one is worked on.
-template <typename T, int TS, int W, int K, bool HOLD, bool TOKEN, bool AHEAD>
+template <typename T, int TS, int K, bool HOLD, bool TOKEN, bool AHEAD>
 __global__ void __launch_bounds__(block_threads(TS)) norm_bwd_kernel(NormProblem q, int teams, int rows, float* __restrict__ parts) {
   __shared__ __attribute__((aligned(16))) float lds[lds_floats<TS>()];
   const int lane = threadIdx.x % TS, team = blockIdx.x * (block_threads(TS) / TS) + threadIdx.x / TS;
@@ -209,28 +203,28 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_bwd_kernel(NormProblem
   const float inv_d = 1.0f / (float)q.d;
   const bool grouped = q.gate && !TOKEN;
   int turn = 0;
-  vec<W> wa_held[HOLD ? K : 1], wb_held[HOLD ? K : 1], gate_held[HOLD && !TOKEN ? K : 1], sum_wa[K], sum_wb[K], sum_gate[TOKEN ? 1 : K];
+  vec wa_held[HOLD ? K : 1], wb_held[HOLD ? K : 1], gate_held[HOLD && !TOKEN ? K : 1], sum_wa[K], sum_wb[K], sum_gate[TOKEN ? 1 : K];
   int col[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     col[k] = (k * TS + lane) * W;
-    sum_wa[k] = sum_wb[k] = vec<W>{};
-    if constexpr (!TOKEN) sum_gate[k] = vec<W>{};
-    if constexpr (HOLD && !TOKEN) gate_held[k] = vec<W>{};
+    sum_wa[k] = sum_wb[k] = vec{};
+    if constexpr (!TOKEN) sum_gate[k] = vec{};
+    if constexpr (HOLD && !TOKEN) gate_held[k] = vec{};
     if constexpr (HOLD) {
-      wa_held[k] = wb_held[k] = vec<W>{};
+      wa_held[k] = wb_held[k] = vec{};
       if (col[k] < q.d) {
-        if (q.w_after) wa_held[k] = load_f32<W>(q.w_after + col[k]);
-        if (q.w_before) wb_held[k] = load_f32<W>(q.w_before + col[k]);
+        if (q.w_after) wa_held[k] = load_f32(q.w_after + col[k]);
+        if (q.w_before) wb_held[k] = load_f32(q.w_before + col[k]);
       }
     }
   }
   const bool needs_y = q.dy && (q.w_after || q.gate);
   const int t_begin = team * rows, t_end = min(t_begin + rows, q.T);
   int open = -1;
-  auto at_col = [&](const float* w, int k) __attribute__((always_inline)) -> vec<W> { return col[k] < q.d ? load_f32<W>(w + col[k]) : vec<W>{}; };
-  auto wa = [&](int k) __attribute__((always_inline)) -> vec<W> { if constexpr (HOLD) return wa_held[k]; else return at_col(q.w_after, k); };
-  auto wb = [&](int k) __attribute__((always_inline)) -> vec<W> { if constexpr (HOLD) return wb_held[k]; else return at_col(q.w_before, k); };
+  auto at_col = [&](const float* w, int k) __attribute__((always_inline)) -> vec { return col[k] < q.d ? load_f32(w + col[k]) : vec{}; };
+  auto wa = [&](int k) __attribute__((always_inline)) -> vec { if constexpr (HOLD) return wa_held[k]; else return at_col(q.w_after, k); };
+  auto wb = [&](int k) __attribute__((always_inline)) -> vec { if constexpr (HOLD) return wb_held[k]; else return at_col(q.w_before, k); };
   auto close_gate = [&](int group) __attribute__((always_inline)) {
     if constexpr (!TOKEN) {
       const long begin = (long)group * q.gate_rows;
@@ -240,12 +234,12 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_bwd_kernel(NormProblem
 #pragma unroll
       for (int k = 0; k < K; ++k)
         if (col[k] < q.d) {
-          store<W>(to + col[k], add ? sum_gate[k] + load_f32<W>(to + col[k]) : sum_gate[k]);
-          sum_gate[k] = vec<W>{};
+          store(to + col[k], add ? sum_gate[k] + load_f32(to + col[k]) : sum_gate[k]);
+          sum_gate[k] = vec{};
         }
     }
   };
-  struct Row { Piece<T, W> x[K], y[K], g[K], h[K]; } now, next;
+  struct Row { Piece<T> x[K], y[K], g[K], h[K]; } now, next;
   auto fetch = [&](Row& to, int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -286,48 +280,48 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_bwd_kernel(NormProblem
     } else {
       fetch(now, t);
     }
-    vec<W> token_gate[TOKEN ? K : 1];
+    vec token_gate[TOKEN ? K : 1];
     if constexpr (TOKEN) {
 #pragma unroll
       for (int k = 0; k < K; ++k) token_gate[k] = at_col(q.gate + row, k);
     }
-    auto gate = [&](int k) __attribute__((always_inline)) -> vec<W> {
+    auto gate = [&](int k) __attribute__((always_inline)) -> vec {
       if constexpr (TOKEN) return token_gate[k];
       else if constexpr (HOLD) return gate_held[k];
       else return at_col(q.gate + (long)open * q.d, k);
     };
-    vec<W> g[K];
+    vec g[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) g[k] = now.g[k].get();
     if (q.w_before) {
       float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const vec<W> v = now.x[k].get();
-        s[0] += sum_of<W>(v * v);
-        s[1] += sum_of<W>(now.h[k].get() * wb(k) * v);
+        const vec v = now.x[k].get();
+        s[0] += sum_of(v * v);
+        s[1] += sum_of(now.h[k].get() * wb(k) * v);
       }
       team_sum<TS>(s, lds, turn);
       const float i = 1.0f / sqrtf(s[0] * inv_d + q.eps), mean = s[1] * i * inv_d;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const vec<W> unit = now.x[k].get() * i, dh = now.h[k].get();
+        const vec unit = now.x[k].get() * i, dh = now.h[k].get();
         sum_wb[k] += dh * unit;
         g[k] += (dh * wb(k) - unit * mean) * i;
       }
     }
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (col[k] < q.d) store<W>(dx + row + col[k], g[k] * q.alpha);
+      if (col[k] < q.d) store(dx + row + col[k], g[k] * q.alpha);
     if (!q.dy) continue;
     float i = 1.f, mean = 0.f;
     if (q.w_after) {
       float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const vec<W> v = now.y[k].get();
-        s[0] += sum_of<W>(v * v);
-        s[1] += sum_of<W>((q.gate ? g[k] * gate(k) : g[k]) * wa(k) * v);
+        const vec v = now.y[k].get();
+        s[0] += sum_of(v * v);
+        s[1] += sum_of((q.gate ? g[k] * gate(k) : g[k]) * wa(k) * v);
       }
       team_sum<TS>(s, lds, turn);
       i = 1.0f / sqrtf(s[0] * inv_d + q.eps);
@@ -335,13 +329,13 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_bwd_kernel(NormProblem
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const vec<W> unit = now.y[k].get() * i;
-      vec<W> u = g[k];
+      const vec unit = now.y[k].get() * i;
+      vec u = g[k];
       if (q.gate) {
-        const vec<W> d_gate = q.w_after ? u * unit * wa(k) : u * unit;
+        const vec d_gate = q.w_after ? u * unit * wa(k) : u * unit;
         if constexpr (TOKEN) {
           float* to = q.d_gate + row + col[k];
-          if (col[k] < q.d) store<W>(to, q.accumulate ? d_gate + load_f32<W>(to) : d_gate);
+          if (col[k] < q.d) store(to, q.accumulate ? d_gate + load_f32(to) : d_gate);
         } else {
           sum_gate[k] += d_gate;
         }
@@ -351,15 +345,15 @@ __global__ void __launch_bounds__(block_threads(TS)) norm_bwd_kernel(NormProblem
         sum_wa[k] += u * unit;
         u = (u * wa(k) - unit * mean) * i;
       }
-      if (col[k] < q.d) store<W>(dy + row + col[k], u);
+      if (col[k] < q.d) store(dy + row + col[k], u);
     }
   }
   if (grouped && open >= 0) close_gate(open);
 #pragma unroll
   for (int k = 0; k < K; ++k)
     if (col[k] < q.d) {
-      if (q.w_before) store<W>(mine + (long)lists.wb * q.d + col[k], sum_wb[k]);
-      if (q.w_after) store<W>(mine + (long)lists.wa * q.d + col[k], sum_wa[k]);
+      if (q.w_before) store(mine + (long)lists.wb * q.d + col[k], sum_wb[k]);
+      if (q.w_after) store(mine + (long)lists.wa * q.d + col[k], sum_wa[k]);
     }
 }
 
@@ -410,27 +404,27 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(NormProblem q, int team
   }
 }
 
-// Threads of a team, elements of each and steps of those; HOLD: see the backward pass.
-template <int TS_, int W_, int K_, bool HOLD_ = true> struct Team { static constexpr int TS = TS_, W = W_, K = K_; static constexpr bool HOLD = HOLD_; };
+// Threads of a team and pieces of each; HOLD: see the backward pass.
+template <int TS_, int K_, bool HOLD_ = true> struct Team { static constexpr int TS = TS_, K = K_; static constexpr bool HOLD = HOLD_; };
 // Forward (bf16, all parts, us): a row at a time 16384 x 2048 50 (5.4 TB/s), 8192 x 4096 49, 4096 x 8192 52; two or four rows at a time, which leave room for fewer
 // teams, 53 and 56, 56 and 64, 60; 32768 x 1024 by one wave with two steps 59, by 256 threads of four elements 66.
 template <typename F> int with_fwd_team(int d, F f) {
-  if (d <= 512) return f(Team<64, 8, 1>());
-  if (d <= 1024) return f(Team<64, 8, 2>());
-  if (d <= 2048) return f(Team<256, 8, 1>());
-  if (d <= 4096) return f(Team<512, 8, 1>());
-  if (d <= 8192) return f(Team<1024, 8, 1>());
-  return f(Team<1024, 8, 2>());
+  if (d <= 512) return f(Team<64, 1>());
+  if (d <= 1024) return f(Team<64, 2>());
+  if (d <= 2048) return f(Team<256, 1>());
+  if (d <= 4096) return f(Team<512, 1>());
+  if (d <= 8192) return f(Team<1024, 1>());
+  return f(Team<1024, 2>());
 }
 // Backward (8192 x 4096, bf16, all parts, 256 or 512 teams, us): 256 threads, 16 elements each 91, with the next row ahead 84; 512 threads, 8 elements, a row
 // ahead 82 (4.9 TB/s, what a copy takes); 1024 threads 109 to 127; two to four rows at a time instead of one ahead 103 to 141.
 template <typename F> int with_bwd_team(int d, F f) {
-  if (d <= 512) return f(Team<64, 8, 1>());
-  if (d <= 1024) return f(Team<64, 8, 2>());
-  if (d <= 2048) return f(Team<256, 8, 1>());
-  if (d <= 4096) return f(Team<512, 8, 1>());
-  if (d <= 8192) return f(Team<1024, 8, 1>());
-  return f(Team<1024, 8, 2, false>());
+  if (d <= 512) return f(Team<64, 1>());
+  if (d <= 1024) return f(Team<64, 2>());
+  if (d <= 2048) return f(Team<256, 1>());
+  if (d <= 4096) return f(Team<512, 1>());
+  if (d <= 8192) return f(Team<1024, 1>());
+  return f(Team<1024, 2, false>());
 }
 
 }  // namespace
@@ -452,8 +446,8 @@ int launch_norm_fwd(const NormProblem& q, hipStream_t s) {
     constexpr int per = block_threads(C::TS) / C::TS;
     const int most = 256 * 2048 / C::TS, teams = q.T < most ? q.T : most;
     const dim3 grid((unsigned)cdiv(teams, per)), block(block_threads(C::TS));
-    if (q.dt == MOE_F32) norm_fwd_kernel<float, C::TS, C::W, C::K><<<grid, block, 0, s>>>(q, teams);
-    else norm_fwd_kernel<bf16, C::TS, C::W, C::K><<<grid, block, 0, s>>>(q, teams);
+    if (q.dt == MOE_F32) norm_fwd_kernel<float, C::TS, C::K><<<grid, block, 0, s>>>(q, teams);
+    else norm_fwd_kernel<bf16, C::TS, C::K><<<grid, block, 0, s>>>(q, teams);
     MOE_LAUNCH_CHECK();
     return (int)MOE_OK;
   });
@@ -467,10 +461,10 @@ int launch_norm_bwd(const NormProblem& q, const NormPlan& p, float* ws, hipStrea
     constexpr bool AHEAD16 = C::TS < 1024, AHEAD32 = AHEAD16 && C::K == 1;
     const dim3 grid((unsigned)cdiv(p.teams, per)), block(block_threads(C::TS));
     const bool token = q.gate && q.gate_rows == 1;
-    if (q.dt == MOE_F32 && !token) norm_bwd_kernel<float, C::TS, C::W, C::K, C::HOLD, false, AHEAD32><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
-    else if (q.dt == MOE_F32) norm_bwd_kernel<float, C::TS, C::W, C::K, C::HOLD, true, AHEAD32><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
-    else if (!token) norm_bwd_kernel<bf16, C::TS, C::W, C::K, C::HOLD, false, AHEAD16><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
-    else norm_bwd_kernel<bf16, C::TS, C::W, C::K, C::HOLD, true, AHEAD16><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
+    if (q.dt == MOE_F32 && !token) norm_bwd_kernel<float, C::TS, C::K, C::HOLD, false, AHEAD32><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
+    else if (q.dt == MOE_F32) norm_bwd_kernel<float, C::TS, C::K, C::HOLD, true, AHEAD32><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
+    else if (!token) norm_bwd_kernel<bf16, C::TS, C::K, C::HOLD, false, AHEAD16><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
+    else norm_bwd_kernel<bf16, C::TS, C::K, C::HOLD, true, AHEAD16><<<grid, block, 0, s>>>(q, p.teams, p.rows, ws);
     MOE_LAUNCH_CHECK();
     return (int)MOE_OK;
   });
