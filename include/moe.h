@@ -495,7 +495,7 @@ int moe_embedding_bwd(const int32_t* tokens, const void* dy /*[T,d]*/, moe_dtype
  * [ceil(T/gate_rows),d] fp32: gate_rows = T (or more) one vector, 1 a row per token, a sequence's length
  * a row per sequence.  y = NULL: no block ends here (the first one starts): out = x is not written and
  * h is made from x; w_after, gate and out are NULL then and alpha is 1.  d is a multiple of 16, at most
- * MOE_NORM_MAX_WIDTH, T at most MOE_NORM_MAX_ROWS.  The squares of a row are summed in fp32: elements of some 1e18 are too large.
+ * MOE_NORM_MAX_WIDTH, T at most MOE_NORM_MAX_ROWS.  The squares of a row are summed in fp32, whose range elements of some 1e17 pass.
  * out may be x or y; else outputs share no memory with inputs or each other.
  * T = 0: nothing is enqueued.
  *

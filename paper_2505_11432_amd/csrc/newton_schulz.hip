@@ -1,5 +1,5 @@
 // Orthogonalised updates (Muon): u / |u| through Newton-Schulz steps, a batch of matrices at a time.
-//   m = mu m + f g,  u = f g + mu m (or m),  X = u / |u|_F,  steps X <- (a I + b A + c A^2) X with A = X X^T,  p = p (1 - lr wd) - lr s X
+//   m = mu m + f g,  u = f g + mu m (or m),  X = u / max(|u|_F, eps),  steps X <- (a I + b A + c A^2) X with A = X X^T,  p = p (1 - lr wd) - lr s X
 // For matrices with more rows than columns A = X^T X, on the smaller side, and the steps multiply from the right.
 // Bound by the matrix cores: a step multiplies m^2 (3 n + m) times per m x n matrix, m <= n, with A and R = b A + c A^2 symmetric and half of their tiles
 // computed (the other half is mirrored).
@@ -10,7 +10,8 @@
 // like a singular value of its own size and is multiplied by up to a = 3.4 in every later step, 485 in five.  X is therefore carried as two fp16, hi + 2^-11 lo
 // (22 bits), a step adds R X, whose operand is hi, to a (hi + lo): what is left out, R lo, has no part in directions that A does not have.  Relative error
 // (2-norm) of matrices with singular values flat, falling as i^-0.5, as i^-1.5, and 64 of 512: 6e-4, 6e-4, 9e-4, 1.7e-3 measured (of rank 1 1.9e-3, of small full ones,
-// 65 x 512, 1.2e-3); 9e-4, 8e-4, 1.1e-3, 2.3e-3 by a model of these roundings in 64 bits, which gives 2.6e-3, 3.2e-3, 1.6e-2, 3.0e-2 for X in one fp16 and 2.1e-2, 2.6e-2, 0.13, 0.24 for bf16 throughout.
+// 65 x 512, 1.2e-3); 9e-4, 8e-4, 1.1e-3, 2.3e-3 by a model of these roundings in 64 bits, which gives 2.6e-3, 3.2e-3, 1.6e-2, 3.0e-2 for X in one fp16 and
+// 2.1e-2, 2.6e-2, 0.13, 0.24 for bf16 throughout.
 //
 // Every product reads both operands along the contraction (rows of 128 bytes per step of 64), so X is kept in both orientations: as it lies (hi, lo) and
 // transposed (hi).  Matrices are padded with zeros to multiples of 128 in the workspace, which changes no value.
@@ -114,8 +115,8 @@ struct Product {
 
 // Tiles of 256 x 256 by eight waves, 128 x 64 each, one workgroup per CU that walks a list of tiles.  Operands go from memory to an LDS ring of two steps of
 // 64 directly; the lower four waves, one per SIMD, issue the loads while the others multiply.  The loads of a tile's first step are issued before the results
-// of the tile in front are stored.  Two 4096 x 14336: the Gram matrices 392 us, 1.26 PFLOP/s of the tiles computed, R X with X rewritten 905 us, 1.06 PFLOP/s, matrix
-// cores 49 % busy at 2.06 GHz; of 64 times 2048 x 1408 787 us, 0.66 PFLOP/s: 22 steps of some 1.1 us and 40 us of results, 0.75 MB of memory per tile, which all CUs
+// of the tile in front are stored.  Two 4096 x 14336: the Gram matrices 411 us, 1.24 PFLOP/s of the tiles computed, R X with X rewritten 936 us, 1.03 PFLOP/s, matrix
+// cores 50 % busy at 1.96 GHz; of 64 times 2048 x 1408 789 us, 0.66 PFLOP/s: 22 steps of some 1.1 us and 40 us of results, 0.75 MB of memory per tile, which all CUs
 // move at once (half of the CUs begun half a tile later: 2 % slower).  128 x 256 by two workgroups per CU took 8.2 ms for that update, this 6.75.
 constexpr int BM = 256, BN = 256, BK = 64, NW = 8, LOADERS = 4;
 constexpr int WTM = 128, WTN = 64, FM = WTM / 16, FN = WTN / 16, TM = WTM / 32, TN = WTN / 32;

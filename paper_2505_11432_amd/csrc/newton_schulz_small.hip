@@ -1,5 +1,5 @@
 // Orthogonalised updates of matrices with a side of at most 64: all steps on the Gram matrix alone, which fits one workgroup.
-//   A = X X^T (64 x 64, X over its norm),  each step  R = b A + c A^2,  Q <- (a I + R) Q,  A <- (a I + R) A (a I + R),  in the end  O = Q X
+//   A = X X^T (64 x 64, X over its norm or eps),  each step  R = b A + c A^2,  Q <- (a I + R) Q,  A <- (a I + R) A (a I + R),  in the end  O = Q X
 // Where both sides are small the general way is a row of launches that each take longer to start than to run: here it is four (the norm, parts of A by slabs of
 // the longer side, the steps, Q X), and X is read twice and never written.  64 x 2048 71 us (5 the norm, 10 the parts of A, 50 the steps, a chain of products on one
 // CU, 9 Q X), 64 times 64 x 512 72, 16 times 32 x 4096 90; the general way 87, 116, 172, and 62 and 66 for a single 64 x 64.

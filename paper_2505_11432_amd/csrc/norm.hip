@@ -417,7 +417,8 @@ template <typename F> int with_fwd_team(int d, F f) {
   return f(Team<1024, 2>());
 }
 // Backward (8192 x 4096, bf16, all parts, 256 or 512 teams, us): 256 threads, 16 elements each 91, with the next row ahead 84; 512 threads, 8 elements, a row
-// ahead 82 (4.9 TB/s, what a copy takes); 1024 threads 109 to 127; two to four rows at a time instead of one ahead 103 to 141.
+// ahead 82 (4.9 TB/s, what a copy takes); 1024 threads 109 to 127; two to four rows at a time instead of one ahead 103 to 141.  Wider rows have 1024 threads all the
+// same: 4096 x 8192 99, 6144 x 5120 110, 2048 x 16384, which keeps no weights in registers, 292.
 template <typename F> int with_bwd_team(int d, F f) {
   if (d <= 512) return f(Team<64, 1>());
   if (d <= 1024) return f(Team<64, 2>());
@@ -431,7 +432,8 @@ template <typename F> int with_bwd_team(int d, F f) {
 
 NormPlan norm_bwd_plan(int T, int d, moe_dtype dt, bool after, bool gate, bool before) {
   NormPlan p{};
-  // as many teams as run at a time; of few rows two each (777 x 1040, fp32, with 1, 2, 3, 4, 6: 19.8, 15.4, 15.6, 16.6, 19.8 us)
+  // as many teams as run at a time; of few rows two each (777 x 1040, fp32, with 1, 2, 3, 4, 6: 19.8, 15.4, 15.6, 16.6, 19.8 us; other sizes of few rows were not
+  // tried with other teams, whose sums weigh more the wider the rows: 1024 x 4096, bf16, 28.6, 1025 x 4096 23.0)
   const int most = d <= 1024 ? 2048 : d <= 2048 ? 512 : 256;
   p.rows = T <= 1024 ? cdiv(T, 512) : cdiv(T, most);
   if (p.rows < 1) p.rows = 1;
